@@ -302,6 +302,162 @@ dba_status dba_row_scan_static(const void* logits_dev, int32_t logit_dtype, int3
                                float* top_val_dev, int32_t* top_idx_dev, void* cuda_stream);
 size_t dba_row_scan_static_max_bytes(void);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------
+ * The decoder's state beside the step: a tree of tokens per sequence over a paged cache of keys and values.
+ *
+ * The step hands back, for every beam slot, the slot it extends (backptr) and its token; the decoder's attention
+ * layers then need the keys and values of each hypothesis' own past.  Here they are never re-ordered.  A sequence
+ * (a sentence of dba_step, or any other) has `places`:
+ *   - places 0 .. A-1, A = 32 * words: the arena.  Its slots hold the tokens of the tree, in no order;
+ *   - places A .. A + ctx_len - 1: the context, tokens in order, seen by every open row of the sequence.
+ * Place p of sequence b is row p % page_size of page table[b * table_stride + p / page_size] of the cache.
+ * Row i of a sequence (a hypothesis of the beam, or a drafted token) has a mask of A bits (words 32-bit words, bit j
+ * of word w = slot 32 w + j): the slots on its path through the tree, its own token's among them.  A row whose mask is
+ * empty is closed (finished or empty hypothesis): it sees nothing, its output is zero.
+ * dba_tree_advance turns back-pointers into the next masks and gives every new token a free slot; slots that no row
+ * sees any more are free; slots that all open rows see are settled: dba_tree_commit copies them, once, to the
+ * end of the context.  One loop over steps is:
+ *     dba_tree_advance -> dba_tree_commit -> per layer: dba_tree_append, dba_tree_attend -> logits -> dba_step
+ * A tree of drafted tokens is verified the same way (rows = drafted tokens; accepting a path = advancing from its
+ * last row).  rows = 1 is plain decoding.  With masks == NULL every row sees the whole context (attention of the
+ * beam's rows over an encoded source, for instance).
+ *
+ * Conventions are the step's: nothing throws; argument errors are found on the host; calls only enqueue work on the
+ * handle's stream; the caller owns all device memory; calls on one handle must not overlap.  Keys, values and queries
+ * are of one type (dba_dtype); every sum and softmax statistic is fp32.
+ *   Limits: rows <= 64, words <= 128, head_dim <= 256, head_dim and every stride a multiple of 16 bytes, pointers
+ *   16-byte aligned, heads a multiple of kv_heads, max_pages * page_size < 2^31.  Other shapes: DBA_ERR_UNSUPPORTED.
+ *   The cache may be larger than 2^31 elements.
+ * What only the device can see is not returned by calls that do not wait: a page number outside the cache (the place
+ * counts as absent: not read, not written), an arena without a free slot, a table without room for settled tokens,
+ * a place or position outside its range, a bounded wait that ran out.  Each sets a bit that dba_tree_status reports.
+ */
+typedef struct dba_tree dba_tree;
+
+typedef struct {
+    int32_t B;                 /* sequences                                                                     */
+    int32_t rows;              /* most rows per sequence: beam size, or drafted tokens                          */
+    int32_t heads, kv_heads;   /* query heads, key/value heads (head h reads key head h / (heads / kv_heads))   */
+    int32_t head_dim;
+    int32_t page_size;         /* places per page                                                               */
+    int32_t max_pages;         /* pages per sequence: entries of a table row                                    */
+    int32_t words;             /* arena words per sequence (A = 32 * words slots); 0: no arena, masks are NULL  */
+    int32_t dtype;             /* dba_dtype of queries, keys, values and outputs                                */
+} dba_tree_config;
+
+/* A cache: element (page, token, head, d) of layer l at base + l*layer_stride + page*page_stride + token*token_stride +
+ * head*head_stride + d, in elements, for k and v alike. */
+typedef struct {
+    void *k, *v;
+    int32_t num_pages, layers;
+    int64_t page_stride, token_stride, head_stride, layer_stride;
+} dba_kv_cache;
+
+/* New tokens: arrays of N tokens; element (t, head, d) at base + t*token_stride + head*head_stride + d. */
+typedef struct {
+    int32_t N;
+    const void *k, *v;
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const void* q;             /* optional: queries of the same tokens, rotated into q_out (which may be q)       */
+    void* q_out;
+    int64_t q_token_stride, q_head_stride, qo_token_stride, qo_head_stride;
+    const int32_t* place;      /* [N] place in the token's sequence; negative: keys and values are not stored     */
+    const int32_t* seq;        /* [N] the token's sequence; NULL: token t belongs to sequence t / (N / B)          */
+    const int32_t* position;   /* [N] row of cos / sin; negative: not rotated.  NULL: nothing is rotated           */
+    const float *cos, *sin;    /* [positions, rot_dim / 2]                                                        */
+    int32_t positions, rot_dim;/* rot_dim even, <= head_dim: the first rot_dim dimensions are rotated              */
+    int32_t pairs;             /* 0: dimension d turns with d + rot_dim/2;  1: dimension 2d with 2d + 1            */
+} dba_tree_tokens;
+
+/* Queries and outputs: element (b, i, head, d) at base + b*seq_stride + i*row_stride + head*head_stride + d. */
+typedef struct {
+    int32_t rows;              /* rows per sequence of this call, <= the configuration's                          */
+    const void* q;
+    int64_t q_seq_stride, q_row_stride, q_head_stride;
+    void* out;
+    int64_t out_seq_stride, out_row_stride, out_head_stride;
+    float* lse;                /* optional, [B, rows, heads]: log of the sum of exponentials (natural), -inf where nothing is seen */
+    float scale;
+} dba_tree_query;
+
+/* The tree after a step (all device memory; any pointer may be NULL except masks). */
+typedef struct {
+    int32_t* masks;            /* [B, rows_out, words]                                                          */
+    int32_t* slot;             /* [B, rows_out] place of the row's new token; -1: closed, or the arena is full      */
+    int32_t* position;         /* [B, rows_out] how many tokens come before it; -1: closed                       */
+    int32_t* ctx_len;          /* [B] context length once the settled tokens have been committed                 */
+    int32_t* top;              /* [B] one past the highest slot any row sees                                     */
+    int32_t* commit_src;       /* [B, 32 * words] settled slots in the order of their positions, -1 beyond        */
+    int32_t* commit_n;         /* [B] how many                                                                  */
+} dba_tree_next;
+
+enum {                          /* bits of dba_tree_status */
+    DBA_TREE_TIMEOUT = 1,       /* a bounded device-side wait gave up: that call's outputs are NaN               */
+    DBA_TREE_BAD_PAGE = 2,      /* a page number outside the cache                                              */
+    DBA_TREE_ARENA_FULL = 4,    /* dba_tree_advance found no free slot for some row                             */
+    DBA_TREE_NO_ROOM = 8,       /* settled tokens do not fit the sequence's table: none was settled             */
+    DBA_TREE_BAD_INDEX = 16     /* a place, sequence or position outside its range                              */
+};
+
+/* Bytes of device workspace a handle needs (256-byte aligned base); depends on the current device. */
+dba_status dba_tree_workspace_bytes(const dba_tree_config* cfg, size_t* bytes);
+/* The handle keeps the configuration, the stream and its place in the workspace; the trees themselves (masks, lengths,
+ * tables) are the caller's arrays.  Enqueues one memset; does not synchronise. */
+dba_status dba_tree_init(const dba_tree_config* cfg, void* workspace_dev, size_t workspace_bytes, void* cuda_stream,
+                         dba_tree** out);
+
+/*
+ * Stores the keys and values of N tokens at their places of one layer's cache, rotating the keys by their positions
+ * on the way, and rotates the tokens' queries: (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin), computed in fp32 and
+ * rounded once.  Two tokens must not have the same place of the same sequence.
+ */
+dba_status dba_tree_append(dba_tree* h, const dba_tree_tokens* tokens, const dba_kv_cache* cache, const int32_t* table_dev,
+                           int64_t table_stride);
+
+/*
+ * Attention of every row over the places it sees, one layer:  out = sum_p softmax_p(scale <q, k_p>) v_p.
+ *   ctx_len_dev [B];  masks_dev [B, rows, words] or NULL;  top_dev [B] or NULL: slots from top[b] on are seen by no row
+ *   (NULL: the whole arena is looked at).
+ * Keys and values at places no row of the sequence sees are not used, whatever they hold; a value that is not finite
+ * reaches only the rows that see it.  Scores that are not finite give unspecified results for their row.
+ */
+dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* query, const dba_kv_cache* cache, const int32_t* table_dev,
+                           int64_t table_stride, const int32_t* ctx_len_dev, const int32_t* masks_dev, const int32_t* top_dev);
+
+/*
+ * The tree after a step: row j of the new tree extends row backptr[b, j] of the old one (masks_in: [B, rows_in, words]) if
+ * 0 <= backptr < rows_in, or row backptr - rows_in of the new tree itself if that is an earlier row; any other
+ * value closes it.  A row is also closed where score[b, j] is -inf or token[b, j] == eos_id (the step's empty and
+ * finished slots; both arrays optional: give dba_step's outputs), and a row that extends a closed row of the same call.
+ * (An old row with an empty mask stands for the context alone: masks of zeros are a sequence's start.)
+ * The j-th open row gets the j-th lowest slot that no row's past holds.  Slots that the pasts of all open rows
+ * hold are settled: they leave the masks and are listed for dba_tree_commit (their slots are not given out in this
+ * call).  Positions count the tokens before the new one: ctx_len + those on the row's path.
+ *   slot_pos_dev [B, 32 * words], rows slot_pos_stride apart: position of the token in each slot; written for new
+ *   slots, kept by the caller from call to call.   masks_in and next->masks must not overlap.
+ */
+dba_status dba_tree_advance(dba_tree* h, int32_t rows_in, const int32_t* masks_in_dev, int32_t rows_out,
+                            const int32_t* backptr_dev, const float* score_dev, const int32_t* token_dev, int32_t eos_id,
+                            int32_t* slot_pos_dev, int64_t slot_pos_stride, const int32_t* ctx_len_dev,
+                            const dba_tree_next* next);
+
+/*
+ * Copies the settled tokens to the end of the context in every layer of the cache: token i of sequence b from slot
+ * src[b, i] to place A + ctx_len[b] - n[b] + i (ctx_len being dba_tree_advance's new lengths).
+ */
+dba_status dba_tree_commit(dba_tree* h, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride,
+                           const int32_t* ctx_len_dev, const int32_t* src_dev, const int32_t* n_dev);
+
+/* The bits set since the last call (cleared by it).  Synchronises the stream. */
+dba_status dba_tree_status(dba_tree* h, uint32_t* bits);
+uint64_t dba_tree_launch_count(const dba_tree* h);
+/* Testing aid, as dba_test_hook: shortens the bounded waits of the attention kernel; drop_item >= 0 withholds that
+ * tile of every thread block's sequence, so that the wait for it runs out. */
+dba_status dba_tree_test_hook(dba_tree* h, int64_t wait_clocks, int32_t drop_item);
+/* Frees the handle (not the workspace). NULL is allowed. */
+void dba_tree_destroy(dba_tree* h);
+
 #ifdef __cplusplus
 }
 #endif

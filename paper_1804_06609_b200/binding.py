@@ -16,7 +16,9 @@ FLAG_ADJUST_OFF, FLAG_LENGTH_NORM, FLAG_HOST_STAGING, FLAG_PRUNE_NORMALISED, FLA
 
 EXPORTS = ["dba_workspace_bytes", "dba_init", "dba_reset", "dba_step", "dba_step_fused", "dba_step_host", "dba_finalize",
            "dba_timing_enable", "dba_timing_read", "dba_counters", "dba_launch_count", "dba_test_hook", "dba_destroy", "dba_status_string", "dba_row_scan_scratch_bytes", "dba_row_scan",
-           "dba_row_scan_static", "dba_row_scan_static_max_bytes", "dba_project_scan_scratch_bytes", "dba_project_scan"]
+           "dba_row_scan_static", "dba_row_scan_static_max_bytes", "dba_project_scan_scratch_bytes", "dba_project_scan",
+           "dba_tree_workspace_bytes", "dba_tree_init", "dba_tree_append", "dba_tree_attend", "dba_tree_advance", "dba_tree_commit",
+           "dba_tree_status", "dba_tree_launch_count", "dba_tree_test_hook", "dba_tree_destroy"]
 
 
 class DbaError(RuntimeError):
@@ -73,6 +75,18 @@ def lib():
         L.dba_project_scan_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         L.dba_project_scan.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, C.c_size_t,
                                        vp, vp, vp, vp]
+        L.dba_tree_workspace_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+        L.dba_tree_init.argtypes = [vp, vp, C.c_size_t, vp, C.POINTER(vp)]
+        L.dba_tree_append.argtypes = [vp, vp, vp, vp, C.c_int64]
+        L.dba_tree_attend.argtypes = [vp, vp, vp, vp, C.c_int64, vp, vp, vp]
+        L.dba_tree_advance.argtypes = [vp, C.c_int32, vp, C.c_int32, vp, vp, vp, C.c_int32, vp, C.c_int64, vp, vp]
+        L.dba_tree_commit.argtypes = [vp, vp, vp, C.c_int64, vp, vp, vp]
+        L.dba_tree_status.argtypes = [vp, C.POINTER(C.c_uint32)]
+        L.dba_tree_launch_count.argtypes = [vp]
+        L.dba_tree_launch_count.restype = C.c_uint64
+        L.dba_tree_test_hook.argtypes = [vp, C.c_int64, C.c_int32]
+        L.dba_tree_destroy.argtypes = [vp]
+        L.dba_tree_destroy.restype = None
         _lib = L
     return _lib
 

@@ -1,0 +1,138 @@
+// Device helpers of the token tree: places to cache rows, and the division of attention work among blocks.
+#pragma once
+#include "dba_device.cuh"
+#include "tree_internal.h"
+
+namespace dba {
+
+// Element offset of a place of sequence b in one layer's cache; -1 where there is no such row (the place is outside the
+// table, or the table names a page outside the cache: recorded in the status word).  64 bits: a cache may be longer
+// than 2^31 elements.
+__device__ __forceinline__ int64_t tree_row(const TreePages& pg, int b, int place) {
+    const unsigned page = (unsigned)place / (unsigned)pg.page_size;
+    if (place < 0 || page >= (unsigned)pg.max_pages) return -1;
+    const int32_t id = __ldg(pg.table + (int64_t)b * pg.table_stride + page);
+    if ((unsigned)id >= (unsigned)pg.num_pages) { atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_PAGE); return -1; }
+    return (int64_t)id * pg.page_stride + (int64_t)((unsigned)place - page * (unsigned)pg.page_size) * pg.token_stride;
+}
+
+// Keys of a sequence are walked in tiles of `kt` places: first the arena up to the highest slot in use, then the
+// context (each starts a tile of its own).  A sequence with nothing to see has one (empty) tile, so that somebody
+// writes its zeros.
+__device__ __forceinline__ int tree_top(const TreeAttend& a, int b) {
+    if (!a.masks) return 0;
+    return a.top ? min(max(__ldg(a.top + b), 0), a.A) : a.A;
+}
+__device__ __forceinline__ int tree_ctx(const TreeAttend& a, int b) { return min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap); }
+__device__ __forceinline__ int tree_tiles(const TreeAttend& a, int b, int kt) {
+    return max(1, (tree_top(a, b) + kt - 1) / kt + (tree_ctx(a, b) + kt - 1) / kt);
+}
+
+// The work of a call: items (sequence, key head, block of rows), sequence by sequence, each tree_tiles() tiles long, laid
+// end to end and cut into `used` equal runs, one per block.  A run may begin and end inside an item; an item cut by a
+// run's end is finished by tree_combine_kernel.
+struct TreeRun {
+    long long t, t_end, total;         // this block's tiles
+    long long seq_t;                   // first tile of sequence b
+    int b, used;
+};
+__device__ __forceinline__ long long tree_run_start(int c, long long total, int used) { return (long long)c * total / used; }
+__device__ __forceinline__ int tree_run_owner(long long t, long long total, int used) { return (int)(((t + 1) * used - 1) / total); }
+
+struct TreeRunShared { long long sums[33]; long long seq_t; int b; };
+
+// Called by all NT threads of a block; the lengths are scanned by the block itself (B numbers out of the L2), so no
+// kernel has to plan ahead and no length comes to the host.  `least`: tiles a run should have before the work is cut further.
+template <int NT>
+__device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int least, TreeRunShared* sh) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.B + NT - 1) / NT, b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
+    long long sum = 0;
+    for (int b = b_lo; b < b_hi; ++b) sum += (long long)tree_tiles(a, b, kt) * items_per_seq;
+    long long pre = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(kFullMask, pre, o);
+        if (lane >= o) pre += v;
+    }
+    if (lane == 31) sh->sums[warp] = pre;
+    __syncthreads();
+    long long before = 0, total = 0;
+    for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) before += sh->sums[w];
+        total += sh->sums[w];
+    }
+    pre += before - sum;                                   // tiles before this thread's sequences
+    TreeRun r;
+    r.total = total;
+    r.used = (int)min((long long)gridDim.x, max(1LL, total / least));
+    r.t = r.t_end = 0;
+    if ((int)blockIdx.x < r.used) {
+        r.t = tree_run_start(blockIdx.x, total, r.used);
+        r.t_end = tree_run_start(blockIdx.x + 1, total, r.used);
+        if (r.t >= pre && r.t < pre + sum) {
+            int b = b_lo;
+            for (;;) {
+                const long long len = (long long)tree_tiles(a, b, kt) * items_per_seq;
+                if (r.t < pre + len) break;
+                pre += len; ++b;
+            }
+            sh->b = b; sh->seq_t = pre;
+        }
+    }
+    __syncthreads();
+    r.b = sh->b; r.seq_t = sh->seq_t;
+    return r;
+}
+
+// One piece of a run: a stretch of one item's tiles.
+struct TreePiece {
+    int b, h, rb;                      // sequence, key head, block of rows
+    int tile, tiles, item_tiles;       // first tile, how many, of how many
+    int arena_tiles, top, ctx;
+    int slot;                          // where a partial result goes: 0 the run's first piece, 1 a later (its last) one
+    bool whole;                        // the item begins and ends in this piece
+};
+__device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int row_blocks, bool first, TreePiece* p) {
+    if (r.t >= r.t_end) return false;
+    const int per_seq = a.K * row_blocks;
+    int T = tree_tiles(a, r.b, kt);
+    while (r.t >= r.seq_t + (long long)T * per_seq) {       // (at most one step: runs have no gaps)
+        r.seq_t += (long long)T * per_seq; ++r.b;
+        T = tree_tiles(a, r.b, kt);
+    }
+    const int off = (int)(r.t - r.seq_t), item = off / T;
+    p->b = r.b; p->h = item / row_blocks; p->rb = item - p->h * row_blocks;
+    p->tile = off - item * T;
+    p->item_tiles = T;
+    p->tiles = (int)min((long long)(T - p->tile), r.t_end - r.t);
+    p->top = tree_top(a, r.b); p->ctx = tree_ctx(a, r.b);
+    p->arena_tiles = (p->top + kt - 1) / kt;
+    p->whole = p->tile == 0 && p->tiles == T;
+    p->slot = first ? 0 : 1;
+    r.t += p->tiles;
+    return true;
+}
+// The first key place of a tile and how many places of it exist.
+__device__ __forceinline__ void tree_tile_span(const TreeAttend& a, const TreePiece& p, int tile, int kt, int* place, int* count) {
+    if (tile < p.arena_tiles) { *place = tile * kt; *count = min(kt, p.top - *place); return; }
+    const int c = (tile - p.arena_tiles) * kt;
+    *place = a.A + c; *count = max(0, min(kt, p.ctx - c));
+}
+// What the combining kernel is told: block c (whose run begins inside an item begun by block c - 1) names the item and
+// the last block working on it.
+__device__ __forceinline__ void tree_write_meta(const TreeAttend& a, const TreeRun& r, const TreePiece* first_piece, int kt, int row_blocks) {
+    int4 m = make_int4(-1, 0, 0, 0);
+    if (first_piece && first_piece->tile > 0) {
+        const TreePiece& p = *first_piece;
+        const long long begin = tree_run_start(blockIdx.x, r.total, r.used) - p.tile;
+        if (tree_run_owner(begin, r.total, r.used) == (int)blockIdx.x - 1) {
+            const int last = tree_run_owner(begin + p.item_tiles - 1, r.total, r.used);
+            const long long prev = tree_run_start((int)blockIdx.x - 1, r.total, r.used);
+            m = make_int4(p.b, p.h * row_blocks + p.rb, last, prev == begin ? 0 : 1);
+        }
+    }
+    a.meta[blockIdx.x] = m;
+}
+
+}  // namespace dba
