@@ -15,6 +15,7 @@ struct dba_tree {
     float *part_ml, *part_o;
     long long wait_clocks;
     int drop_item;
+    uint32_t calls;                // of the attention
     uint64_t launches;
 };
 
@@ -164,8 +165,11 @@ dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* q, const dba_kv_ca
     a.q_seq = q->q_seq_stride; a.q_row = q->q_row_stride; a.q_head = q->q_head_stride;
     a.o_seq = q->out_seq_stride; a.o_row = q->out_row_stride; a.o_head = q->out_head_stride;
     a.scale_log2e = (float)((double)q->scale * 1.4426950408889634);
+    if (a.scale_log2e == 0.f) a.scale_log2e = 1e-37f;         // all scores alike; the kernels multiply -inf by it
     a.part_o = h->part_o; a.part_ml = h->part_ml; a.meta = h->meta;
     a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
+    if (++h->calls == 0) h->calls = 1;         // (0: no call has failed)
+    a.call = h->calls;
     int n = 0;
     // (planned for the configuration's rows: the workspace was sized for that)
     const cudaError_t e = launch_tree_attend(a, plan_tree_attend(c.dtype, c.rows * a.G, c.head_dim, h->sm_count), c.dtype, h->stream, &n);

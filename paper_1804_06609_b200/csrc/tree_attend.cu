@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
             live[i] = r < rows_here;
             if (a.masks && live[i]) {                    // an empty mask closes the row
                 uint32_t any = 0;
-                for (int w = 0; w < a.W; ++w) any |= __ldg(mask[i] + w);
+                for (int w = 0; w < (pc.top + 31) / 32; ++w) any |= __ldg(mask[i] + w);
                 live[i] = any != 0;
             }
 #pragma unroll
@@ -237,6 +237,15 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(const TreeAttend a, i
     grid_dependency_wait();
     allow_dependents();
     const int lane = threadIdx.x & 31;
+    if (a.pages.status[1] == a.call) {       // a wait of this call ran out: nothing it wrote can be trusted
+        const int64_t rows = (int64_t)a.B * a.n * a.H, blocks = (int64_t)gridDim.x * gridDim.y, me = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+        for (int64_t i = me * 256 + threadIdx.x; i < rows * a.D; i += blocks * 256) {
+            const int64_t r = i / a.D, tok = r / a.H, b = tok / a.n;
+            tree_store((T*)a.out + b * a.o_seq + (tok - b * a.n) * a.o_row + (r - tok * a.H) * a.o_head + (i - r * a.D), __int_as_float(0x7fc00000));
+            if (a.lse && i == r * a.D) a.lse[r] = __int_as_float(0x7fc00000);
+        }
+        return;
+    }
     const int4 meta = a.meta[blockIdx.x];
     if (meta.x < 0) return;
     const int M = a.n * a.G, row_blocks = (M + item_rows - 1) / item_rows;
@@ -279,15 +288,20 @@ template <typename T, int DP>
 cudaError_t launch_plain(const TreeAttend& a, int grid, cudaStream_t st) {
     return launch_after(tree_attend_plain_kernel<T, DP>, dim3(grid), dim3(kGThreads), sizeof(GSmem<DP>), st, a);
 }
-template <typename T>
-cudaError_t launch_plain_t(const TreeAttend& a, int grid, cudaStream_t st) {
-    return a.D <= 64 ? launch_plain<T, 64>(a, grid, st) : a.D <= 128 ? launch_plain<T, 128>(a, grid, st) : launch_plain<T, 256>(a, grid, st);
+cudaError_t launch_fp32(const TreeAttend& a, int grid, cudaStream_t st) {
+    return a.D <= 64 ? launch_plain<float, 64>(a, grid, st) : a.D <= 128 ? launch_plain<float, 128>(a, grid, st) : launch_plain<float, 256>(a, grid, st);
 }
 
 }  // namespace
 
 TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count) {
     TreeAttendPlan p{};
+    if (tree_mma_usable(dtype, D)) {
+        p.tensor = true;
+        p.rows = tree_mma_rows();
+        p.grid = tree_mma_blocks_per_sm(D) * sm_count;
+        return p;
+    }
     p.rows = kGRows;
     p.grid = 2 * sm_count;                 // two blocks of up to 105 KB of shared memory share an SM
     return p;
@@ -297,14 +311,14 @@ cudaError_t configure_tree_attend() {
     cudaError_t e = configure_plain<float, 64>();
     if (e == cudaSuccess) e = configure_plain<float, 128>();
     if (e == cudaSuccess) e = configure_plain<float, 256>();
-    if (e == cudaSuccess) e = configure_plain<__nv_bfloat16, 64>();
-    if (e == cudaSuccess) e = configure_plain<__nv_bfloat16, 128>();
     if (e == cudaSuccess) e = configure_plain<__nv_bfloat16, 256>();
+    if (e == cudaSuccess) e = configure_tree_mma();
     return e;
 }
 
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
-    cudaError_t e = dtype == DBA_F32 ? launch_plain_t<float>(a, plan.grid, st) : launch_plain_t<__nv_bfloat16>(a, plan.grid, st);
+    cudaError_t e = plan.tensor ? launch_tree_mma(a, plan.grid, st)
+                    : dtype == DBA_F32 ? launch_fp32(a, plan.grid, st) : launch_plain<__nv_bfloat16, 256>(a, plan.grid, st);
     if (e != cudaSuccess) return e;
     const int rows = a.n * a.G < plan.rows ? a.n * a.G : plan.rows;
     const dim3 grid(plan.grid, (rows + 7) / 8);

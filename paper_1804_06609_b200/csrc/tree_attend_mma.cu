@@ -1,0 +1,555 @@
+// Attention of the rows of a token tree over a paged cache on the tensor cores: bf16, head sizes up to 128.
+//
+// For one (sequence, key head) the rows of all its query heads are one matrix Q [rows, D], and
+//     S = Q K^T (tcgen05.mma, both operands in shared memory),  P = 2^(scale log2(e) S - m),  O += P V (P from tensor memory),
+// tile by tile of 64 keys, so a key and a value leave HBM once per 128 rows however many hypotheses read them.
+//
+// A block is one stream of tiles (its run of the work, see tree_device.cuh); two (head size 128) or three (64) blocks
+// share an SM, so that the steps of one, load -> S -> P -> O, fall into the gaps of the others.  Roles:
+//   warps 0-3  softmax: thread = row = lane of tensor memory.  Reads the row's 64 scores, keeps a reference m and the sum
+//              of the exponentials in fp32, writes P (bf16: half a unit in the 8th bit of every probability, as the
+//              matrix instruction needs it; the sum is taken before the rounding) over the scores.  m is only raised when the tile's maximum
+//              is more than 2^8 above it; then the row's O is rescaled in tensor memory.  Quotients are unaffected.
+//   warp 4     one thread issues the matrix instructions; allocates the tensor memory.
+//   warps 5-6  loader: 16-byte cp.async with zero fill, every place looked up in the page table by itself, so pages of any
+//              size may end inside a tile; written in the 128-byte swizzle both operand forms want: keys K-major, values
+//              MN-major ([key][d] either way).  Rows that do not exist, or that no row of the sequence sees, are zeros.
+// Values that are not finite would reach all rows of the tile through 0 * inf: in arena tiles (the only ones that rows see
+// differently) the loader looks its values over, puts zeros in their place and says so; the rows that do see such
+// a slot add it at the end.
+// Every wait on an mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
+#include <cuda_bf16.h>
+
+#include "tree_device.cuh"
+
+namespace dba {
+
+namespace {
+
+constexpr int kMRows = 128;                 // rows of an item (lanes of tensor memory)
+constexpr int kMKeys = 64;                  // keys of a tile
+constexpr int kMStages = 5;                 // tiles of keys or values in shared memory
+constexpr int kMLag = kMStages - 2;         // copies in flight behind the one being issued
+constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
+constexpr int kMThreads = 128 + 32 + kLoadThreads;
+constexpr int kBadSlots = 8;
+constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
+constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
+
+template <int DP> struct MConf {
+    static constexpr int stage_bytes = kMKeys * DP * 2;
+    static constexpr int q_bytes = kMRows * DP * 2;
+    static constexpr int q_bufs = DP == 64 ? 2 : 1;
+    static constexpr int s_bufs = DP == 64 ? 1 : 2;
+    static constexpr int blocks_per_sm = DP == 64 ? 3 : 2;
+    static constexpr int tmem_cols = DP == 64 ? 128 : 256;
+    static constexpr int o_col = 0, s_col = DP;
+};
+
+template <int DP> struct MSmem {
+    using C = MConf<DP>;
+    alignas(1024) unsigned char q[C::q_bufs][C::q_bytes];
+    alignas(1024) unsigned char kv[kMStages][C::stage_bytes];
+    uint64_t full[kMStages], empty[kMStages];
+    uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
+    uint64_t q_empty[C::q_bufs];
+    uint64_t pv_done, o_free, told;
+    uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
+    uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
+    uint32_t look[kLoadWarps][kMStages];    // (each loader warp for itself) 1 + the piece whose values in this stage are to be looked over, or 0
+    uint64_t last;
+    uint32_t tmem_base;
+    int abort_flag;
+    TreeRunShared run;
+};
+
+__device__ __forceinline__ uint32_t msmem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait.  False: the block is winding down.
+__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    const long long t0 = clock64();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)
+            if (mbar_try(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (clock64() - t0 > limit) break;
+    }
+    *abort_flag = 1;
+    return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return mbar_try(bar, parity) || mbar_wait_slow(bar, parity, abort_flag, limit);
+}
+// The same for a whole warp that works in step: every lane gets one answer.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag, limit));
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Shared-memory operand in the 128-byte swizzle; `lead`: bytes between blocks of 64 columns of an MN-major operand.
+__device__ __forceinline__ uint64_t sw128_desc(uint32_t addr, uint32_t lead) {
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lead >> 4) & 0x3fffu) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// bf16 x bf16 -> fp32, M = 128
+__host__ __device__ constexpr uint32_t mma_idesc(int n, bool b_mn_major) {
+    return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(kMRows >> 4) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives on the mbarrier once every matrix instruction issued so far by this thread has completed
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* u) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+          "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+          "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(addr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]),
+        "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
+        "r"(u[30]), "r"(u[31])
+        : "memory");
+}
+// Waits for the loads issued so far; the registers are named so that nothing that uses them is moved before the wait.
+__device__ __forceinline__ void tm_wait_ld(uint32_t* u) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
+          "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]),
+          "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]), "+r"(u[25]), "+r"(u[26]), "+r"(u[27]),
+          "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31])
+        :: "memory");
+}
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// bits 0-15: lo, 16-31: hi
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// bf16 halves of a word that are not finite, zeroed; *found is set if there are any
+__device__ __forceinline__ uint32_t only_finite(uint32_t x, bool* found) {
+    uint32_t r = x;
+    if ((x & 0x00007f80u) == 0x00007f80u) { r &= 0xffff0000u; *found = true; }
+    if ((x & 0x7f800000u) == 0x7f800000u) { r &= 0x0000ffffu; *found = true; }
+    return r;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
+    using C = MConf<DP>;
+    extern __shared__ __align__(1024) unsigned char mraw[];
+    MSmem<DP>& sm = *reinterpret_cast<MSmem<DP>*>(mraw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abort_flag = &sm.abort_flag;
+    const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
+    const int M = a.n * a.G, row_blocks = (M + kMRows - 1) / kMRows;
+
+    if (tid == 0) {
+        for (int s = 0; s < kMStages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
+        // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
+        // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
+        // may be a product ahead of it)
+        for (int s = 0; s < C::s_bufs; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s]), 4); }
+        for (int s = 0; s < C::q_bufs; ++s) mbar_init(msmem_u32(&sm.q_empty[s]), 1);
+        mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), 4);
+        mbar_init(msmem_u32(&sm.last), 1);
+        for (int i = 0; i < kBadSlots; ++i) sm.bad[i] = 0;
+        sm.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 4) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(msmem_u32(&sm.tmem_base)), "r"(C::tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    grid_dependency_wait();
+    allow_dependents();
+    TreeRun run = tree_run<kMThreads>(a, kMKeys, a.K * row_blocks, 1, &sm.run);      // (has the block's barriers)
+    tc_after();
+    const uint32_t tmem = sm.tmem_base;
+    TreePiece pc;
+
+    if (warp >= 5) {
+        // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
+        constexpr int CH = DP / 8;                     // 16-byte chunks of a row
+        constexpr int RW = 32 / CH;                    // rows the warp copies at a time
+        const int lw = warp - 5, ch = lane % CH, sub = lane / CH;
+        const bool ch_in = ch * 8 < a.D;
+        const uint32_t ch_kv = (uint32_t)(ch >> 3) * (kMKeys * 128), ch_q = (uint32_t)(ch >> 3) * (kMRows * 128);
+        uint32_t step = 0, handed = 0;                 // copies issued, and handed on to the matrix products
+        bool ok = true;
+        auto hand_on = [&]() {                         // copy `handed` has landed
+            const uint32_t s = handed % kMStages, look = sm.look[lw][s];
+            if (look) {
+                bool found = false;
+#pragma unroll 4
+                for (int j = 0; j < 32 / RW; ++j) {
+                    const int r = lw * 32 + j * RW + sub;
+                    uint4* p = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + ((ch & 7) ^ (r & 7)) * 16);
+                    uint4 x = *p;
+                    bool f = false;
+                    x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
+                    if (f) { *p = x; found = true; }
+                }
+                if (found) sm.bad[(look - 1) % kBadSlots] = look;
+            }
+            fence_async_proxy();
+            __syncwarp();
+            if (lane == 0 && (int)handed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[s]));
+            ++handed;
+        };
+        // waits for a barrier on which it may depend that everything issued has been handed on
+        auto wait_all_handed = [&](uint32_t bar, uint32_t parity) {
+            if (__all_sync(kFullMask, mbar_try(bar, parity))) return true;
+            cp_wait<0>();
+            while (handed < step) hand_on();
+            return mbar_wait_warp(bar, parity, abort_flag, limit);
+        };
+        // one tile of keys or values; `at`: the cache row of the warp's row `lane`, -1 for zeros
+        auto load = [&](const void* base, int64_t at, int h, uint32_t look) {
+            const uint32_t s = step % kMStages, use = step / kMStages;
+            if (use > 0 && !mbar_wait_warp(msmem_u32(&sm.empty[s]), (use - 1) & 1u, abort_flag, limit)) return false;
+            const __nv_bfloat16* p = (const __nv_bfloat16*)base + (int64_t)h * a.pages.head_stride + ch * 8;
+            const uint32_t dst = msmem_u32(sm.kv[s]) + ch_kv;
+#pragma unroll
+            for (int j = 0; j < 32 / RW; ++j) {
+                const int64_t row = __shfl_sync(kFullMask, at, j * RW + sub);
+                const int r = lw * 32 + j * RW + sub;
+                const bool in = row >= 0 && ch_in;
+                cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16, in ? (const void*)(p + row) : a.k, in ? 16u : 0u);
+            }
+            cp_commit();
+            if (lane == 0) sm.look[lw][s] = look;
+            __syncwarp();
+            ++step;
+            cp_wait<kMLag>();
+            if (step - handed > kMLag) hand_on();
+            return true;
+        };
+        bool first = true;
+        int piece = 0, tile_no = 0;
+        while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
+            first = false;
+            // queries of the item: beyond the rows (to the next 32) and the head size, zeros
+            const uint32_t qb = piece % C::q_bufs, q_use = piece / C::q_bufs;
+            if (q_use > 0 && !wait_all_handed(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u)) { ok = false; break; }
+            {
+                const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (int64_t)pc.b * a.q_seq + ch * 8;
+                const uint32_t dst = msmem_u32(sm.q[qb]) + ch_q;
+                const int rows_here = min(kMRows, M - pc.rb * kMRows), rows_pad = (rows_here + 31) / 32 * 32;
+#pragma unroll 2
+                for (int r = lw * RW + sub; r < rows_pad; r += kLoadWarps * RW) {
+                    const int rr = pc.rb * kMRows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
+                    const bool in = r < rows_here && ch_in;
+                    cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16,
+                               in ? (const void*)(q + (int64_t)tok * a.q_row + (int64_t)head * a.q_head) : a.q, in ? 16u : 0u);
+                }                                       // (they join the first keys' group)
+            }
+            int64_t v_at = -1;
+            uint32_t v_look = 0;
+            for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++tile_no) {
+                int place, count;
+                tree_tile_span(a, pc, t, kMKeys, &place, &count);
+                const int mine = place + lw * 32 + lane;
+                bool want = lw * 32 + lane < count;
+                uint32_t look = 0;
+                if (t < pc.arena_tiles) {               // slots no row of the sequence sees are not read
+                    const int w = (place >> 5) + lw;
+                    uint32_t any = 0;
+                    if (w < a.W)
+                        for (int i = lane; i < a.n; i += 32) any |= __ldg(a.masks + ((int64_t)pc.b * a.n + i) * a.W + w);
+                    any = __reduce_or_sync(kFullMask, any);
+                    want = want && ((any >> lane) & 1u);
+                    look = (uint32_t)piece + 1;
+                }
+                const int64_t at = want ? tree_row(a.pages, pc.b, mine) : -1;
+                const uint32_t there = __ballot_sync(kFullMask, at >= 0);
+                if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
+                if (!load(a.k, at, pc.h, 0)) { ok = false; break; }
+                // one S in tensor memory: K0 V0 K1 V1 ..;  two: K0 K1 V0 K2 V1 .. (the products run one tile ahead)
+                if (C::s_bufs == 1) {
+                    if (!load(a.v, at, pc.h, look)) { ok = false; break; }
+                } else {
+                    if (t > pc.tile && !load(a.v, v_at, pc.h, v_look)) { ok = false; break; }
+                    v_at = at; v_look = look;
+                }
+            }
+            if (C::s_bufs > 1 && ok && !load(a.v, v_at, pc.h, v_look)) ok = false;
+            ++piece;
+        }
+        cp_wait<0>();
+        while (ok && handed < step) hand_on();
+    } else if (warp == 4) {
+        // ------------------------------------------------------------------ matrix products
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
+            const int ks_n = (a.D + 15) / 16;
+            uint32_t step = 0;
+            bool ok = true, first = true;
+            int piece = 0;
+            uint32_t g = 0;
+            auto scores = [&](uint32_t gi, int qb) {
+                const uint32_t s = step % kMStages;
+                if (!mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit)) return false;
+                tc_after();
+                const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]), 16), dk = sw128_desc(msmem_u32(sm.kv[s]), 16);
+                const uint32_t d = tmem + C::s_col + (gi % C::s_bufs) * kMKeys;
+                for (int ks = 0; ks < ks_n; ++ks)       // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns
+                    mma_ss(d, dq + (uint64_t)((ks >> 2) * (kMRows * 128 / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kMKeys * 128 / 16) + (ks & 3) * 2),
+                           idesc_s | negate, ks != 0);
+                mma_commit(msmem_u32(&sm.empty[s]));
+                mma_commit(msmem_u32(&sm.s_full[gi % C::s_bufs]));
+                mbar_arrive(msmem_u32(&sm.s_full[gi % C::s_bufs]));
+                ++step;
+                return true;
+            };
+            while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
+                first = false;
+                const int qb = piece % C::q_bufs;
+                ok = scores(g, qb);
+                if (ok && pc.tiles == 1) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                for (int t = 0; t < pc.tiles && ok; ++t, ++g) {
+                    if (C::s_bufs > 1 && t + 1 < pc.tiles) {
+                        if (!(ok = scores(g + 1, qb))) break;
+                        if (t + 2 == pc.tiles) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                    }
+                    const uint32_t sb = g % C::s_bufs, s = step % kMStages;
+                    if (!(ok = mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit))) break;
+                    if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
+                    if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
+                    tc_after();
+                    const uint64_t dv = sw128_desc(msmem_u32(sm.kv[s]), kMKeys * 128);
+                    const uint32_t p = tmem + C::s_col + sb * kMKeys;
+#pragma unroll
+                    for (int ks = 0; ks < kMKeys / 16; ++ks)          // 16 keys = two groups of eight rows of 128 bytes
+                        mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, (t | ks) != 0);
+                    mma_commit(msmem_u32(&sm.empty[s]));
+                    mma_commit(msmem_u32(&sm.pv_done));
+                    if (t + 1 == pc.tiles) mbar_arrive(msmem_u32(&sm.told));
+                    ++step;
+                    if (C::s_bufs == 1 && t + 1 < pc.tiles) {
+                        if (!(ok = scores(g + 1, qb))) break;
+                        if (t + 2 == pc.tiles) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                    }
+                }
+                ++piece;
+            }
+            // nothing of this block is in flight when it leaves, whatever happened
+            mma_commit(msmem_u32(&sm.last));
+            for (int i = 0; i < 1000000 && !mbar_try(msmem_u32(&sm.last), 0); ++i) {}
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax: a row per thread
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const float scale = fabsf(a.scale_log2e);
+        bool ok = true, first = true;
+        int piece = 0;
+        uint32_t g = 0;
+        if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, kMKeys, row_blocks);
+        while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
+            if (first && tid == 0) tree_write_meta(a, run, &pc, kMKeys, row_blocks);
+            first = false;
+            const int row = warp * 32 + lane, rr = pc.rb * kMRows + row;
+            const bool active = pc.rb * kMRows + warp * 32 < M;       // the warp has rows
+            const int tok = min(rr, M - 1) / a.G, head = pc.h * a.G + rr - tok * a.G;
+            const uint32_t* mask = a.masks ? a.masks + ((int64_t)pc.b * a.n + tok) * a.W : nullptr;
+            bool live = rr < M;
+            if (active && mask) {                                     // an empty mask closes the row
+                uint32_t any = 0;
+#pragma unroll 8
+                for (int w = 0; w < (pc.top + 31) / 32; ++w) any |= __ldg(mask + w);
+                live = live && any != 0;
+            }
+            float ref = neg_inf(), sum = 0.f;
+            for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++g) {
+                const uint32_t sb = g % C::s_bufs;
+                uint32_t see0 = 0xffffffffu, see1 = 0xffffffffu;
+                if (active && t < pc.arena_tiles) {
+                    see0 = __ldg(mask + 2 * t);
+                    see1 = 2 * t + 1 < a.W ? __ldg(mask + 2 * t + 1) : 0u;
+                }
+                if (!mbar_wait_warp(msmem_u32(&sm.s_full[sb]), (g / C::s_bufs) & 1u, abort_flag, limit)) { ok = false; break; }
+                if (active) {
+                    tc_after();
+                    see0 &= sm.seen[g % kBadSlots][0]; see1 &= sm.seen[g % kBadSlots][1];
+                    if (!live) see0 = see1 = 0;
+                    uint32_t u[kMKeys];
+                    tm_ld32(tmem + lanes + C::s_col + sb * kMKeys, u);
+                    tm_ld32(tmem + lanes + C::s_col + sb * kMKeys + 32, u + 32);
+                    tm_wait_ld(u);
+                    tm_wait_ld(u + 32);
+                    float x[kMKeys];
+#pragma unroll
+                    for (int j = 0; j < kMKeys; ++j) x[j] = __uint_as_float(u[j]);
+                    if (__any_sync(kFullMask, (see0 & see1) != 0xffffffffu)) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            if (!((see0 >> j) & 1u)) x[j] = neg_inf();
+                            if (!((see1 >> j) & 1u)) x[32 + j] = neg_inf();
+                        }
+                    }
+                    float m0 = x[0], m1 = x[1], m2 = x[2], m3 = x[3];
+#pragma unroll
+                    for (int j = 4; j < kMKeys; j += 4) { m0 = fmaxf(m0, x[j]); m1 = fmaxf(m1, x[j + 1]); m2 = fmaxf(m2, x[j + 2]); m3 = fmaxf(m3, x[j + 3]); }
+                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;     // (scale 0 and nothing seen: NaN, not above anything)
+                    const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
+                    if (__any_sync(kFullMask, raise)) {
+                        const float factor = raise ? ex2(ref - top) : 1.f;             // 0 where nothing has been seen before
+                        if (raise) { ref = top; sum *= factor; }
+                        if (t > pc.tile) {
+                            if (!mbar_wait_warp(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                            tc_after();
+#pragma unroll 1
+                            for (int c = 0; c < DP; c += 32) {
+                                uint32_t o[32];
+                                tm_ld32(tmem + lanes + C::o_col + c, o);
+                                tm_wait_ld(o);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
+                                tm_st32(tmem + lanes + C::o_col + c, o);
+                            }
+                        }
+                    }
+                    const float shift = ref == neg_inf() ? 0.f : -ref;
+                    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                    uint32_t p[kMKeys / 2];
+#pragma unroll
+                    for (int j = 0; j < kMKeys; j += 4) {
+                        const float e0 = ex2(fmaf(x[j], scale, shift)), e1 = ex2(fmaf(x[j + 1], scale, shift));
+                        const float e2 = ex2(fmaf(x[j + 2], scale, shift)), e3 = ex2(fmaf(x[j + 3], scale, shift));
+                        s0 += e0; s1 += e1; s2 += e2; s3 += e3;
+                        p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
+                    }
+                    sum += (s0 + s1) + (s2 + s3);
+                    tm_st32(tmem + lanes + C::s_col + sb * kMKeys, p);
+                    tm_wait_st();
+                    tc_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(msmem_u32(&sm.p_ready[sb]));
+            }
+            if (!ok) break;
+            if (!mbar_wait_warp(msmem_u32(&sm.told), piece & 1, abort_flag, limit)) { ok = false; break; }
+            if (!mbar_wait_warp(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+            if (active) {
+                tc_after();
+                const bool bad = sm.bad[piece % kBadSlots] == (uint32_t)piece + 1;
+                const float inv = pc.whole && sum > 0.f ? 1.f / sum : 1.f;
+                const int64_t part = (int64_t)(2 * blockIdx.x + pc.slot) * kMRows + row;
+                __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)pc.b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
+#pragma unroll 1
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t u[32];
+                    __syncwarp();
+                    tm_ld32(tmem + lanes + C::o_col + c, u);
+                    tm_wait_ld(u);
+                    if (rr >= M) continue;
+                    float o[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) o[j] = sum == 0.f ? 0.f : __uint_as_float(u[j]);
+                    if (bad && live)       // values that are not finite, at the slots this row sees
+                        for (int j = pc.tile * kMKeys; j < min((pc.tile + pc.tiles) * kMKeys, pc.top); ++j) {
+                            if (!((__ldg(mask + (j >> 5)) >> (j & 31)) & 1u)) continue;
+                            const int64_t at = tree_row(a.pages, pc.b, j);
+                            if (at < 0) continue;
+                            const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + at + (int64_t)pc.h * a.pages.head_stride;
+#pragma unroll 1
+                            for (int d = c; d < min(c + 32, a.D); ++d) {
+                                const float x = __bfloat162float(v[d]);
+                                if (!(fabsf(x) <= 3.4e38f)) {
+#pragma unroll
+                                    for (int k = 0; k < 32; ++k) if (k == d - c) o[k] += x;
+                                }
+                            }
+                        }
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        if (c + j >= a.D) continue;
+                        if (pc.whole) {
+                            uint4 w;
+                            w.x = pack_bf16(o[j] * inv, o[j + 1] * inv); w.y = pack_bf16(o[j + 2] * inv, o[j + 3] * inv);
+                            w.z = pack_bf16(o[j + 4] * inv, o[j + 5] * inv); w.w = pack_bf16(o[j + 6] * inv, o[j + 7] * inv);
+                            *reinterpret_cast<uint4*>(out + c + j) = w;
+                        } else {
+                            float4* po = reinterpret_cast<float4*>(a.part_o + part * a.D + c + j);
+                            po[0] = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                            po[1] = make_float4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                        }
+                    }
+                }
+                if (rr < M) {
+                    if (!pc.whole) { a.part_ml[2 * part] = ref; a.part_ml[2 * part + 1] = sum; }
+                    else if (a.lse) a.lse[((int64_t)pc.b * a.n + tok) * a.H + head] = sum == 0.f ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+                }
+                tc_before();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(msmem_u32(&sm.o_free));
+            ++piece;
+        }
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
+    if (tid == 0 && sm.abort_flag) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
+}
+
+template <int DP>
+cudaError_t configure_mma() {
+    return cudaFuncSetAttribute(tree_attend_mma_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP>));
+}
+template <int DP>
+cudaError_t launch_mma(const TreeAttend& a, int grid, cudaStream_t st) {
+    const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
+    return launch_after(tree_attend_mma_kernel<DP>, dim3(grid), dim3(kMThreads), sizeof(MSmem<DP>), st, a, negate);
+}
+
+}  // namespace
+
+bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
+int tree_mma_rows() { return kMRows; }
+int tree_mma_blocks_per_sm(int D) { return D <= 64 ? MConf<64>::blocks_per_sm : MConf<128>::blocks_per_sm; }
+cudaError_t configure_tree_mma() {
+    const cudaError_t e = configure_mma<64>();
+    return e == cudaSuccess ? configure_mma<128>() : e;
+}
+cudaError_t launch_tree_mma(const TreeAttend& a, int grid, cudaStream_t st) {
+    return a.D <= 64 ? launch_mma<64>(a, grid, st) : launch_mma<128>(a, grid, st);
+}
+
+}  // namespace dba

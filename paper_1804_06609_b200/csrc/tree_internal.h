@@ -39,6 +39,7 @@ struct TreeAttend {
     int4* meta;                        // [grid] item shared with the block before this one, if that block is the first on it
     long long wait_clocks;
     int drop_item;
+    uint32_t call;                     // number of the call: what a failed wait leaves in the second status word
 };
 
 struct TreeAttendPlan {
@@ -50,6 +51,12 @@ struct TreeAttendPlan {
 // The most an item's partial results take, for the workspace.
 TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count);
 cudaError_t configure_tree_attend();
+// the tensor-core kernel (tree_attend_mma.cu)
+bool tree_mma_usable(int dtype, int D);
+int tree_mma_rows();
+int tree_mma_blocks_per_sm(int D);
+cudaError_t configure_tree_mma();
+cudaError_t launch_tree_mma(const TreeAttend& a, int grid, cudaStream_t st);
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
 cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K,
                                int32_t D, int dtype, cudaStream_t st, int* launches);

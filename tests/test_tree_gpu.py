@@ -295,6 +295,28 @@ def test_a_handle_works_on_its_own_stream(dba):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("D,drop", [(64, 0), (128, 0), (128, 3)])
+def test_a_wait_that_runs_out_is_reported(dba, D, drop):
+    """The tensor-core kernel's waits are bounded: with one tile's hand-over withheld and a 1 ms limit the call ends, its
+    outputs are NaN, the status says why, and the next call is right."""
+    B, n, H, K, ps, W = 2, 3, 4, 2, 16, 1
+    rng = torch.Generator().manual_seed(13)
+    per = (32 + 40000) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, "bf16")
+    masks = _masks(rng, B, n, W, 0.3, closed=0.0).cuda()
+    q = torch.randn(B, n, H, D, generator=rng).to(torch.bfloat16).cuda()
+    c = torch.tensor([40000, 39000], dtype=torch.int32).cuda()          # some four tiles for every block
+    t = _tree(dba, B, n, H, K, D, ps, per, W)
+    lse = torch.zeros(B, n, H, device="cuda")
+    want = t.attend(q, k, v, table, c, masks, lse=lse).clone()
+    assert t.status() == 0 and torch.isfinite(want.float()).all()
+    t.test_hook(wait_clocks=2_000_000, drop_item=drop)
+    got = t.attend(q, k, v, table, c, masks, lse=lse)
+    assert t.status() == dba.TREE_TIMEOUT and torch.isnan(got.float()).all() and torch.isnan(lse).all()
+    t.test_hook()
+    assert torch.equal(t.attend(q, k, v, table, c, masks, lse=lse), want) and torch.isfinite(lse).all() and t.status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ append
 @pytest.mark.parametrize("N,H,K,D,rot,pairs,dtype,hnd,inplace", [
     (1, 1, 1, 64, 64, False, "bf16", False, False), (10, 8, 2, 128, 128, False, "bf16", False, True), (40, 8, 2, 128, 64, True, "bf16", True, False),
