@@ -29,7 +29,6 @@ namespace {
 constexpr int kMRows = 128;                 // rows of an item (lanes of tensor memory)
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kMStages = 5;                 // tiles of keys or values in shared memory
-constexpr int kMLag = kMStages - 2;         // copies in flight behind the one being issued
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
 constexpr int kMThreads = 128 + 32 + kLoadThreads;
 constexpr int kBadSlots = 8;
@@ -56,7 +55,6 @@ template <int DP> struct MSmem {
     uint64_t pv_done, o_free, told;
     uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
     uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
-    uint32_t look[kLoadWarps][kMStages];    // (each loader warp for itself) 1 + the piece whose values in this stage are to be looked over, or 0
     uint64_t last;
     uint32_t tmem_base;
     int abort_flag;
@@ -95,8 +93,9 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// arrives on the mbarrier when this thread's copies so far have landed
+__device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -178,7 +177,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
     const int M = a.n * a.G, row_blocks = (M + kMRows - 1) / kMRows;
 
     if (tid == 0) {
-        for (int s = 0; s < kMStages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
+        for (int s = 0; s < kMStages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads); mbar_init(msmem_u32(&sm.empty[s]), 1); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
         // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
         // may be a product ahead of it)
@@ -209,36 +208,12 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
         const int lw = warp - 5, ch = lane % CH, sub = lane / CH;
         const bool ch_in = ch * 8 < a.D;
         const uint32_t ch_kv = (uint32_t)(ch >> 3) * (kMKeys * 128), ch_q = (uint32_t)(ch >> 3) * (kMRows * 128);
-        uint32_t step = 0, handed = 0;                 // copies issued, and handed on to the matrix products
+        uint32_t step = 0;                             // copies issued
         bool ok = true;
-        auto hand_on = [&]() {                         // copy `handed` has landed
-            const uint32_t s = handed % kMStages, look = sm.look[lw][s];
-            if (look) {
-                bool found = false;
-#pragma unroll 4
-                for (int j = 0; j < 32 / RW; ++j) {
-                    const int r = lw * 32 + j * RW + sub;
-                    uint4* p = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + ((ch & 7) ^ (r & 7)) * 16);
-                    uint4 x = *p;
-                    bool f = false;
-                    x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
-                    if (f) { *p = x; found = true; }
-                }
-                if (found) sm.bad[(look - 1) % kBadSlots] = look;
-            }
-            fence_async_proxy();
-            __syncwarp();
-            if (lane == 0 && (int)handed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[s]));
-            ++handed;
-        };
-        // waits for a barrier on which it may depend that everything issued has been handed on
-        auto wait_all_handed = [&](uint32_t bar, uint32_t parity) {
-            if (__all_sync(kFullMask, mbar_try(bar, parity))) return true;
-            cp_wait<0>();
-            while (handed < step) hand_on();
-            return mbar_wait_warp(bar, parity, abort_flag, limit);
-        };
-        // one tile of keys or values; `at`: the cache row of the warp's row `lane`, -1 for zeros
+        // One tile of keys or values; `at`: the cache row of the warp's row `lane`, -1 for zeros.  The stage is handed on by the
+        // copies themselves; the issuing thread of the matrix products has the fence between their writes and its reads
+        // (here it would wait for every copy in flight: twice the time on long contexts).  look > 0: values of an arena
+        // tile (of piece look - 1), waited for and looked over first.
         auto load = [&](const void* base, int64_t at, int h, uint32_t look) {
             const uint32_t s = step % kMStages, use = step / kMStages;
             if (use > 0 && !mbar_wait_warp(msmem_u32(&sm.empty[s]), (use - 1) & 1u, abort_flag, limit)) return false;
@@ -251,12 +226,23 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                 const bool in = row >= 0 && ch_in;
                 cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16, in ? (const void*)(p + row) : a.k, in ? 16u : 0u);
             }
-            cp_commit();
-            if (lane == 0) sm.look[lw][s] = look;
-            __syncwarp();
+            const uint32_t bar = msmem_u32(&sm.full[s]);
+            if (look) {
+                cp_wait_all();
+                bool found = false;
+#pragma unroll 4
+                for (int j = 0; j < 32 / RW; ++j) {
+                    const int r = lw * 32 + j * RW + sub;
+                    uint4* v = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + ((ch & 7) ^ (r & 7)) * 16);
+                    uint4 x = *v;
+                    bool f = false;
+                    x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
+                    if (f) { *v = x; found = true; }
+                }
+                if (found) sm.bad[(look - 1) % kBadSlots] = look;
+                if ((int)step != a.drop_item) mbar_arrive(bar);
+            } else if ((int)step != a.drop_item) cp_arrive(bar);
             ++step;
-            cp_wait<kMLag>();
-            if (step - handed > kMLag) hand_on();
             return true;
         };
         bool first = true;
@@ -265,7 +251,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
             first = false;
             // queries of the item: beyond the rows (to the next 32) and the head size, zeros
             const uint32_t qb = piece % C::q_bufs, q_use = piece / C::q_bufs;
-            if (q_use > 0 && !wait_all_handed(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u)) { ok = false; break; }
+            if (q_use > 0 && !mbar_wait_warp(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             {
                 const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (int64_t)pc.b * a.q_seq + ch * 8;
                 const uint32_t dst = msmem_u32(sm.q[qb]) + ch_q;
@@ -276,7 +262,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                     const bool in = r < rows_here && ch_in;
                     cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16,
                                in ? (const void*)(q + (int64_t)tok * a.q_row + (int64_t)head * a.q_head) : a.q, in ? 16u : 0u);
-                }                                       // (they join the first keys' group)
+                }                                       // (the first keys' arrival counts them too)
             }
             int64_t v_at = -1;
             uint32_t v_look = 0;
@@ -310,8 +296,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
             if (C::s_bufs > 1 && ok && !load(a.v, v_at, pc.h, v_look)) ok = false;
             ++piece;
         }
-        cp_wait<0>();
-        while (ok && handed < step) hand_on();
+        cp_wait_all();
     } else if (warp == 4) {
         // ------------------------------------------------------------------ matrix products
         if (lane == 0) {
@@ -324,6 +309,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
             auto scores = [&](uint32_t gi, int qb) {
                 const uint32_t s = step % kMStages;
                 if (!mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit)) return false;
+                fence_async_proxy();                   // the copies' writes (generic) before the products' reads
                 tc_after();
                 const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]), 16), dk = sw128_desc(msmem_u32(sm.kv[s]), 16);
                 const uint32_t d = tmem + C::s_col + (gi % C::s_bufs) * kMKeys;
@@ -350,6 +336,7 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                     if (!(ok = mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit))) break;
                     if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
                     if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
+                    fence_async_proxy();
                     tc_after();
                     const uint64_t dv = sw128_desc(msmem_u32(sm.kv[s]), kMKeys * 128);
                     const uint32_t p = tmem + C::s_col + sb * kMKeys;
