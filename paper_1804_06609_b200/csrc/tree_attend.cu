@@ -298,8 +298,8 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count) {
     TreeAttendPlan p{};
     if (tree_mma_usable(dtype, D)) {
         p.tensor = true;
-        p.rows = tree_mma_rows();
-        p.grid = tree_mma_blocks_per_sm(D) * sm_count;
+        p.rows = tree_mma_rows(M);
+        p.grid = tree_mma_blocks_per_sm(D, p.rows) * sm_count;
         return p;
     }
     p.rows = kGRows;
@@ -317,7 +317,7 @@ cudaError_t configure_tree_attend() {
 }
 
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
-    cudaError_t e = plan.tensor ? launch_tree_mma(a, plan.grid, st)
+    cudaError_t e = plan.tensor ? launch_tree_mma(a, plan.rows, plan.grid, st)
                     : dtype == DBA_F32 ? launch_fp32(a, plan.grid, st) : launch_plain<__nv_bfloat16, 256>(a, plan.grid, st);
     if (e != cudaSuccess) return e;
     const int rows = a.n * a.G < plan.rows ? a.n * a.G : plan.rows;

@@ -26,36 +26,39 @@ namespace dba {
 
 namespace {
 
-constexpr int kMRows = 128;                 // rows of an item (lanes of tensor memory)
+constexpr int kMRows = 128;                 // rows of the matrix instructions (lanes of tensor memory)
 constexpr int kMKeys = 64;                  // keys of a tile
-constexpr int kMStages = 5;                 // tiles of keys or values in shared memory
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
-constexpr int kMThreads = 128 + 32 + kLoadThreads;
 constexpr int kBadSlots = 8;
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
 
-template <int DP> struct MConf {
+// SW softmax warps = items of up to 32 SW rows.  The products always work on 128 rows; with SW = 1 the other 96 are whatever
+// follows the queries in shared memory, and nobody reads their results.
+template <int DP, int SW> struct MConf {
+    static constexpr int rows = 32 * SW;
+    static constexpr int threads = 32 * (SW + 1 + kLoadWarps);
+    static constexpr int stages = SW == 1 && DP == 128 ? 6 : 5;      // tiles of keys or values in shared memory
     static constexpr int stage_bytes = kMKeys * DP * 2;
-    static constexpr int q_bytes = kMRows * DP * 2;
-    static constexpr int q_bufs = DP == 64 ? 2 : 1;
+    static constexpr int q_half = rows * 128;                        // 64 columns of the queries
+    static constexpr int q_bytes = rows * DP * 2;
+    static constexpr int q_bufs = DP == 64 || SW == 1 ? 2 : 1;
     static constexpr int s_bufs = DP == 64 ? 1 : 2;
-    static constexpr int blocks_per_sm = DP == 64 ? 3 : 2;
+    static constexpr int blocks_per_sm = DP == 128 ? 2 : SW == 1 ? 4 : 3;
     static constexpr int tmem_cols = DP == 64 ? 128 : 256;
     static constexpr int o_col = 0, s_col = DP;
 };
 
-template <int DP> struct MSmem {
-    using C = MConf<DP>;
+template <int DP, int SW> struct MSmem {
+    using C = MConf<DP, SW>;
     alignas(1024) unsigned char q[C::q_bufs][C::q_bytes];
-    alignas(1024) unsigned char kv[kMStages][C::stage_bytes];
-    uint64_t full[kMStages], empty[kMStages];
+    alignas(1024) unsigned char kv[C::stages][C::stage_bytes];
+    uint64_t full[C::stages], empty[C::stages];
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
     uint64_t q_empty[C::q_bufs];
-    uint64_t pv_done, o_free, told;
+    uint64_t pv_done, o_free, told, last;
     uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
     uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
-    uint64_t last;
     uint32_t tmem_base;
     int abort_flag;
     TreeRunShared run;
@@ -70,30 +73,29 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Bounded wait.  False: the block is winding down.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    const long long t0 = clock64();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 32; ++i)
-            if (mbar_try(bar, parity)) return true;
-        if (*abort_flag) return false;
-        if (clock64() - t0 > limit) break;
-    }
-    *abort_flag = 1;
-    return false;
-}
+// Bounded wait of a whole warp in step: every lane gets one answer.  False: the block is winding down.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    return mbar_try(bar, parity) || mbar_wait_slow(bar, parity, abort_flag, limit);
-}
-// The same for a whole warp that works in step: every lane gets one answer.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    return __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag, limit));
+    if (__all_sync(kFullMask, mbar_try(bar, parity))) return true;
+    const long long t0 = clock64();
+    bool done = false;
+#pragma unroll 1
+    for (uint32_t i = 1; !done; ++i) {
+        done = __all_sync(kFullMask, mbar_try(bar, parity));
+        if (!done && (i & 31u) == 0) {
+            const bool late = *abort_flag != 0 || clock64() - t0 > limit;
+            if (__any_sync(kFullMask, late)) {
+                *abort_flag = 1;
+                return false;
+            }
+        }
+    }
+    return true;
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // arrives on the mbarrier when this thread's copies so far have landed
 __device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -119,11 +121,14 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// Consecutive columns of this thread's lane of tensor memory.  Load and wait are one statement: between them the registers
+// are still being written, and the compiler may copy or reuse registers between any two statements.
 __device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* u) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
           "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
           "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
@@ -141,15 +146,6 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
         "r"(u[30]), "r"(u[31])
         : "memory");
 }
-// Waits for the loads issued so far; the registers are named so that nothing that uses them is moved before the wait.
-__device__ __forceinline__ void tm_wait_ld(uint32_t* u) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
-          "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]),
-          "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]), "+r"(u[25]), "+r"(u[26]), "+r"(u[27]),
-          "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31])
-        :: "memory");
-}
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // bits 0-15: lo, 16-31: hi
@@ -166,57 +162,77 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x, bool* found) {
     return r;
 }
 
-template <int DP>
-__global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
-    using C = MConf<DP>;
+template <int DP, int SW>
+__global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
+    using C = MConf<DP, SW>;
     extern __shared__ __align__(1024) unsigned char mraw[];
-    MSmem<DP>& sm = *reinterpret_cast<MSmem<DP>*>(mraw);
+    MSmem<DP, SW>& sm = *reinterpret_cast<MSmem<DP, SW>*>(mraw);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abort_flag = &sm.abort_flag;
     const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
-    const int M = a.n * a.G, row_blocks = (M + kMRows - 1) / kMRows;
+    const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows;
 
     if (tid == 0) {
-        for (int s = 0; s < kMStages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads); mbar_init(msmem_u32(&sm.empty[s]), 1); }
+        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads); mbar_init(msmem_u32(&sm.empty[s]), 1); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
         // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
         // may be a product ahead of it)
-        for (int s = 0; s < C::s_bufs; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s]), 4); }
+        for (int s = 0; s < C::s_bufs; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s]), SW); }
         for (int s = 0; s < C::q_bufs; ++s) mbar_init(msmem_u32(&sm.q_empty[s]), 1);
-        mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), 4);
+        mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), SW);
         mbar_init(msmem_u32(&sm.last), 1);
         for (int i = 0; i < kBadSlots; ++i) sm.bad[i] = 0;
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 4) {
+    if (warp == SW) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(msmem_u32(&sm.tmem_base)), "r"(C::tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_before();
     grid_dependency_wait();
     allow_dependents();
-    TreeRun run = tree_run<kMThreads>(a, kMKeys, a.K * row_blocks, 1, &sm.run);      // (has the block's barriers)
+    TreeRun run = tree_run<C::threads>(a, kMKeys, a.K * row_blocks, 1, &sm.run);      // (has the block's barriers)
     tc_after();
     const uint32_t tmem = sm.tmem_base;
-    TreePiece pc;
+    // every role walks the pieces of the run for itself, one ahead of its work: the next piece's numbers come out of the L2
+    TreePiece pc, nx;
+    bool more = tree_next_piece(a, run, kMKeys, row_blocks, true, &nx);
 
-    if (warp >= 5) {
+    if (warp > SW) {
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
         constexpr int CH = DP / 8;                     // 16-byte chunks of a row
         constexpr int RW = 32 / CH;                    // rows the warp copies at a time
-        const int lw = warp - 5, ch = lane % CH, sub = lane / CH;
+        const int lw = warp - SW - 1, ch = lane % CH, sub = lane / CH;
         const bool ch_in = ch * 8 < a.D;
-        const uint32_t ch_kv = (uint32_t)(ch >> 3) * (kMKeys * 128), ch_q = (uint32_t)(ch >> 3) * (kMRows * 128);
+        const uint32_t ch_kv = (uint32_t)(ch >> 3) * (kMKeys * 128), ch_q = (uint32_t)(ch >> 3) * C::q_half;
+        const uint32_t swz = ((uint32_t)ch & 7u) << 4;
         uint32_t step = 0;                             // copies issued
-        bool ok = true;
+        int owed = -1;                                 // copy of an arena tile's values that is to be looked over before it is handed on
+        uint32_t owed_piece = 0;
+        auto look_over = [&]() {                       // (its copies have landed)
+            const uint32_t s = (uint32_t)owed % C::stages;
+            bool found = false;
+#pragma unroll 4
+            for (int j = 0; j < 32 / RW; ++j) {
+                const int r = lw * 32 + j * RW + sub;
+                uint4* v = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)));
+                uint4 x = *v;
+                bool f = false;
+                x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
+                if (f) { *v = x; found = true; }
+            }
+            if (found) sm.bad[owed_piece % kBadSlots] = owed_piece + 1;
+            if (owed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[s]));
+            owed = -1;
+        };
         // One tile of keys or values; `at`: the cache row of the warp's row `lane`, -1 for zeros.  The stage is handed on by the
         // copies themselves; the issuing thread of the matrix products has the fence between their writes and its reads
-        // (here it would wait for every copy in flight: twice the time on long contexts).  look > 0: values of an arena
-        // tile (of piece look - 1), waited for and looked over first.
-        auto load = [&](const void* base, int64_t at, int h, uint32_t look) {
-            const uint32_t s = step % kMStages, use = step / kMStages;
-            if (use > 0 && !mbar_wait_warp(msmem_u32(&sm.empty[s]), (use - 1) & 1u, abort_flag, limit)) return false;
+        // (here it would wait for every copy in flight: twice the time on long contexts).  look: values of an arena
+        // tile, looked over once the next copy but one has been issued.
+        auto load = [&](const void* base, int64_t at, int h, bool look, int piece) {
+            const uint32_t s = step % C::stages, use = step / C::stages;
+            if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[s]), (use - 1) & 1u, abort_flag, limit)) return false;
             const __nv_bfloat16* p = (const __nv_bfloat16*)base + (int64_t)h * a.pages.head_stride + ch * 8;
             const uint32_t dst = msmem_u32(sm.kv[s]) + ch_kv;
 #pragma unroll
@@ -224,207 +240,237 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                 const int64_t row = __shfl_sync(kFullMask, at, j * RW + sub);
                 const int r = lw * 32 + j * RW + sub;
                 const bool in = row >= 0 && ch_in;
-                cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16, in ? (const void*)(p + row) : a.k, in ? 16u : 0u);
+                cp_async16(dst + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)), in ? (const void*)(p + row) : a.k, in ? 16u : 0u);
             }
-            const uint32_t bar = msmem_u32(&sm.full[s]);
-            if (look) {
-                cp_wait_all();
-                bool found = false;
-#pragma unroll 4
-                for (int j = 0; j < 32 / RW; ++j) {
-                    const int r = lw * 32 + j * RW + sub;
-                    uint4* v = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + ((ch & 7) ^ (r & 7)) * 16);
-                    uint4 x = *v;
-                    bool f = false;
-                    x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
-                    if (f) { *v = x; found = true; }
-                }
-                if (found) sm.bad[(look - 1) % kBadSlots] = look;
-                if ((int)step != a.drop_item) mbar_arrive(bar);
-            } else if ((int)step != a.drop_item) cp_arrive(bar);
+            cp_commit();
+            if (!look && (int)step != a.drop_item) cp_arrive(msmem_u32(&sm.full[s]));
+            if (owed >= 0 && (look || (int)step - owed >= 2)) {
+                if ((int)step - owed == 1) cp_wait<1>(); else cp_wait<2>();
+                look_over();
+            }
+            if (look) { owed = (int)step; owed_piece = (uint32_t)piece; }
             ++step;
             return true;
         };
-        bool first = true;
+        // the tile being looked up, one ahead of the one being copied
+        int f_t = 0, f_count = 0, f_row = 0, f_id = 0;
+        bool f_arena = false, f_in = false;
+        uint32_t f_m0 = 0, f_m1 = 0;
+        auto look_up = [&](const TreePiece& p, int t) {
+            int place;
+            tree_tile_span(a, p, t, kMKeys, &place, &f_count);
+            f_t = t;
+            f_arena = t < p.arena_tiles;
+            f_in = lw * 32 + lane < f_count;
+            f_m0 = f_m1 = 0;
+            if (f_arena) {
+                const int w = (place >> 5) + lw;
+                const uint32_t* mk = a.masks + (int64_t)p.b * a.n * a.W + w;
+                if (w < a.W) {
+                    if (lane < a.n) f_m0 = __ldg(mk + (int64_t)lane * a.W);
+                    if (lane + 32 < a.n) f_m1 = __ldg(mk + (int64_t)(lane + 32) * a.W);
+                }
+            }
+            const unsigned at = (unsigned)(place + lw * 32 + lane), page = at / (unsigned)a.pages.page_size;
+            f_row = (int)(at - page * (unsigned)a.pages.page_size);
+            f_in = f_in && page < (unsigned)a.pages.max_pages;
+            f_id = f_in ? __ldg(a.pages.table + (int64_t)p.b * a.pages.table_stride + page) : 0;
+        };
+        bool ok = true;
         int piece = 0, tile_no = 0;
-        while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
-            first = false;
-            // queries of the item: beyond the rows (to the next 32) and the head size, zeros
+        if (more) look_up(nx, nx.tile);
+        while (more) {
+            pc = nx;
+            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
+            // queries of the item: beyond the rows and the head size, zeros
             const uint32_t qb = piece % C::q_bufs, q_use = piece / C::q_bufs;
-            if (q_use > 0 && !mbar_wait_warp(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+            if (q_use > 0) {
+                if (owed >= 0) { cp_wait<0>(); look_over(); }          // (the queries' buffer may be waiting for it)
+                if (!mbar_wait(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+            }
             {
                 const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (int64_t)pc.b * a.q_seq + ch * 8;
                 const uint32_t dst = msmem_u32(sm.q[qb]) + ch_q;
-                const int rows_here = min(kMRows, M - pc.rb * kMRows), rows_pad = (rows_here + 31) / 32 * 32;
-#pragma unroll 2
+                const int rows_here = min(C::rows, M - pc.rb * C::rows), rows_pad = (rows_here + 31) / 32 * 32;
+#pragma unroll 4
                 for (int r = lw * RW + sub; r < rows_pad; r += kLoadWarps * RW) {
-                    const int rr = pc.rb * kMRows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
+                    const int rr = pc.rb * C::rows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
                     const bool in = r < rows_here && ch_in;
-                    cp_async16(dst + r * 128 + (((uint32_t)ch & 7u) ^ ((uint32_t)r & 7u)) * 16,
+                    cp_async16(dst + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)),
                                in ? (const void*)(q + (int64_t)tok * a.q_row + (int64_t)head * a.q_head) : a.q, in ? 16u : 0u);
                 }                                       // (the first keys' arrival counts them too)
             }
             int64_t v_at = -1;
-            uint32_t v_look = 0;
+            bool v_look = false;
             for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++tile_no) {
-                int place, count;
-                tree_tile_span(a, pc, t, kMKeys, &place, &count);
-                const int mine = place + lw * 32 + lane;
-                bool want = lw * 32 + lane < count;
-                uint32_t look = 0;
-                if (t < pc.arena_tiles) {               // slots no row of the sequence sees are not read
-                    const int w = (place >> 5) + lw;
-                    uint32_t any = 0;
-                    if (w < a.W)
-                        for (int i = lane; i < a.n; i += 32) any |= __ldg(a.masks + ((int64_t)pc.b * a.n + i) * a.W + w);
-                    any = __reduce_or_sync(kFullMask, any);
-                    want = want && ((any >> lane) & 1u);
-                    look = (uint32_t)piece + 1;
+                if (f_arena) {                          // slots no row of the sequence sees are not read
+                    const uint32_t any = __reduce_or_sync(kFullMask, f_m0 | f_m1);
+                    f_in = f_in && ((any >> lane) & 1u);
                 }
-                const int64_t at = want ? tree_row(a.pages, pc.b, mine) : -1;
-                const uint32_t there = __ballot_sync(kFullMask, at >= 0);
+                if (f_in && (unsigned)f_id >= (unsigned)a.pages.num_pages) {
+                    atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
+                    f_in = false;
+                }
+                const int64_t at = f_in ? (int64_t)f_id * a.pages.page_stride + (int64_t)f_row * a.pages.token_stride : -1;
+                const bool look = f_arena;
+                const uint32_t there = __ballot_sync(kFullMask, f_in);
                 if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
-                if (!load(a.k, at, pc.h, 0)) { ok = false; break; }
+                if (t + 1 < pc.tile + pc.tiles) look_up(pc, t + 1);
+                else if (more) look_up(nx, nx.tile);
+                if (!load(a.k, at, pc.h, false, piece)) { ok = false; break; }
                 // one S in tensor memory: K0 V0 K1 V1 ..;  two: K0 K1 V0 K2 V1 .. (the products run one tile ahead)
                 if (C::s_bufs == 1) {
-                    if (!load(a.v, at, pc.h, look)) { ok = false; break; }
+                    if (!load(a.v, at, pc.h, look, piece)) { ok = false; break; }
                 } else {
-                    if (t > pc.tile && !load(a.v, v_at, pc.h, v_look)) { ok = false; break; }
+                    if (t > pc.tile && !load(a.v, v_at, pc.h, v_look, piece)) { ok = false; break; }
                     v_at = at; v_look = look;
                 }
             }
-            if (C::s_bufs > 1 && ok && !load(a.v, v_at, pc.h, v_look)) ok = false;
+            if (!ok || (C::s_bufs > 1 && !load(a.v, v_at, pc.h, v_look, piece))) { ok = false; break; }
             ++piece;
         }
-        cp_wait_all();
-    } else if (warp == 4) {
-        // ------------------------------------------------------------------ matrix products
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
-            const int ks_n = (a.D + 15) / 16;
-            uint32_t step = 0;
-            bool ok = true, first = true;
-            int piece = 0;
-            uint32_t g = 0;
-            auto scores = [&](uint32_t gi, int qb) {
-                const uint32_t s = step % kMStages;
-                if (!mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit)) return false;
+        cp_wait<0>();
+        if (ok && owed >= 0) look_over();
+    } else if (warp == SW) {
+        // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
+        constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
+        const int ks_n = (a.D + 15) / 16;
+        const uint32_t q0 = msmem_u32(sm.q[0]), kv0 = msmem_u32(sm.kv[0]);
+        uint32_t stage = 0, phase = 0;                 // of the next copy
+        uint32_t g = 0;
+        int piece = 0;
+        bool ok = true;
+        auto next_stage = [&]() { if (++stage == C::stages) { stage = 0; phase ^= 1u; } };
+        // the scores of tile gi of the block's sequence; `last`: of its piece
+        auto scores = [&](uint32_t gi, uint32_t qb, bool last) {
+            if (!mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit)) return false;
+            if (lane == 0) {
                 fence_async_proxy();                   // the copies' writes (generic) before the products' reads
                 tc_after();
-                const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]), 16), dk = sw128_desc(msmem_u32(sm.kv[s]), 16);
-                const uint32_t d = tmem + C::s_col + (gi % C::s_bufs) * kMKeys;
+                const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(kv0 + stage * C::stage_bytes, 16);
+                const uint32_t sb = gi % C::s_bufs, d = tmem + C::s_col + sb * kMKeys;
+#pragma unroll 1
                 for (int ks = 0; ks < ks_n; ++ks)       // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns
-                    mma_ss(d, dq + (uint64_t)((ks >> 2) * (kMRows * 128 / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kMKeys * 128 / 16) + (ks & 3) * 2),
+                    mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kMKeys * 128 / 16) + (ks & 3) * 2),
                            idesc_s | negate, ks != 0);
-                mma_commit(msmem_u32(&sm.empty[s]));
-                mma_commit(msmem_u32(&sm.s_full[gi % C::s_bufs]));
-                mbar_arrive(msmem_u32(&sm.s_full[gi % C::s_bufs]));
-                ++step;
-                return true;
-            };
-            while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
-                first = false;
-                const int qb = piece % C::q_bufs;
-                ok = scores(g, qb);
-                if (ok && pc.tiles == 1) mma_commit(msmem_u32(&sm.q_empty[qb]));
-                for (int t = 0; t < pc.tiles && ok; ++t, ++g) {
-                    if (C::s_bufs > 1 && t + 1 < pc.tiles) {
-                        if (!(ok = scores(g + 1, qb))) break;
-                        if (t + 2 == pc.tiles) mma_commit(msmem_u32(&sm.q_empty[qb]));
-                    }
-                    const uint32_t sb = g % C::s_bufs, s = step % kMStages;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.full[s]), (step / kMStages) & 1u, abort_flag, limit))) break;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
-                    if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
+                mma_commit(msmem_u32(&sm.empty[stage]));
+                mma_commit(msmem_u32(&sm.s_full[sb]));
+                mbar_arrive(msmem_u32(&sm.s_full[sb]));
+                if (last) mma_commit(msmem_u32(&sm.q_empty[qb]));
+            }
+            __syncwarp();
+            next_stage();
+            return true;
+        };
+        while (ok && more) {
+            pc = nx;
+            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
+            const uint32_t qb = (uint32_t)piece % C::q_bufs;
+            ok = scores(g, qb, pc.tiles == 1);
+#pragma unroll 1
+            for (int t = 0; t < pc.tiles && ok; ++t, ++g) {
+                // one S in tensor memory: S0 O0 S1 O1 ..;  two: S0 S1 O0 S2 O1 ..
+                if (C::s_bufs > 1 && t + 1 < pc.tiles && !(ok = scores(g + 1, qb, t + 2 == pc.tiles))) break;
+                const uint32_t sb = g % C::s_bufs;
+                if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
+                if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
+                if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
+                if (lane == 0) {
                     fence_async_proxy();
                     tc_after();
-                    const uint64_t dv = sw128_desc(msmem_u32(sm.kv[s]), kMKeys * 128);
+                    const uint64_t dv = sw128_desc(kv0 + stage * C::stage_bytes, kMKeys * 128);
                     const uint32_t p = tmem + C::s_col + sb * kMKeys;
 #pragma unroll
                     for (int ks = 0; ks < kMKeys / 16; ++ks)          // 16 keys = two groups of eight rows of 128 bytes
                         mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, (t | ks) != 0);
-                    mma_commit(msmem_u32(&sm.empty[s]));
+                    mma_commit(msmem_u32(&sm.empty[stage]));
                     mma_commit(msmem_u32(&sm.pv_done));
                     if (t + 1 == pc.tiles) mbar_arrive(msmem_u32(&sm.told));
-                    ++step;
-                    if (C::s_bufs == 1 && t + 1 < pc.tiles) {
-                        if (!(ok = scores(g + 1, qb))) break;
-                        if (t + 2 == pc.tiles) mma_commit(msmem_u32(&sm.q_empty[qb]));
-                    }
                 }
-                ++piece;
+                __syncwarp();
+                next_stage();
+                if (C::s_bufs == 1 && t + 1 < pc.tiles && !(ok = scores(g + 1, qb, t + 2 == pc.tiles))) break;
             }
-            // nothing of this block is in flight when it leaves, whatever happened
-            mma_commit(msmem_u32(&sm.last));
-            for (int i = 0; i < 1000000 && !mbar_try(msmem_u32(&sm.last), 0); ++i) {}
+            ++piece;
         }
-        __syncwarp();
+        // nothing of this block is in flight when it leaves, whatever happened
+        if (lane == 0) mma_commit(msmem_u32(&sm.last));
+        for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last), 0)); ++i) {}
     } else {
         // ------------------------------------------------------------------ softmax: a row per thread
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         const float scale = fabsf(a.scale_log2e);
-        bool ok = true, first = true;
+        const int row = warp * 32 + lane;
+        bool ok = true;
         int piece = 0;
         uint32_t g = 0;
-        if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, kMKeys, row_blocks);
-        while (ok && tree_next_piece(a, run, kMKeys, row_blocks, first, &pc)) {
-            if (first && tid == 0) tree_write_meta(a, run, &pc, kMKeys, row_blocks);
-            first = false;
-            const int row = warp * 32 + lane, rr = pc.rb * kMRows + row;
-            const bool active = pc.rb * kMRows + warp * 32 < M;       // the warp has rows
-            const int tok = min(rr, M - 1) / a.G, head = pc.h * a.G + rr - tok * a.G;
-            const uint32_t* mask = a.masks ? a.masks + ((int64_t)pc.b * a.n + tok) * a.W : nullptr;
-            bool live = rr < M;
-            if (active && mask) {                                     // an empty mask closes the row
-                uint32_t any = 0;
-#pragma unroll 8
-                for (int w = 0; w < (pc.top + 31) / 32; ++w) any |= __ldg(mask + w);
-                live = live && any != 0;
+        if (tid == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
+        // the row's mask words of the tile to come
+        uint32_t next0 = 0, next1 = 0;
+        const uint32_t* mask = nullptr;
+        auto mask_of = [&](const TreePiece& p) {
+            const int rr = min(p.rb * C::rows + row, M - 1);
+            return a.masks ? a.masks + ((int64_t)p.b * a.n + rr / a.G) * a.W : nullptr;
+        };
+        auto fetch_mask = [&](const TreePiece& p, const uint32_t* mk, int t) {
+            if (t < p.arena_tiles) {
+                next0 = __ldg(mk + 2 * t);
+                next1 = 2 * t + 1 < a.W ? __ldg(mk + 2 * t + 1) : 0u;
             }
+        };
+        const uint32_t* next_mask = nullptr;
+        if (more) { next_mask = mask_of(nx); fetch_mask(nx, next_mask, nx.tile); }
+        while (ok && more) {
+            pc = nx;
+            mask = next_mask;
+            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
+            const int rr = pc.rb * C::rows + row;
+            const bool active = pc.rb * C::rows + warp * 32 < M;      // the warp has rows
+            const int tok = min(rr, M - 1) / a.G, head = pc.h * a.G + rr - tok * a.G;
+            uint32_t any = a.masks ? 0u : 1u;                         // an empty mask closes the row: its words, as the tiles come by
+            if (a.masks)
+                for (int w = 0; w < min(2 * pc.tile, (pc.top + 31) / 32); ++w) any |= __ldg(mask + w);      // (those before a piece that begins inside)
             float ref = neg_inf(), sum = 0.f;
             for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++g) {
                 const uint32_t sb = g % C::s_bufs;
-                uint32_t see0 = 0xffffffffu, see1 = 0xffffffffu;
-                if (active && t < pc.arena_tiles) {
-                    see0 = __ldg(mask + 2 * t);
-                    see1 = 2 * t + 1 < a.W ? __ldg(mask + 2 * t + 1) : 0u;
-                }
-                if (!mbar_wait_warp(msmem_u32(&sm.s_full[sb]), (g / C::s_bufs) & 1u, abort_flag, limit)) { ok = false; break; }
+                uint32_t see0, see1;
+                if (t < pc.arena_tiles) { see0 = next0; see1 = next1; any |= see0 | see1; }
+                else see0 = see1 = any ? 0xffffffffu : 0u;
+                if (rr >= M) see0 = see1 = 0;
+                if (t + 1 < pc.tile + pc.tiles) fetch_mask(pc, mask, t + 1);
+                else if (more) { next_mask = mask_of(nx); fetch_mask(nx, next_mask, nx.tile); }
+                if (!mbar_wait(msmem_u32(&sm.s_full[sb]), (g / C::s_bufs) & 1u, abort_flag, limit)) { ok = false; break; }
                 if (active) {
                     tc_after();
                     see0 &= sm.seen[g % kBadSlots][0]; see1 &= sm.seen[g % kBadSlots][1];
-                    if (!live) see0 = see1 = 0;
                     uint32_t u[kMKeys];
                     tm_ld32(tmem + lanes + C::s_col + sb * kMKeys, u);
                     tm_ld32(tmem + lanes + C::s_col + sb * kMKeys + 32, u + 32);
-                    tm_wait_ld(u);
-                    tm_wait_ld(u + 32);
-                    float x[kMKeys];
-#pragma unroll
-                    for (int j = 0; j < kMKeys; ++j) x[j] = __uint_as_float(u[j]);
                     if (__any_sync(kFullMask, (see0 & see1) != 0xffffffffu)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
-                            if (!((see0 >> j) & 1u)) x[j] = neg_inf();
-                            if (!((see1 >> j) & 1u)) x[32 + j] = neg_inf();
+                            if (!((see0 >> j) & 1u)) u[j] = 0xff800000u;
+                            if (!((see1 >> j) & 1u)) u[32 + j] = 0xff800000u;
                         }
                     }
-                    float m0 = x[0], m1 = x[1], m2 = x[2], m3 = x[3];
+                    float m0 = __uint_as_float(u[0]), m1 = __uint_as_float(u[1]), m2 = __uint_as_float(u[2]), m3 = __uint_as_float(u[3]);
 #pragma unroll
-                    for (int j = 4; j < kMKeys; j += 4) { m0 = fmaxf(m0, x[j]); m1 = fmaxf(m1, x[j + 1]); m2 = fmaxf(m2, x[j + 2]); m3 = fmaxf(m3, x[j + 3]); }
-                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;     // (scale 0 and nothing seen: NaN, not above anything)
+                    for (int j = 4; j < kMKeys; j += 4) {
+                        m0 = fmaxf(m0, __uint_as_float(u[j])); m1 = fmaxf(m1, __uint_as_float(u[j + 1]));
+                        m2 = fmaxf(m2, __uint_as_float(u[j + 2])); m3 = fmaxf(m3, __uint_as_float(u[j + 3]));
+                    }
+                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
                     const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
                     if (__any_sync(kFullMask, raise)) {
                         const float factor = raise ? ex2(ref - top) : 1.f;             // 0 where nothing has been seen before
                         if (raise) { ref = top; sum *= factor; }
                         if (t > pc.tile) {
-                            if (!mbar_wait_warp(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                            if (!mbar_wait(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
                             tc_after();
 #pragma unroll 1
                             for (int c = 0; c < DP; c += 32) {
                                 uint32_t o[32];
                                 tm_ld32(tmem + lanes + C::o_col + c, o);
-                                tm_wait_ld(o);
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
                                 tm_st32(tmem + lanes + C::o_col + c, o);
@@ -436,8 +482,8 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                     uint32_t p[kMKeys / 2];
 #pragma unroll
                     for (int j = 0; j < kMKeys; j += 4) {
-                        const float e0 = ex2(fmaf(x[j], scale, shift)), e1 = ex2(fmaf(x[j + 1], scale, shift));
-                        const float e2 = ex2(fmaf(x[j + 2], scale, shift)), e3 = ex2(fmaf(x[j + 3], scale, shift));
+                        const float e0 = ex2(fmaf(__uint_as_float(u[j]), scale, shift)), e1 = ex2(fmaf(__uint_as_float(u[j + 1]), scale, shift));
+                        const float e2 = ex2(fmaf(__uint_as_float(u[j + 2]), scale, shift)), e3 = ex2(fmaf(__uint_as_float(u[j + 3]), scale, shift));
                         s0 += e0; s1 += e1; s2 += e2; s3 += e3;
                         p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
                     }
@@ -450,39 +496,23 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                 if (lane == 0) mbar_arrive(msmem_u32(&sm.p_ready[sb]));
             }
             if (!ok) break;
-            if (!mbar_wait_warp(msmem_u32(&sm.told), piece & 1, abort_flag, limit)) { ok = false; break; }
-            if (!mbar_wait_warp(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+            if (!mbar_wait(msmem_u32(&sm.told), piece & 1, abort_flag, limit)) { ok = false; break; }
+            if (!mbar_wait(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             if (active) {
                 tc_after();
                 const bool bad = sm.bad[piece % kBadSlots] == (uint32_t)piece + 1;
                 const float inv = pc.whole && sum > 0.f ? 1.f / sum : 1.f;
-                const int64_t part = (int64_t)(2 * blockIdx.x + pc.slot) * kMRows + row;
+                const int64_t part = (int64_t)(2 * blockIdx.x + pc.slot) * C::rows + row;
                 __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)pc.b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
 #pragma unroll 1
                 for (int c = 0; c < DP; c += 32) {
                     uint32_t u[32];
                     __syncwarp();
                     tm_ld32(tmem + lanes + C::o_col + c, u);
-                    tm_wait_ld(u);
                     if (rr >= M) continue;
                     float o[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) o[j] = sum == 0.f ? 0.f : __uint_as_float(u[j]);
-                    if (bad && live)       // values that are not finite, at the slots this row sees
-                        for (int j = pc.tile * kMKeys; j < min((pc.tile + pc.tiles) * kMKeys, pc.top); ++j) {
-                            if (!((__ldg(mask + (j >> 5)) >> (j & 31)) & 1u)) continue;
-                            const int64_t at = tree_row(a.pages, pc.b, j);
-                            if (at < 0) continue;
-                            const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + at + (int64_t)pc.h * a.pages.head_stride;
-#pragma unroll 1
-                            for (int d = c; d < min(c + 32, a.D); ++d) {
-                                const float x = __bfloat162float(v[d]);
-                                if (!(fabsf(x) <= 3.4e38f)) {
-#pragma unroll
-                                    for (int k = 0; k < 32; ++k) if (k == d - c) o[k] += x;
-                                }
-                            }
-                        }
 #pragma unroll
                     for (int j = 0; j < 32; j += 8) {
                         if (c + j >= a.D) continue;
@@ -498,6 +528,19 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
                         }
                     }
                 }
+                if (bad && rr < M && sum > 0.f)        // values that are not finite, at the slots this row sees, onto what has been written
+                    for (int j = pc.tile * kMKeys; j < min((pc.tile + pc.tiles) * kMKeys, pc.top); ++j) {
+                        if (!((__ldg(mask + (j >> 5)) >> (j & 31)) & 1u)) continue;
+                        const int64_t at = tree_row(a.pages, pc.b, j);
+                        if (at < 0) continue;
+                        const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + at + (int64_t)pc.h * a.pages.head_stride;
+                        for (int d = 0; d < a.D; ++d) {
+                            const float x = __bfloat162float(v[d]);
+                            if (fabsf(x) <= 3.4e38f) continue;
+                            if (pc.whole) out[d] = __float2bfloat16_rn(__bfloat162float(out[d]) + x);
+                            else a.part_o[part * a.D + d] += x;
+                        }
+                    }
                 if (rr < M) {
                     if (!pc.whole) { a.part_ml[2 * part] = ref; a.part_ml[2 * part + 1] = sum; }
                     else if (a.lse) a.lse[((int64_t)pc.b * a.n + tok) * a.H + head] = sum == 0.f ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
@@ -512,31 +555,37 @@ __global__ void __launch_bounds__(kMThreads, MConf<DP>::blocks_per_sm) tree_atte
     tc_before();
     __syncthreads();
     tc_after();
-    if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
+    if (warp == SW) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
     if (tid == 0 && sm.abort_flag) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
 }
 
-template <int DP>
+template <int DP, int SW>
 cudaError_t configure_mma() {
-    return cudaFuncSetAttribute(tree_attend_mma_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP>));
+    return cudaFuncSetAttribute(tree_attend_mma_kernel<DP, SW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP, SW>));
 }
-template <int DP>
+template <int DP, int SW>
 cudaError_t launch_mma(const TreeAttend& a, int grid, cudaStream_t st) {
     const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
-    return launch_after(tree_attend_mma_kernel<DP>, dim3(grid), dim3(kMThreads), sizeof(MSmem<DP>), st, a, negate);
+    return launch_after(tree_attend_mma_kernel<DP, SW>, dim3(grid), dim3(MConf<DP, SW>::threads), sizeof(MSmem<DP, SW>), st, a, negate);
 }
 
 }  // namespace
 
 bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
-int tree_mma_rows() { return kMRows; }
-int tree_mma_blocks_per_sm(int D) { return D <= 64 ? MConf<64>::blocks_per_sm : MConf<128>::blocks_per_sm; }
-cudaError_t configure_tree_mma() {
-    const cudaError_t e = configure_mma<64>();
-    return e == cudaSuccess ? configure_mma<128>() : e;
+// Rows of an item: one softmax warp where the rows of a key head fit it, else four.
+int tree_mma_rows(int M) { return M <= 32 ? 32 : kMRows; }
+int tree_mma_blocks_per_sm(int D, int rows) {
+    return D <= 64 ? (rows == 32 ? MConf<64, 1>::blocks_per_sm : MConf<64, 4>::blocks_per_sm) : rows == 32 ? MConf<128, 1>::blocks_per_sm : MConf<128, 4>::blocks_per_sm;
 }
-cudaError_t launch_tree_mma(const TreeAttend& a, int grid, cudaStream_t st) {
-    return a.D <= 64 ? launch_mma<64>(a, grid, st) : launch_mma<128>(a, grid, st);
+cudaError_t configure_tree_mma() {
+    cudaError_t e = configure_mma<64, 1>();
+    if (e == cudaSuccess) e = configure_mma<64, 4>();
+    if (e == cudaSuccess) e = configure_mma<128, 1>();
+    return e == cudaSuccess ? configure_mma<128, 4>() : e;
+}
+cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
+    if (rows == 32) return a.D <= 64 ? launch_mma<64, 1>(a, grid, st) : launch_mma<128, 1>(a, grid, st);
+    return a.D <= 64 ? launch_mma<64, 4>(a, grid, st) : launch_mma<128, 4>(a, grid, st);
 }
 
 }  // namespace dba

@@ -53,10 +53,10 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count);
 cudaError_t configure_tree_attend();
 // the tensor-core kernel (tree_attend_mma.cu)
 bool tree_mma_usable(int dtype, int D);
-int tree_mma_rows();
-int tree_mma_blocks_per_sm(int D);
+int tree_mma_rows(int M);
+int tree_mma_blocks_per_sm(int D, int rows);
 cudaError_t configure_tree_mma();
-cudaError_t launch_tree_mma(const TreeAttend& a, int grid, cudaStream_t st);
+cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st);
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
 cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K,
                                int32_t D, int dtype, cudaStream_t st, int* launches);
