@@ -230,54 +230,97 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
     }
 }
 
-// Finishes the items that several blocks worked on: block (c, y) takes eight rows of the item that attention block c
-// shares with the ones before and after it, a warp per row, the pieces in their order (so that equal inputs give equal bits).
+// Finishes the items that several blocks worked on.  Block c of the attention names in meta[c] the item it shares with block
+// c - 1 if that one was the item's first: those are the items there are.  Every block here lists them and takes every
+// gridDim-th row of theirs: a warp per row where few pieces meet, all eight warps on a row (each an eighth of its pieces)
+// where many do.  Pieces are added in a fixed order, so equal inputs give equal bits.
+constexpr int kCombineThreads = 256, kCombineWarps = 8, kCombineMany = 8;
+
 template <typename T>
-__global__ void __launch_bounds__(256) tree_combine_kernel(const TreeAttend a, int item_rows) {
+__global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeAttend a, int item_rows, int blocks) {
+    extern __shared__ int32_t shared_items[];              // [blocks]
+    __shared__ int32_t counts[kCombineWarps], most[kCombineWarps];
+    __shared__ float sums[kCombineWarps][kTreeMaxDim];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     grid_dependency_wait();
     allow_dependents();
-    const int lane = threadIdx.x & 31;
     if (a.pages.status[1] == a.call) {       // a wait of this call ran out: nothing it wrote can be trusted
-        const int64_t rows = (int64_t)a.B * a.n * a.H, blocks = (int64_t)gridDim.x * gridDim.y, me = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-        for (int64_t i = me * 256 + threadIdx.x; i < rows * a.D; i += blocks * 256) {
+        const int64_t rows = (int64_t)a.B * a.n * a.H;
+        for (int64_t i = (int64_t)blockIdx.x * kCombineThreads + tid; i < rows * a.D; i += (int64_t)gridDim.x * kCombineThreads) {
             const int64_t r = i / a.D, tok = r / a.H, b = tok / a.n;
             tree_store((T*)a.out + b * a.o_seq + (tok - b * a.n) * a.o_row + (r - tok * a.H) * a.o_head + (i - r * a.D), __int_as_float(0x7fc00000));
             if (a.lse && i == r * a.D) a.lse[r] = __int_as_float(0x7fc00000);
         }
         return;
     }
-    const int4 meta = a.meta[blockIdx.x];
-    if (meta.x < 0) return;
-    const int M = a.n * a.G, row_blocks = (M + item_rows - 1) / item_rows;
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    const int b = meta.x, h = meta.y / row_blocks, rb = meta.y - h * row_blocks, rr = rb * item_rows + r;
-    if (r >= item_rows || rr >= M) return;
-    const int c0 = (int)blockIdx.x - 1, n = meta.z - c0 + 1;
-    auto place = [&](int i) { return (int64_t)(2 * (c0 + i) + (i == 0 ? meta.w : 0)) * item_rows + r; };
-    float m = neg_inf();
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, a.part_ml[2 * place(i)]);
-    m = warp_max(m);
-    const float ref = m == neg_inf() ? 0.f : m;
-    float l = 0.f;
-    for (int i = lane; i < n; i += 32) l += a.part_ml[2 * place(i) + 1] * exp2f(a.part_ml[2 * place(i)] - ref);
-    l = warp_sum(l);
-    const int tok = rr / a.G, head = h * a.G + rr - tok * a.G;
-    T* out = (T*)a.out + (int64_t)b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    for (int d = 4 * lane; d < a.D; d += 128) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const int64_t at = place(i);
-            const float w = exp2f(a.part_ml[2 * at] - ref);
-            const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * a.D + d);
-            o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
+    const int M = a.n * a.G, row_blocks = (M + item_rows - 1) / item_rows, rows = min(M, item_rows);
+    int n_items = 0, n_most = 0;
+    for (int c0 = 0; c0 < blocks; c0 += kCombineThreads) {
+        const int c = c0 + tid;
+        const int4 meta = c < blocks ? a.meta[c] : make_int4(-1, 0, 0, 0);
+        const uint32_t mine = __ballot_sync(kFullMask, meta.x >= 0);
+        const int pieces = meta.x >= 0 ? meta.z - c + 2 : 0;
+        if (lane == 0) counts[warp] = __popc(mine);
+        const int wm = __reduce_max_sync(kFullMask, pieces);
+        if (lane == 0) most[warp] = wm;
+        __syncthreads();
+        int before = n_items + __popc(mine & ((1u << lane) - 1u));
+        for (int w = 0; w < kCombineWarps; ++w) {
+            if (w < warp) before += counts[w];
+            n_items += counts[w];
+            n_most = max(n_most, most[w]);
         }
-        const float x[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) tree_store(out + d + j, l == 0.f ? 0.f : x[j] * inv);
+        if (meta.x >= 0) shared_items[before] = c;
+        __syncthreads();
     }
-    if (a.lse && lane == 0) a.lse[((int64_t)b * a.n + tok) * a.H + head] = l == 0.f ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+    const bool many = n_most > kCombineMany;
+    const int step = many ? gridDim.x : gridDim.x * kCombineWarps;
+    for (int task = many ? blockIdx.x : blockIdx.x * kCombineWarps + warp; task < n_items * rows; task += step) {
+        const int item = task / rows, r = task - item * rows, c = shared_items[item];
+        const int4 meta = a.meta[c];
+        const int b = meta.x, h = meta.y / row_blocks, rb = meta.y - h * row_blocks, rr = rb * item_rows + r;
+        if (rr >= M) continue;                             // (the same for all warps of a task)
+        const int first = c - 1, n = meta.z - first + 1;
+        auto place = [&](int i) { return (int64_t)(2 * (first + i) + (i == 0 ? meta.w : 0)) * item_rows + r; };
+        float m = neg_inf();
+        for (int i = lane; i < n; i += 32) m = fmaxf(m, a.part_ml[2 * place(i)]);
+        m = warp_max(m);
+        const float ref = m == neg_inf() ? 0.f : m;
+        float l = 0.f;
+        for (int i = lane; i < n; i += 32) l += a.part_ml[2 * place(i) + 1] * exp2f(a.part_ml[2 * place(i)] - ref);
+        l = warp_sum(l);
+        const int tok = rr / a.G, head = h * a.G + rr - tok * a.G;
+        T* out = (T*)a.out + (int64_t)b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int i0 = many ? warp : 0, di = many ? kCombineWarps : 1;
+        for (int d = 4 * lane; d < a.D; d += 128) {
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int i = i0; i < n; i += di) {
+                const int64_t at = place(i);
+                const float w = exp2f(a.part_ml[2 * at] - ref);
+                const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * a.D + d);
+                o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
+            }
+            const float x[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (many) sums[warp][d + j] = x[j];
+                else tree_store(out + d + j, l == 0.f ? 0.f : x[j] * inv);
+            }
+        }
+        if (many) {
+            __syncthreads();
+            if (tid < a.D) {
+                float x = 0.f;
+#pragma unroll
+                for (int w = 0; w < kCombineWarps; ++w) x += sums[w][tid];
+                tree_store(out + tid, l == 0.f ? 0.f : x * inv);
+            }
+            __syncthreads();
+        }
+        if (a.lse && lane == 0 && (!many || warp == 0)) a.lse[((int64_t)b * a.n + tok) * a.H + head] = l == 0.f ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+    }
 }
 
 template <typename T, int DP>
@@ -296,6 +339,7 @@ cudaError_t launch_fp32(const TreeAttend& a, int grid, cudaStream_t st) {
 
 TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count) {
     TreeAttendPlan p{};
+    p.combine = 2 * sm_count;
     if (tree_mma_usable(dtype, D)) {
         p.tensor = true;
         p.rows = tree_mma_rows(M);
@@ -313,6 +357,9 @@ cudaError_t configure_tree_attend() {
     if (e == cudaSuccess) e = configure_plain<float, 256>();
     if (e == cudaSuccess) e = configure_plain<__nv_bfloat16, 256>();
     if (e == cudaSuccess) e = configure_tree_mma();
+    // the same division of shared memory and L1 as the kernel before, or the SMs change over between the two
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_combine_kernel<float>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_combine_kernel<__nv_bfloat16>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     return e;
 }
 
@@ -320,10 +367,9 @@ cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, 
     cudaError_t e = plan.tensor ? launch_tree_mma(a, plan.rows, plan.grid, st)
                     : dtype == DBA_F32 ? launch_fp32(a, plan.grid, st) : launch_plain<__nv_bfloat16, 256>(a, plan.grid, st);
     if (e != cudaSuccess) return e;
-    const int rows = a.n * a.G < plan.rows ? a.n * a.G : plan.rows;
-    const dim3 grid(plan.grid, (rows + 7) / 8);
-    e = dtype == DBA_F32 ? launch_after(tree_combine_kernel<float>, grid, dim3(256), 0, st, a, plan.rows)
-                         : launch_after(tree_combine_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, a, plan.rows);
+    const size_t list = (size_t)plan.grid * sizeof(int32_t);
+    e = dtype == DBA_F32 ? launch_after(tree_combine_kernel<float>, dim3(plan.combine), dim3(kCombineThreads), list, st, a, plan.rows, plan.grid)
+                         : launch_after(tree_combine_kernel<__nv_bfloat16>, dim3(plan.combine), dim3(kCombineThreads), list, st, a, plan.rows, plan.grid);
     *launches += 2;
     return e;
 }

@@ -29,7 +29,7 @@ namespace {
 constexpr int kMRows = 128;                 // rows of the matrix instructions (lanes of tensor memory)
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
-constexpr int kBadSlots = 8;
+constexpr int kBadSlots = 16;               // more than the tiles the loader may be ahead by
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
 
@@ -38,21 +38,28 @@ constexpr float kRaise = 8.f;               // how far (powers of two) a score m
 template <int DP, int SW> struct MConf {
     static constexpr int rows = 32 * SW;
     static constexpr int threads = 32 * (SW + 1 + kLoadWarps);
-    static constexpr int stages = SW == 1 && DP == 128 ? 6 : 5;      // tiles of keys or values in shared memory
+    static constexpr int stages = DP == 128 ? (SW == 1 ? 6 : 5) : SW == 1 ? 5 : 9;      // tiles of keys or values in shared memory
     static constexpr int stage_bytes = kMKeys * DP * 2;
     static constexpr int q_half = rows * 128;                        // 64 columns of the queries
     static constexpr int q_bytes = rows * DP * 2;
     static constexpr int q_bufs = DP == 64 || SW == 1 ? 2 : 1;
-    static constexpr int s_bufs = DP == 64 ? 1 : 2;
-    static constexpr int blocks_per_sm = DP == 128 ? 2 : SW == 1 ? 4 : 3;
-    static constexpr int tmem_cols = DP == 64 ? 128 : 256;
+    static constexpr int s_bufs = DP == 64 && SW == 1 ? 1 : 2;
+    static constexpr int blocks_per_sm = DP == 64 && SW == 1 ? 4 : 2;
+    static constexpr int tmem_cols = s_bufs == 1 ? 128 : 256;
     static constexpr int o_col = 0, s_col = DP;
+    // stages that lie before the queries: with one softmax warp the products' other rows are read up to 96 rows before and
+    // after the queries
+    static constexpr int pre = SW == 1 ? (DP == 64 ? 2 : 1) : 0;
+    static constexpr int q_at = pre * stage_bytes;
+    static constexpr int tile_bytes = stages * stage_bytes + q_bufs * q_bytes;
+    static_assert(SW > 1 || (q_at >= 96 * 128 && q_at + q_bufs * q_bytes - q_half + kMRows * 128 <= tile_bytes), "rows beside the queries");
+    // where a stage of keys or values lies
+    static __device__ __forceinline__ uint32_t stage_at(uint32_t s) { return s * stage_bytes + (pre == 0 || (int)s >= pre ? q_bufs * q_bytes : 0); }
 };
 
 template <int DP, int SW> struct MSmem {
     using C = MConf<DP, SW>;
-    alignas(1024) unsigned char q[C::q_bufs][C::q_bytes];
-    alignas(1024) unsigned char kv[C::stages][C::stage_bytes];
+    alignas(1024) unsigned char tiles[C::tile_bytes];       // keys, values and queries
     uint64_t full[C::stages], empty[C::stages];
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
     uint64_t q_empty[C::q_bufs];
@@ -147,6 +154,14 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
         : "memory");
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// two fp32 operations in one instruction
+__device__ __forceinline__ void fma2(float& x, float& y, float a0, float a1, float b, float c) {
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(x), "=f"(y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a0, float a1) {
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(x), "+f"(y) : "f"(a0), "f"(a1));
+}
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // bits 0-15: lo, 16-31: hi
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -167,7 +182,12 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     using C = MConf<DP, SW>;
     extern __shared__ __align__(1024) unsigned char mraw[];
     MSmem<DP, SW>& sm = *reinterpret_cast<MSmem<DP, SW>*>(mraw);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    // The warp's role: 0 .. SW-1 softmax, SW products, then the loaders.  A warp reaches the quarter of the tensor memory's lanes
+    // that its number modulo 4 names, and issues from the scheduler of that number: with one softmax warp the blocks of an
+    // SM take different ones (all on one scheduler: 140 us instead of 90 on 256 sentences of 20 short rows).
+    const int quarter = SW == 1 ? (blockIdx.x / (gridDim.x / C::blocks_per_sm)) & 3 : 0;
+    const int warp = SW == 1 ? ((tid >> 5) + 4 - quarter) & 3 : tid >> 5;
     volatile int* abort_flag = &sm.abort_flag;
     const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
     const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows;
@@ -202,80 +222,83 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     if (warp > SW) {
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
         constexpr int CH = DP / 8;                     // 16-byte chunks of a row
-        constexpr int RW = 32 / CH;                    // rows the warp copies at a time
+        constexpr int RW = 32 / CH, NJ = 32 / RW;      // rows the warp copies at a time, and how often
         const int lw = warp - SW - 1, ch = lane % CH, sub = lane / CH;
-        const bool ch_in = ch * 8 < a.D;
-        const uint32_t ch_kv = (uint32_t)(ch >> 3) * (kMKeys * 128), ch_q = (uint32_t)(ch >> 3) * C::q_half;
-        const uint32_t swz = ((uint32_t)ch & 7u) << 4;
-        uint32_t step = 0;                             // copies issued
+        const bool ch_in = ch * 8 < a.D, full_head = a.D == DP;
+        const uint32_t tiles = msmem_u32(sm.tiles);
+        // this lane's place in rows sub, sub + RW, ..: the swizzle moves a chunk by the row's last three bits
+        const uint32_t in_kv = (uint32_t)(ch >> 3) * (kMKeys * 128) + (uint32_t)(lw * 32 + sub) * 128;
+        const uint32_t swz = ((uint32_t)(ch & 7) ^ (uint32_t)sub) << 4;
+        uint32_t step = 0, stage = 0, phase = 1;       // copies issued; the next one's stage (a barrier's first wait does not wait)
         int owed = -1;                                 // copy of an arena tile's values that is to be looked over before it is handed on
-        uint32_t owed_piece = 0;
+        uint32_t owed_piece = 0, owed_stage = 0;
         auto look_over = [&]() {                       // (its copies have landed)
-            const uint32_t s = (uint32_t)owed % C::stages;
             bool found = false;
 #pragma unroll 4
-            for (int j = 0; j < 32 / RW; ++j) {
-                const int r = lw * 32 + j * RW + sub;
-                uint4* v = reinterpret_cast<uint4*>(sm.kv[s] + ch_kv + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)));
+            for (int j = 0; j < NJ; ++j) {
+                uint4* v = reinterpret_cast<uint4*>(sm.tiles + C::stage_at(owed_stage) + in_kv + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)));
                 uint4 x = *v;
                 bool f = false;
                 x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
                 if (f) { *v = x; found = true; }
             }
             if (found) sm.bad[owed_piece % kBadSlots] = owed_piece + 1;
-            if (owed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[s]));
+            if (owed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[owed_stage]));
             owed = -1;
         };
-        // One tile of keys or values; `at`: the cache row of the warp's row `lane`, -1 for zeros.  The stage is handed on by the
-        // copies themselves; the issuing thread of the matrix products has the fence between their writes and its reads
-        // (here it would wait for every copy in flight: twice the time on long contexts).  look: values of an arena
-        // tile, looked over once the next copy but one has been issued.
-        auto load = [&](const void* base, int64_t at, int h, bool look, int piece) {
-            const uint32_t s = step % C::stages, use = step / C::stages;
-            if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[s]), (use - 1) & 1u, abort_flag, limit)) return false;
-            const __nv_bfloat16* p = (const __nv_bfloat16*)base + (int64_t)h * a.pages.head_stride + ch * 8;
-            const uint32_t dst = msmem_u32(sm.kv[s]) + ch_kv;
+        // One tile of keys or values: rows of the warp that exist (`there`) at row offsets at[j] (in 16 bytes), zeros for the others.
+        // The stage is handed on by the copies themselves; the issuing thread of the matrix products has the fence between
+        // their writes and its reads (here it would wait for every copy in flight: twice the time on long contexts).
+        // look: values of an arena tile, looked over once the next copy but one has been issued.
+        auto load = [&](const char* base, const uint32_t (&at)[NJ], uint32_t there, bool look, int piece) {
+            if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) return false;
+            const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
+            if (there == 0xffffffffu && full_head) {
 #pragma unroll
-            for (int j = 0; j < 32 / RW; ++j) {
-                const int64_t row = __shfl_sync(kFullMask, at, j * RW + sub);
-                const int r = lw * 32 + j * RW + sub;
-                const bool in = row >= 0 && ch_in;
-                cp_async16(dst + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)), in ? (const void*)(p + row) : a.k, in ? 16u : 0u);
+                for (int j = 0; j < NJ; ++j)
+                    cp_async16(dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), base + (uint64_t)at[j] * 16, 16u);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const bool in = ((there >> (j * RW + sub)) & 1u) && ch_in;
+                    cp_async16(dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? base + (uint64_t)at[j] * 16 : (const char*)a.k, in ? 16u : 0u);
+                }
             }
             cp_commit();
-            if (!look && (int)step != a.drop_item) cp_arrive(msmem_u32(&sm.full[s]));
+            if (!look && (int)step != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
             if (owed >= 0 && (look || (int)step - owed >= 2)) {
                 if ((int)step - owed == 1) cp_wait<1>(); else cp_wait<2>();
                 look_over();
             }
-            if (look) { owed = (int)step; owed_piece = (uint32_t)piece; }
+            if (look) { owed = (int)step; owed_piece = (uint32_t)piece; owed_stage = stage; }
             ++step;
+            if (++stage == C::stages) { stage = 0; phase ^= 1u; }
             return true;
         };
         // the tile being looked up, one ahead of the one being copied
-        int f_t = 0, f_count = 0, f_row = 0, f_id = 0;
+        int f_row = 0, f_id = 0;
         bool f_arena = false, f_in = false;
         uint32_t f_m0 = 0, f_m1 = 0;
         auto look_up = [&](const TreePiece& p, int t) {
-            int place;
-            tree_tile_span(a, p, t, kMKeys, &place, &f_count);
-            f_t = t;
+            int place, count;
+            tree_tile_span(a, p, t, kMKeys, &place, &count);
             f_arena = t < p.arena_tiles;
-            f_in = lw * 32 + lane < f_count;
+            f_in = lw * 32 + lane < count;
             f_m0 = f_m1 = 0;
             if (f_arena) {
                 const int w = (place >> 5) + lw;
                 const uint32_t* mk = a.masks + (int64_t)p.b * a.n * a.W + w;
                 if (w < a.W) {
-                    if (lane < a.n) f_m0 = __ldg(mk + (int64_t)lane * a.W);
-                    if (lane + 32 < a.n) f_m1 = __ldg(mk + (int64_t)(lane + 32) * a.W);
+                    if (lane < a.n) f_m0 = __ldg(mk + lane * a.W);
+                    if (lane + 32 < a.n) f_m1 = __ldg(mk + (lane + 32) * a.W);
                 }
             }
-            const unsigned at = (unsigned)(place + lw * 32 + lane), page = at / (unsigned)a.pages.page_size;
-            f_row = (int)(at - page * (unsigned)a.pages.page_size);
-            f_in = f_in && page < (unsigned)a.pages.max_pages;
+            const uint32_t at = (uint32_t)(place + lw * 32 + lane), page = tree_page(a.pages, at);
+            f_row = (int)(at - page * (uint32_t)a.pages.page_size);
+            f_in = f_in && page < (uint32_t)a.pages.max_pages;
             f_id = f_in ? __ldg(a.pages.table + (int64_t)p.b * a.pages.table_stride + page) : 0;
         };
+        const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;        // rows in 16 bytes
         bool ok = true;
         int piece = 0, tile_no = 0;
         if (more) look_up(nx, nx.tile);
@@ -283,50 +306,66 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             pc = nx;
             more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
             // queries of the item: beyond the rows and the head size, zeros
-            const uint32_t qb = piece % C::q_bufs, q_use = piece / C::q_bufs;
-            if (q_use > 0) {
+            const uint32_t qb = (uint32_t)piece % C::q_bufs;
+            if (piece >= C::q_bufs) {
                 if (owed >= 0) { cp_wait<0>(); look_over(); }          // (the queries' buffer may be waiting for it)
-                if (!mbar_wait(msmem_u32(&sm.q_empty[qb]), (q_use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                if (!mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             }
             {
-                const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (int64_t)pc.b * a.q_seq + ch * 8;
-                const uint32_t dst = msmem_u32(sm.q[qb]) + ch_q;
-                const int rows_here = min(C::rows, M - pc.rb * C::rows), rows_pad = (rows_here + 31) / 32 * 32;
-#pragma unroll 4
-                for (int r = lw * RW + sub; r < rows_pad; r += kLoadWarps * RW) {
-                    const int rr = pc.rb * C::rows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
-                    const bool in = r < rows_here && ch_in;
-                    cp_async16(dst + r * 128 + (swz ^ (((uint32_t)r & 7u) << 4)),
-                               in ? (const void*)(q + (int64_t)tok * a.q_row + (int64_t)head * a.q_head) : a.q, in ? 16u : 0u);
+                const int rows_here = min(C::rows, M - pc.rb * C::rows);
+                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * a.G * a.q_head + ch * 8);
+                const uint32_t dst = tiles + C::q_at + qb * C::q_bytes + (uint32_t)(ch >> 3) * C::q_half + (uint32_t)sub * 128;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows_here; r0 += 32) {          // a lane finds one row, and every lane copies chunks of all
+                    const int rr = min(pc.rb * C::rows + r0 + lane, M - 1), tok = rr / a.G;
+                    const int64_t mine = 2 * ((int64_t)tok * a.q_row + (int64_t)(rr - tok * a.G) * a.q_head);
+#pragma unroll
+                    for (int jj = 0; jj < NJ / kLoadWarps; ++jj) {
+                        const int j = jj * kLoadWarps + lw;
+                        const int64_t at = __shfl_sync(kFullMask, mine, j * RW + sub);
+                        const bool in = r0 + j * RW + sub < rows_here && ch_in;
+                        cp_async16(dst + (r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? q + at : (const char*)a.q, in ? 16u : 0u);
+                    }
                 }                                       // (the first keys' arrival counts them too)
             }
-            int64_t v_at = -1;
+            const char* const kb = (const char*)a.k + 2 * ((int64_t)pc.h * a.pages.head_stride + ch * 8);
+            const char* const vb = (const char*)a.v + 2 * ((int64_t)pc.h * a.pages.head_stride + ch * 8);
+            uint32_t v_at[NJ], v_there = 0;
             bool v_look = false;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) v_at[j] = 0;
+#pragma unroll 1
             for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++tile_no) {
                 if (f_arena) {                          // slots no row of the sequence sees are not read
                     const uint32_t any = __reduce_or_sync(kFullMask, f_m0 | f_m1);
                     f_in = f_in && ((any >> lane) & 1u);
                 }
-                if (f_in && (unsigned)f_id >= (unsigned)a.pages.num_pages) {
+                if (f_in && (uint32_t)f_id >= (uint32_t)a.pages.num_pages) {
                     atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
                     f_in = false;
                 }
-                const int64_t at = f_in ? (int64_t)f_id * a.pages.page_stride + (int64_t)f_row * a.pages.token_stride : -1;
+                // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
+                const uint32_t mine = f_in ? (uint32_t)((int64_t)f_id * page16 + (int64_t)f_row * token16) : 0u;
                 const bool look = f_arena;
                 const uint32_t there = __ballot_sync(kFullMask, f_in);
                 if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
                 if (t + 1 < pc.tile + pc.tiles) look_up(pc, t + 1);
                 else if (more) look_up(nx, nx.tile);
-                if (!load(a.k, at, pc.h, false, piece)) { ok = false; break; }
+                uint32_t at[NJ];
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) at[j] = __shfl_sync(kFullMask, mine, j * RW + sub);
+                if (!load(kb, at, there, false, piece)) { ok = false; break; }
                 // one S in tensor memory: K0 V0 K1 V1 ..;  two: K0 K1 V0 K2 V1 .. (the products run one tile ahead)
                 if (C::s_bufs == 1) {
-                    if (!load(a.v, at, pc.h, look, piece)) { ok = false; break; }
+                    if (!load(vb, at, there, look, piece)) { ok = false; break; }
                 } else {
-                    if (t > pc.tile && !load(a.v, v_at, pc.h, v_look, piece)) { ok = false; break; }
-                    v_at = at; v_look = look;
+                    if (t > pc.tile && !load(vb, v_at, v_there, v_look, piece)) { ok = false; break; }
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) v_at[j] = at[j];
+                    v_there = there; v_look = look;
                 }
             }
-            if (!ok || (C::s_bufs > 1 && !load(a.v, v_at, pc.h, v_look, piece))) { ok = false; break; }
+            if (!ok || (C::s_bufs > 1 && !load(vb, v_at, v_there, v_look, piece))) { ok = false; break; }
             ++piece;
         }
         cp_wait<0>();
@@ -335,7 +374,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
         constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
         const int ks_n = (a.D + 15) / 16;
-        const uint32_t q0 = msmem_u32(sm.q[0]), kv0 = msmem_u32(sm.kv[0]);
+        const uint32_t tiles = msmem_u32(sm.tiles), q0 = tiles + C::q_at - quarter * (32 * 128);      // the queries are the lanes from 32 quarter on
         uint32_t stage = 0, phase = 0;                 // of the next copy
         uint32_t g = 0;
         int piece = 0;
@@ -347,7 +386,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             if (lane == 0) {
                 fence_async_proxy();                   // the copies' writes (generic) before the products' reads
                 tc_after();
-                const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(kv0 + stage * C::stage_bytes, 16);
+                const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(tiles + C::stage_at(stage), 16);
                 const uint32_t sb = gi % C::s_bufs, d = tmem + C::s_col + sb * kMKeys;
 #pragma unroll 1
                 for (int ks = 0; ks < ks_n; ++ks)       // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns
@@ -378,7 +417,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 if (lane == 0) {
                     fence_async_proxy();
                     tc_after();
-                    const uint64_t dv = sw128_desc(kv0 + stage * C::stage_bytes, kMKeys * 128);
+                    const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
                     const uint32_t p = tmem + C::s_col + sb * kMKeys;
 #pragma unroll
                     for (int ks = 0; ks < kMKeys / 16; ++ks)          // 16 keys = two groups of eight rows of 128 bytes
@@ -398,13 +437,13 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last), 0)); ++i) {}
     } else {
         // ------------------------------------------------------------------ softmax: a row per thread
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const uint32_t lanes = (uint32_t)((SW == 1 ? quarter : warp) * 32) << 16;
         const float scale = fabsf(a.scale_log2e);
         const int row = warp * 32 + lane;
         bool ok = true;
         int piece = 0;
         uint32_t g = 0;
-        if (tid == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
+        if (warp == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
         // the row's mask words of the tile to come
         uint32_t next0 = 0, next1 = 0;
         const uint32_t* mask = nullptr;
@@ -482,9 +521,11 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                     uint32_t p[kMKeys / 2];
 #pragma unroll
                     for (int j = 0; j < kMKeys; j += 4) {
-                        const float e0 = ex2(fmaf(__uint_as_float(u[j]), scale, shift)), e1 = ex2(fmaf(__uint_as_float(u[j + 1]), scale, shift));
-                        const float e2 = ex2(fmaf(__uint_as_float(u[j + 2]), scale, shift)), e3 = ex2(fmaf(__uint_as_float(u[j + 3]), scale, shift));
-                        s0 += e0; s1 += e1; s2 += e2; s3 += e3;
+                        float e0, e1, e2, e3;
+                        fma2(e0, e1, __uint_as_float(u[j]), __uint_as_float(u[j + 1]), scale, shift);
+                        fma2(e2, e3, __uint_as_float(u[j + 2]), __uint_as_float(u[j + 3]), scale, shift);
+                        e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
+                        add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
                         p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
                     }
                     sum += (s0 + s1) + (s2 + s3);

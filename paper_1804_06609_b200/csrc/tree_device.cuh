@@ -5,11 +5,15 @@
 
 namespace dba {
 
+// place / page_size without a division: for places below 2^31, (place * mul) >> (32 + shift) with the numbers the host works out
+__device__ __forceinline__ uint32_t tree_page(const TreePages& pg, uint32_t place) {
+    return pg.page_size == 1 ? place : __umulhi(place, pg.page_mul) >> pg.page_shift;
+}
 // Element offset of a place of sequence b in one layer's cache; -1 where there is no such row (the place is outside the
 // table, or the table names a page outside the cache: recorded in the status word).  64 bits: a cache may be longer
 // than 2^31 elements.
 __device__ __forceinline__ int64_t tree_row(const TreePages& pg, int b, int place) {
-    const unsigned page = (unsigned)place / (unsigned)pg.page_size;
+    const unsigned page = tree_page(pg, (unsigned)place);
     if (place < 0 || page >= (unsigned)pg.max_pages) return -1;
     const int32_t id = __ldg(pg.table + (int64_t)b * pg.table_stride + page);
     if ((unsigned)id >= (unsigned)pg.num_pages) { atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_PAGE); return -1; }

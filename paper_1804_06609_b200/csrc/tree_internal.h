@@ -18,6 +18,8 @@ struct TreePages {
     int32_t num_pages, max_pages, page_size;
     int64_t page_stride, token_stride, head_stride;   // elements
     uint32_t* status;
+    uint32_t page_mul;                                // page_size's multiplier and shift (see tree_page)
+    int32_t page_shift;
 };
 
 // Attention, all sizes of one call.
@@ -43,7 +45,7 @@ struct TreeAttend {
 };
 
 struct TreeAttendPlan {
-    int grid;                          // blocks of the attention kernel
+    int grid, combine;                 // blocks of the attention kernel and of the one that joins its pieces
     int rows;                          // rows of an item
     bool tensor;                       // tcgen05 kernel
 };
