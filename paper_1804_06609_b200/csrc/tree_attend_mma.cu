@@ -124,6 +124,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// One lane of a warp in step, the same every time.  The matrix instructions take their operands from uniform registers: issued
+// under this predicate they cost some 20 cycles, under `lane == 0` some 100 to 200.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(yes)::"memory");
+    return yes != 0;
+}
 // arrives on the mbarrier once every matrix instruction issued so far by this thread has completed
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -373,7 +380,6 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     } else if (warp == SW) {
         // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
         constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
-        const int ks_n = (a.D + 15) / 16;
         const uint32_t tiles = msmem_u32(sm.tiles), q0 = tiles + C::q_at - quarter * (32 * 128);      // the queries are the lanes from 32 quarter on
         uint32_t stage = 0, phase = 0;                 // of the next copy
         uint32_t g = 0;
@@ -383,13 +389,14 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         // the scores of tile gi of the block's sequence; `last`: of its piece
         auto scores = [&](uint32_t gi, uint32_t qb, bool last) {
             if (!mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit)) return false;
-            if (lane == 0) {
+            const uint32_t sb = gi % C::s_bufs;
+            const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(tiles + C::stage_at(stage), 16);
+            const uint32_t d = tmem + C::s_col + sb * kMKeys;
+            if (elect_one()) {
                 fence_async_proxy();                   // the copies' writes (generic) before the products' reads
                 tc_after();
-                const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(tiles + C::stage_at(stage), 16);
-                const uint32_t sb = gi % C::s_bufs, d = tmem + C::s_col + sb * kMKeys;
-#pragma unroll 1
-                for (int ks = 0; ks < ks_n; ++ks)       // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns
+#pragma unroll
+                for (int ks = 0; ks < DP / 16; ++ks)    // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns (zeros beyond the head size)
                     mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kMKeys * 128 / 16) + (ks & 3) * 2),
                            idesc_s | negate, ks != 0);
                 mma_commit(msmem_u32(&sm.empty[stage]));
@@ -414,11 +421,11 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
                 if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
                 if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
-                if (lane == 0) {
+                const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
+                const uint32_t p = tmem + C::s_col + sb * kMKeys;
+                if (elect_one()) {
                     fence_async_proxy();
                     tc_after();
-                    const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
-                    const uint32_t p = tmem + C::s_col + sb * kMKeys;
 #pragma unroll
                     for (int ks = 0; ks < kMKeys / 16; ++ks)          // 16 keys = two groups of eight rows of 128 bytes
                         mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, (t | ks) != 0);
@@ -433,7 +440,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             ++piece;
         }
         // nothing of this block is in flight when it leaves, whatever happened
-        if (lane == 0) mma_commit(msmem_u32(&sm.last));
+        if (elect_one()) mma_commit(msmem_u32(&sm.last));
         for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last), 0)); ++i) {}
     } else {
         // ------------------------------------------------------------------ softmax: a row per thread
