@@ -11,6 +11,7 @@ struct dba_tree {
     cudaStream_t stream;
     int64_t ctx_cap;               // context places a table row holds
     uint32_t* status;
+    uint32_t* turns;
     int4* meta;
     float *part_ml, *part_o;
     long long wait_clocks;
@@ -54,6 +55,7 @@ size_t carve_tree(dba_tree* h, void* base) {
     const dba_tree_config& c = h->c;
     const TreeAttendPlan p = plan_tree_attend(c.dtype, c.rows * (c.heads / c.kv_heads), c.head_dim, h->sm_count);
     h->status = cv.take<uint32_t>(64);
+    h->turns = cv.take<uint32_t>(kTreeTurns);
     h->meta = cv.take<int4>(p.grid);
     h->part_ml = cv.take<float>((size_t)2 * p.grid * p.rows * 2);
     h->part_o = cv.take<float>((size_t)2 * p.grid * p.rows * c.head_dim);
@@ -125,7 +127,7 @@ dba_status dba_tree_init(const dba_tree_config* cfg, void* workspace_dev, size_t
     h->stream = (cudaStream_t)cuda_stream;
     cudaError_t e = configure_tree_attend();
     if (e == cudaSuccess) e = configure_tree_advance();
-    if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 256, h->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 256 + 4 * kTreeTurns, h->stream);     // (the turns lie behind it)
     if (e != cudaSuccess) { delete h; return DBA_ERR_CUDA; }
     *out = h;
     return DBA_OK;
@@ -174,7 +176,7 @@ dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* q, const dba_kv_ca
     a.o_seq = q->out_seq_stride; a.o_row = q->out_row_stride; a.o_head = q->out_head_stride;
     a.scale_log2e = (float)((double)q->scale * 1.4426950408889634);
     if (a.scale_log2e == 0.f) a.scale_log2e = 1e-37f;         // all scores alike; the kernels multiply -inf by it
-    a.part_o = h->part_o; a.part_ml = h->part_ml; a.meta = h->meta;
+    a.part_o = h->part_o; a.part_ml = h->part_ml; a.meta = h->meta; a.turns = h->turns;
     a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
     if (++h->calls == 0) h->calls = 1;         // (0: no call has failed)
     a.call = h->calls;

@@ -30,6 +30,7 @@ constexpr int kMRows = 128;                 // rows of the matrix instructions (
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
 constexpr int kBadSlots = 16;               // more than the tiles the loader may be ahead by
+constexpr int kPieces = 8;                  // more than the pieces the loader may be ahead by (a piece is two copies at least)
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
 
@@ -64,10 +65,12 @@ template <int DP, int SW> struct MSmem {
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
     uint64_t q_empty[C::q_bufs];
     uint64_t pv_done, o_free, told, last;
+    uint64_t published[kPieces];
+    int4 piece[kPieces][2];                 // (in turn) what the loader tells the others of a piece
     uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
     uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
     uint32_t tmem_base;
-    int abort_flag;
+    int abort_flag, turn, scheduler[4];
     TreeRunShared run;
 };
 
@@ -149,15 +152,20 @@ __device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* u) {
           "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* u) {
+__device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t* u) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(addr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
-        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]),
-        "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
-        "r"(u[30]), "r"(u[31])
+        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
         : "memory");
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -190,17 +198,12 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     extern __shared__ __align__(1024) unsigned char mraw[];
     MSmem<DP, SW>& sm = *reinterpret_cast<MSmem<DP, SW>*>(mraw);
     const int tid = threadIdx.x, lane = tid & 31;
-    // The warp's role: 0 .. SW-1 softmax, SW products, then the loaders.  A warp reaches the quarter of the tensor memory's lanes
-    // that its number modulo 4 names, and issues from the scheduler of that number: with one softmax warp the blocks of an
-    // SM take different ones (all on one scheduler: 140 us instead of 90 on 256 sentences of 20 short rows).
-    const int quarter = SW == 1 ? (blockIdx.x / (gridDim.x / C::blocks_per_sm)) & 3 : 0;
-    const int warp = SW == 1 ? ((tid >> 5) + 4 - quarter) & 3 : tid >> 5;
     volatile int* abort_flag = &sm.abort_flag;
     const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
     const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows;
 
     if (tid == 0) {
-        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads); mbar_init(msmem_u32(&sm.empty[s]), 1); }
+        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
         // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
         // may be a product ahead of it)
@@ -208,10 +211,31 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         for (int s = 0; s < C::q_bufs; ++s) mbar_init(msmem_u32(&sm.q_empty[s]), 1);
         mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), SW);
         mbar_init(msmem_u32(&sm.last), 1);
+        for (int i = 0; i < kPieces; ++i) mbar_init(msmem_u32(&sm.published[i]), 1);
         for (int i = 0; i < kBadSlots; ++i) sm.bad[i] = 0;
         sm.abort_flag = 0;
+        if (SW == 1) {
+            uint32_t sm_id;
+            asm volatile("mov.u32 %0, %smid;" : "=r"(sm_id));
+            sm.turn = (int)(atomicAdd(a.turns + sm_id % kTreeTurns, 1u) & 3u);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (SW == 1 && lane == 0) {
+        uint32_t slot;
+        asm volatile("mov.u32 %0, %warpid;" : "=r"(slot));
+        sm.scheduler[tid >> 5] = (int)(slot & 3u);
+    }
+    __syncthreads();
+    // The warp's role: 0 .. SW-1 softmax, SW products, then the loaders.  A warp reaches the quarter of the tensor memory's lanes
+    // that its number modulo 4 names, and issues from the scheduler of that number.  With one softmax warp to a block of
+    // four warps, the blocks of an SM take turns, so that their softmax warps do not share a scheduler.
+    int quarter = 0;
+    if (SW == 1) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) if (sm.scheduler[w] == sm.turn) quarter = w;
+    }
+    const int warp = SW == 1 ? ((tid >> 5) + 4 - quarter) & 3 : tid >> 5;
     if (warp == SW) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(msmem_u32(&sm.tmem_base)), "r"(C::tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -222,9 +246,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     TreeRun run = tree_run<C::threads>(a, kMKeys, a.K * row_blocks, 1, &sm.run);      // (has the block's barriers)
     tc_after();
     const uint32_t tmem = sm.tmem_base;
-    // every role walks the pieces of the run for itself, one ahead of its work: the next piece's numbers come out of the L2
-    TreePiece pc, nx;
-    bool more = tree_next_piece(a, run, kMKeys, row_blocks, true, &nx);
+    const int total = (int)(run.t_end - run.t);        // tiles of this block
 
     if (warp > SW) {
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
@@ -272,6 +294,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 }
             }
             cp_commit();
+            if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
             if (!look && (int)step != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
             if (owed >= 0 && (look || (int)step - owed >= 2)) {
                 if ((int)step - owed == 1) cp_wait<1>(); else cp_wait<2>();
@@ -305,12 +328,21 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             f_in = f_in && page < (uint32_t)a.pages.max_pages;
             f_id = f_in ? __ldg(a.pages.table + (int64_t)p.b * a.pages.table_stride + page) : 0;
         };
+        // The loader walks the pieces of the run, one ahead (the next piece's numbers come out of the L2), and tells the others.
+        TreePiece pc, nx;
+        bool more = tree_next_piece(a, run, kMKeys, row_blocks, true, &nx);
+        if (lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
         const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;        // rows in 16 bytes
         bool ok = true;
         int piece = 0, tile_no = 0;
         if (more) look_up(nx, nx.tile);
         while (more) {
             pc = nx;
+            if (lw == 0 && lane == 0) {
+                sm.piece[piece % kPieces][0] = make_int4(pc.b, pc.h, pc.rb, pc.top);
+                sm.piece[piece % kPieces][1] = make_int4(pc.tile, pc.tiles, pc.arena_tiles, pc.slot | (pc.whole ? 2 : 0));
+                mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
+            }
             more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
             // queries of the item: beyond the rows and the head size, zeros
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
@@ -408,15 +440,15 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             next_stage();
             return true;
         };
-        while (ok && more) {
-            pc = nx;
-            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
+        while (ok && (int)g < total) {
+            if (!(ok = mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit))) break;
+            const int n_tiles = sm.piece[piece % kPieces][1].y;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
-            ok = scores(g, qb, pc.tiles == 1);
+            ok = scores(g, qb, n_tiles == 1);
 #pragma unroll 1
-            for (int t = 0; t < pc.tiles && ok; ++t, ++g) {
+            for (int t = 0; t < n_tiles && ok; ++t, ++g) {
                 // one S in tensor memory: S0 O0 S1 O1 ..;  two: S0 S1 O0 S2 O1 ..
-                if (C::s_bufs > 1 && t + 1 < pc.tiles && !(ok = scores(g + 1, qb, t + 2 == pc.tiles))) break;
+                if (C::s_bufs > 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
                 const uint32_t sb = g % C::s_bufs;
                 if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
                 if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
@@ -431,11 +463,11 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                         mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, (t | ks) != 0);
                     mma_commit(msmem_u32(&sm.empty[stage]));
                     mma_commit(msmem_u32(&sm.pv_done));
-                    if (t + 1 == pc.tiles) mbar_arrive(msmem_u32(&sm.told));
+                    if (t + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
                 }
                 __syncwarp();
                 next_stage();
-                if (C::s_bufs == 1 && t + 1 < pc.tiles && !(ok = scores(g + 1, qb, t + 2 == pc.tiles))) break;
+                if (C::s_bufs == 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
             }
             ++piece;
         }
@@ -450,93 +482,100 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         bool ok = true;
         int piece = 0;
         uint32_t g = 0;
-        if (warp == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
-        // the row's mask words of the tile to come
-        uint32_t next0 = 0, next1 = 0;
-        const uint32_t* mask = nullptr;
-        auto mask_of = [&](const TreePiece& p) {
-            const int rr = min(p.rb * C::rows + row, M - 1);
-            return a.masks ? a.masks + ((int64_t)p.b * a.n + rr / a.G) * a.W : nullptr;
-        };
-        auto fetch_mask = [&](const TreePiece& p, const uint32_t* mk, int t) {
-            if (t < p.arena_tiles) {
-                next0 = __ldg(mk + 2 * t);
-                next1 = 2 * t + 1 < a.W ? __ldg(mk + 2 * t + 1) : 0u;
-            }
-        };
-        const uint32_t* next_mask = nullptr;
-        if (more) { next_mask = mask_of(nx); fetch_mask(nx, next_mask, nx.tile); }
-        while (ok && more) {
-            pc = nx;
-            mask = next_mask;
-            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
-            const int rr = pc.rb * C::rows + row;
-            const bool active = pc.rb * C::rows + warp * 32 < M;      // the warp has rows
-            const int tok = min(rr, M - 1) / a.G, head = pc.h * a.G + rr - tok * a.G;
+        while (ok && (int)g < total) {
+            if (!mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit)) { ok = false; break; }
+            const int4 i0 = sm.piece[piece % kPieces][0], i1 = sm.piece[piece % kPieces][1];
+            const int p_b = i0.x, p_top = i0.w, p_tile = i1.x, p_end = i1.x + i1.y, p_arena = i1.z;
+            const int rr = i0.z * C::rows + row;
+            const bool active = i0.z * C::rows + warp * 32 < M;       // the warp has rows
+            const int tok = min(rr, M - 1) / a.G;
+            // the row's mask words of the tile to come
+            const uint32_t* mask = a.masks ? a.masks + ((int64_t)p_b * a.n + tok) * a.W : nullptr;
+            uint32_t next0 = 0, next1 = 0;
+            auto fetch_mask = [&](int t) {
+                if (t < p_arena) {
+                    next0 = __ldg(mask + 2 * t);
+                    next1 = 2 * t + 1 < a.W ? __ldg(mask + 2 * t + 1) : 0u;
+                }
+            };
+            fetch_mask(p_tile);
             uint32_t any = a.masks ? 0u : 1u;                         // an empty mask closes the row: its words, as the tiles come by
             if (a.masks)
-                for (int w = 0; w < min(2 * pc.tile, (pc.top + 31) / 32); ++w) any |= __ldg(mask + w);      // (those before a piece that begins inside)
+                for (int w = 0; w < min(2 * p_tile, (p_top + 31) / 32); ++w) any |= __ldg(mask + w);      // (those before a piece that begins inside)
             float ref = neg_inf(), sum = 0.f;
-            for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++g) {
+#pragma unroll 1
+            for (int t = p_tile; t < p_end; ++t, ++g) {
                 const uint32_t sb = g % C::s_bufs;
                 uint32_t see0, see1;
-                if (t < pc.arena_tiles) { see0 = next0; see1 = next1; any |= see0 | see1; }
+                if (t < p_arena) { see0 = next0; see1 = next1; any |= see0 | see1; }
                 else see0 = see1 = any ? 0xffffffffu : 0u;
                 if (rr >= M) see0 = see1 = 0;
-                if (t + 1 < pc.tile + pc.tiles) fetch_mask(pc, mask, t + 1);
-                else if (more) { next_mask = mask_of(nx); fetch_mask(nx, next_mask, nx.tile); }
+                if (t + 1 < p_end) fetch_mask(t + 1);
                 if (!mbar_wait(msmem_u32(&sm.s_full[sb]), (g / C::s_bufs) & 1u, abort_flag, limit)) { ok = false; break; }
                 if (active) {
                     tc_after();
                     see0 &= sm.seen[g % kBadSlots][0]; see1 &= sm.seen[g % kBadSlots][1];
+                    // 32 columns at a time; where no row of the warp sees any of them (the end of the arena or of the context), none
+                    const bool half[2] = {__any_sync(kFullMask, see0 != 0) != 0, __any_sync(kFullMask, see1 != 0) != 0};
                     uint32_t u[kMKeys];
-                    tm_ld32(tmem + lanes + C::s_col + sb * kMKeys, u);
-                    tm_ld32(tmem + lanes + C::s_col + sb * kMKeys + 32, u + 32);
-                    if (__any_sync(kFullMask, (see0 & see1) != 0xffffffffu)) {
+                    float m0 = neg_inf(), m1 = m0, m2 = m0, m3 = m0;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (!((see0 >> j) & 1u)) u[j] = 0xff800000u;
-                            if (!((see1 >> j) & 1u)) u[32 + j] = 0xff800000u;
+                    for (int h = 0; h < 2; ++h) {
+                        if (!half[h]) continue;
+                        const uint32_t see = h ? see1 : see0;
+                        uint32_t* x = u + 32 * h;
+                        tm_ld32(tmem + lanes + C::s_col + sb * kMKeys + 32 * h, x);
+                        if (__any_sync(kFullMask, see != 0xffffffffu)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (!(see & (1u << j))) x[j] = 0xff800000u;
                         }
-                    }
-                    float m0 = __uint_as_float(u[0]), m1 = __uint_as_float(u[1]), m2 = __uint_as_float(u[2]), m3 = __uint_as_float(u[3]);
 #pragma unroll
-                    for (int j = 4; j < kMKeys; j += 4) {
-                        m0 = fmaxf(m0, __uint_as_float(u[j])); m1 = fmaxf(m1, __uint_as_float(u[j + 1]));
-                        m2 = fmaxf(m2, __uint_as_float(u[j + 2])); m3 = fmaxf(m3, __uint_as_float(u[j + 3]));
+                        for (int j = 0; j < 32; j += 4) {
+                            m0 = fmaxf(m0, __uint_as_float(x[j])); m1 = fmaxf(m1, __uint_as_float(x[j + 1]));
+                            m2 = fmaxf(m2, __uint_as_float(x[j + 2])); m3 = fmaxf(m3, __uint_as_float(x[j + 3]));
+                        }
                     }
                     const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
                     const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
                     if (__any_sync(kFullMask, raise)) {
                         const float factor = raise ? ex2(ref - top) : 1.f;             // 0 where nothing has been seen before
                         if (raise) { ref = top; sum *= factor; }
-                        if (t > pc.tile) {
+                        if (t > p_tile) {
                             if (!mbar_wait(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
                             tc_after();
 #pragma unroll 1
-                            for (int c = 0; c < DP; c += 32) {
-                                uint32_t o[32];
-                                tm_ld32(tmem + lanes + C::o_col + c, o);
+                            for (int c = 0; c < DP; c += 16) {
+                                uint32_t o[16];
+                                tm_ld16(tmem + lanes + C::o_col + c, o);
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
-                                tm_st32(tmem + lanes + C::o_col + c, o);
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
+                                tm_st16(tmem + lanes + C::o_col + c, o);
                             }
                         }
                     }
                     const float shift = ref == neg_inf() ? 0.f : -ref;
                     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-                    uint32_t p[kMKeys / 2];
 #pragma unroll
-                    for (int j = 0; j < kMKeys; j += 4) {
-                        float e0, e1, e2, e3;
-                        fma2(e0, e1, __uint_as_float(u[j]), __uint_as_float(u[j + 1]), scale, shift);
-                        fma2(e2, e3, __uint_as_float(u[j + 2]), __uint_as_float(u[j + 3]), scale, shift);
-                        e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
-                        add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
-                        p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t p[16];
+                        if (half[h]) {
+                            const uint32_t* x = u + 32 * h;
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                float e0, e1, e2, e3;
+                                fma2(e0, e1, __uint_as_float(x[j]), __uint_as_float(x[j + 1]), scale, shift);
+                                fma2(e2, e3, __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]), scale, shift);
+                                e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
+                                add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
+                                p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) p[j] = 0;
+                        }
+                        tm_st16(tmem + lanes + C::s_col + sb * kMKeys + 16 * h, p);
                     }
                     sum += (s0 + s1) + (s2 + s3);
-                    tm_st32(tmem + lanes + C::s_col + sb * kMKeys, p);
                     tm_wait_st();
                     tc_before();
                 }
@@ -549,25 +588,27 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             if (active) {
                 tc_after();
                 const bool bad = sm.bad[piece % kBadSlots] == (uint32_t)piece + 1;
-                const float inv = pc.whole && sum > 0.f ? 1.f / sum : 1.f;
-                const int64_t part = (int64_t)(2 * blockIdx.x + pc.slot) * C::rows + row;
-                __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)pc.b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
+                const bool whole = i1.w & 2;
+                const float inv = !(sum > 0.f) ? 0.f : whole ? __frcp_rn(sum) : 1.f;
+                const int p_h = sm.piece[piece % kPieces][0].y, head = p_h * a.G + rr - tok * a.G;
+                const int64_t part = (int64_t)(2 * blockIdx.x + (i1.w & 1)) * C::rows + row;
+                __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)p_b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
 #pragma unroll 1
-                for (int c = 0; c < DP; c += 32) {
-                    uint32_t u[32];
+                for (int c = 0; c < DP; c += 16) {
+                    uint32_t u[16];
                     __syncwarp();
-                    tm_ld32(tmem + lanes + C::o_col + c, u);
+                    tm_ld16(tmem + lanes + C::o_col + c, u);
                     if (rr >= M) continue;
-                    float o[32];
+                    float o[16];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) o[j] = sum == 0.f ? 0.f : __uint_as_float(u[j]);
+                    for (int j = 0; j < 16; ++j) o[j] = sum == 0.f ? 0.f : __uint_as_float(u[j]) * inv;      // (a closed row's O may hold anything)
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
+                    for (int j = 0; j < 16; j += 8) {
                         if (c + j >= a.D) continue;
-                        if (pc.whole) {
+                        if (whole) {
                             uint4 w;
-                            w.x = pack_bf16(o[j] * inv, o[j + 1] * inv); w.y = pack_bf16(o[j + 2] * inv, o[j + 3] * inv);
-                            w.z = pack_bf16(o[j + 4] * inv, o[j + 5] * inv); w.w = pack_bf16(o[j + 6] * inv, o[j + 7] * inv);
+                            w.x = pack_bf16(o[j], o[j + 1]); w.y = pack_bf16(o[j + 2], o[j + 3]);
+                            w.z = pack_bf16(o[j + 4], o[j + 5]); w.w = pack_bf16(o[j + 6], o[j + 7]);
                             *reinterpret_cast<uint4*>(out + c + j) = w;
                         } else {
                             float4* po = reinterpret_cast<float4*>(a.part_o + part * a.D + c + j);
@@ -577,21 +618,21 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                     }
                 }
                 if (bad && rr < M && sum > 0.f)        // values that are not finite, at the slots this row sees, onto what has been written
-                    for (int j = pc.tile * kMKeys; j < min((pc.tile + pc.tiles) * kMKeys, pc.top); ++j) {
+                    for (int j = p_tile * kMKeys; j < min(p_end * kMKeys, p_top); ++j) {
                         if (!((__ldg(mask + (j >> 5)) >> (j & 31)) & 1u)) continue;
-                        const int64_t at = tree_row(a.pages, pc.b, j);
+                        const int64_t at = tree_row(a.pages, p_b, j);
                         if (at < 0) continue;
-                        const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + at + (int64_t)pc.h * a.pages.head_stride;
+                        const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + at + (int64_t)p_h * a.pages.head_stride;
                         for (int d = 0; d < a.D; ++d) {
                             const float x = __bfloat162float(v[d]);
                             if (fabsf(x) <= 3.4e38f) continue;
-                            if (pc.whole) out[d] = __float2bfloat16_rn(__bfloat162float(out[d]) + x);
+                            if (whole) out[d] = __float2bfloat16_rn(__bfloat162float(out[d]) + x);
                             else a.part_o[part * a.D + d] += x;
                         }
                     }
                 if (rr < M) {
-                    if (!pc.whole) { a.part_ml[2 * part] = ref; a.part_ml[2 * part + 1] = sum; }
-                    else if (a.lse) a.lse[((int64_t)pc.b * a.n + tok) * a.H + head] = sum == 0.f ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+                    if (!whole) { a.part_ml[2 * part] = ref; a.part_ml[2 * part + 1] = sum; }
+                    else if (a.lse) a.lse[((int64_t)p_b * a.n + tok) * a.H + head] = sum == 0.f ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
                 }
                 tc_before();
             }

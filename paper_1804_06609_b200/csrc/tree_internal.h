@@ -10,6 +10,7 @@ namespace dba {
 constexpr int kTreeMaxRows = 64;       // rows per sequence (one bit each in a 64-bit mask of ancestors)
 constexpr int kTreeMaxWords = 128;     // arena words per sequence
 constexpr int kTreeMaxDim = 256;
+constexpr int kTreeTurns = 256;        // SMs told apart by number
 
 // What a kernel needs to find the rows of one layer's cache.
 struct TreePages {
@@ -38,6 +39,7 @@ struct TreeAttend {
     // split work: the tiles of all items are dealt out in equal contiguous runs
     float* part_o;                     // [2 * grid][rows of an item][D]: unfinished first and last items of a block's run
     float* part_ml;                    // [2 * grid][rows of an item][2]: their maxima (of the scaled scores, in powers of two) and sums
+    uint32_t* turns;                   // [kTreeTurns] a counter per SM, which goes on from call to call: blocks on an SM take turns by it
     int4* meta;                        // [grid] item shared with the block before this one, if that block is the first on it
     long long wait_clocks;
     int drop_item;
