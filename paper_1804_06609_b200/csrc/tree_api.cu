@@ -53,7 +53,7 @@ struct TreeCarver {
 size_t carve_tree(dba_tree* h, void* base) {
     TreeCarver cv{(char*)base};
     const dba_tree_config& c = h->c;
-    const TreeAttendPlan p = plan_tree_attend(c.dtype, c.rows * (c.heads / c.kv_heads), c.head_dim, h->sm_count);
+    const TreeAttendPlan p = plan_tree_attend(c.dtype, c.rows * (c.heads / c.kv_heads), c.kv_heads, c.head_dim, h->sm_count);
     h->status = cv.take<uint32_t>(64);
     h->turns = cv.take<uint32_t>(kTreeTurns);
     h->meta = cv.take<int4>(p.grid);
@@ -182,7 +182,9 @@ dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* q, const dba_kv_ca
     a.call = h->calls;
     int n = 0;
     // (planned for the configuration's rows: the workspace was sized for that)
-    const cudaError_t e = launch_tree_attend(a, plan_tree_attend(c.dtype, c.rows * a.G, c.head_dim, h->sm_count), c.dtype, h->stream, &n);
+    const TreeAttendPlan plan = plan_tree_attend(c.dtype, c.rows * a.G, c.kv_heads, c.head_dim, h->sm_count);
+    a.item_heads = plan.item_heads;
+    const cudaError_t e = launch_tree_attend(a, plan, c.dtype, h->stream, &n);
     h->launches += n;
     return launched(e);
 }

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
     TreePiece pc;
     bool first = true;
     if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, KT, row_blocks);
-    while (tree_next_piece(a, run, KT, row_blocks, first, &pc)) {
+    while (tree_next_piece(a, run, KT, a.K, row_blocks, first, &pc)) {
         if (first && tid == 0) tree_write_meta(a, run, &pc, KT, row_blocks);
         first = false;
         const int rows_here = min(kGRows, M - pc.rb * kGRows);
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
         }
         return;
     }
-    const int M = a.n * a.G, row_blocks = (M + item_rows - 1) / item_rows, rows = min(M, item_rows);
+    const int M = a.n * a.G, head_rows = item_rows / a.item_heads, row_blocks = (M + head_rows - 1) / head_rows, per_head = min(M, head_rows), rows = a.item_heads * per_head;
     int n_items = 0, n_most = 0;
     for (int c0 = 0; c0 < blocks; c0 += kCombineThreads) {
         const int c = c0 + tid;
@@ -278,10 +278,11 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     for (int task = many ? blockIdx.x : blockIdx.x * kCombineWarps + warp; task < n_items * rows; task += step) {
         const int item = task / rows, r = task - item * rows, c = shared_items[item];
         const int4 meta = a.meta[c];
-        const int b = meta.x, h = meta.y / row_blocks, rb = meta.y - h * row_blocks, rr = rb * item_rows + r;
+        const int b = meta.x, group = meta.y / row_blocks, rb = meta.y - group * row_blocks;
+        const int in_item = r / per_head, in_head = r - in_item * per_head, h = group * a.item_heads + in_item, rr = rb * head_rows + in_head;
         if (rr >= M) continue;                             // (the same for all warps of a task)
         const int first = c - 1, n = meta.z - first + 1;
-        auto place = [&](int i) { return (int64_t)(2 * (first + i) + (i == 0 ? meta.w : 0)) * item_rows + r; };
+        auto place = [&](int i) { return (int64_t)(2 * (first + i) + (i == 0 ? meta.w : 0)) * item_rows + in_item * head_rows + in_head; };
         float m = neg_inf();
         for (int i = lane; i < n; i += 32) m = fmaxf(m, a.part_ml[2 * place(i)]);
         m = warp_max(m);
@@ -337,16 +338,16 @@ cudaError_t launch_fp32(const TreeAttend& a, int grid, cudaStream_t st) {
 
 }  // namespace
 
-TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count) {
+TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
     TreeAttendPlan p{};
     p.combine = 2 * sm_count;
     if (tree_mma_usable(dtype, D)) {
         p.tensor = true;
-        p.rows = tree_mma_rows(M);
-        p.grid = tree_mma_blocks_per_sm(D, p.rows) * sm_count;
+        tree_mma_plan(M, K, D, sm_count, &p);
         return p;
     }
     p.rows = kGRows;
+    p.item_heads = 1;
     p.grid = 2 * sm_count;                 // two blocks of up to 105 KB of shared memory share an SM
     return p;
 }

@@ -34,18 +34,23 @@ constexpr int kPieces = 8;                  // more than the pieces the loader m
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
 
-// SW softmax warps = items of up to 32 SW rows.  The products always work on 128 rows; with SW = 1 the other 96 are whatever
-// follows the queries in shared memory, and nobody reads their results.
-template <int DP, int SW> struct MConf {
-    static constexpr int rows = 32 * SW;
+// SW softmax warps; an item is a block of rows of HP key heads.
+//   <DP, 4, 1>  up to 128 rows of one key head
+//   <DP, 4, 4>  up to 32 rows of each of four neighbouring key heads, a softmax warp to each.  Four products per tile, each of
+//               which writes the quarter of the lanes that is its head's.  The four share what a tile costs beside its
+//               bytes: its look-ups, masks and the way through the roles.
+//   <DP, 1, 1>  up to 32 rows of one key head, where there are not four to take.  The other 96 rows of the products are what
+//               lies around the queries in shared memory, and nobody reads their results.
+template <int DP, int SW, int HP> struct MConf {
+    static constexpr int rows = 32 * SW / HP;                        // of a key head
     static constexpr int threads = 32 * (SW + 1 + kLoadWarps);
-    static constexpr int stages = DP == 128 ? (SW == 1 ? 6 : 5) : SW == 1 ? 5 : 9;      // tiles of keys or values in shared memory
-    static constexpr int stage_bytes = kMKeys * DP * 2;
-    static constexpr int q_half = rows * 128;                        // 64 columns of the queries
-    static constexpr int q_bytes = rows * DP * 2;
-    static constexpr int q_bufs = DP == 64 || SW == 1 ? 2 : 1;
+    static constexpr int stages = HP == 4 ? 3 : DP == 128 ? (SW == 1 ? 6 : 5) : SW == 1 ? 5 : 9;      // tiles of keys or values in shared memory
+    static constexpr int head_bytes = kMKeys * DP * 2, stage_bytes = HP * head_bytes;
+    static constexpr int q_half = 32 * SW * 128;                     // 64 columns of the queries
+    static constexpr int q_bytes = 32 * SW * DP * 2;
+    static constexpr int q_bufs = SW == 1 || (DP == 64 && HP == 1) ? 2 : 1;
     static constexpr int s_bufs = DP == 64 && SW == 1 ? 1 : 2;
-    static constexpr int blocks_per_sm = DP == 64 && SW == 1 ? 4 : 2;
+    static constexpr int blocks_per_sm = DP == 64 && SW == 1 ? 4 : DP == 128 && HP == 4 ? 1 : 2;
     static constexpr int tmem_cols = s_bufs == 1 ? 128 : 256;
     static constexpr int o_col = 0, s_col = DP;
     // stages that lie before the queries: with one softmax warp the products' other rows are read up to 96 rows before and
@@ -58,8 +63,8 @@ template <int DP, int SW> struct MConf {
     static __device__ __forceinline__ uint32_t stage_at(uint32_t s) { return s * stage_bytes + (pre == 0 || (int)s >= pre ? q_bufs * q_bytes : 0); }
 };
 
-template <int DP, int SW> struct MSmem {
-    using C = MConf<DP, SW>;
+template <int DP, int SW, int HP> struct MSmem {
+    using C = MConf<DP, SW, HP>;
     alignas(1024) unsigned char tiles[C::tile_bytes];       // keys, values and queries
     uint64_t full[C::stages], empty[C::stages];
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
@@ -119,13 +124,24 @@ __device__ __forceinline__ uint64_t sw128_desc(uint32_t addr, uint32_t lead) {
 __host__ __device__ constexpr uint32_t mma_idesc(int n, bool b_mn_major) {
     return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(kMRows >> 4) << 24;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+// `only` >= 0: of the accumulator's lanes, only the quarter of that number is written
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, int only) {
+    if (only < 0)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(only == 0 ? 0u : ~0u), "r"(only == 1 ? 0u : ~0u),
+                     "r"(only == 2 ? 0u : ~0u), "r"(only == 3 ? 0u : ~0u) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, int only) {
+    if (only < 0)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(only == 0 ? 0u : ~0u), "r"(only == 1 ? 0u : ~0u),
+                     "r"(only == 2 ? 0u : ~0u), "r"(only == 3 ? 0u : ~0u) : "memory");
 }
 // One lane of a warp in step, the same every time.  The matrix instructions take their operands from uniform registers: issued
 // under this predicate they cost some 20 cycles, under `lane == 0` some 100 to 200.
@@ -192,15 +208,15 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x, bool* found) {
     return r;
 }
 
-template <int DP, int SW>
-__global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
-    using C = MConf<DP, SW>;
+template <int DP, int SW, int HP>
+__global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
+    using C = MConf<DP, SW, HP>;
     extern __shared__ __align__(1024) unsigned char mraw[];
-    MSmem<DP, SW>& sm = *reinterpret_cast<MSmem<DP, SW>*>(mraw);
+    MSmem<DP, SW, HP>& sm = *reinterpret_cast<MSmem<DP, SW, HP>*>(mraw);
     const int tid = threadIdx.x, lane = tid & 31;
     volatile int* abort_flag = &sm.abort_flag;
     const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
-    const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows;
+    const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows, groups = a.K / HP;
 
     if (tid == 0) {
         for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
@@ -243,7 +259,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     tc_before();
     grid_dependency_wait();
     allow_dependents();
-    TreeRun run = tree_run<C::threads>(a, kMKeys, a.K * row_blocks, 1, &sm.run);      // (has the block's barriers)
+    TreeRun run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, 1, &sm.run);      // (has the block's barriers)
     tc_after();
     const uint32_t tmem = sm.tmem_base;
     const int total = (int)(run.t_end - run.t);        // tiles of this block
@@ -255,6 +271,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         const int lw = warp - SW - 1, ch = lane % CH, sub = lane / CH;
         const bool ch_in = ch * 8 < a.D, full_head = a.D == DP;
         const uint32_t tiles = msmem_u32(sm.tiles);
+        const int64_t head2 = 2 * a.pages.head_stride;          // bytes from a key head to the next
         // this lane's place in rows sub, sub + RW, ..: the swizzle moves a chunk by the row's last three bits
         const uint32_t in_kv = (uint32_t)(ch >> 3) * (kMKeys * 128) + (uint32_t)(lw * 32 + sub) * 128;
         const uint32_t swz = ((uint32_t)(ch & 7) ^ (uint32_t)sub) << 4;
@@ -264,8 +281,9 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         auto look_over = [&]() {                       // (its copies have landed)
             bool found = false;
 #pragma unroll 4
-            for (int j = 0; j < NJ; ++j) {
-                uint4* v = reinterpret_cast<uint4*>(sm.tiles + C::stage_at(owed_stage) + in_kv + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)));
+            for (int i = 0; i < HP * NJ; ++i) {
+                const int w = i / NJ, j = i - w * NJ;
+                uint4* v = reinterpret_cast<uint4*>(sm.tiles + C::stage_at(owed_stage) + w * C::head_bytes + in_kv + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)));
                 uint4 x = *v;
                 bool f = false;
                 x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
@@ -284,13 +302,20 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
             if (there == 0xffffffffu && full_head) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    cp_async16(dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), base + (uint64_t)at[j] * 16, 16u);
+                for (int j = 0; j < NJ; ++j) {
+                    const char* src = base + (uint64_t)at[j] * 16;
+#pragma unroll
+                    for (int w = 0; w < HP; ++w)
+                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), src + w * head2, 16u);
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const bool in = ((there >> (j * RW + sub)) & 1u) && ch_in;
-                    cp_async16(dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? base + (uint64_t)at[j] * 16 : (const char*)a.k, in ? 16u : 0u);
+                    const char* src = in ? base + (uint64_t)at[j] * 16 : (const char*)a.k;
+#pragma unroll
+                    for (int w = 0; w < HP; ++w)
+                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? src + w * head2 : src, in ? 16u : 0u);
                 }
             }
             cp_commit();
@@ -330,7 +355,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
         };
         // The loader walks the pieces of the run, one ahead (the next piece's numbers come out of the L2), and tells the others.
         TreePiece pc, nx;
-        bool more = tree_next_piece(a, run, kMKeys, row_blocks, true, &nx);
+        bool more = tree_next_piece(a, run, kMKeys, groups, row_blocks, true, &nx);
         if (lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
         const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;        // rows in 16 bytes
         bool ok = true;
@@ -343,7 +368,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 sm.piece[piece % kPieces][1] = make_int4(pc.tile, pc.tiles, pc.arena_tiles, pc.slot | (pc.whole ? 2 : 0));
                 mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
             }
-            more = tree_next_piece(a, run, kMKeys, row_blocks, false, &nx);
+            more = tree_next_piece(a, run, kMKeys, groups, row_blocks, false, &nx);
             // queries of the item: beyond the rows and the head size, zeros
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
             if (piece >= C::q_bufs) {
@@ -352,7 +377,7 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             }
             {
                 const int rows_here = min(C::rows, M - pc.rb * C::rows);
-                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * a.G * a.q_head + ch * 8);
+                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head + ch * 8);
                 const uint32_t dst = tiles + C::q_at + qb * C::q_bytes + (uint32_t)(ch >> 3) * C::q_half + (uint32_t)sub * 128;
 #pragma unroll 1
                 for (int r0 = 0; r0 < rows_here; r0 += 32) {          // a lane finds one row, and every lane copies chunks of all
@@ -363,12 +388,15 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                         const int j = jj * kLoadWarps + lw;
                         const int64_t at = __shfl_sync(kFullMask, mine, j * RW + sub);
                         const bool in = r0 + j * RW + sub < rows_here && ch_in;
-                        cp_async16(dst + (r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? q + at : (const char*)a.q, in ? 16u : 0u);
+#pragma unroll
+                        for (int w = 0; w < HP; ++w)
+                            cp_async16(dst + (w * 32 + r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)),
+                                       in ? q + at + 2 * (int64_t)(w * a.G) * a.q_head : (const char*)a.q, in ? 16u : 0u);
                     }
                 }                                       // (the first keys' arrival counts them too)
             }
-            const char* const kb = (const char*)a.k + 2 * ((int64_t)pc.h * a.pages.head_stride + ch * 8);
-            const char* const vb = (const char*)a.v + 2 * ((int64_t)pc.h * a.pages.head_stride + ch * 8);
+            const char* const kb = (const char*)a.k + pc.h * HP * head2 + ch * 16;
+            const char* const vb = (const char*)a.v + pc.h * HP * head2 + ch * 16;
             uint32_t v_at[NJ], v_there = 0;
             bool v_look = false;
 #pragma unroll
@@ -428,9 +456,11 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 fence_async_proxy();                   // the copies' writes (generic) before the products' reads
                 tc_after();
 #pragma unroll
-                for (int ks = 0; ks < DP / 16; ++ks)    // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns (zeros beyond the head size)
-                    mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kMKeys * 128 / 16) + (ks & 3) * 2),
-                           idesc_s | negate, ks != 0);
+                for (int w = 0; w < HP; ++w)
+#pragma unroll
+                    for (int ks = 0; ks < DP / 16; ++ks)    // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns (zeros beyond the head size)
+                        mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2),
+                               dk + (uint64_t)((w * C::head_bytes + (ks >> 2) * (kMKeys * 128)) / 16 + (ks & 3) * 2), idesc_s | negate, ks != 0, HP > 1 ? w : -1);
                 mma_commit(msmem_u32(&sm.empty[stage]));
                 mma_commit(msmem_u32(&sm.s_full[sb]));
                 mbar_arrive(msmem_u32(&sm.s_full[sb]));
@@ -459,8 +489,10 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                     fence_async_proxy();
                     tc_after();
 #pragma unroll
-                    for (int ks = 0; ks < kMKeys / 16; ++ks)          // 16 keys = two groups of eight rows of 128 bytes
-                        mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, (t | ks) != 0);
+                    for (int w = 0; w < HP; ++w)
+#pragma unroll
+                        for (int ks = 0; ks < kMKeys / 16; ++ks)      // 16 keys = two groups of eight rows of 128 bytes
+                            mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)((w * C::head_bytes + ks * 2048) / 16), idesc_o, (t | ks) != 0, HP > 1 ? w : -1);
                     mma_commit(msmem_u32(&sm.empty[stage]));
                     mma_commit(msmem_u32(&sm.pv_done));
                     if (t + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
@@ -486,8 +518,8 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
             if (!mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit)) { ok = false; break; }
             const int4 i0 = sm.piece[piece % kPieces][0], i1 = sm.piece[piece % kPieces][1];
             const int p_b = i0.x, p_top = i0.w, p_tile = i1.x, p_end = i1.x + i1.y, p_arena = i1.z;
-            const int rr = i0.z * C::rows + row;
-            const bool active = i0.z * C::rows + warp * 32 < M;       // the warp has rows
+            const int rr = i0.z * C::rows + (HP > 1 ? lane : row);
+            const bool active = HP > 1 || i0.z * C::rows + warp * 32 < M;       // the warp has rows
             const int tok = min(rr, M - 1) / a.G;
             // the row's mask words of the tile to come
             const uint32_t* mask = a.masks ? a.masks + ((int64_t)p_b * a.n + tok) * a.W : nullptr;
@@ -590,8 +622,8 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
                 const bool bad = sm.bad[piece % kBadSlots] == (uint32_t)piece + 1;
                 const bool whole = i1.w & 2;
                 const float inv = !(sum > 0.f) ? 0.f : whole ? __frcp_rn(sum) : 1.f;
-                const int p_h = sm.piece[piece % kPieces][0].y, head = p_h * a.G + rr - tok * a.G;
-                const int64_t part = (int64_t)(2 * blockIdx.x + (i1.w & 1)) * C::rows + row;
+                const int p_h = sm.piece[piece % kPieces][0].y * HP + (HP > 1 ? warp : 0), head = p_h * a.G + rr - tok * a.G;
+                const int64_t part = (int64_t)(2 * blockIdx.x + (i1.w & 1)) * (32 * SW) + row;
                 __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)p_b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
 #pragma unroll 1
                 for (int c = 0; c < DP; c += 16) {
@@ -648,33 +680,43 @@ __global__ void __launch_bounds__(MConf<DP, SW>::threads, MConf<DP, SW>::blocks_
     if (tid == 0 && sm.abort_flag) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
 }
 
-template <int DP, int SW>
+template <int DP, int SW, int HP>
 cudaError_t configure_mma() {
-    return cudaFuncSetAttribute(tree_attend_mma_kernel<DP, SW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP, SW>));
+    return cudaFuncSetAttribute(tree_attend_mma_kernel<DP, SW, HP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP, SW, HP>));
 }
-template <int DP, int SW>
+template <int DP, int SW, int HP>
 cudaError_t launch_mma(const TreeAttend& a, int grid, cudaStream_t st) {
     const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
-    return launch_after(tree_attend_mma_kernel<DP, SW>, dim3(grid), dim3(MConf<DP, SW>::threads), sizeof(MSmem<DP, SW>), st, a, negate);
+    return launch_after(tree_attend_mma_kernel<DP, SW, HP>, dim3(grid), dim3(MConf<DP, SW, HP>::threads), sizeof(MSmem<DP, SW, HP>), st, a, negate);
+}
+template <int DP>
+int blocks_mma(int rows, int heads) {
+    return rows == 32 ? MConf<DP, 1, 1>::blocks_per_sm : heads == 4 ? MConf<DP, 4, 4>::blocks_per_sm : MConf<DP, 4, 1>::blocks_per_sm;
+}
+template <int DP>
+cudaError_t launch_mma_d(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
+    return rows == 32 ? launch_mma<DP, 1, 1>(a, grid, st) : a.item_heads == 4 ? launch_mma<DP, 4, 4>(a, grid, st) : launch_mma<DP, 4, 1>(a, grid, st);
 }
 
 }  // namespace
 
 bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
-// Rows of an item: one softmax warp where the rows of a key head fit it, else four.
-int tree_mma_rows(int M) { return M <= 32 ? 32 : kMRows; }
-int tree_mma_blocks_per_sm(int D, int rows) {
-    return D <= 64 ? (rows == 32 ? MConf<64, 1>::blocks_per_sm : MConf<64, 4>::blocks_per_sm) : rows == 32 ? MConf<128, 1>::blocks_per_sm : MConf<128, 4>::blocks_per_sm;
+// Up to 32 rows to a key head: four heads at a time where their number allows, else one softmax warp.
+void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p) {
+    p->item_heads = M <= 32 && K % 4 == 0 ? 4 : 1;
+    p->rows = M <= 32 && p->item_heads == 1 ? 32 : kMRows;
+    p->grid = sm_count * (D <= 64 ? blocks_mma<64>(p->rows, p->item_heads) : blocks_mma<128>(p->rows, p->item_heads));
 }
 cudaError_t configure_tree_mma() {
-    cudaError_t e = configure_mma<64, 1>();
-    if (e == cudaSuccess) e = configure_mma<64, 4>();
-    if (e == cudaSuccess) e = configure_mma<128, 1>();
-    return e == cudaSuccess ? configure_mma<128, 4>() : e;
+    cudaError_t e = configure_mma<64, 1, 1>();
+    if (e == cudaSuccess) e = configure_mma<64, 4, 1>();
+    if (e == cudaSuccess) e = configure_mma<64, 4, 4>();
+    if (e == cudaSuccess) e = configure_mma<128, 1, 1>();
+    if (e == cudaSuccess) e = configure_mma<128, 4, 1>();
+    return e == cudaSuccess ? configure_mma<128, 4, 4>() : e;
 }
 cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
-    if (rows == 32) return a.D <= 64 ? launch_mma<64, 1>(a, grid, st) : launch_mma<128, 1>(a, grid, st);
-    return a.D <= 64 ? launch_mma<64, 4>(a, grid, st) : launch_mma<128, 4>(a, grid, st);
+    return a.D <= 64 ? launch_mma_d<64>(a, rows, grid, st) : launch_mma_d<128>(a, rows, grid, st);
 }
 
 }  // namespace dba

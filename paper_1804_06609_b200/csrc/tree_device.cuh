@@ -91,15 +91,15 @@ __device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int 
 
 // One piece of a run: a stretch of one item's tiles.
 struct TreePiece {
-    int b, h, rb;                      // sequence, key head, block of rows
+    int b, h, rb;                      // sequence, key head (or group of heads), block of rows
     int tile, tiles, item_tiles;       // first tile, how many, of how many
     int arena_tiles, top, ctx;
     int slot;                          // where a partial result goes: 0 the run's first piece, 1 a later (its last) one
     bool whole;                        // the item begins and ends in this piece
 };
-__device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int row_blocks, bool first, TreePiece* p) {
+__device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int groups, int row_blocks, bool first, TreePiece* p) {
     if (r.t >= r.t_end) return false;
-    const int per_seq = a.K * row_blocks;
+    const int per_seq = groups * row_blocks;
     int T = tree_tiles(a, r.b, kt);
     while (r.t >= r.seq_t + (long long)T * per_seq) {       // (at most one step: runs have no gaps)
         r.seq_t += (long long)T * per_seq; ++r.b;

@@ -33,6 +33,7 @@ struct TreeAttend {
     const uint32_t* masks;             // null: no arena is looked at, every row sees the context
     const int32_t* top;
     int32_t B, n, H, K, G, D;          // G = H / K query heads per key head; M = n * G rows per (sequence, key head)
+    int32_t item_heads;                // key heads an item has, each a share of its rows
     int32_t W, A, ctx_cap;             // arena words and slots, context places the table holds
     int64_t q_seq, q_row, q_head, o_seq, o_row, o_head;
     float scale_log2e;                 // softmax in powers of two
@@ -48,17 +49,16 @@ struct TreeAttend {
 
 struct TreeAttendPlan {
     int grid, combine;                 // blocks of the attention kernel and of the one that joins its pieces
-    int rows;                          // rows of an item
+    int rows, item_heads;              // rows of an item (all its key heads together), and its key heads
     bool tensor;                       // tcgen05 kernel
 };
 
 // The most an item's partial results take, for the workspace.
-TreeAttendPlan plan_tree_attend(int dtype, int M, int D, int sm_count);
+TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count);
 cudaError_t configure_tree_attend();
 // the tensor-core kernel (tree_attend_mma.cu)
 bool tree_mma_usable(int dtype, int D);
-int tree_mma_rows(int M);
-int tree_mma_blocks_per_sm(int D, int rows);
+void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p);
 cudaError_t configure_tree_mma();
 cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st);
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
