@@ -55,12 +55,12 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
     const int M = a.n * a.G, row_blocks = (M + kGRows - 1) / kGRows;
     grid_dependency_wait();
     allow_dependents();
-    TreeRun run = tree_run<kGThreads>(a, KT, a.K * row_blocks, 1, &sm.run);
+    TreeRun run = tree_run<kGThreads>(a, KT, a.K * row_blocks, 0, 1, &sm.run);
     TreePiece pc;
     bool first = true;
-    if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, KT, row_blocks);
-    while (tree_next_piece(a, run, KT, a.K, row_blocks, first, &pc)) {
-        if (first && tid == 0) tree_write_meta(a, run, &pc, KT, row_blocks);
+    if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, row_blocks, 0);
+    while (tree_next_piece(a, run, KT, a.K, row_blocks, 0, first, &pc)) {
+        if (first && tid == 0) tree_write_meta(a, run, &pc, row_blocks, 0);
         first = false;
         const int rows_here = min(kGRows, M - pc.rb * kGRows);
         __syncthreads();

@@ -30,7 +30,8 @@ constexpr int kMRows = 128;                 // rows of the matrix instructions (
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
 constexpr int kBadSlots = 16;               // more than the tiles the loader may be ahead by
-constexpr int kPieces = 8;                  // more than the pieces the loader may be ahead by (a piece is two copies at least)
+constexpr int kItemUnits = 2;               // what an item costs beside its tiles, in tiles (see tree_device.cuh)
+constexpr int kPieces = 4;                  // pieces the loader may be ahead by
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
 
@@ -43,7 +44,8 @@ constexpr float kRaise = 8.f;               // how far (powers of two) a score m
 //               lies around the queries in shared memory, and nobody reads their results.
 template <int DP, int SW, int HP> struct MConf {
     static constexpr int rows = 32 * SW / HP;                        // of a key head
-    static constexpr int threads = 32 * (SW + 1 + kLoadWarps);
+    static constexpr int inspectors = SW == 4 ? 1 : 0;               // with one softmax warp the products' warp looks values over itself
+    static constexpr int threads = 32 * (SW + 1 + inspectors + kLoadWarps);
     static constexpr int stages = HP == 4 ? 3 : DP == 128 ? (SW == 1 ? 6 : 5) : SW == 1 ? 5 : 9;      // tiles of keys or values in shared memory
     static constexpr int head_bytes = kMKeys * DP * 2, stage_bytes = HP * head_bytes;
     static constexpr int q_half = 32 * SW * 128;                     // 64 columns of the queries
@@ -66,11 +68,11 @@ template <int DP, int SW, int HP> struct MConf {
 template <int DP, int SW, int HP> struct MSmem {
     using C = MConf<DP, SW, HP>;
     alignas(1024) unsigned char tiles[C::tile_bytes];       // keys, values and queries
-    uint64_t full[C::stages], empty[C::stages];
+    uint64_t full[C::stages], empty[C::stages], landed[C::stages];
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
     uint64_t q_empty[C::q_bufs];
     uint64_t pv_done, o_free, told, last;
-    uint64_t published[kPieces];
+    uint64_t published[kPieces], released[kPieces];
     int4 piece[kPieces][2];                 // (in turn) what the loader tells the others of a piece
     uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
     uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
@@ -109,8 +111,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // arrives on the mbarrier when this thread's copies so far have landed
 __device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -208,6 +209,19 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x, bool* found) {
     return r;
 }
 
+// Looks a stage of an arena tile's values over (a warp in step): halves that are not finite become zeros.
+__device__ __forceinline__ bool look_over(unsigned char* stage, int bytes, int lane) {
+    bool found = false;
+#pragma unroll 4
+    for (int i = lane * 16; i < bytes; i += 512) {
+        uint4 x = *reinterpret_cast<uint4*>(stage + i);
+        bool f = false;
+        x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
+        if (f) { *reinterpret_cast<uint4*>(stage + i) = x; found = true; }
+    }
+    return __any_sync(kFullMask, found);
+}
+
 template <int DP, int SW, int HP>
 __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
     using C = MConf<DP, SW, HP>;
@@ -219,7 +233,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows, groups = a.K / HP;
 
     if (tid == 0) {
-        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
+        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); mbar_init(msmem_u32(&sm.landed[s]), kLoadThreads); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
         // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
         // may be a product ahead of it)
@@ -227,7 +241,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         for (int s = 0; s < C::q_bufs; ++s) mbar_init(msmem_u32(&sm.q_empty[s]), 1);
         mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), SW);
         mbar_init(msmem_u32(&sm.last), 1);
-        for (int i = 0; i < kPieces; ++i) mbar_init(msmem_u32(&sm.published[i]), 1);
+        for (int i = 0; i < kPieces; ++i) { mbar_init(msmem_u32(&sm.published[i]), 1); mbar_init(msmem_u32(&sm.released[i]), SW + 1 + C::inspectors); }
         for (int i = 0; i < kBadSlots; ++i) sm.bad[i] = 0;
         sm.abort_flag = 0;
         if (SW == 1) {
@@ -259,45 +273,27 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     tc_before();
     grid_dependency_wait();
     allow_dependents();
-    TreeRun run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, 1, &sm.run);      // (has the block's barriers)
+    TreeRun run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, kItemUnits, 1, &sm.run);      // (has the block's barriers)
     tc_after();
     const uint32_t tmem = sm.tmem_base;
-    const int total = (int)(run.t_end - run.t);        // tiles of this block
-
-    if (warp > SW) {
+    if (warp > SW + C::inspectors) {
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
         constexpr int CH = DP / 8;                     // 16-byte chunks of a row
         constexpr int RW = 32 / CH, NJ = 32 / RW;      // rows the warp copies at a time, and how often
-        const int lw = warp - SW - 1, ch = lane % CH, sub = lane / CH;
+        const int lw = warp - SW - C::inspectors - 1, ch = lane % CH, sub = lane / CH;
         const bool ch_in = ch * 8 < a.D, full_head = a.D == DP;
         const uint32_t tiles = msmem_u32(sm.tiles);
         const int64_t head2 = 2 * a.pages.head_stride;          // bytes from a key head to the next
         // this lane's place in rows sub, sub + RW, ..: the swizzle moves a chunk by the row's last three bits
         const uint32_t in_kv = (uint32_t)(ch >> 3) * (kMKeys * 128) + (uint32_t)(lw * 32 + sub) * 128;
         const uint32_t swz = ((uint32_t)(ch & 7) ^ (uint32_t)sub) << 4;
-        uint32_t step = 0, stage = 0, phase = 1;       // copies issued; the next one's stage (a barrier's first wait does not wait)
-        int owed = -1;                                 // copy of an arena tile's values that is to be looked over before it is handed on
-        uint32_t owed_piece = 0, owed_stage = 0;
-        auto look_over = [&]() {                       // (its copies have landed)
-            bool found = false;
-#pragma unroll 4
-            for (int i = 0; i < HP * NJ; ++i) {
-                const int w = i / NJ, j = i - w * NJ;
-                uint4* v = reinterpret_cast<uint4*>(sm.tiles + C::stage_at(owed_stage) + w * C::head_bytes + in_kv + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)));
-                uint4 x = *v;
-                bool f = false;
-                x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
-                if (f) { *v = x; found = true; }
-            }
-            if (found) sm.bad[owed_piece % kBadSlots] = owed_piece + 1;
-            if (owed != a.drop_item) mbar_arrive(msmem_u32(&sm.full[owed_stage]));
-            owed = -1;
-        };
+        int step = 0;
+        uint32_t stage = 0, phase = 1;                 // copies issued; the next one's stage (a barrier's first wait does not wait)
         // One tile of keys or values: rows of the warp that exist (`there`) at row offsets at[j] (in 16 bytes), zeros for the others.
         // The stage is handed on by the copies themselves; the issuing thread of the matrix products has the fence between
         // their writes and its reads (here it would wait for every copy in flight: twice the time on long contexts).
-        // look: values of an arena tile, looked over once the next copy but one has been issued.
-        auto load = [&](const char* base, const uint32_t (&at)[NJ], uint32_t there, bool look, int piece) {
+        // look: values of an arena tile, which somebody looks over before they are handed on.
+        auto load = [&](const char* base, const uint32_t (&at)[NJ], uint32_t there, bool look) {
             if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) return false;
             const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
             if (there == 0xffffffffu && full_head) {
@@ -318,14 +314,8 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                         cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? src + w * head2 : src, in ? 16u : 0u);
                 }
             }
-            cp_commit();
             if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
-            if (!look && (int)step != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
-            if (owed >= 0 && (look || (int)step - owed >= 2)) {
-                if ((int)step - owed == 1) cp_wait<1>(); else cp_wait<2>();
-                look_over();
-            }
-            if (look) { owed = (int)step; owed_piece = (uint32_t)piece; owed_stage = stage; }
+            if (step != a.drop_item) cp_arrive(msmem_u32(look && C::inspectors ? &sm.landed[stage] : &sm.full[stage]));
             ++step;
             if (++stage == C::stages) { stage = 0; phase ^= 1u; }
             return true;
@@ -355,26 +345,24 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         };
         // The loader walks the pieces of the run, one ahead (the next piece's numbers come out of the L2), and tells the others.
         TreePiece pc, nx;
-        bool more = tree_next_piece(a, run, kMKeys, groups, row_blocks, true, &nx);
-        if (lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, kMKeys, row_blocks);
+        bool more = tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, true, &nx);
+        if (lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, row_blocks, kItemUnits);
         const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;        // rows in 16 bytes
         bool ok = true;
         int piece = 0, tile_no = 0;
         if (more) look_up(nx, nx.tile);
         while (more) {
             pc = nx;
+            if (lw == 0 && piece >= kPieces && !mbar_wait(msmem_u32(&sm.released[piece % kPieces]), (piece / kPieces - 1) & 1, abort_flag, limit)) { ok = false; break; }
             if (lw == 0 && lane == 0) {
                 sm.piece[piece % kPieces][0] = make_int4(pc.b, pc.h, pc.rb, pc.top);
                 sm.piece[piece % kPieces][1] = make_int4(pc.tile, pc.tiles, pc.arena_tiles, pc.slot | (pc.whole ? 2 : 0));
                 mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
             }
-            more = tree_next_piece(a, run, kMKeys, groups, row_blocks, false, &nx);
+            more = tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, false, &nx);
             // queries of the item: beyond the rows and the head size, zeros
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
-            if (piece >= C::q_bufs) {
-                if (owed >= 0) { cp_wait<0>(); look_over(); }          // (the queries' buffer may be waiting for it)
-                if (!mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
-            }
+            if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             {
                 const int rows_here = min(C::rows, M - pc.rb * C::rows);
                 const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head + ch * 8);
@@ -421,22 +409,26 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 uint32_t at[NJ];
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) at[j] = __shfl_sync(kFullMask, mine, j * RW + sub);
-                if (!load(kb, at, there, false, piece)) { ok = false; break; }
+                if (!load(kb, at, there, false)) { ok = false; break; }
                 // one S in tensor memory: K0 V0 K1 V1 ..;  two: K0 K1 V0 K2 V1 .. (the products run one tile ahead)
                 if (C::s_bufs == 1) {
-                    if (!load(vb, at, there, look, piece)) { ok = false; break; }
+                    if (!load(vb, at, there, look)) { ok = false; break; }
                 } else {
-                    if (t > pc.tile && !load(vb, v_at, v_there, v_look, piece)) { ok = false; break; }
+                    if (t > pc.tile && !load(vb, v_at, v_there, v_look)) { ok = false; break; }
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) v_at[j] = at[j];
                     v_there = there; v_look = look;
                 }
             }
-            if (!ok || (C::s_bufs > 1 && !load(vb, v_at, v_there, v_look, piece))) { ok = false; break; }
+            if (!ok || (C::s_bufs > 1 && !load(vb, v_at, v_there, v_look))) { ok = false; break; }
             ++piece;
         }
-        cp_wait<0>();
-        if (ok && owed >= 0) look_over();
+        if (ok && lw == 0 &&                            // the end of the run
+            (piece < kPieces || mbar_wait(msmem_u32(&sm.released[piece % kPieces]), (piece / kPieces - 1) & 1, abort_flag, limit)) && lane == 0) {
+            sm.piece[piece % kPieces][1] = make_int4(0, 0, 0, 0);
+            mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
+        }
+        cp_wait_all();
     } else if (warp == SW) {
         // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
         constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
@@ -470,9 +462,11 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
             next_stage();
             return true;
         };
-        while (ok && (int)g < total) {
+        while (ok) {
             if (!(ok = mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit))) break;
-            const int n_tiles = sm.piece[piece % kPieces][1].y;
+            const int4 i1 = sm.piece[piece % kPieces][1];
+            const int n_tiles = i1.y;
+            if (n_tiles == 0) break;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
             ok = scores(g, qb, n_tiles == 1);
 #pragma unroll 1
@@ -481,6 +475,10 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 if (C::s_bufs > 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
                 const uint32_t sb = g % C::s_bufs;
                 if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
+                if (!C::inspectors && i1.x + t < i1.z && look_over(sm.tiles + C::stage_at(stage), C::stage_bytes, lane)) {
+                    if (lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                    __syncwarp();
+                }
                 if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
                 if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
                 const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
@@ -501,11 +499,41 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 next_stage();
                 if (C::s_bufs == 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
             }
+            if (ok && lane == 0) mbar_arrive(msmem_u32(&sm.released[piece % kPieces]));
             ++piece;
         }
         // nothing of this block is in flight when it leaves, whatever happened
         if (elect_one()) mma_commit(msmem_u32(&sm.last));
         for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last), 0)); ++i) {}
+    } else if (C::inspectors && warp == SW + 1) {
+        // ------------------------------------------------------------------ inspector: values of arena tiles
+        uint32_t stage = 0;
+        uint32_t uses[C::stages];                      // how often each stage has held values to be looked over
+#pragma unroll
+        for (int i = 0; i < C::stages; ++i) uses[i] = 0;
+        for (int piece = 0;; ++piece) {
+            if (!mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit)) break;
+            const int4 i1 = sm.piece[piece % kPieces][1];
+            if (i1.y == 0) break;
+            const int n_arena = min(i1.y, max(0, i1.z - i1.x));      // its first so many tiles are of the arena
+            const uint32_t begin = stage;
+            bool ok = true;
+            for (int t = 0; t < n_arena && ok; ++t) {
+                // the tile's values among the piece's copies: K0 K1 V0 K2 V1 .. (the last V alone)
+                const int at = C::s_bufs > 1 ? (t + 1 < i1.y ? 2 * t + 2 : 2 * t + 1) : 2 * t + 1;
+                const uint32_t s = (begin + (uint32_t)at) % C::stages;
+                uint32_t use = 0;
+#pragma unroll
+                for (int i = 0; i < C::stages; ++i) if (i == (int)s) use = uses[i]++;
+                if (!(ok = mbar_wait(msmem_u32(&sm.landed[s]), use & 1u, abort_flag, limit))) break;
+                if (look_over(sm.tiles + C::stage_at(s), C::stage_bytes, lane) && lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(msmem_u32(&sm.full[s])), "r"((uint32_t)kLoadThreads) : "memory");
+            }
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(msmem_u32(&sm.released[piece % kPieces]));
+            stage = (begin + 2u * (uint32_t)i1.y) % C::stages;
+        }
     } else {
         // ------------------------------------------------------------------ softmax: a row per thread
         const uint32_t lanes = (uint32_t)((SW == 1 ? quarter : warp) * 32) << 16;
@@ -514,9 +542,10 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         bool ok = true;
         int piece = 0;
         uint32_t g = 0;
-        while (ok && (int)g < total) {
+        while (ok) {
             if (!mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit)) { ok = false; break; }
             const int4 i0 = sm.piece[piece % kPieces][0], i1 = sm.piece[piece % kPieces][1];
+            if (i1.y == 0) break;
             const int p_b = i0.x, p_top = i0.w, p_tile = i1.x, p_end = i1.x + i1.y, p_arena = i1.z;
             const int rr = i0.z * C::rows + (HP > 1 ? lane : row);
             const bool active = HP > 1 || i0.z * C::rows + warp * 32 < M;       // the warp has rows
@@ -669,7 +698,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 tc_before();
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(msmem_u32(&sm.o_free));
+            if (lane == 0) { mbar_arrive(msmem_u32(&sm.o_free)); mbar_arrive(msmem_u32(&sm.released[piece % kPieces])); }
             ++piece;
         }
     }

@@ -32,12 +32,13 @@ __device__ __forceinline__ int tree_tiles(const TreeAttend& a, int b, int kt) {
     return max(1, (tree_top(a, b) + kt - 1) / kt + (tree_ctx(a, b) + kt - 1) / kt);
 }
 
-// The work of a call: items (sequence, key head, block of rows), sequence by sequence, each tree_tiles() tiles long, laid
-// end to end and cut into `used` equal runs, one per block.  A run may begin and end inside an item; an item cut by a
-// run's end is finished by tree_combine_kernel.
+// The work of a call: items (sequence, key head or group of them, block of rows), sequence by sequence, each `extra` units
+// for what an item costs beside its tiles and then a unit for each of its tree_tiles() tiles, laid end to end and cut into
+// `used` equal runs, one per block.  A run may begin and end inside an item; an item cut by a run's end is finished by
+// tree_combine_kernel.
 struct TreeRun {
-    long long t, t_end, total;         // this block's tiles
-    long long seq_t;                   // first tile of sequence b
+    long long t, t_end, total;         // this block's units
+    long long seq_t;                   // first unit of sequence b
     int b, used;
 };
 __device__ __forceinline__ long long tree_run_start(int c, long long total, int used) { return (long long)c * total / used; }
@@ -46,13 +47,13 @@ __device__ __forceinline__ int tree_run_owner(long long t, long long total, int 
 struct TreeRunShared { long long sums[33]; long long seq_t; int b; };
 
 // Called by all NT threads of a block; the lengths are scanned by the block itself (B numbers out of the L2), so no
-// kernel has to plan ahead and no length comes to the host.  `least`: tiles a run should have before the work is cut further.
+// kernel has to plan ahead and no length comes to the host.  `least`: units a run should have before the work is cut further.
 template <int NT>
-__device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int least, TreeRunShared* sh) {
+__device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int extra, int least, TreeRunShared* sh) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.B + NT - 1) / NT, b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
     long long sum = 0;
-    for (int b = b_lo; b < b_hi; ++b) sum += (long long)tree_tiles(a, b, kt) * items_per_seq;
+    for (int b = b_lo; b < b_hi; ++b) sum += (long long)(tree_tiles(a, b, kt) + extra) * items_per_seq;
     long long pre = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -66,7 +67,7 @@ __device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int 
         if (w < warp) before += sh->sums[w];
         total += sh->sums[w];
     }
-    pre += before - sum;                                   // tiles before this thread's sequences
+    pre += before - sum;                                   // units before this thread's sequences
     TreeRun r;
     r.total = total;
     r.used = (int)min((long long)gridDim.x, max(1LL, total / least));
@@ -77,7 +78,7 @@ __device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int 
         if (r.t >= pre && r.t < pre + sum) {
             int b = b_lo;
             for (;;) {
-                const long long len = (long long)tree_tiles(a, b, kt) * items_per_seq;
+                const long long len = (long long)(tree_tiles(a, b, kt) + extra) * items_per_seq;
                 if (r.t < pre + len) break;
                 pre += len; ++b;
             }
@@ -97,25 +98,30 @@ struct TreePiece {
     int slot;                          // where a partial result goes: 0 the run's first piece, 1 a later (its last) one
     bool whole;                        // the item begins and ends in this piece
 };
-__device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int groups, int row_blocks, bool first, TreePiece* p) {
-    if (r.t >= r.t_end) return false;
+// (a run's end within an item's extra units leaves the item to the next run)
+__device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int groups, int row_blocks, int extra, bool first, TreePiece* p) {
     const int per_seq = groups * row_blocks;
-    int T = tree_tiles(a, r.b, kt);
-    while (r.t >= r.seq_t + (long long)T * per_seq) {       // (at most one step: runs have no gaps)
-        r.seq_t += (long long)T * per_seq; ++r.b;
-        T = tree_tiles(a, r.b, kt);
+    while (r.t < r.t_end) {
+        int len = tree_tiles(a, r.b, kt) + extra;
+        while (r.t >= r.seq_t + (long long)len * per_seq) {     // (at most one step: runs have no gaps)
+            r.seq_t += (long long)len * per_seq; ++r.b;
+            len = tree_tiles(a, r.b, kt) + extra;
+        }
+        const int off = (int)(r.t - r.seq_t), item = off / len, in_item = off - item * len;
+        const int T = len - extra, end = (int)min((long long)len, (long long)in_item + (r.t_end - r.t));
+        r.t += end - in_item;
+        p->tile = max(0, in_item - extra);
+        p->tiles = end - extra - p->tile;
+        if (p->tiles <= 0) continue;
+        p->b = r.b; p->h = item / row_blocks; p->rb = item - p->h * row_blocks;
+        p->item_tiles = T;
+        p->top = tree_top(a, r.b); p->ctx = tree_ctx(a, r.b);
+        p->arena_tiles = (p->top + kt - 1) / kt;
+        p->whole = p->tile == 0 && p->tiles == T;
+        p->slot = first ? 0 : 1;
+        return true;
     }
-    const int off = (int)(r.t - r.seq_t), item = off / T;
-    p->b = r.b; p->h = item / row_blocks; p->rb = item - p->h * row_blocks;
-    p->tile = off - item * T;
-    p->item_tiles = T;
-    p->tiles = (int)min((long long)(T - p->tile), r.t_end - r.t);
-    p->top = tree_top(a, r.b); p->ctx = tree_ctx(a, r.b);
-    p->arena_tiles = (p->top + kt - 1) / kt;
-    p->whole = p->tile == 0 && p->tiles == T;
-    p->slot = first ? 0 : 1;
-    r.t += p->tiles;
-    return true;
+    return false;
 }
 // The first key place of a tile and how many places of it exist.
 __device__ __forceinline__ void tree_tile_span(const TreeAttend& a, const TreePiece& p, int tile, int kt, int* place, int* count) {
@@ -123,17 +129,17 @@ __device__ __forceinline__ void tree_tile_span(const TreeAttend& a, const TreePi
     const int c = (tile - p.arena_tiles) * kt;
     *place = a.A + c; *count = max(0, min(kt, p.ctx - c));
 }
-// What the combining kernel is told: block c (whose run begins inside an item begun by block c - 1) names the item and
-// the last block working on it.
-__device__ __forceinline__ void tree_write_meta(const TreeAttend& a, const TreeRun& r, const TreePiece* first_piece, int kt, int row_blocks) {
+// What the combining kernel is told: block c (whose run begins inside an item whose first tile is block c - 1's) names the
+// item, the last block working on it, and which of block c - 1's two places holds its piece.
+__device__ __forceinline__ void tree_write_meta(const TreeAttend& a, const TreeRun& r, const TreePiece* first_piece, int row_blocks, int extra) {
     int4 m = make_int4(-1, 0, 0, 0);
     if (first_piece && first_piece->tile > 0) {
         const TreePiece& p = *first_piece;
-        const long long begin = tree_run_start(blockIdx.x, r.total, r.used) - p.tile;
+        const long long begin = tree_run_start(blockIdx.x, r.total, r.used) - p.tile;      // the unit of its first tile
         if (tree_run_owner(begin, r.total, r.used) == (int)blockIdx.x - 1) {
             const int last = tree_run_owner(begin + p.item_tiles - 1, r.total, r.used);
             const long long prev = tree_run_start((int)blockIdx.x - 1, r.total, r.used);
-            m = make_int4(p.b, p.h * row_blocks + p.rb, last, prev == begin ? 0 : 1);
+            m = make_int4(p.b, p.h * row_blocks + p.rb, last, prev >= begin - extra ? 0 : 1);
         }
     }
     a.meta[blockIdx.x] = m;
