@@ -296,22 +296,23 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         auto load = [&](const char* base, const uint32_t (&at)[NJ], uint32_t there, bool look) {
             if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) return false;
             const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
+            const char* from[HP];                       // (rows that do not exist are at 0 and of no bytes)
+#pragma unroll
+            for (int w = 0; w < HP; ++w) from[w] = base + w * head2;
             if (there == 0xffffffffu && full_head) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const char* src = base + (uint64_t)at[j] * 16;
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
                     for (int w = 0; w < HP; ++w)
-                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), src + w * head2, 16u);
-                }
+                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[w] + (uint64_t)at[j] * 16, 16u);
             } else {
+                const uint32_t mine = ch_in ? there >> sub : 0u;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
-                    const bool in = ((there >> (j * RW + sub)) & 1u) && ch_in;
-                    const char* src = in ? base + (uint64_t)at[j] * 16 : (const char*)a.k;
+                    const uint32_t bytes = (mine >> (j * RW)) & 1u ? 16u : 0u;
 #pragma unroll
                     for (int w = 0; w < HP; ++w)
-                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), in ? src + w * head2 : src, in ? 16u : 0u);
+                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[w] + (uint64_t)at[j] * 16, bytes);
                 }
             }
             if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
@@ -365,26 +366,29 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
             if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             {
                 const int rows_here = min(C::rows, M - pc.rb * C::rows);
-                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head + ch * 8);
+                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head) + (ch_in ? ch * 16 : 0);
+                const char* from[HP];
+#pragma unroll
+                for (int w = 0; w < HP; ++w) from[w] = q + 2 * (int64_t)(w * a.G) * a.q_head;
                 const uint32_t dst = tiles + C::q_at + qb * C::q_bytes + (uint32_t)(ch >> 3) * C::q_half + (uint32_t)sub * 128;
 #pragma unroll 1
                 for (int r0 = 0; r0 < rows_here; r0 += 32) {          // a lane finds one row, and every lane copies chunks of all
-                    const int rr = min(pc.rb * C::rows + r0 + lane, M - 1), tok = rr / a.G;
+                    const int rr = min(pc.rb * C::rows + r0 + lane, M - 1), tok = a.G == 1 ? rr : rr / a.G;
                     const int64_t mine = 2 * ((int64_t)tok * a.q_row + (int64_t)(rr - tok * a.G) * a.q_head);
+                    const int left = ch_in ? rows_here - r0 - sub : 0;
 #pragma unroll
                     for (int jj = 0; jj < NJ / kLoadWarps; ++jj) {
                         const int j = jj * kLoadWarps + lw;
                         const int64_t at = __shfl_sync(kFullMask, mine, j * RW + sub);
-                        const bool in = r0 + j * RW + sub < rows_here && ch_in;
+                        const uint32_t bytes = j * RW < left ? 16u : 0u;
+                        const uint32_t to = dst + (r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
 #pragma unroll
-                        for (int w = 0; w < HP; ++w)
-                            cp_async16(dst + (w * 32 + r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)),
-                                       in ? q + at + 2 * (int64_t)(w * a.G) * a.q_head : (const char*)a.q, in ? 16u : 0u);
+                        for (int w = 0; w < HP; ++w) cp_async16(to + w * 32 * 128, from[w] + at, bytes);
                     }
                 }                                       // (the first keys' arrival counts them too)
             }
-            const char* const kb = (const char*)a.k + pc.h * HP * head2 + ch * 16;
-            const char* const vb = (const char*)a.v + pc.h * HP * head2 + ch * 16;
+            const char* const kb = (const char*)a.k + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
+            const char* const vb = (const char*)a.v + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
             uint32_t v_at[NJ], v_there = 0;
             bool v_look = false;
 #pragma unroll
@@ -732,7 +736,7 @@ cudaError_t launch_mma_d(const TreeAttend& a, int rows, int grid, cudaStream_t s
 bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
 // Up to 32 rows to a key head: four heads at a time where their number allows, else one softmax warp.
 void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p) {
-    p->item_heads = M <= 32 && K % 4 == 0 ? 4 : 1;
+    p->item_heads = M <= 32 && K % 4 == 0 && D <= 64 ? 4 : 1;
     p->rows = M <= 32 && p->item_heads == 1 ? 32 : kMRows;
     p->grid = sm_count * (D <= 64 ? blocks_mma<64>(p->rows, p->item_heads) : blocks_mma<128>(p->rows, p->item_heads));
 }

@@ -40,6 +40,8 @@ struct TreeRun {
     long long t, t_end, total;         // this block's units
     long long seq_t;                   // first unit of sequence b
     int b, used;
+    int item, in_item;                 // where the run stands: item of sequence b (-1: to be worked out), unit of the item
+    int top, ctx, len;                 // of sequence b
 };
 __device__ __forceinline__ long long tree_run_start(int c, long long total, int used) { return (long long)c * total / used; }
 __device__ __forceinline__ int tree_run_owner(long long t, long long total, int used) { return (int)(((t + 1) * used - 1) / total); }
@@ -86,7 +88,7 @@ __device__ TreeRun tree_run(const TreeAttend& a, int kt, int items_per_seq, int 
         }
     }
     __syncthreads();
-    r.b = sh->b; r.seq_t = sh->seq_t;
+    r.b = sh->b; r.seq_t = sh->seq_t; r.item = -1;
     return r;
 }
 
@@ -100,26 +102,27 @@ struct TreePiece {
 };
 // (a run's end within an item's extra units leaves the item to the next run)
 __device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int groups, int row_blocks, int extra, bool first, TreePiece* p) {
-    const int per_seq = groups * row_blocks;
     while (r.t < r.t_end) {
-        int len = tree_tiles(a, r.b, kt) + extra;
-        while (r.t >= r.seq_t + (long long)len * per_seq) {     // (at most one step: runs have no gaps)
-            r.seq_t += (long long)len * per_seq; ++r.b;
-            len = tree_tiles(a, r.b, kt) + extra;
+        if (r.item < 0) {              // a new sequence (the first one may be entered anywhere)
+            r.top = tree_top(a, r.b); r.ctx = tree_ctx(a, r.b);
+            r.len = max(1, (r.top + kt - 1) / kt + (r.ctx + kt - 1) / kt) + extra;
+            const long long off = r.t - r.seq_t;
+            r.item = off ? (int)(off / r.len) : 0;
+            r.in_item = (int)(off - (long long)r.item * r.len);
         }
-        const int off = (int)(r.t - r.seq_t), item = off / len, in_item = off - item * len;
-        const int T = len - extra, end = (int)min((long long)len, (long long)in_item + (r.t_end - r.t));
-        r.t += end - in_item;
-        p->tile = max(0, in_item - extra);
+        const int end = (int)min((long long)r.len, (long long)r.in_item + (r.t_end - r.t)), T = r.len - extra;
+        p->b = r.b; p->top = r.top; p->ctx = r.ctx;
+        p->h = row_blocks == 1 ? r.item : r.item / row_blocks; p->rb = r.item - p->h * row_blocks;
+        p->tile = max(0, r.in_item - extra);
         p->tiles = end - extra - p->tile;
-        if (p->tiles <= 0) continue;
-        p->b = r.b; p->h = item / row_blocks; p->rb = item - p->h * row_blocks;
         p->item_tiles = T;
-        p->top = tree_top(a, r.b); p->ctx = tree_ctx(a, r.b);
-        p->arena_tiles = (p->top + kt - 1) / kt;
+        p->arena_tiles = (r.top + kt - 1) / kt;
         p->whole = p->tile == 0 && p->tiles == T;
         p->slot = first ? 0 : 1;
-        return true;
+        r.t += end - r.in_item;
+        r.in_item = 0;
+        if (++r.item == groups * row_blocks) { r.item = -1; r.seq_t = r.t; ++r.b; }
+        if (p->tiles > 0) return true;
     }
     return false;
 }
