@@ -201,25 +201,36 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// bf16 halves of a word that are not finite, zeroed; *found is set if there are any
-__device__ __forceinline__ uint32_t only_finite(uint32_t x, bool* found) {
-    uint32_t r = x;
-    if ((x & 0x00007f80u) == 0x00007f80u) { r &= 0xffff0000u; *found = true; }
-    if ((x & 0x7f800000u) == 0x7f800000u) { r &= 0x0000ffffu; *found = true; }
-    return r;
+// a word whose bf16 halves that are not finite are zeroed
+__device__ __forceinline__ uint32_t only_finite(uint32_t x) {
+    if ((x & 0x00007f80u) == 0x00007f80u) x &= 0xffff0000u;
+    if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+    return x;
 }
-
-// Looks a stage of an arena tile's values over (a warp in step): halves that are not finite become zeros.
-__device__ __forceinline__ bool look_over(unsigned char* stage, int bytes, int lane) {
-    bool found = false;
-#pragma unroll 4
-    for (int i = lane * 16; i < bytes; i += 512) {
-        uint4 x = *reinterpret_cast<uint4*>(stage + i);
-        bool f = false;
-        x.x = only_finite(x.x, &f); x.y = only_finite(x.y, &f); x.z = only_finite(x.z, &f); x.w = only_finite(x.w, &f);
-        if (f) { *reinterpret_cast<uint4*>(stage + i) = x; found = true; }
+// bits that show whether a bf16 half of a word is not finite (its exponent is all ones)
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// Looks a stage of an arena tile's values over (a warp in step): halves that are not finite become zeros.  They are rare:
+// loads go eight at a time, and are gone through again only where something was found.
+template <int BYTES>
+__device__ __forceinline__ bool look_over(unsigned char* stage, int lane) {
+    uint4* const mine = reinterpret_cast<uint4*>(stage) + lane;
+    uint32_t seen = 0;
+#pragma unroll 1
+    for (int i = 0; i < BYTES / 16; i += 8 * 32) {
+        uint4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = mine[i + 32 * k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) seen |= not_finite(x[k].x) | not_finite(x[k].y) | not_finite(x[k].z) | not_finite(x[k].w);
     }
-    return __any_sync(kFullMask, found);
+    if (!__any_sync(kFullMask, seen != 0)) return false;
+#pragma unroll 1
+    for (int i = 0; i < BYTES / 16; i += 32) {
+        uint4 x = mine[i];
+        x.x = only_finite(x.x); x.y = only_finite(x.y); x.z = only_finite(x.z); x.w = only_finite(x.w);
+        mine[i] = x;
+    }
+    return true;
 }
 
 template <int DP, int SW, int HP>
@@ -479,7 +490,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 if (C::s_bufs > 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
                 const uint32_t sb = g % C::s_bufs;
                 if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
-                if (!C::inspectors && i1.x + t < i1.z && look_over(sm.tiles + C::stage_at(stage), C::stage_bytes, lane)) {
+                if (!C::inspectors && i1.x + t < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(stage), lane)) {
                     if (lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
                     __syncwarp();
                 }
@@ -530,7 +541,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
 #pragma unroll
                 for (int i = 0; i < C::stages; ++i) if (i == (int)s) use = uses[i]++;
                 if (!(ok = mbar_wait(msmem_u32(&sm.landed[s]), use & 1u, abort_flag, limit))) break;
-                if (look_over(sm.tiles + C::stage_at(s), C::stage_bytes, lane) && lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                if (look_over<C::stage_bytes>(sm.tiles + C::stage_at(s), lane) && lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
                 __syncwarp();
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(msmem_u32(&sm.full[s])), "r"((uint32_t)kLoadThreads) : "memory");
             }
@@ -658,29 +669,27 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 const int p_h = sm.piece[piece % kPieces][0].y * HP + (HP > 1 ? warp : 0), head = p_h * a.G + rr - tok * a.G;
                 const int64_t part = (int64_t)(2 * blockIdx.x + (i1.w & 1)) * (32 * SW) + row;
                 __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)p_b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
-#pragma unroll 1
-                for (int c = 0; c < DP; c += 16) {
-                    uint32_t u[16];
-                    __syncwarp();
-                    tm_ld16(tmem + lanes + C::o_col + c, u);
-                    if (rr >= M) continue;
-                    float o[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[j] = sum == 0.f ? 0.f : __uint_as_float(u[j]) * inv;      // (a closed row's O may hold anything)
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t u[32];
+                    tm_ld32(tmem + lanes + C::o_col + c, u);
 #pragma unroll
-                    for (int j = 0; j < 16; j += 8) {
-                        if (c + j >= a.D) continue;
+                    for (int j = 0; j < 32; ++j) u[j] = sum == 0.f ? 0u : __float_as_uint(__uint_as_float(u[j]) * inv);      // (a closed row's O may hold anything)
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        const bool in = rr < M && c + j < a.D;
                         if (whole) {
                             uint4 w;
-                            w.x = pack_bf16(o[j], o[j + 1]); w.y = pack_bf16(o[j + 2], o[j + 3]);
-                            w.z = pack_bf16(o[j + 4], o[j + 5]); w.w = pack_bf16(o[j + 6], o[j + 7]);
-                            *reinterpret_cast<uint4*>(out + c + j) = w;
-                        } else {
-                            float4* po = reinterpret_cast<float4*>(a.part_o + part * a.D + c + j);
-                            po[0] = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                            po[1] = make_float4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                            w.x = pack_bf16(__uint_as_float(u[j]), __uint_as_float(u[j + 1])); w.y = pack_bf16(__uint_as_float(u[j + 2]), __uint_as_float(u[j + 3]));
+                            w.z = pack_bf16(__uint_as_float(u[j + 4]), __uint_as_float(u[j + 5])); w.w = pack_bf16(__uint_as_float(u[j + 6]), __uint_as_float(u[j + 7]));
+                            if (in) *reinterpret_cast<uint4*>(out + c + j) = w;
+                        } else if (in) {
+                            uint4* po = reinterpret_cast<uint4*>(a.part_o + part * a.D + c + j);
+                            po[0] = make_uint4(u[j], u[j + 1], u[j + 2], u[j + 3]);
+                            po[1] = make_uint4(u[j + 4], u[j + 5], u[j + 6], u[j + 7]);
                         }
                     }
+                    __syncwarp();
                 }
                 if (bad && rr < M && sum > 0.f)        // values that are not finite, at the slots this row sees, onto what has been written
                     for (int j = p_tile * kMKeys; j < min(p_end * kMKeys, p_top); ++j) {
