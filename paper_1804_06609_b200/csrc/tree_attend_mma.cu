@@ -29,8 +29,9 @@ namespace {
 constexpr int kMRows = 128;                 // rows of the matrix instructions (lanes of tensor memory)
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
-constexpr int kBadSlots = 16;               // more than the tiles the loader may be ahead by
+constexpr int kBadSlots = 8;               // more than the tiles the loader may be ahead by
 constexpr int kItemUnits = 2;               // what an item costs beside its tiles, in tiles (see tree_device.cuh)
+constexpr uint32_t kNoRow = 0xffffffffu;
 constexpr int kPieces = 4;                  // pieces the loader may be ahead by
 constexpr long long kMWaitClocks = 4000000000LL;       // about two seconds
 constexpr float kRaise = 8.f;               // how far (powers of two) a score may lie above the reference
@@ -68,7 +69,7 @@ template <int DP, int SW, int HP> struct MConf {
 template <int DP, int SW, int HP> struct MSmem {
     using C = MConf<DP, SW, HP>;
     alignas(1024) unsigned char tiles[C::tile_bytes];       // keys, values and queries
-    uint64_t full[C::stages], empty[C::stages], landed[C::stages];
+    uint64_t full[C::stages], empty[C::stages], landed[C::inspectors ? C::stages : 1];
     uint64_t s_full[C::s_bufs], p_ready[C::s_bufs];
     uint64_t q_empty[C::q_bufs];
     uint64_t pv_done, o_free, told, last;
@@ -78,7 +79,10 @@ template <int DP, int SW, int HP> struct MSmem {
     uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
     uint32_t tmem_base;
     int abort_flag, turn, scheduler[4];
-    TreeRunShared run;
+    union {
+        TreeRunShared run;                  // (until the roles begin)
+        uint32_t rows[2][kMKeys];           // the last two tiles' rows in the cache, in 16 bytes; kNoRow: none
+    };
 };
 
 __device__ __forceinline__ uint32_t msmem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -90,15 +94,15 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Bounded wait of a whole warp in step: every lane gets one answer.  False: the block is winding down.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-    if (__all_sync(kFullMask, mbar_try(bar, parity))) return true;
+// Bounded wait of a whole warp in step: every lane gets one answer.  False: the block is winding down.  (The usual case, that
+// the phase is over, is looked at in place; the loop is one function for all roles: instructions are what the short
+// items of this kernel wait for most.)
+__device__ __noinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
     const long long t0 = clock64();
-    bool done = false;
 #pragma unroll 1
-    for (uint32_t i = 1; !done; ++i) {
-        done = __all_sync(kFullMask, mbar_try(bar, parity));
-        if (!done && (i & 31u) == 0) {
+    for (uint32_t i = 1;; ++i) {
+        if (__all_sync(kFullMask, mbar_try(bar, parity))) return true;
+        if ((i & 31u) == 0) {
             const bool late = *abort_flag != 0 || clock64() - t0 > limit;
             if (__any_sync(kFullMask, late)) {
                 *abort_flag = 1;
@@ -106,7 +110,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             }
         }
     }
-    return true;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+    return __all_sync(kFullMask, mbar_try(bar, parity)) || mbar_wait_long(bar, parity, abort_flag, limit);
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     const int M = a.n * a.G, row_blocks = (M + C::rows - 1) / C::rows, groups = a.K / HP;
 
     if (tid == 0) {
-        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); mbar_init(msmem_u32(&sm.landed[s]), kLoadThreads); }
+        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); if (C::inspectors) mbar_init(msmem_u32(&sm.landed[s]), kLoadThreads); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
         // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
         // may be a product ahead of it)
@@ -285,159 +291,146 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     grid_dependency_wait();
     allow_dependents();
     TreeRun run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, kItemUnits, 1, &sm.run);      // (has the block's barriers)
+    __syncthreads();           // its numbers have been read: their place is used again
     tc_after();
     const uint32_t tmem = sm.tmem_base;
     if (warp > SW + C::inspectors) {
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
         constexpr int CH = DP / 8;                     // 16-byte chunks of a row
         constexpr int RW = 32 / CH, NJ = 32 / RW;      // rows the warp copies at a time, and how often
+        constexpr int LAG = C::s_bufs - 1;             // tiles by which the values' copies follow the keys', as the products do
         const int lw = warp - SW - C::inspectors - 1, ch = lane % CH, sub = lane / CH;
-        const bool ch_in = ch * 8 < a.D, full_head = a.D == DP;
+        const bool ch_in = ch * 8 < a.D;
         const uint32_t tiles = msmem_u32(sm.tiles);
         const int64_t head2 = 2 * a.pages.head_stride;          // bytes from a key head to the next
         // this lane's place in rows sub, sub + RW, ..: the swizzle moves a chunk by the row's last three bits
         const uint32_t in_kv = (uint32_t)(ch >> 3) * (kMKeys * 128) + (uint32_t)(lw * 32 + sub) * 128;
         const uint32_t swz = ((uint32_t)(ch & 7) ^ (uint32_t)sub) << 4;
-        int step = 0;
-        uint32_t stage = 0, phase = 1;                 // copies issued; the next one's stage (a barrier's first wait does not wait)
-        // One tile of keys or values: rows of the warp that exist (`there`) at row offsets at[j] (in 16 bytes), zeros for the others.
-        // The stage is handed on by the copies themselves; the issuing thread of the matrix products has the fence between
-        // their writes and its reads (here it would wait for every copy in flight: twice the time on long contexts).
-        // look: values of an arena tile, which somebody looks over before they are handed on.
-        auto load = [&](const char* base, const uint32_t (&at)[NJ], uint32_t there, bool look) {
-            if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) return false;
-            const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
-            const char* from[HP];                       // (rows that do not exist are at 0 and of no bytes)
-#pragma unroll
-            for (int w = 0; w < HP; ++w) from[w] = base + w * head2;
-            if (there == 0xffffffffu && full_head) {
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int w = 0; w < HP; ++w)
-                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[w] + (uint64_t)at[j] * 16, 16u);
-            } else {
-                const uint32_t mine = ch_in ? there >> sub : 0u;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const uint32_t bytes = (mine >> (j * RW)) & 1u ? 16u : 0u;
-#pragma unroll
-                    for (int w = 0; w < HP; ++w)
-                        cp_async16(dst + w * C::head_bytes + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[w] + (uint64_t)at[j] * 16, bytes);
-                }
-            }
-            if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
-            if (step != a.drop_item) cp_arrive(msmem_u32(look && C::inspectors ? &sm.landed[stage] : &sm.full[stage]));
-            ++step;
-            if (++stage == C::stages) { stage = 0; phase ^= 1u; }
-            return true;
-        };
-        // the tile being looked up, one ahead of the one being copied
-        int f_row = 0, f_id = 0;
-        bool f_arena = false, f_in = false;
-        uint32_t f_m0 = 0, f_m1 = 0;
-        auto look_up = [&](const TreePiece& p, int t) {
-            int place, count;
-            tree_tile_span(a, p, t, kMKeys, &place, &count);
-            f_arena = t < p.arena_tiles;
-            f_in = lw * 32 + lane < count;
-            f_m0 = f_m1 = 0;
-            if (f_arena) {
-                const int w = (place >> 5) + lw;
-                const uint32_t* mk = a.masks + (int64_t)p.b * a.n * a.W + w;
-                if (w < a.W) {
-                    if (lane < a.n) f_m0 = __ldg(mk + lane * a.W);
-                    if (lane + 32 < a.n) f_m1 = __ldg(mk + (lane + 32) * a.W);
-                }
-            }
-            const uint32_t at = (uint32_t)(place + lw * 32 + lane), page = tree_page(a.pages, at);
-            f_row = (int)(at - page * (uint32_t)a.pages.page_size);
-            f_in = f_in && page < (uint32_t)a.pages.max_pages;
-            f_id = f_in ? __ldg(a.pages.table + (int64_t)p.b * a.pages.table_stride + page) : 0;
-        };
-        // The loader walks the pieces of the run, one ahead (the next piece's numbers come out of the L2), and tells the others.
-        TreePiece pc, nx;
-        bool more = tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, true, &nx);
-        if (lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, row_blocks, kItemUnits);
         const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;        // rows in 16 bytes
-        bool ok = true;
-        int piece = 0, tile_no = 0;
-        if (more) look_up(nx, nx.tile);
-        while (more) {
-            pc = nx;
-            if (lw == 0 && piece >= kPieces && !mbar_wait(msmem_u32(&sm.released[piece % kPieces]), (piece / kPieces - 1) & 1, abort_flag, limit)) { ok = false; break; }
-            if (lw == 0 && lane == 0) {
-                sm.piece[piece % kPieces][0] = make_int4(pc.b, pc.h, pc.rb, pc.top);
-                sm.piece[piece % kPieces][1] = make_int4(pc.tile, pc.tiles, pc.arena_tiles, pc.slot | (pc.whole ? 2 : 0));
-                mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
-            }
-            more = tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, false, &nx);
-            // queries of the item: beyond the rows and the head size, zeros
-            const uint32_t qb = (uint32_t)piece % C::q_bufs;
-            if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
-            {
-                const int rows_here = min(C::rows, M - pc.rb * C::rows);
-                const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head) + (ch_in ? ch * 16 : 0);
-                const char* from[HP];
-#pragma unroll
-                for (int w = 0; w < HP; ++w) from[w] = q + 2 * (int64_t)(w * a.G) * a.q_head;
-                const uint32_t dst = tiles + C::q_at + qb * C::q_bytes + (uint32_t)(ch >> 3) * C::q_half + (uint32_t)sub * 128;
+        int step = 0;
+        uint32_t stage = 0, phase = 1;                 // of the next copy (a barrier's first wait does not wait)
+        // The loader walks the pieces of the run and tells the others.  Tiles are looked up one ahead of the one being copied:
+        // numbers, masks and page entries come out of the L2.
+        TreePiece pc, nx;
+        int piece = -1, tile_no = 0, t = 0, f_row = 0, f_id = 0;
+        bool f_arena = false, f_in = false, ok = true;
+        uint32_t f_m0 = 0, f_m1 = 0;
+        pc.tile = pc.tiles = pc.top = pc.ctx = pc.b = pc.h = pc.rb = pc.arena_tiles = pc.slot = 0; pc.whole = false;
 #pragma unroll 1
-                for (int r0 = 0; r0 < rows_here; r0 += 32) {          // a lane finds one row, and every lane copies chunks of all
-                    const int rr = min(pc.rb * C::rows + r0 + lane, M - 1), tok = a.G == 1 ? rr : rr / a.G;
-                    const int64_t mine = 2 * ((int64_t)tok * a.q_row + (int64_t)(rr - tok * a.G) * a.q_head);
-                    const int left = ch_in ? rows_here - r0 - sub : 0;
-#pragma unroll
-                    for (int jj = 0; jj < NJ / kLoadWarps; ++jj) {
-                        const int j = jj * kLoadWarps + lw;
-                        const int64_t at = __shfl_sync(kFullMask, mine, j * RW + sub);
-                        const uint32_t bytes = j * RW < left ? 16u : 0u;
-                        const uint32_t to = dst + (r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
-#pragma unroll
-                        for (int w = 0; w < HP; ++w) cp_async16(to + w * 32 * 128, from[w] + at, bytes);
+        for (;;) {
+            // --- the tile looked up last
+            const int c_row = f_row, c_id = f_id, c_t = t;
+            const bool c_arena = f_arena;
+            bool c_in = f_in;
+            const uint32_t c_any = f_m0 | f_m1;
+            const bool last = c_t + 1 == pc.tile + pc.tiles;
+            bool more = true;
+            // --- look the next one up: of this piece, or the first of the next
+            if (piece < 0 || last) {
+                more = tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, piece < 0, &nx);
+                if (piece < 0 && lw == 0 && lane == 0) tree_write_meta(a, run, more ? &nx : nullptr, row_blocks, kItemUnits);
+                t = nx.tile;
+            } else { nx = pc; t = c_t + 1; }
+            if (more) {
+                int place, count;
+                tree_tile_span(a, nx, t, kMKeys, &place, &count);
+                f_arena = t < nx.arena_tiles;
+                f_in = lw * 32 + lane < count;
+                f_m0 = f_m1 = 0;
+                if (f_arena) {
+                    const int w = (place >> 5) + lw;
+                    const uint32_t* mk = a.masks + (int64_t)nx.b * a.n * a.W + w;
+                    if (w < a.W) {
+                        if (lane < a.n) f_m0 = __ldg(mk + lane * a.W);
+                        if (lane + 32 < a.n) f_m1 = __ldg(mk + (lane + 32) * a.W);
                     }
-                }                                       // (the first keys' arrival counts them too)
+                }
+                const uint32_t at = (uint32_t)(place + lw * 32 + lane), page = tree_page(a.pages, at);
+                f_row = (int)(at - page * (uint32_t)a.pages.page_size);
+                f_in = f_in && page < (uint32_t)a.pages.max_pages;
+                f_id = f_in ? __ldg(a.pages.table + (int64_t)nx.b * a.pages.table_stride + page) : 0;
             }
-            const char* const kb = (const char*)a.k + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
-            const char* const vb = (const char*)a.v + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
-            uint32_t v_at[NJ], v_there = 0;
-            bool v_look = false;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) v_at[j] = 0;
+            if (piece >= 0) {
+                const uint32_t qb = (uint32_t)piece % C::q_bufs;
+                if (c_t == pc.tile) {                  // a new piece: the others are told, and its item's queries fetched
+                    if (lw == 0 && piece >= kPieces && !mbar_wait(msmem_u32(&sm.released[piece % kPieces]), (piece / kPieces - 1) & 1, abort_flag, limit)) { ok = false; break; }
+                    if (lw == 0 && lane == 0) {
+                        sm.piece[piece % kPieces][0] = make_int4(pc.b, pc.h, pc.rb, pc.top);
+                        sm.piece[piece % kPieces][1] = make_int4(pc.tile, pc.tiles, pc.arena_tiles, pc.slot | (pc.whole ? 2 : 0));
+                        mbar_arrive(msmem_u32(&sm.published[piece % kPieces]));
+                    }
+                    if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                    // beyond the rows and the head size, zeros
+                    const int rows_here = min(C::rows, M - pc.rb * C::rows);
+                    const char* q = (const char*)a.q + 2 * ((int64_t)pc.b * a.q_seq + (int64_t)pc.h * HP * a.G * a.q_head) + (ch_in ? ch * 16 : 0);
+                    const uint32_t dst = tiles + C::q_at + qb * C::q_bytes + (uint32_t)(ch >> 3) * C::q_half + (uint32_t)sub * 128;
 #pragma unroll 1
-            for (int t = pc.tile; t < pc.tile + pc.tiles; ++t, ++tile_no) {
-                if (f_arena) {                          // slots no row of the sequence sees are not read
-                    const uint32_t any = __reduce_or_sync(kFullMask, f_m0 | f_m1);
-                    f_in = f_in && ((any >> lane) & 1u);
+                    for (int r0 = 0; r0 < rows_here; r0 += 32) {      // a lane finds one row, and every lane copies chunks of all
+                        const int rr = min(pc.rb * C::rows + r0 + lane, M - 1), tok = a.G == 1 ? rr : rr / a.G;
+                        const int64_t mine = 2 * ((int64_t)tok * a.q_row + (int64_t)(rr - tok * a.G) * a.q_head);
+                        const int left = ch_in ? rows_here - r0 - sub : 0;
+#pragma unroll 2
+                        for (int j = lw; j < NJ; j += kLoadWarps) {
+                            const char* from = q + __shfl_sync(kFullMask, mine, j * RW + sub);
+                            const uint32_t bytes = j * RW < left ? 16u : 0u;
+                            const uint32_t to = dst + (r0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+#pragma unroll
+                            for (int w = 0; w < HP; ++w) cp_async16(to + w * 32 * 128, from + 2 * (int64_t)(w * a.G) * a.q_head, bytes);
+                        }
+                    }                                   // (the first keys' arrival counts them too)
                 }
-                if (f_in && (uint32_t)f_id >= (uint32_t)a.pages.num_pages) {
+                // --- where its rows are
+                if (c_arena) {                          // slots no row of the sequence sees are not read
+                    const uint32_t any = __reduce_or_sync(kFullMask, c_any);
+                    c_in = c_in && ((any >> lane) & 1u);
+                }
+                if (c_in && (uint32_t)c_id >= (uint32_t)a.pages.num_pages) {
                     atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
-                    f_in = false;
+                    c_in = false;
                 }
-                // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
-                const uint32_t mine = f_in ? (uint32_t)((int64_t)f_id * page16 + (int64_t)f_row * token16) : 0u;
-                const bool look = f_arena;
-                const uint32_t there = __ballot_sync(kFullMask, f_in);
+                const uint32_t there = __ballot_sync(kFullMask, c_in);
                 if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
-                if (t + 1 < pc.tile + pc.tiles) look_up(pc, t + 1);
-                else if (more) look_up(nx, nx.tile);
-                uint32_t at[NJ];
+                // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
+                sm.rows[tile_no & 1][lw * 32 + lane] = c_in ? (uint32_t)((int64_t)c_id * page16 + (int64_t)c_row * token16) : kNoRow;
+                __syncwarp();
+                // --- copies: the keys, the values LAG tiles behind, and after the last keys the values that are left.  The stage
+                // is handed on by the copies themselves; the issuing thread of the matrix products has the fence between their
+                // writes and its reads (here it would wait for every copy in flight: twice the time on long contexts).  Values of
+                // an arena tile go through the inspector first.
+                const int n_copies = 2 + (LAG && last ? 1 : 0);
+#pragma unroll 1
+                for (int k = 0; k < n_copies; ++k) {
+                    const int of = k == 0 ? c_t : k == 1 ? c_t - LAG : c_t;      // the tile
+                    if (of < pc.tile) continue;
+                    const bool look = k > 0 && of < pc.arena_tiles && C::inspectors;
+                    if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) { ok = false; break; }
+                    const char* base = (const char*)(k == 0 ? a.k : a.v) + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
+                    const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
+                    const uint32_t* rows = &sm.rows[(tile_no - (c_t - of)) & 1][lw * 32 + sub];
+                    uint32_t at[NJ];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) at[j] = __shfl_sync(kFullMask, mine, j * RW + sub);
-                if (!load(kb, at, there, false)) { ok = false; break; }
-                // one S in tensor memory: K0 V0 K1 V1 ..;  two: K0 K1 V0 K2 V1 .. (the products run one tile ahead)
-                if (C::s_bufs == 1) {
-                    if (!load(vb, at, there, look)) { ok = false; break; }
-                } else {
-                    if (t > pc.tile && !load(vb, v_at, v_there, v_look)) { ok = false; break; }
+                    for (int j = 0; j < NJ; ++j) at[j] = rows[j * RW];
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) v_at[j] = at[j];
-                    v_there = there; v_look = look;
+                    for (int j = 0; j < NJ; ++j) {
+                        const uint32_t bytes = at[j] != kNoRow && ch_in ? 16u : 0u;
+                        const char* from = base + (uint64_t)(at[j] != kNoRow ? at[j] : 0u) * 16;
+                        const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+#pragma unroll
+                        for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, bytes);
+                    }
+                    if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
+                    if (step != a.drop_item) cp_arrive(msmem_u32(look ? &sm.landed[C::inspectors ? stage : 0] : &sm.full[stage]));
+                    ++step;
+                    if (++stage == C::stages) { stage = 0; phase ^= 1u; }
                 }
+                if (!ok) break;
+                ++tile_no;
             }
-            if (!ok || (C::s_bufs > 1 && !load(vb, v_at, v_there, v_look))) { ok = false; break; }
-            ++piece;
+            if (!more) break;
+            if (piece < 0 || last) ++piece;
+            pc = nx;
         }
+        ++piece;
         if (ok && lw == 0 &&                            // the end of the run
             (piece < kPieces || mbar_wait(msmem_u32(&sm.released[piece % kPieces]), (piece / kPieces - 1) & 1, abort_flag, limit)) && lane == 0) {
             sm.piece[piece % kPieces][1] = make_int4(0, 0, 0, 0);
@@ -449,73 +442,74 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
         const uint32_t tiles = msmem_u32(sm.tiles), q0 = tiles + C::q_at - quarter * (32 * 128);      // the queries are the lanes from 32 quarter on
         uint32_t stage = 0, phase = 0;                 // of the next copy
-        uint32_t g = 0;
         int piece = 0;
         bool ok = true;
         auto next_stage = [&]() { if (++stage == C::stages) { stage = 0; phase ^= 1u; } };
-        // the scores of tile gi of the block's sequence; `last`: of its piece
-        auto scores = [&](uint32_t gi, uint32_t qb, bool last) {
-            if (!mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit)) return false;
-            const uint32_t sb = gi % C::s_bufs;
-            const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(tiles + C::stage_at(stage), 16);
-            const uint32_t d = tmem + C::s_col + sb * kMKeys;
-            if (elect_one()) {
-                fence_async_proxy();                   // the copies' writes (generic) before the products' reads
-                tc_after();
-#pragma unroll
-                for (int w = 0; w < HP; ++w)
-#pragma unroll
-                    for (int ks = 0; ks < DP / 16; ++ks)    // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns (zeros beyond the head size)
-                        mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2),
-                               dk + (uint64_t)((w * C::head_bytes + (ks >> 2) * (kMKeys * 128)) / 16 + (ks & 3) * 2), idesc_s | negate, ks != 0, HP > 1 ? w : -1);
-                mma_commit(msmem_u32(&sm.empty[stage]));
-                mma_commit(msmem_u32(&sm.s_full[sb]));
-                mbar_arrive(msmem_u32(&sm.s_full[sb]));
-                if (last) mma_commit(msmem_u32(&sm.q_empty[qb]));
-            }
-            __syncwarp();
-            next_stage();
-            return true;
-        };
-        while (ok) {
-            if (!(ok = mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit))) break;
+        constexpr int LAG = C::s_bufs - 1;             // one S in tensor memory: S0 O0 S1 O1 ..;  two: S0 S1 O0 S2 O1 ..
+        uint32_t n_s = 0, n_o = 0;                     // tiles whose scores, and whose outputs, have been issued
+#pragma unroll 1
+        for (;; ++piece) {
+            if (!mbar_wait(msmem_u32(&sm.published[piece % kPieces]), (piece / kPieces) & 1, abort_flag, limit)) break;
             const int4 i1 = sm.piece[piece % kPieces][1];
             const int n_tiles = i1.y;
             if (n_tiles == 0) break;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
-            ok = scores(g, qb, n_tiles == 1);
 #pragma unroll 1
-            for (int t = 0; t < n_tiles && ok; ++t, ++g) {
-                // one S in tensor memory: S0 O0 S1 O1 ..;  two: S0 S1 O0 S2 O1 ..
-                if (C::s_bufs > 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
-                const uint32_t sb = g % C::s_bufs;
-                if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
-                if (!C::inspectors && i1.x + t < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(stage), lane)) {
-                    if (lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+            for (int t = 0; t < n_tiles + LAG; ++t) {
+                if (t < n_tiles) {
+                    if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
+                    const uint32_t sb = n_s % C::s_bufs;
+                    const uint64_t dq = sw128_desc(q0 + qb * C::q_bytes, 16), dk = sw128_desc(tiles + C::stage_at(stage), 16);
+                    const uint32_t d = tmem + C::s_col + sb * kMKeys;
+                    if (elect_one()) {
+                        fence_async_proxy();           // the copies' writes (generic) before the products' reads
+                        tc_after();
+#pragma unroll
+                        for (int w = 0; w < HP; ++w)
+#pragma unroll
+                            for (int ks = 0; ks < DP / 16; ++ks)      // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns (zeros beyond the head size)
+                                mma_ss(d, dq + (uint64_t)((ks >> 2) * (C::q_half / 16) + (ks & 3) * 2),
+                                       dk + (uint64_t)((w * C::head_bytes + (ks >> 2) * (kMKeys * 128)) / 16 + (ks & 3) * 2), idesc_s | negate, ks != 0, HP > 1 ? w : -1);
+                        mma_commit(msmem_u32(&sm.empty[stage]));
+                        mma_commit(msmem_u32(&sm.s_full[sb]));
+                        mbar_arrive(msmem_u32(&sm.s_full[sb]));
+                        if (t + 1 == n_tiles) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                    }
                     __syncwarp();
+                    ++n_s;
+                    next_stage();
                 }
-                if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (g / C::s_bufs) & 1u, abort_flag, limit))) break;
-                if (t == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
-                const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
-                const uint32_t p = tmem + C::s_col + sb * kMKeys;
-                if (elect_one()) {
-                    fence_async_proxy();
-                    tc_after();
+                if (t >= LAG) {
+                    const int of = t - LAG;
+                    const uint32_t sb = n_o % C::s_bufs;
+                    if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
+                    if (!C::inspectors && i1.x + of < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(stage), lane)) {
+                        if (lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                        __syncwarp();
+                    }
+                    if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (n_o / C::s_bufs) & 1u, abort_flag, limit))) break;
+                    if (of == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
+                    const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
+                    const uint32_t p = tmem + C::s_col + sb * kMKeys;
+                    if (elect_one()) {
+                        fence_async_proxy();
+                        tc_after();
 #pragma unroll
-                    for (int w = 0; w < HP; ++w)
+                        for (int w = 0; w < HP; ++w)
 #pragma unroll
-                        for (int ks = 0; ks < kMKeys / 16; ++ks)      // 16 keys = two groups of eight rows of 128 bytes
-                            mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)((w * C::head_bytes + ks * 2048) / 16), idesc_o, (t | ks) != 0, HP > 1 ? w : -1);
-                    mma_commit(msmem_u32(&sm.empty[stage]));
-                    mma_commit(msmem_u32(&sm.pv_done));
-                    if (t + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
+                            for (int ks = 0; ks < kMKeys / 16; ++ks)  // 16 keys = two groups of eight rows of 128 bytes
+                                mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)((w * C::head_bytes + ks * 2048) / 16), idesc_o, (of | ks) != 0, HP > 1 ? w : -1);
+                        mma_commit(msmem_u32(&sm.empty[stage]));
+                        mma_commit(msmem_u32(&sm.pv_done));
+                        if (of + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
+                    }
+                    __syncwarp();
+                    ++n_o;
+                    next_stage();
                 }
-                __syncwarp();
-                next_stage();
-                if (C::s_bufs == 1 && t + 1 < n_tiles && !(ok = scores(g + 1, qb, t + 2 == n_tiles))) break;
             }
-            if (ok && lane == 0) mbar_arrive(msmem_u32(&sm.released[piece % kPieces]));
-            ++piece;
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(msmem_u32(&sm.released[piece % kPieces]));
         }
         // nothing of this block is in flight when it leaves, whatever happened
         if (elect_one()) mma_commit(msmem_u32(&sm.last));
@@ -669,7 +663,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 const int p_h = sm.piece[piece % kPieces][0].y * HP + (HP > 1 ? warp : 0), head = p_h * a.G + rr - tok * a.G;
                 const int64_t part = (int64_t)(2 * blockIdx.x + (i1.w & 1)) * (32 * SW) + row;
                 __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)p_b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < DP; c += 32) {
                     uint32_t u[32];
                     tm_ld32(tmem + lanes + C::o_col + c, u);
