@@ -38,7 +38,7 @@ constexpr float kRaise = 8.f;               // how far (powers of two) a score m
 
 // SW softmax warps; an item is a block of rows of HP key heads.
 //   <DP, 4, 1>  up to 128 rows of one key head
-//   <DP, 4, 4>  up to 32 rows of each of four neighbouring key heads, a softmax warp to each.  Four products per tile, each of
+//   <64, 4, 4>  up to 32 rows of each of four neighbouring key heads, a softmax warp to each.  Four products per tile, each of
 //               which writes the quarter of the lanes that is its head's.  The four share what a tile costs beside its
 //               bytes: its look-ups, masks and the way through the roles.
 //   <DP, 1, 1>  up to 32 rows of one key head, where there are not four to take.  The other 96 rows of the products are what
@@ -53,7 +53,7 @@ template <int DP, int SW, int HP> struct MConf {
     static constexpr int q_bytes = 32 * SW * DP * 2;
     static constexpr int q_bufs = SW == 1 || (DP == 64 && HP == 1) ? 2 : 1;
     static constexpr int s_bufs = DP == 64 && SW == 1 ? 1 : 2;
-    static constexpr int blocks_per_sm = DP == 64 && SW == 1 ? 4 : DP == 128 && HP == 4 ? 1 : 2;
+    static constexpr int blocks_per_sm = DP == 64 && SW == 1 ? 4 : 2;
     static constexpr int tmem_cols = s_bufs == 1 ? 128 : 256;
     static constexpr int o_col = 0, s_col = DP;
     // stages that lie before the queries: with one softmax warp the products' other rows are read up to 96 rows before and
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         // numbers, masks and page entries come out of the L2.
         TreePiece pc, nx;
         int piece = -1, tile_no = 0, t = 0, f_row = 0, f_id = 0;
-        bool f_arena = false, f_in = false, ok = true;
+        bool f_arena = false, f_in = false, ok = true, whole = false, whole_before = false;
         uint32_t f_m0 = 0, f_m1 = 0;
         pc.tile = pc.tiles = pc.top = pc.ctx = pc.b = pc.h = pc.rb = pc.arena_tiles = pc.slot = 0; pc.whole = false;
 #pragma unroll 1
@@ -390,6 +390,8 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 }
                 const uint32_t there = __ballot_sync(kFullMask, c_in);
                 if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
+                whole_before = whole;
+                whole = there == 0xffffffffu && a.D == DP;       // every byte of the warp's rows is there to be copied
                 // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
                 sm.rows[tile_no & 1][lw * 32 + lane] = c_in ? (uint32_t)((int64_t)c_id * page16 + (int64_t)c_row * token16) : kNoRow;
                 __syncwarp();
@@ -410,13 +412,23 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                     uint32_t at[NJ];
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) at[j] = rows[j * RW];
+                    if (HP == 1 && (of == c_t ? whole : whole_before)) {
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        const uint32_t bytes = at[j] != kNoRow && ch_in ? 16u : 0u;
-                        const char* from = base + (uint64_t)(at[j] != kNoRow ? at[j] : 0u) * 16;
-                        const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+                        for (int j = 0; j < NJ; ++j) {
+                            const char* from = base + (uint64_t)at[j] * 16;
+                            const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
 #pragma unroll
-                        for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, bytes);
+                            for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, 16u);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) {
+                            const uint32_t bytes = at[j] != kNoRow && ch_in ? 16u : 0u;
+                            const char* from = base + (uint64_t)(at[j] != kNoRow ? at[j] : 0u) * 16;
+                            const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+#pragma unroll
+                            for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, bytes);
+                        }
                     }
                     if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
                     if (step != a.drop_item) cp_arrive(msmem_u32(look ? &sm.landed[C::inspectors ? stage : 0] : &sm.full[stage]));
@@ -725,34 +737,29 @@ cudaError_t launch_mma(const TreeAttend& a, int grid, cudaStream_t st) {
     const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
     return launch_after(tree_attend_mma_kernel<DP, SW, HP>, dim3(grid), dim3(MConf<DP, SW, HP>::threads), sizeof(MSmem<DP, SW, HP>), st, a, negate);
 }
-template <int DP>
-int blocks_mma(int rows, int heads) {
-    return rows == 32 ? MConf<DP, 1, 1>::blocks_per_sm : heads == 4 ? MConf<DP, 4, 4>::blocks_per_sm : MConf<DP, 4, 1>::blocks_per_sm;
-}
-template <int DP>
-cudaError_t launch_mma_d(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
-    return rows == 32 ? launch_mma<DP, 1, 1>(a, grid, st) : a.item_heads == 4 ? launch_mma<DP, 4, 4>(a, grid, st) : launch_mma<DP, 4, 1>(a, grid, st);
-}
-
 }  // namespace
 
 bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
-// Up to 32 rows to a key head: four heads at a time where their number allows, else one softmax warp.
+// Up to 32 rows to a key head: four heads of up to 64 at a time where their number allows (beside one softmax warp to a block:
+// 172 against 262 us on 4 x 131071 keys of 8 heads of 64, one row each; heads of 128 lose by it, 185 against 172 us), else
+// one softmax warp.
 void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p) {
     p->item_heads = M <= 32 && K % 4 == 0 && D <= 64 ? 4 : 1;
     p->rows = M <= 32 && p->item_heads == 1 ? 32 : kMRows;
-    p->grid = sm_count * (D <= 64 ? blocks_mma<64>(p->rows, p->item_heads) : blocks_mma<128>(p->rows, p->item_heads));
+    p->grid = sm_count * (D > 64 ? (p->rows == 32 ? MConf<128, 1, 1>::blocks_per_sm : MConf<128, 4, 1>::blocks_per_sm)
+                          : p->item_heads == 4 ? MConf<64, 4, 4>::blocks_per_sm
+                          : p->rows == 32 ? MConf<64, 1, 1>::blocks_per_sm : MConf<64, 4, 1>::blocks_per_sm);
 }
 cudaError_t configure_tree_mma() {
     cudaError_t e = configure_mma<64, 1, 1>();
     if (e == cudaSuccess) e = configure_mma<64, 4, 1>();
     if (e == cudaSuccess) e = configure_mma<64, 4, 4>();
     if (e == cudaSuccess) e = configure_mma<128, 1, 1>();
-    if (e == cudaSuccess) e = configure_mma<128, 4, 1>();
-    return e == cudaSuccess ? configure_mma<128, 4, 4>() : e;
+    return e == cudaSuccess ? configure_mma<128, 4, 1>() : e;
 }
 cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
-    return a.D <= 64 ? launch_mma_d<64>(a, rows, grid, st) : launch_mma_d<128>(a, rows, grid, st);
+    if (a.D > 64) return rows == 32 ? launch_mma<128, 1, 1>(a, grid, st) : launch_mma<128, 4, 1>(a, grid, st);
+    return a.item_heads == 4 ? launch_mma<64, 4, 4>(a, grid, st) : rows == 32 ? launch_mma<64, 1, 1>(a, grid, st) : launch_mma<64, 4, 1>(a, grid, st);
 }
 
 }  // namespace dba
