@@ -1,13 +1,15 @@
-// Attention of the rows of a token tree over a paged cache, plain kernel: every type and head size, fp32 arithmetic on the
-// general cores.  It serves fp32 (whose products the tensor cores would round to 10 bits) and head sizes over 128.
+// Attention of the rows of a token tree over a paged cache on the general cores: fp32 (whose products the tensor cores would
+// round to 10 bits) and head sizes over 128.  And the kernel that joins the pieces of either attention kernel.
 //
 // softmax over the places p a row sees:  o = sum_p 2^(x_p - m) v_p / sum_p 2^(x_p - m),  x = scale log2(e) <q, k>,  with the
 // running maximum m and sum kept per row while the keys go by once; a tile's contribution is rescaled when m rises.
 //
-// A block of 128 threads works on 32 rows of one (sequence, key head): 8 row groups x 16 threads.  Thread (g, c) computes
-// the scores of rows g, g+8, g+16, g+24 with keys c, c+16, ... of the tile, and of the output the same rows x columns
-// 4c .. 4c+3 (+64, ...), so a row's statistics stay in the 16 threads that use them and the probabilities
-// cross through shared memory within a warp only.
+// A block of 128 threads works on 8 RI rows of one (sequence, key head): 8 row groups x 16 threads.  Thread (g, c) computes the
+// scores of rows g, g+8, .. with keys c, c+16, ... of the tile, and of the output the same rows x columns 4c .. 4c+3 (+64,
+// ...), so a row's statistics stay in the 16 threads that use them and the probabilities cross through shared memory
+// within a warp only.  RI = 1 .. 4 by the number of rows, so that few rows are computed for nothing.  Products and sums go two
+// at a time (fma.rn.f32x2), which leaves issue slots to the loads from shared memory that feed them.
+// The keys of the next tile and the values of this one are on their way (cp.async) while the scores are computed.
 #include <cuda_bf16.h>
 
 #include "tree_device.cuh"
@@ -17,73 +19,130 @@ namespace dba {
 namespace {
 
 constexpr int kGRows = 32, kGThreads = 128;
+constexpr int kGItemUnits = 1;              // what an item costs beside its tiles, in tiles
 
-template <typename T> struct TreeVec;
-template <> struct TreeVec<float> {
-    static constexpr int n = 4;
-    __device__ static void load(const float* p, float* r) { const float4 v = *reinterpret_cast<const float4*>(p); r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w; }
-};
-template <> struct TreeVec<__nv_bfloat16> {
-    static constexpr int n = 8;
-    __device__ static void load(const __nv_bfloat16* p, float* r) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { r[2 * i] = __uint_as_float(u[i] << 16); r[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-    }
-};
 __device__ __forceinline__ void tree_store(float* p, float x) { *p = x; }
 __device__ __forceinline__ void tree_store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
+__device__ __forceinline__ float g_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }     // (within 2^-22)
+// (a0, a1) += (b0, b1) * (c0, c1)
+__device__ __forceinline__ void pair_fma(float2& a, float b0, float b1, float c0, float c1) {
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %5};\n\tfma.rn.f32x2 x, y, z, x;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a.x), "+f"(a.y) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
 template <int DP> struct GSmem {
-    static constexpr int kt = 8192 / DP;               // keys per tile: 32 KB of fp32 keys, as much of values
-    float q[kGRows][DP + 4];
-    float k[kt][DP + 4];
-    float v[kt][DP + 4];
+    static constexpr int kt = DP == 64 ? 64 : DP == 128 ? 32 : 16;     // keys per tile: 16 KB of fp32
+    static constexpr int pitch = DP + 4;                               // (16 rows at a time without a conflict of banks)
+    float q[kGRows][pitch];
+    float k[2][kt][pitch];
+    float v[kt][pitch];
     float p[kGRows][kt + 4];
-    int64_t row[kt];
+    int64_t row[2][kt];
     TreeRunShared run;
 };
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const TreeAttend a) {
+__device__ __forceinline__ void g_copy16(float* dst, const float* src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(in ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void g_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void g_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// One tile of keys or values; rows at -1 and what lies beyond the head size are zeros.  fp32 is copied; bf16 is widened on the
+// way, through registers.
+template <int DP>
+__device__ __forceinline__ void g_load(const TreeAttend& a, const float* base, const int64_t* row, float (*dst)[DP + 4]) {
+    constexpr int CH = DP / 4;
+#pragma unroll
+    for (int i = threadIdx.x; i < GSmem<DP>::kt * CH; i += kGThreads) {
+        const int r = i / CH, d = (i - r * CH) * 4;
+        const bool in = row[r] >= 0 && d < a.D;
+        g_copy16(&dst[r][d], in ? base + row[r] + d : base, in);
+    }
+}
+template <int DP>
+__device__ __forceinline__ void g_load(const TreeAttend& a, const __nv_bfloat16* base, const int64_t* row, float (*dst)[DP + 4]) {
+    constexpr int CH = DP / 8;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < GSmem<DP>::kt * CH; i += kGThreads) {
+        const int r = i / CH, d = (i - r * CH) * 8;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (row[r] >= 0 && d < a.D) x = *reinterpret_cast<const uint4*>(base + row[r] + d);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { dst[r][d + 2 * j] = __uint_as_float(u[j] << 16); dst[r][d + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
+    }
+}
+// How many fp32 a thread brings in at a time, and whether one of them is not finite.
+template <int N> struct TreeCopiedN {
+    static constexpr int n = N;
+    __device__ static bool not_finite(const float* p) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) odd = odd || (__float_as_uint(p[i]) & 0x7f800000u) == 0x7f800000u;
+        return odd;
+    }
+};
+template <typename T> struct TreeCopied;
+template <> struct TreeCopied<float> : TreeCopiedN<4> {};
+template <> struct TreeCopied<__nv_bfloat16> : TreeCopiedN<8> {};
+__device__ __forceinline__ float g_widen(float x) { return x; }
+__device__ __forceinline__ float g_widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+template <typename T, int DP, int RI>
+__global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plain_kernel(const TreeAttend a) {
     using S = GSmem<DP>;
-    constexpr int KT = S::kt, NK = KT / 16, NC = DP / 64, VN = TreeVec<T>::n;
+    constexpr int KT = S::kt, NK = KT / 16, NC = DP / 64, ROWS = 8 * RI;
     extern __shared__ __align__(16) unsigned char raw[];
     S& sm = *reinterpret_cast<S*>(raw);
     const int tid = threadIdx.x, grp = tid >> 4, c = tid & 15;
-    const int M = a.n * a.G, row_blocks = (M + kGRows - 1) / kGRows;
+    const int M = a.n * a.G, row_blocks = (M + ROWS - 1) / ROWS;
     grid_dependency_wait();
     allow_dependents();
-    TreeRun run = tree_run<kGThreads>(a, KT, a.K * row_blocks, 0, 1, &sm.run);
+    TreeRun run = tree_run<kGThreads>(a, KT, a.K * row_blocks, kGItemUnits, 1, &sm.run);
     TreePiece pc;
     bool first = true;
-    if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, row_blocks, 0);
-    while (tree_next_piece(a, run, KT, a.K, row_blocks, 0, first, &pc)) {
-        if (first && tid == 0) tree_write_meta(a, run, &pc, row_blocks, 0);
+    if (run.t >= run.t_end && tid == 0) tree_write_meta(a, run, nullptr, row_blocks, kGItemUnits);
+    for (;;) {
+        const bool more = tree_next_piece(a, run, KT, a.K, row_blocks, kGItemUnits, first, &pc);
+        if (first && tid == 0) tree_write_meta(a, run, more ? &pc : nullptr, row_blocks, kGItemUnits);
+        if (!more) break;
         first = false;
-        const int rows_here = min(kGRows, M - pc.rb * kGRows);
-        __syncthreads();
-        for (int i = tid; i < kGRows * (DP / VN); i += kGThreads) {       // queries, zero beyond the rows and the head size
-            const int r = i / (DP / VN), d = (i - r * (DP / VN)) * VN;
-            float x[VN];
-#pragma unroll
-            for (int j = 0; j < VN; ++j) x[j] = 0.f;
+        const int rows_here = min(ROWS, M - pc.rb * ROWS);
+        const T* const kb = (const T*)a.k + (int64_t)pc.h * a.pages.head_stride;
+        const T* const vb = (const T*)a.v + (int64_t)pc.h * a.pages.head_stride;
+        auto find_rows = [&](int t) {                      // rows of a tile in the cache
+            if (t < pc.tile + pc.tiles)
+                for (int i = tid; i < KT; i += kGThreads) {
+                    int place, count;
+                    tree_tile_span(a, pc, t, KT, &place, &count);
+                    sm.row[t & 1][i] = i < count ? tree_row(a.pages, pc.b, place + i) : -1;
+                }
+        };
+        __syncthreads();                                   // the last piece is done with
+        find_rows(pc.tile);
+        for (int i = tid; i < ROWS * DP; i += kGThreads) { // queries, zero beyond the rows and the head size
+            const int r = i / DP, d = i - r * DP;
+            float x = 0.f;
             if (r < rows_here && d < a.D) {
-                const int rr = pc.rb * kGRows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
-                TreeVec<T>::load((const T*)a.q + (int64_t)pc.b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d, x);
+                const int rr = pc.rb * ROWS + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
+                x = g_widen(((const T*)a.q)[(int64_t)pc.b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d]);
             }
-#pragma unroll
-            for (int j = 0; j < VN; ++j) sm.q[r][d + j] = x[j];
+            sm.q[r][d] = x;
         }
-        float m[4], l[4], o[4][NC * 4];
-        const uint32_t* mask[4];
-        bool live[4];
+        __syncthreads();
+        g_load<DP>(a, kb, sm.row[pc.tile & 1], sm.k[pc.tile & 1]);
+        g_commit();
+        find_rows(pc.tile + 1);
+        float m[RI], l[RI];
+        float2 o[RI][NC * 2];
+        const uint32_t* mask[RI];
+        bool live[RI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RI; ++i) {
             m[i] = neg_inf(); l[i] = 0.f;
             const int r = grp + 8 * i;
-            const int tok = min(pc.rb * kGRows + r, M - 1) / a.G;
+            const int tok = min(pc.rb * ROWS + r, M - 1) / a.G;
             mask[i] = a.masks ? a.masks + ((int64_t)pc.b * a.n + tok) * a.W : nullptr;
             live[i] = r < rows_here;
             if (a.masks && live[i]) {                    // an empty mask closes the row
@@ -92,68 +151,59 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
                 live[i] = any != 0;
             }
 #pragma unroll
-            for (int j = 0; j < NC * 4; ++j) o[i][j] = 0.f;
+            for (int j = 0; j < NC * 2; ++j) o[i][j] = make_float2(0.f, 0.f);
         }
+#pragma unroll 1
         for (int t = pc.tile; t < pc.tile + pc.tiles; ++t) {
             int place, count;
             tree_tile_span(a, pc, t, KT, &place, &count);
             const bool arena = t < pc.arena_tiles;
-            __syncthreads();                               // the last tile has been used
-            for (int i = tid; i < KT; i += kGThreads)
-                sm.row[i] = i < count ? tree_row(a.pages, pc.b, place + i) : -1;
-            __syncthreads();
-            for (int i = tid; i < KT * (DP / VN); i += kGThreads) {
-                const int r = i / (DP / VN), d = (i - r * (DP / VN)) * VN;
-                float x[VN], y[VN];
+            g_wait<0>();
+            __syncthreads();                               // this tile's keys and the next one's rows are there; the last values have been used
+            g_load<DP>(a, vb, sm.row[t & 1], sm.v);
+            g_commit();
+            if (t + 1 < pc.tile + pc.tiles) g_load<DP>(a, kb, sm.row[(t + 1) & 1], sm.k[(t + 1) & 1]);
+            g_commit();
+            float2 s[RI][NK];
 #pragma unroll
-                for (int j = 0; j < VN; ++j) x[j] = y[j] = 0.f;
-                if (sm.row[r] >= 0 && d < a.D) {
-                    const int64_t at = sm.row[r] + (int64_t)pc.h * a.pages.head_stride + d;
-                    TreeVec<T>::load((const T*)a.k + at, x);
-                    TreeVec<T>::load((const T*)a.v + at, y);
-                }
+            for (int i = 0; i < RI; ++i)
 #pragma unroll
-                for (int j = 0; j < VN; ++j) { sm.k[r][d + j] = x[j]; sm.v[r][d + j] = y[j]; }
-            }
-            __syncthreads();
-            float s[4][NK];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < NK; ++j) s[i][j] = 0.f;
-#pragma unroll 2
+                for (int j = 0; j < NK; ++j) s[i][j] = make_float2(0.f, 0.f);
+#pragma unroll 4
             for (int d = 0; d < DP; d += 4) {
-                float4 qv[4];
+                float4 qv[RI];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[grp + 8 * i][d]);
+                for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[grp + 8 * i][d]);
 #pragma unroll
                 for (int j = 0; j < NK; ++j) {
-                    const float4 kv = *reinterpret_cast<const float4*>(&sm.k[c + 16 * j][d]);
+                    const float4 kv = *reinterpret_cast<const float4*>(&sm.k[t & 1][c + 16 * j][d]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[i][j] = fmaf(qv[i].x, kv.x, fmaf(qv[i].y, kv.y, fmaf(qv[i].z, kv.z, fmaf(qv[i].w, kv.w, s[i][j]))));
+                    for (int i = 0; i < RI; ++i) {
+                        pair_fma(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
+                        pair_fma(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
+                    }
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float top = neg_inf();
+            for (int i = 0; i < RI; ++i) {
+                float x[NK], top = neg_inf();
 #pragma unroll
                 for (int j = 0; j < NK; ++j) {
                     const int kk = c + 16 * j;
-                    bool see = live[i] && kk < count && sm.row[kk] >= 0;
+                    bool see = live[i] && kk < count && sm.row[t & 1][kk] >= 0;
                     if (arena && see) see = (__ldg(mask[i] + ((place + kk) >> 5)) >> ((place + kk) & 31)) & 1u;
-                    s[i][j] = see ? s[i][j] * a.scale_log2e : neg_inf();
-                    top = fmaxf(top, s[i][j]);
+                    x[j] = see ? (s[i][j].x + s[i][j].y) * a.scale_log2e : neg_inf();
+                    top = fmaxf(top, x[j]);
                 }
 #pragma unroll
                 for (int k = 8; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, k));
                 const float mn = fmaxf(m[i], top);
                 const float ref = mn == neg_inf() ? 0.f : mn;
-                const float corr = exp2f(m[i] - ref);          // 0 while nothing has been seen
+                const float corr = g_ex2(m[i] - ref);          // 0 while nothing has been seen
                 float sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < NK; ++j) {
-                    const float e = exp2f(s[i][j] - ref);
+                    const float e = g_ex2(x[j] - ref);
                     sm.p[grp + 8 * i][c + 16 * j] = e;
                     sum += e;
                 }
@@ -162,68 +212,77 @@ __global__ void __launch_bounds__(kGThreads) tree_attend_plain_kernel(const Tree
                 l[i] = fmaf(l[i], corr, sum);
                 m[i] = mn;
 #pragma unroll
-                for (int j = 0; j < NC * 4; ++j) o[i][j] *= corr;
+                for (int j = 0; j < NC * 2; ++j) { o[i][j].x *= corr; o[i][j].y *= corr; }
             }
-            __syncwarp();
-            if (arena) {        // values some row does not see: zero times whatever they hold is kept out
+            g_wait<1>();                                   // the values (the next keys may still be on their way)
+            // Values of the arena, which some rows see and some do not: zero times whatever they hold has to be kept out where
+            // they are not finite.  Each thread looks over what it has copied.
+            bool odd = false;
+            if (arena)
+                for (int i = tid; i < KT * (DP / TreeCopied<T>::n); i += kGThreads)
+                    odd = odd || TreeCopied<T>::not_finite(&sm.v[i / (DP / TreeCopied<T>::n)][i % (DP / TreeCopied<T>::n) * TreeCopied<T>::n]);
+            odd = __syncthreads_or(odd);
+            // (the tile after the next takes this one's place among the rows)
+            if (odd) {
 #pragma unroll 1
                 for (int k = 0; k < count; ++k) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < RI; ++i) {
                         const bool see = live[i] && ((__ldg(mask[i] + ((place + k) >> 5)) >> ((place + k) & 31)) & 1u);
                         const float e = sm.p[grp + 8 * i][k];
 #pragma unroll
                         for (int cc = 0; cc < NC; ++cc) {
                             const float4 vv = *reinterpret_cast<const float4*>(&sm.v[k][cc * 64 + 4 * c]);
-                            if (see) {
-                                o[i][4 * cc + 0] = fmaf(e, vv.x, o[i][4 * cc + 0]); o[i][4 * cc + 1] = fmaf(e, vv.y, o[i][4 * cc + 1]);
-                                o[i][4 * cc + 2] = fmaf(e, vv.z, o[i][4 * cc + 2]); o[i][4 * cc + 3] = fmaf(e, vv.w, o[i][4 * cc + 3]);
-                            }
+                            if (see) { pair_fma(o[i][2 * cc], e, e, vv.x, vv.y); pair_fma(o[i][2 * cc + 1], e, e, vv.z, vv.w); }
                         }
                     }
                 }
             } else {
-#pragma unroll 4
-                for (int k = 0; k < count; ++k) {
-                    float e[4];
+#pragma unroll 2
+                for (int k = 0; k < KT; k += 4) {          // (rows that do not exist are zeros, and so are their probabilities)
+                    float4 e[RI];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = sm.p[grp + 8 * i][k];
+                    for (int i = 0; i < RI; ++i) e[i] = *reinterpret_cast<const float4*>(&sm.p[grp + 8 * i][k]);
 #pragma unroll
-                    for (int cc = 0; cc < NC; ++cc) {
-                        const float4 vv = *reinterpret_cast<const float4*>(&sm.v[k][cc * 64 + 4 * c]);
+                    for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            o[i][4 * cc + 0] = fmaf(e[i], vv.x, o[i][4 * cc + 0]); o[i][4 * cc + 1] = fmaf(e[i], vv.y, o[i][4 * cc + 1]);
-                            o[i][4 * cc + 2] = fmaf(e[i], vv.z, o[i][4 * cc + 2]); o[i][4 * cc + 3] = fmaf(e[i], vv.w, o[i][4 * cc + 3]);
+                        for (int cc = 0; cc < NC; ++cc) {
+                            const float4 vv = *reinterpret_cast<const float4*>(&sm.v[k + kk][cc * 64 + 4 * c]);
+#pragma unroll
+                            for (int i = 0; i < RI; ++i) {
+                                const float w = kk == 0 ? e[i].x : kk == 1 ? e[i].y : kk == 2 ? e[i].z : e[i].w;
+                                pair_fma(o[i][2 * cc], w, w, vv.x, vv.y); pair_fma(o[i][2 * cc + 1], w, w, vv.z, vv.w);
+                            }
                         }
-                    }
                 }
             }
-            __syncwarp();                                  // the probabilities have been read
+            find_rows(t + 2);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RI; ++i) {
             const int r = grp + 8 * i;
             if (r >= rows_here) continue;
             if (pc.whole) {
-                const int rr = pc.rb * kGRows + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
+                const int rr = pc.rb * ROWS + r, tok = rr / a.G, head = pc.h * a.G + rr - tok * a.G;
                 T* out = (T*)a.out + (int64_t)pc.b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head;
                 const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
 #pragma unroll
-                for (int cc = 0; cc < NC; ++cc)
+                for (int cc = 0; cc < NC; ++cc) {
+                    const float y[4] = {o[i][2 * cc].x, o[i][2 * cc].y, o[i][2 * cc + 1].x, o[i][2 * cc + 1].y};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int d = cc * 64 + 4 * c + j;
-                        if (d < a.D) tree_store(out + d, l[i] == 0.f ? 0.f : o[i][4 * cc + j] * inv);
+                        if (d < a.D) tree_store(out + d, l[i] == 0.f ? 0.f : y[j] * inv);
                     }
+                }
                 if (a.lse && c == 0) a.lse[((int64_t)pc.b * a.n + tok) * a.H + head] = l[i] == 0.f ? neg_inf() : (m[i] + log2f(l[i])) * 0.6931471805599453f;
             } else {
-                const int64_t at = (int64_t)(2 * blockIdx.x + pc.slot) * kGRows + r;
+                const int64_t at = (int64_t)(2 * blockIdx.x + pc.slot) * ROWS + r;
                 if (c == 0) { a.part_ml[2 * at] = m[i]; a.part_ml[2 * at + 1] = l[i]; }
 #pragma unroll
                 for (int cc = 0; cc < NC; ++cc) {
                     const int d = cc * 64 + 4 * c;
-                    if (d < a.D) *reinterpret_cast<float4*>(a.part_o + at * a.D + d) = make_float4(o[i][4 * cc], o[i][4 * cc + 1], o[i][4 * cc + 2], o[i][4 * cc + 3]);
+                    if (d < a.D) *reinterpret_cast<float4*>(a.part_o + at * a.D + d) = make_float4(o[i][2 * cc].x, o[i][2 * cc].y, o[i][2 * cc + 1].x, o[i][2 * cc + 1].y);
                 }
             }
         }
@@ -324,16 +383,25 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int RI>
 cudaError_t configure_plain() {
-    return cudaFuncSetAttribute(tree_attend_plain_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GSmem<DP>));
+    return cudaFuncSetAttribute(tree_attend_plain_kernel<T, DP, RI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GSmem<DP>));
 }
 template <typename T, int DP>
-cudaError_t launch_plain(const TreeAttend& a, int grid, cudaStream_t st) {
-    return launch_after(tree_attend_plain_kernel<T, DP>, dim3(grid), dim3(kGThreads), sizeof(GSmem<DP>), st, a);
+cudaError_t configure_plain_rows() {
+    cudaError_t e = configure_plain<T, DP, 1>();
+    if (e == cudaSuccess) e = configure_plain<T, DP, 2>();
+    if (e == cudaSuccess) e = configure_plain<T, DP, 3>();
+    return e == cudaSuccess ? configure_plain<T, DP, 4>() : e;
 }
-cudaError_t launch_fp32(const TreeAttend& a, int grid, cudaStream_t st) {
-    return a.D <= 64 ? launch_plain<float, 64>(a, grid, st) : a.D <= 128 ? launch_plain<float, 128>(a, grid, st) : launch_plain<float, 256>(a, grid, st);
+template <typename T, int DP, int RI>
+cudaError_t launch_plain(const TreeAttend& a, int grid, cudaStream_t st) {
+    return launch_after(tree_attend_plain_kernel<T, DP, RI>, dim3(grid), dim3(kGThreads), sizeof(GSmem<DP>), st, a);
+}
+template <typename T, int DP>
+cudaError_t launch_plain_rows(const TreeAttend& a, int rows, int grid, cudaStream_t st) {
+    return rows == 8 ? launch_plain<T, DP, 1>(a, grid, st) : rows == 16 ? launch_plain<T, DP, 2>(a, grid, st)
+           : rows == 24 ? launch_plain<T, DP, 3>(a, grid, st) : launch_plain<T, DP, 4>(a, grid, st);
 }
 
 }  // namespace
@@ -346,17 +414,19 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
         tree_mma_plan(M, K, D, sm_count, &p);
         return p;
     }
-    p.rows = kGRows;
+    // the fewest blocks of rows of at most 32, and of those the fewest rows
+    const int blocks = (M + kGRows - 1) / kGRows;
+    p.rows = ((M + blocks - 1) / blocks + 7) / 8 * 8;
     p.item_heads = 1;
-    p.grid = 2 * sm_count;                 // two blocks of up to 105 KB of shared memory share an SM
+    p.grid = (D <= 128 ? 3 : 2) * sm_count;         // blocks that an SM's shared memory holds (65, 75 and 88 KB each)
     return p;
 }
 
 cudaError_t configure_tree_attend() {
-    cudaError_t e = configure_plain<float, 64>();
-    if (e == cudaSuccess) e = configure_plain<float, 128>();
-    if (e == cudaSuccess) e = configure_plain<float, 256>();
-    if (e == cudaSuccess) e = configure_plain<__nv_bfloat16, 256>();
+    cudaError_t e = configure_plain_rows<float, 64>();
+    if (e == cudaSuccess) e = configure_plain_rows<float, 128>();
+    if (e == cudaSuccess) e = configure_plain_rows<float, 256>();
+    if (e == cudaSuccess) e = configure_plain_rows<__nv_bfloat16, 256>();
     if (e == cudaSuccess) e = configure_tree_mma();
     // the same division of shared memory and L1 as the kernel before, or the SMs change over between the two
     if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_combine_kernel<float>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
@@ -365,8 +435,12 @@ cudaError_t configure_tree_attend() {
 }
 
 cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
-    cudaError_t e = plan.tensor ? launch_tree_mma(a, plan.rows, plan.grid, st)
-                    : dtype == DBA_F32 ? launch_fp32(a, plan.grid, st) : launch_plain<__nv_bfloat16, 256>(a, plan.grid, st);
+    cudaError_t e;
+    if (plan.tensor) e = launch_tree_mma(a, plan.rows, plan.grid, st);
+    else if (dtype == DBA_BF16) e = launch_plain_rows<__nv_bfloat16, 256>(a, plan.rows, plan.grid, st);
+    else if (a.D <= 64) e = launch_plain_rows<float, 64>(a, plan.rows, plan.grid, st);
+    else if (a.D <= 128) e = launch_plain_rows<float, 128>(a, plan.rows, plan.grid, st);
+    else e = launch_plain_rows<float, 256>(a, plan.rows, plan.grid, st);
     if (e != cudaSuccess) return e;
     const size_t list = (size_t)plan.grid * sizeof(int32_t);
     e = dtype == DBA_F32 ? launch_after(tree_combine_kernel<float>, dim3(plan.combine), dim3(kCombineThreads), list, st, a, plan.rows, plan.grid)
