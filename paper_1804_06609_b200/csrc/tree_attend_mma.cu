@@ -29,7 +29,7 @@ namespace {
 constexpr int kMRows = 128;                 // rows of the matrix instructions (lanes of tensor memory)
 constexpr int kMKeys = 64;                  // keys of a tile
 constexpr int kLoadWarps = 2, kLoadThreads = 32 * kLoadWarps;
-constexpr int kBadSlots = 8;               // more than the tiles the loader may be ahead by
+constexpr int kSeen = 8;               // more than the tiles the loader may be ahead by
 constexpr int kItemUnits = 2;               // what an item costs beside its tiles, in tiles (see tree_device.cuh)
 constexpr uint32_t kNoRow = 0xffffffffu;
 constexpr int kPieces = 4;                  // pieces the loader may be ahead by
@@ -75,8 +75,8 @@ template <int DP, int SW, int HP> struct MSmem {
     uint64_t pv_done, o_free, told, last;
     uint64_t published[kPieces], released[kPieces];
     int4 piece[kPieces][2];                 // (in turn) what the loader tells the others of a piece
-    uint32_t seen[kBadSlots][kLoadWarps];   // places of the tile that exist (by tile, in turn)
-    uint32_t bad[kBadSlots];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
+    uint32_t seen[kSeen][kLoadWarps];   // places of the tile that exist (by tile, in turn)
+    uint32_t bad[kPieces];                // (by piece, in turn) 1 + the last piece that had a value that is not finite in an arena tile
     uint32_t tmem_base;
     int abort_flag, turn, scheduler[4];
     union {
@@ -175,6 +175,23 @@ __device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* u) {
           "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tm_ld64(uint32_t addr, uint32_t* u) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+          "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+          "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31]), "=r"(u[32]), "=r"(u[33]), "=r"(u[34]), "=r"(u[35]), "=r"(u[36]),
+          "=r"(u[37]), "=r"(u[38]), "=r"(u[39]), "=r"(u[40]), "=r"(u[41]), "=r"(u[42]), "=r"(u[43]), "=r"(u[44]), "=r"(u[45]),
+          "=r"(u[46]), "=r"(u[47]), "=r"(u[48]), "=r"(u[49]), "=r"(u[50]), "=r"(u[51]), "=r"(u[52]), "=r"(u[53]), "=r"(u[54]),
+          "=r"(u[55]), "=r"(u[56]), "=r"(u[57]), "=r"(u[58]), "=r"(u[59]), "=r"(u[60]), "=r"(u[61]), "=r"(u[62]), "=r"(u[63])
+        : "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t* u) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -259,7 +276,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), SW);
         mbar_init(msmem_u32(&sm.last), 1);
         for (int i = 0; i < kPieces; ++i) { mbar_init(msmem_u32(&sm.published[i]), 1); mbar_init(msmem_u32(&sm.released[i]), SW + 1 + C::inspectors); }
-        for (int i = 0; i < kBadSlots; ++i) sm.bad[i] = 0;
+        for (int i = 0; i < kPieces; ++i) sm.bad[i] = 0;
         sm.abort_flag = 0;
         if (SW == 1) {
             uint32_t sm_id;
@@ -389,7 +406,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                     c_in = false;
                 }
                 const uint32_t there = __ballot_sync(kFullMask, c_in);
-                if (lane == 0) sm.seen[tile_no % kBadSlots][lw] = there;
+                if (lane == 0) sm.seen[tile_no % kSeen][lw] = there;
                 whole_before = whole;
                 whole = there == 0xffffffffu && a.D == DP;       // every byte of the warp's rows is there to be copied
                 // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
@@ -496,7 +513,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                     const uint32_t sb = n_o % C::s_bufs;
                     if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
                     if (!C::inspectors && i1.x + of < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(stage), lane)) {
-                        if (lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                        if (lane == 0) sm.bad[piece % kPieces] = (uint32_t)piece + 1;
                         __syncwarp();
                     }
                     if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (n_o / C::s_bufs) & 1u, abort_flag, limit))) break;
@@ -547,7 +564,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
 #pragma unroll
                 for (int i = 0; i < C::stages; ++i) if (i == (int)s) use = uses[i]++;
                 if (!(ok = mbar_wait(msmem_u32(&sm.landed[s]), use & 1u, abort_flag, limit))) break;
-                if (look_over<C::stage_bytes>(sm.tiles + C::stage_at(s), lane) && lane == 0) sm.bad[piece % kBadSlots] = (uint32_t)piece + 1;
+                if (look_over<C::stage_bytes>(sm.tiles + C::stage_at(s), lane) && lane == 0) sm.bad[piece % kPieces] = (uint32_t)piece + 1;
                 __syncwarp();
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(msmem_u32(&sm.full[s])), "r"((uint32_t)kLoadThreads) : "memory");
             }
@@ -596,17 +613,17 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 if (!mbar_wait(msmem_u32(&sm.s_full[sb]), (g / C::s_bufs) & 1u, abort_flag, limit)) { ok = false; break; }
                 if (active) {
                     tc_after();
-                    see0 &= sm.seen[g % kBadSlots][0]; see1 &= sm.seen[g % kBadSlots][1];
+                    see0 &= sm.seen[g % kSeen][0]; see1 &= sm.seen[g % kSeen][1];
                     // 32 columns at a time; where no row of the warp sees any of them (the end of the arena or of the context), none
                     const bool half[2] = {__any_sync(kFullMask, see0 != 0) != 0, __any_sync(kFullMask, see1 != 0) != 0};
                     uint32_t u[kMKeys];
+                    tm_ld64(tmem + lanes + C::s_col + sb * kMKeys, u);
                     float m0 = neg_inf(), m1 = m0, m2 = m0, m3 = m0;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (!half[h]) continue;
                         const uint32_t see = h ? see1 : see0;
                         uint32_t* x = u + 32 * h;
-                        tm_ld32(tmem + lanes + C::s_col + sb * kMKeys + 32 * h, x);
                         if (__any_sync(kFullMask, see != 0xffffffffu)) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) if (!(see & (1u << j))) x[j] = 0xff800000u;
@@ -669,7 +686,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
             if (!mbar_wait(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             if (active) {
                 tc_after();
-                const bool bad = sm.bad[piece % kBadSlots] == (uint32_t)piece + 1;
+                const bool bad = sm.bad[piece % kPieces] == (uint32_t)piece + 1;
                 const bool whole = i1.w & 2;
                 const float inv = !(sum > 0.f) ? 0.f : whole ? __frcp_rn(sum) : 1.f;
                 const int p_h = sm.piece[piece % kPieces][0].y * HP + (HP > 1 ? warp : 0), head = p_h * a.G + rr - tok * a.G;
