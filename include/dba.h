@@ -393,7 +393,8 @@ typedef struct {
 } dba_tree_next;
 
 enum {                          /* bits of dba_tree_status */
-    DBA_TREE_TIMEOUT = 1,       /* a bounded device-side wait gave up: that call's outputs are NaN               */
+    DBA_TREE_TIMEOUT = 1,       /* a bounded device-side wait gave up: that call's outputs are NaN (short tables: those of the
+                                   items concerned)                                                              */
     DBA_TREE_BAD_PAGE = 2,      /* a page number outside the cache                                              */
     DBA_TREE_ARENA_FULL = 4,    /* dba_tree_advance found no free slot for some row                             */
     DBA_TREE_NO_ROOM = 8,       /* settled tokens do not fit the sequence's table: none was settled             */

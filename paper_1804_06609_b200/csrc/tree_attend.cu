@@ -418,6 +418,7 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
     const int blocks = (M + kGRows - 1) / kGRows;
     p.rows = ((M + blocks - 1) / blocks + 7) / 8 * 8;
     p.item_heads = 1;
+    p.tile = D <= 64 ? GSmem<64>::kt : D <= 128 ? GSmem<128>::kt : GSmem<256>::kt;
     p.grid = (D <= 128 ? 3 : 2) * sm_count;         // blocks that an SM's shared memory holds (65, 75 and 88 KB each)
     return p;
 }
@@ -434,18 +435,20 @@ cudaError_t configure_tree_attend() {
     return e;
 }
 
-cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
+cudaError_t launch_tree_attend(TreeAttend a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
     cudaError_t e;
+    a.whole_items = ((a.masks ? a.A : 0) + plan.tile - 1) / plan.tile + (a.ctx_cap + plan.tile - 1) / plan.tile <= kWholeTiles;
     if (plan.tensor) e = launch_tree_mma(a, plan.rows, plan.grid, st);
     else if (dtype == DBA_BF16) e = launch_plain_rows<__nv_bfloat16, 256>(a, plan.rows, plan.grid, st);
     else if (a.D <= 64) e = launch_plain_rows<float, 64>(a, plan.rows, plan.grid, st);
     else if (a.D <= 128) e = launch_plain_rows<float, 128>(a, plan.rows, plan.grid, st);
     else e = launch_plain_rows<float, 256>(a, plan.rows, plan.grid, st);
-    if (e != cudaSuccess) return e;
+    *launches += 1;
+    if (e != cudaSuccess || a.whole_items) return e;
     const size_t list = (size_t)plan.grid * sizeof(int32_t);
     e = dtype == DBA_F32 ? launch_after(tree_combine_kernel<float>, dim3(plan.combine), dim3(kCombineThreads), list, st, a, plan.rows, plan.grid)
                          : launch_after(tree_combine_kernel<__nv_bfloat16>, dim3(plan.combine), dim3(kCombineThreads), list, st, a, plan.rows, plan.grid);
-    *launches += 2;
+    *launches += 1;
     return e;
 }
 

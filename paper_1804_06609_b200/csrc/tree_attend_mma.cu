@@ -256,8 +256,20 @@ __device__ __forceinline__ bool look_over(unsigned char* stage, int lane) {
     return true;
 }
 
+// The outputs of an item whose block gave up.
+template <int HP>
+__device__ __noinline__ void undo_item(const TreeAttend& a, TreePiece pc, int item_rows) {
+    const int M = a.n * a.G, rows = min(item_rows, M - pc.rb * item_rows);
+    for (int i = threadIdx.x; i < HP * rows * a.D; i += blockDim.x) {
+        const int r = i / a.D, d = i - r * a.D, w = r / rows, rr = pc.rb * item_rows + r - w * rows, tok = rr / a.G;
+        const int head = (pc.h * HP + w) * a.G + rr - tok * a.G;
+        ((__nv_bfloat16*)a.out)[(int64_t)pc.b * a.o_seq + (int64_t)tok * a.o_row + (int64_t)head * a.o_head + d] = __float2bfloat16_rn(__int_as_float(0x7fc00000));
+        if (a.lse && d == 0) a.lse[((int64_t)pc.b * a.n + tok) * a.H + head] = __int_as_float(0x7fc00000);
+    }
+}
+
 template <int DP, int SW, int HP>
-__global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>::blocks_per_sm) tree_attend_mma_kernel(const TreeAttend a, const uint32_t negate) {
+__global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>::blocks_per_sm) tree_attend_mma_kernel(const __grid_constant__ TreeAttend a, const uint32_t negate) {
     using C = MConf<DP, SW, HP>;
     extern __shared__ __align__(1024) unsigned char mraw[];
     MSmem<DP, SW, HP>& sm = *reinterpret_cast<MSmem<DP, SW, HP>*>(mraw);
@@ -742,7 +754,14 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     __syncthreads();
     tc_after();
     if (warp == SW) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
-    if (tid == 0 && sm.abort_flag) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
+    if (sm.abort_flag) {
+        if (tid == 0) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
+        if (a.whole_items) {           // (else the joining kernel sees to it)
+            run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, kItemUnits, 1, &sm.run);
+            TreePiece pc;
+            while (tree_next_piece(a, run, kMKeys, groups, row_blocks, kItemUnits, false, &pc)) undo_item<HP>(a, pc, C::rows);
+        }
+    }
 }
 
 template <int DP, int SW, int HP>
@@ -761,6 +780,7 @@ bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
 // 172 against 262 us on 4 x 131071 keys of 8 heads of 64, one row each; heads of 128 lose by it, 185 against 172 us), else
 // one softmax warp.
 void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p) {
+    p->tile = kMKeys;
     p->item_heads = M <= 32 && K % 4 == 0 && D <= 64 ? 4 : 1;
     p->rows = M <= 32 && p->item_heads == 1 ? 32 : kMRows;
     p->grid = sm_count * (D > 64 ? (p->rows == 32 ? MConf<128, 1, 1>::blocks_per_sm : MConf<128, 4, 1>::blocks_per_sm)

@@ -100,7 +100,8 @@ struct TreePiece {
     int slot;                          // where a partial result goes: 0 the run's first piece, 1 a later (its last) one
     bool whole;                        // the item begins and ends in this piece
 };
-// (a run's end within an item's extra units leaves the item to the next run)
+// (a run's end within an item's extra units leaves the item to the next run; where items stay whole, a run has the items that
+// begin in it)
 __device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r, int kt, int groups, int row_blocks, int extra, bool first, TreePiece* p) {
     while (r.t < r.t_end) {
         if (r.item < 0) {              // a new sequence (the first one may be entered anywhere)
@@ -109,8 +110,14 @@ __device__ __forceinline__ bool tree_next_piece(const TreeAttend& a, TreeRun& r,
             const long long off = r.t - r.seq_t;
             r.item = off ? (int)(off / r.len) : 0;
             r.in_item = (int)(off - (long long)r.item * r.len);
+            if (a.whole_items && r.in_item > 0) {      // (only the run's first item can be one that began before)
+                r.t += r.len - r.in_item;
+                r.in_item = 0;
+                if (++r.item == groups * row_blocks) { r.item = -1; r.seq_t = r.t; ++r.b; }
+                continue;
+            }
         }
-        const int end = (int)min((long long)r.len, (long long)r.in_item + (r.t_end - r.t)), T = r.len - extra;
+        const int end = a.whole_items ? r.len : (int)min((long long)r.len, (long long)r.in_item + (r.t_end - r.t)), T = r.len - extra;
         p->b = r.b; p->top = r.top; p->ctx = r.ctx;
         p->h = row_blocks == 1 ? r.item : r.item / row_blocks; p->rb = r.item - p->h * row_blocks;
         p->tile = max(0, r.in_item - extra);

@@ -23,6 +23,10 @@ struct TreePages {
     int32_t page_shift;
 };
 
+// Items of at most so many tiles (by what a table holds) are not cut among blocks, and the kernel that joins pieces is left
+// out.  MEASURED_WHOLE
+constexpr int kWholeTiles = 8;
+
 // Attention, all sizes of one call.
 struct TreeAttend {
     TreePages pages;
@@ -42,6 +46,7 @@ struct TreeAttend {
     float* part_ml;                    // [2 * grid][rows of an item][2]: their maxima (of the scaled scores, in powers of two) and sums
     uint32_t* turns;                   // [kTreeTurns] a counter per SM, which goes on from call to call: blocks on an SM take turns by it
     int4* meta;                        // [grid] item shared with the block before this one, if that block is the first on it
+    int whole_items;                   // items are not cut (short ones: no second kernel then)
     long long wait_clocks;
     int drop_item;
     uint32_t call;                     // number of the call: what a failed wait leaves in the second status word
@@ -50,6 +55,7 @@ struct TreeAttend {
 struct TreeAttendPlan {
     int grid, combine;                 // blocks of the attention kernel and of the one that joins its pieces
     int rows, item_heads;              // rows of an item (all its key heads together), and its key heads
+    int tile;                          // keys of a tile
     bool tensor;                       // tcgen05 kernel
 };
 
@@ -61,7 +67,7 @@ bool tree_mma_usable(int dtype, int D);
 void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p);
 cudaError_t configure_tree_mma();
 cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st);
-cudaError_t launch_tree_attend(const TreeAttend& a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
+cudaError_t launch_tree_attend(TreeAttend a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
 cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K,
                                int32_t D, int dtype, cudaStream_t st, int* launches);
 cudaError_t launch_tree_commit(const dba_kv_cache& c, const TreePages& pg, int32_t B, int32_t K, int32_t D, int32_t A, int dtype,

@@ -317,6 +317,29 @@ def test_a_wait_that_runs_out_is_reported(dba, D, drop):
     assert torch.equal(t.attend(q, k, v, table, c, masks, lse=lse), want) and torch.isfinite(lse).all() and t.status() == 0
 
 
+@pytest.mark.parametrize("n,H,K,D", [(3, 4, 2, 64), (20, 8, 2, 128), (5, 8, 8, 64)])
+def test_a_wait_that_runs_out_on_short_tables(dba, n, H, K, D):
+    """Items of a few tiles stay whole and no second kernel follows: the blocks that give up undo their own items."""
+    B, ps, W = 40, 16, 1
+    rng = torch.Generator().manual_seed(14)
+    per = (32 + 150) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, "bf16")
+    masks = _masks(rng, B, n, W, 0.3, closed=0.0).cuda()
+    q = torch.randn(B, n, H, D, generator=rng).to(torch.bfloat16).cuda()
+    c = torch.full((B,), 150, dtype=torch.int32).cuda()
+    t = _tree(dba, B, n, H, K, D, ps, per, W)
+    lse = torch.zeros(B, n, H, device="cuda")
+    want = t.attend(q, k, v, table, c, masks, lse=lse).clone()
+    launches = t.launch_count()
+    assert t.status() == 0 and torch.isfinite(want.float()).all()
+    t.test_hook(wait_clocks=2_000_000, drop_item=1)
+    got = t.attend(q, k, v, table, c, masks, lse=lse)
+    assert t.launch_count() == launches + 1
+    assert t.status() == dba.TREE_TIMEOUT and torch.isnan(got.float()).all() and torch.isnan(lse).all()
+    t.test_hook()
+    assert torch.equal(t.attend(q, k, v, table, c, masks, lse=lse), want) and torch.isfinite(lse).all() and t.status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ append
 @pytest.mark.parametrize("N,H,K,D,rot,pairs,dtype,hnd,inplace", [
     (1, 1, 1, 64, 64, False, "bf16", False, False), (10, 8, 2, 128, 128, False, "bf16", False, True), (40, 8, 2, 128, 64, True, "bf16", True, False),
