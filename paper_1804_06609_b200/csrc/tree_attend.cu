@@ -408,7 +408,7 @@ cudaError_t launch_plain_rows(const TreeAttend& a, int rows, int grid, cudaStrea
 
 TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
     TreeAttendPlan p{};
-    p.combine = 2 * sm_count;
+    p.combine = 6 * sm_count;
     if (tree_mma_usable(dtype, D)) {
         p.tensor = true;
         tree_mma_plan(M, K, D, sm_count, &p);
@@ -418,7 +418,6 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
     const int blocks = (M + kGRows - 1) / kGRows;
     p.rows = ((M + blocks - 1) / blocks + 7) / 8 * 8;
     p.item_heads = 1;
-    p.tile = D <= 64 ? GSmem<64>::kt : D <= 128 ? GSmem<128>::kt : GSmem<256>::kt;
     p.grid = (D <= 128 ? 3 : 2) * sm_count;         // blocks that an SM's shared memory holds (65, 75 and 88 KB each)
     return p;
 }
@@ -435,9 +434,21 @@ cudaError_t configure_tree_attend() {
     return e;
 }
 
+// Whether items are left whole, each to one block: without pieces there is nothing to join, and no second kernel.  By the most
+// keys that a table holds, in 64: up to 5 always (one sequence of 250 tokens, 8 heads of 128: 11.2 us whole, 13.6 cut; of 440,
+// 16 heads of 64: 16.9 whole, 14.0 cut); with at least a third as many items as there are blocks, up to 8 (64 sequences of 440,
+// one row: 30.7 whole, 32.3 cut; 256 of 1200: 139 whole, 130 cut), and up to 24 where an item has more than 32 rows,
+// whose pieces are long to write and to join (64 sequences of 1100, 80 rows: 66 whole, 77 cut; of 2400: 120 whole, 116 cut).
+bool stays_whole(const TreeAttend& a, const TreeAttendPlan& plan) {
+    const int64_t most = ((a.masks ? a.A : 0) + 63) / 64 + ((int64_t)a.ctx_cap + 63) / 64;
+    const int rows = plan.rows / plan.item_heads;
+    const int64_t items = (int64_t)a.B * (a.K / plan.item_heads) * ((a.n * a.G + rows - 1) / rows);
+    return most <= 5 || (3 * items >= plan.grid && most <= (rows > 32 ? 24 : 8));
+}
+
 cudaError_t launch_tree_attend(TreeAttend a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches) {
     cudaError_t e;
-    a.whole_items = ((a.masks ? a.A : 0) + plan.tile - 1) / plan.tile + (a.ctx_cap + plan.tile - 1) / plan.tile <= kWholeTiles;
+    a.whole_items = stays_whole(a, plan);
     if (plan.tensor) e = launch_tree_mma(a, plan.rows, plan.grid, st);
     else if (dtype == DBA_BF16) e = launch_plain_rows<__nv_bfloat16, 256>(a, plan.rows, plan.grid, st);
     else if (a.D <= 64) e = launch_plain_rows<float, 64>(a, plan.rows, plan.grid, st);

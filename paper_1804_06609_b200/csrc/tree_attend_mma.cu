@@ -780,7 +780,6 @@ bool tree_mma_usable(int dtype, int D) { return dtype == DBA_BF16 && D <= 128; }
 // 172 against 262 us on 4 x 131071 keys of 8 heads of 64, one row each; heads of 128 lose by it, 185 against 172 us), else
 // one softmax warp.
 void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p) {
-    p->tile = kMKeys;
     p->item_heads = M <= 32 && K % 4 == 0 && D <= 64 ? 4 : 1;
     p->rows = M <= 32 && p->item_heads == 1 ? 32 : kMRows;
     p->grid = sm_count * (D > 64 ? (p->rows == 32 ? MConf<128, 1, 1>::blocks_per_sm : MConf<128, 4, 1>::blocks_per_sm)

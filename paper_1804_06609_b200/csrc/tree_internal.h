@@ -23,10 +23,6 @@ struct TreePages {
     int32_t page_shift;
 };
 
-// Items of at most so many tiles (by what a table holds) are not cut among blocks, and the kernel that joins pieces is left
-// out.  MEASURED_WHOLE
-constexpr int kWholeTiles = 8;
-
 // Attention, all sizes of one call.
 struct TreeAttend {
     TreePages pages;
@@ -55,7 +51,6 @@ struct TreeAttend {
 struct TreeAttendPlan {
     int grid, combine;                 // blocks of the attention kernel and of the one that joins its pieces
     int rows, item_heads;              // rows of an item (all its key heads together), and its key heads
-    int tile;                          // keys of a tile
     bool tensor;                       // tcgen05 kernel
 };
 
