@@ -9,13 +9,13 @@ namespace dba {
 
 namespace {
 
-constexpr int kVThreads = 128;
+constexpr int kVThreads = 256;
 
 struct VSmem {
     int32_t up[kTreeMaxRows];          // earlier row of this call that the row extends, or -1
     int32_t root[kTreeMaxRows];        // old row its chain starts from
     int32_t given[kTreeMaxRows];       // given as open (its chain may still close it)
-    int32_t slot[kTreeMaxRows];
+    int32_t slot[kTreeMaxRows], past[kTreeMaxRows];                // past: tokens of the row's past that hold a slot
     uint64_t chain[kTreeMaxRows];      // earlier rows of this call on the row's path
     uint32_t settled[kTreeMaxWords], used[kTreeMaxWords];
     int32_t free_before[kTreeMaxWords + 1], settled_before[kTreeMaxWords + 1];
@@ -35,6 +35,7 @@ __global__ void __launch_bounds__(kVThreads) tree_advance_kernel(const TreeAdvan
     grid_dependency_wait();
     allow_dependents();
     if (tid == 0) { sm.open = 0; sm.top = 0; }
+    for (int w = tid; w < W; w += kVThreads) { sm.used[w] = 0u; sm.settled[w] = 0xffffffffu; }
     const int ctx = __ldg(a.ctx_len + b);
     if (tid < n) {
         const int64_t at = (int64_t)b * n + tid;
@@ -56,22 +57,24 @@ __global__ void __launch_bounds__(kVThreads) tree_advance_kernel(const TreeAdvan
         sm.chain[tid] = chain;
         if (open) atomicOr((unsigned long long*)&sm.open, 1ull << tid);
         sm.slot[tid] = root;                                       // (for the moment)
+        sm.past[tid] = 0;
     }
     __syncthreads();
     const uint64_t open = sm.open;
     for (int i = tid; i < n * W; i += kVThreads) {
         const int r = i / W, w = i - r * W;
-        base[i] = (open >> r) & 1ull ? __ldg(a.masks_in + ((int64_t)b * a.rows_in + sm.slot[r]) * W + w) : 0u;
+        uint32_t x = 0u;
+        if ((open >> r) & 1ull) {
+            x = __ldg(a.masks_in + ((int64_t)b * a.rows_in + sm.slot[r]) * W + w);
+            if (x) { atomicOr(&sm.used[w], x); atomicAdd(&sm.past[r], __popc(x)); }
+            if (~x) atomicAnd(&sm.settled[w], x);
+        }
+        base[i] = x;
     }
     __syncthreads();
     for (int w = tid; w < W; w += kVThreads) {
-        uint32_t any = 0, all = open ? 0xffffffffu : 0u;
-        for (int r = 0; r < n; ++r) {
-            any |= base[r * W + w];
-            if ((open >> r) & 1ull) all &= base[r * W + w];
-        }
-        sm.used[w] = any; sm.settled[w] = all;
-        sm.free_before[w + 1] = 32 - __popc(any); sm.settled_before[w + 1] = __popc(all);
+        if (!open) sm.settled[w] = 0u;
+        sm.free_before[w + 1] = 32 - __popc(sm.used[w]); sm.settled_before[w + 1] = __popc(sm.settled[w]);
     }
     __syncthreads();
     if (tid < 32) {        // prefix sums over at most 128 words: four to a lane
@@ -117,8 +120,7 @@ __global__ void __launch_bounds__(kVThreads) tree_advance_kernel(const TreeAdvan
                 for (int left = j - sm.free_before[w]; left > 0; --left) z &= z - 1u;
                 slot = 32 * w + __ffs(z) - 1;
             } else atomicOr(a.status, (uint32_t)DBA_TREE_ARENA_FULL);
-            pos = ctx + __popcll(sm.chain[tid]);
-            for (int w = 0; w < W; ++w) pos += __popc(base[tid * W + w]);
+            pos = ctx + sm.past[tid] + __popcll(sm.chain[tid]);
             if (slot >= 0) a.slot_pos[(int64_t)b * a.slot_pos_stride + slot] = pos;
         }
         sm.slot[tid] = slot;
@@ -126,12 +128,13 @@ __global__ void __launch_bounds__(kVThreads) tree_advance_kernel(const TreeAdvan
         if (a.next.slot) a.next.slot[at] = slot;
         if (a.next.position) a.next.position[at] = pos;
     }
-    if (count > 0)
-        for (int w = tid; w < W; w += kVThreads) {
-            int i = sm.settled_before[w];
-            for (uint32_t x = sm.settled[w]; x; x &= x - 1u, ++i) {
-                const int s = 32 * w + __ffs(x) - 1;
-                list_slot[i] = s; list_pos[i] = a.slot_pos[(int64_t)b * a.slot_pos_stride + s];
+    if (count > 0)         // (a thread per slot: the loads of the positions do not wait for one another)
+#pragma unroll 4
+        for (int i = tid; i < A; i += kVThreads) {
+            const uint32_t x = sm.settled[i >> 5], bit = 1u << (i & 31);
+            if (x & bit) {
+                const int at = sm.settled_before[i >> 5] + __popc(x & (bit - 1u));
+                list_slot[at] = i; list_pos[at] = a.slot_pos[(int64_t)b * a.slot_pos_stride + i];
             }
         }
     __syncthreads();

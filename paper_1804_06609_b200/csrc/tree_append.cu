@@ -8,7 +8,7 @@ namespace dba {
 
 namespace {
 
-constexpr int kAThreads = 128;
+constexpr int kAThreads = 128, kCThreads = 256, kCopies = 4;
 
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) TreePack { T x[VEC]; };
 __device__ __forceinline__ float tree_widen(float x) { return x; }
@@ -43,8 +43,8 @@ __global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_t
     const float* cosr = t.cos + (int64_t)(pos < 0 ? 0 : pos) * half;
     const float* sinr = t.sin + (int64_t)(pos < 0 ? 0 : pos) * half;
     const int q_heads = t.q ? H : 0, heads = q_heads + 2 * K;
-#pragma unroll 2
-    for (int u = threadIdx.x; u < heads * per; u += kAThreads) {
+#pragma unroll 1
+    for (int u = threadIdx.x; u < heads * per; u += blockDim.x) {
         const int hd = u / per, j = u - hd * per;
         const T* src; T* dst;
         if (hd < q_heads) {
@@ -83,33 +83,59 @@ __global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_t
     }
 }
 
-// A block per (sequence, layer, keys or values); 16 bytes per thread and turn.
-__global__ void __launch_bounds__(128) tree_commit_kernel(const TreePages pg, char* ck, char* cv, int64_t layer_bytes, int es, int K,
+// A block per (sequence, layer, keys or values).  The places of up to kCThreads tokens are looked up first, one to a thread,
+// so that the chain of loads to a place (slot, page) is gone through once and not for every 16 bytes; then a thread has
+// kCopies copies of 16 bytes in the air.
+__global__ void __launch_bounds__(kCThreads) tree_commit_kernel(const TreePages pg, char* ck, char* cv, int64_t layer_bytes, int es, int K,
                                                           int head_chunks, int A, const int32_t* ctx_len, const int32_t* src, const int32_t* n) {
+    __shared__ int64_t from_at[kCThreads], to_at[kCThreads];
     grid_dependency_wait();
     allow_dependents();
-    const int b = blockIdx.x;
+    const int b = blockIdx.x, tid = threadIdx.x;
     const int count = min(max(__ldg(n + b), 0), A), ctx = __ldg(ctx_len + b);
     char* base = ((blockIdx.y & 1) ? cv : ck) + (int64_t)(blockIdx.y >> 1) * layer_bytes;
     const int per = K * head_chunks;
-#pragma unroll 2
-    for (int u = threadIdx.x; u < count * per; u += 128) {
-        const int i = u / per, w = u - i * per, h = w / head_chunks, ch = w - h * head_chunks;
-        const int from = __ldg(src + (int64_t)b * A + i), to = A + ctx - count + i;
-        const int64_t r0 = (unsigned)from < (unsigned)A ? tree_row(pg, b, from) : -1, r1 = to >= A ? tree_row(pg, b, to) : -1;
-        if (r0 < 0 || r1 < 0) {
-            if (w == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
-            continue;
+    for (int t0 = 0; t0 < count; t0 += kCThreads) {
+        const int tokens = min(kCThreads, count - t0), units = tokens * per;
+        if (t0) __syncthreads();
+        if (tid < tokens) {
+            const int from = __ldg(src + (int64_t)b * A + t0 + tid), to = A + ctx - count + t0 + tid;
+            const int64_t r0 = (unsigned)from < (unsigned)A ? tree_row(pg, b, from) : -1, r1 = to >= A ? tree_row(pg, b, to) : -1;
+            const bool bad = r0 < 0 || r1 < 0;
+            if (bad) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
+            from_at[tid] = bad ? -1 : r0 * es; to_at[tid] = r1 * es;
         }
-        const int64_t in_head = (int64_t)h * pg.head_stride * es + ch * 16;
-        *reinterpret_cast<uint4*>(base + r1 * es + in_head) = *reinterpret_cast<const uint4*>(base + r0 * es + in_head);
+        __syncthreads();
+        for (int first = tid; first < units; first += kCopies * kCThreads) {
+            uint4 x[kCopies];
+            char* to[kCopies];
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c) {
+                const int u = first + c * kCThreads;
+                to[c] = nullptr;
+                if (u < units) {
+                    const int i = u / per, w = u - i * per, h = w / head_chunks, ch = w - h * head_chunks;
+                    const int64_t in_head = (int64_t)h * pg.head_stride * es + ch * 16, at = from_at[i];
+                    if (at >= 0) {
+                        x[c] = *reinterpret_cast<const uint4*>(base + at + in_head);
+                        to[c] = base + to_at[i] + in_head;
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c)
+                if (to[c]) *reinterpret_cast<uint4*>(to[c]) = x[c];
+        }
     }
 }
 
 template <typename T, int VEC>
 cudaError_t launch_append_v(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, cudaStream_t st) {
-    return t.pairs ? launch_after(tree_append_kernel<T, VEC, true>, dim3(t.N), dim3(kAThreads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D)
-                   : launch_after(tree_append_kernel<T, VEC, false>, dim3(t.N), dim3(kAThreads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D);
+    // Blocks of 64 threads once their number fills the machine several times over (8 x 2039 tokens of 48 heads of 128: 65.0
+    // us, 128 threads 67.5, 256 81), of 128 before, where a block's own loop is what takes time (16 x 20 tokens: 4.8, 3.8, 3.6).
+    const int threads = t.N >= 2048 ? 64 : kAThreads;
+    return t.pairs ? launch_after(tree_append_kernel<T, VEC, true>, dim3(t.N), dim3(threads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D)
+                   : launch_after(tree_append_kernel<T, VEC, false>, dim3(t.N), dim3(threads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D);
 }
 
 }  // namespace
@@ -135,7 +161,7 @@ cudaError_t launch_tree_commit(const dba_kv_cache& c, const TreePages& pg, int32
                                const int32_t* ctx_len, const int32_t* src, const int32_t* n, cudaStream_t st, int* launches) {
     *launches += 1;
     const int es = dtype == DBA_F32 ? 4 : 2;
-    return launch_after(tree_commit_kernel, dim3(B, 2 * c.layers), dim3(128), 0, st, pg, (char*)c.k, (char*)c.v, c.layer_stride * es, es, K,
+    return launch_after(tree_commit_kernel, dim3(B, 2 * c.layers), dim3(kCThreads), 0, st, pg, (char*)c.k, (char*)c.v, c.layer_stride * es, es, K,
                         D * es / 16, A, ctx_len, src, n);
 }
 
