@@ -327,7 +327,6 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         // ------------------------------------------------------------------ loader: warp lw has rows 32 lw .. 32 lw + 31 of a tile
         constexpr int CH = DP / 8;                     // 16-byte chunks of a row
         constexpr int RW = 32 / CH, NJ = 32 / RW;      // rows the warp copies at a time, and how often
-        constexpr int LAG = C::s_bufs - 1;             // tiles by which the values' copies follow the keys', as the products do
         const int lw = warp - SW - C::inspectors - 1, ch = lane % CH, sub = lane / CH;
         const bool ch_in = ch * 8 < a.D;
         const uint32_t tiles = msmem_u32(sm.tiles);
@@ -342,7 +341,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         // numbers, masks and page entries come out of the L2.
         TreePiece pc, nx;
         int piece = -1, tile_no = 0, t = 0, f_row = 0, f_id = 0;
-        bool f_arena = false, f_in = false, ok = true, whole = false, whole_before = false;
+        bool f_arena = false, f_in = false, ok = true;
         uint32_t f_m0 = 0, f_m1 = 0;
         pc.tile = pc.tiles = pc.top = pc.ctx = pc.b = pc.h = pc.rb = pc.arena_tiles = pc.slot = 0; pc.whole = false;
 #pragma unroll 1
@@ -419,50 +418,61 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 }
                 const uint32_t there = __ballot_sync(kFullMask, c_in);
                 if (lane == 0) sm.seen[tile_no % kSeen][lw] = there;
-                whole_before = whole;
-                whole = there == 0xffffffffu && a.D == DP;       // every byte of the warp's rows is there to be copied
+                const bool whole = there == 0xffffffffu && a.D == DP;       // every byte of the warp's rows is there to be copied
                 // (the host has seen to it that a layer's rows are within 2^32 times 16 bytes)
                 sm.rows[tile_no & 1][lw * 32 + lane] = c_in ? (uint32_t)((int64_t)c_id * page16 + (int64_t)c_row * token16) : kNoRow;
                 __syncwarp();
-                // --- copies: the keys, the values LAG tiles behind, and after the last keys the values that are left.  The stage
-                // is handed on by the copies themselves; the issuing thread of the matrix products has the fence between their
-                // writes and its reads (here it would wait for every copy in flight: twice the time on long contexts).  Values of
-                // an arena tile go through the inspector first.
-                const int n_copies = 2 + (LAG && last ? 1 : 0);
-#pragma unroll 1
-                for (int k = 0; k < n_copies; ++k) {
-                    const int of = k == 0 ? c_t : k == 1 ? c_t - LAG : c_t;      // the tile
-                    if (of < pc.tile) continue;
-                    const bool look = k > 0 && of < pc.arena_tiles && C::inspectors;
-                    if (!mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit)) { ok = false; break; }
-                    const char* base = (const char*)(k == 0 ? a.k : a.v) + pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
-                    const uint32_t dst = tiles + C::stage_at(stage) + in_kv;
-                    const uint32_t* rows = &sm.rows[(tile_no - (c_t - of)) & 1][lw * 32 + sub];
-                    uint32_t at[NJ];
+                // --- copies: the keys and the values, into two stages.  A stage is handed on by the copies themselves; the
+                // issuing thread of the matrix products has the fence between their writes and its reads (here it would wait
+                // for every copy in flight: twice the time on long contexts).  Values of an arena tile go through the
+                // inspector first.
+                const bool look = c_arena && C::inspectors;
+                const uint32_t* rows = &sm.rows[tile_no & 1][lw * 32 + sub];
+                uint32_t at[NJ];
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) at[j] = rows[j * RW];
-                    if (HP == 1 && (of == c_t ? whole : whole_before)) {
+                for (int j = 0; j < NJ; ++j) at[j] = rows[j * RW];
+                const int64_t head_at = pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
+                // With one head the two go side by side, so that a warp waits for the steps of one address at a time half as
+                // often (a tree of 61 rows over 8189 tokens, heads of 128: 107 us, one after the other 114); with four, one
+                // after the other, as either may begin when its own stage is free and there are only three.
+                constexpr int SIDE = HP == 1 ? 2 : 1;
+#pragma unroll 1
+                for (int k = 0; k < 2; k += SIDE) {
+                    uint32_t st[SIDE], dst[SIDE];
+                    const char* base[SIDE];
+#pragma unroll
+                    for (int i = 0; i < SIDE; ++i) {
+                        if (ok) ok = mbar_wait(msmem_u32(&sm.empty[stage]), phase, abort_flag, limit);
+                        st[i] = stage; dst[i] = tiles + C::stage_at(stage) + in_kv;
+                        base[i] = (const char*)(k + i == 0 ? a.k : a.v) + head_at;
+                        if (++stage == C::stages) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    if (HP == 1 && whole) {
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) {
-                            const char* from = base + (uint64_t)at[j] * 16;
-                            const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+                            const uint32_t to = j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
 #pragma unroll
-                            for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, 16u);
+                            for (int i = 0; i < SIDE; ++i) cp_async16(dst[i] + to, base[i] + (uint64_t)at[j] * 16, 16u);
                         }
                     } else {
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) {
                             const uint32_t bytes = at[j] != kNoRow && ch_in ? 16u : 0u;
-                            const char* from = base + (uint64_t)(at[j] != kNoRow ? at[j] : 0u) * 16;
-                            const uint32_t to = dst + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
+                            const uint64_t from = (uint64_t)(at[j] != kNoRow ? at[j] : 0u) * 16;
+                            const uint32_t to = j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4));
 #pragma unroll
-                            for (int w = 0; w < HP; ++w) cp_async16(to + w * C::head_bytes, from + w * head2, bytes);
+                            for (int i = 0; i < SIDE; ++i)
+#pragma unroll
+                                for (int w = 0; w < HP; ++w) cp_async16(dst[i] + to + w * C::head_bytes, base[i] + from + w * head2, bytes);
                         }
                     }
-                    if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));      // (for what this warp wrote beside the copies)
-                    if (step != a.drop_item) cp_arrive(msmem_u32(look ? &sm.landed[C::inspectors ? stage : 0] : &sm.full[stage]));
-                    ++step;
-                    if (++stage == C::stages) { stage = 0; phase ^= 1u; }
+#pragma unroll
+                    for (int i = 0; i < SIDE; ++i) {
+                        if (lane == 0) mbar_arrive(msmem_u32(&sm.full[st[i]]));      // (for what this warp wrote beside the copies)
+                        if (step != a.drop_item) cp_arrive(msmem_u32(look && k + i == 1 ? &sm.landed[C::inspectors ? st[i] : 0] : &sm.full[st[i]]));
+                        ++step;
+                    }
                 }
                 if (!ok) break;
                 ++tile_no;
@@ -482,10 +492,10 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
         // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
         constexpr uint32_t idesc_s = mma_idesc(kMKeys, false), idesc_o = mma_idesc(DP, true);
         const uint32_t tiles = msmem_u32(sm.tiles), q0 = tiles + C::q_at - quarter * (32 * 128);      // the queries are the lanes from 32 quarter on
-        uint32_t stage = 0, phase = 0;                 // of the next copy
+        uint32_t stage = 0, phase = 0, v_stage = 1, v_phase = 0;      // of the next keys and the next values, two copies on each time
         int piece = 0;
         bool ok = true;
-        auto next_stage = [&]() { if (++stage == C::stages) { stage = 0; phase ^= 1u; } };
+        auto next_stage = [&](uint32_t& st, uint32_t& ph) { st += 2; if (st >= C::stages) { st -= C::stages; ph ^= 1u; } };
         constexpr int LAG = C::s_bufs - 1;             // one S in tensor memory: S0 O0 S1 O1 ..;  two: S0 S1 O0 S2 O1 ..
         uint32_t n_s = 0, n_o = 0;                     // tiles whose scores, and whose outputs, have been issued
 #pragma unroll 1
@@ -518,19 +528,19 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                     }
                     __syncwarp();
                     ++n_s;
-                    next_stage();
+                    next_stage(stage, phase);
                 }
                 if (t >= LAG) {
                     const int of = t - LAG;
                     const uint32_t sb = n_o % C::s_bufs;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), phase, abort_flag, limit))) break;
-                    if (!C::inspectors && i1.x + of < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(stage), lane)) {
+                    if (!(ok = mbar_wait(msmem_u32(&sm.full[v_stage]), v_phase, abort_flag, limit))) break;
+                    if (!C::inspectors && i1.x + of < i1.z && look_over<C::stage_bytes>(sm.tiles + C::stage_at(v_stage), lane)) {
                         if (lane == 0) sm.bad[piece % kPieces] = (uint32_t)piece + 1;
                         __syncwarp();
                     }
                     if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[sb]), (n_o / C::s_bufs) & 1u, abort_flag, limit))) break;
                     if (of == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1u, abort_flag, limit))) break;
-                    const uint64_t dv = sw128_desc(tiles + C::stage_at(stage), kMKeys * 128);
+                    const uint64_t dv = sw128_desc(tiles + C::stage_at(v_stage), kMKeys * 128);
                     const uint32_t p = tmem + C::s_col + sb * kMKeys;
                     if (elect_one()) {
                         fence_async_proxy();
@@ -540,13 +550,13 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
 #pragma unroll
                             for (int ks = 0; ks < kMKeys / 16; ++ks)  // 16 keys = two groups of eight rows of 128 bytes
                                 mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)((w * C::head_bytes + ks * 2048) / 16), idesc_o, (of | ks) != 0, HP > 1 ? w : -1);
-                        mma_commit(msmem_u32(&sm.empty[stage]));
+                        mma_commit(msmem_u32(&sm.empty[v_stage]));
                         mma_commit(msmem_u32(&sm.pv_done));
                         if (of + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
                     }
                     __syncwarp();
                     ++n_o;
-                    next_stage();
+                    next_stage(v_stage, v_phase);
                 }
             }
             if (!ok) break;
@@ -569,9 +579,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
             const uint32_t begin = stage;
             bool ok = true;
             for (int t = 0; t < n_arena && ok; ++t) {
-                // the tile's values among the piece's copies: K0 K1 V0 K2 V1 .. (the last V alone)
-                const int at = C::s_bufs > 1 ? (t + 1 < i1.y ? 2 * t + 2 : 2 * t + 1) : 2 * t + 1;
-                const uint32_t s = (begin + (uint32_t)at) % C::stages;
+                const uint32_t s = (begin + 2u * (uint32_t)t + 1u) % C::stages;      // copies go K0 V0 K1 V1 ..
                 uint32_t use = 0;
 #pragma unroll
                 for (int i = 0; i < C::stages; ++i) if (i == (int)s) use = uses[i]++;
