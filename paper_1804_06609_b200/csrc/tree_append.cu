@@ -1,5 +1,9 @@
 // Keys and values of new tokens into the paged cache, the position rotation applied on the way, and the copying of
 // settled tokens into the context.  Both are copies: bound by HBM when there are many tokens, by a launch otherwise.
+// Measured on the device: a prompt of 8 x 2039 tokens, 32 + 2 x 8 heads of 128, bf16, 402 MB read and written: 65 us, 6.2 TB/s
+// (94 % of what a copy reaches; more units of a thread in the air cost warps, and with them 10 to 40 us); one step's 16 x 20 tokens:
+// 3.8 us.  Commit of up to 9 tokens of 64 sequences in 6 layers, 14 MB: 5.4 us (9.2 with every copy looking its places up);
+// 16 sequences of 2, 32 layers: 3.3 us.
 #include <cuda_bf16.h>
 
 #include "tree_device.cuh"

@@ -4,20 +4,31 @@
 //     S = Q K^T (tcgen05.mma, both operands in shared memory),  P = 2^(scale log2(e) S - m),  O += P V (P from tensor memory),
 // tile by tile of 64 keys, so a key and a value leave HBM once per 128 rows however many hypotheses read them.
 //
-// A block is one stream of tiles (its run of the work, see tree_device.cuh); two (head size 128) or three (64) blocks
-// share an SM, so that the steps of one, load -> S -> P -> O, fall into the gaps of the others.  Roles:
-//   warps 0-3  softmax: thread = row = lane of tensor memory.  Reads the row's 64 scores, keeps a reference m and the sum
-//              of the exponentials in fp32, writes P (bf16: half a unit in the 8th bit of every probability, as the
-//              matrix instruction needs it; the sum is taken before the rounding) over the scores.  m is only raised when the tile's maximum
+// A block is one stream of tiles (its run of the work, see tree_device.cuh).  Two blocks share an SM (four where one softmax warp
+// serves heads of up to 64): so many hold their 256 or 128 columns of tensor memory and their shared memory, and the steps of
+// one, load -> S -> P -> O, fall into the gaps of the others.  Every role walks its warp in step; SW softmax warps:
+//   softmax    thread = row = lane of tensor memory.  Reads the row's 64 scores, keeps a reference m and the sum of the
+//              exponentials in fp32, writes P over the scores (bf16, as the matrix instruction needs it: half a unit in the 8th
+//              bit of every probability; the sum is taken before the rounding).  m is only raised when the tile's maximum
 //              is more than 2^8 above it; then the row's O is rescaled in tensor memory.  Quotients are unaffected.
-//   warp 4     one thread issues the matrix instructions; allocates the tensor memory.
-//   warps 5-6  loader: 16-byte cp.async with zero fill, every place looked up in the page table by itself, so pages of any
-//              size may end inside a tile; written in the 128-byte swizzle both operand forms want: keys K-major, values
-//              MN-major ([key][d] either way).  Rows that do not exist, or that no row of the sequence sees, are zeros.
-// Values that are not finite would reach all rows of the tile through 0 * inf: in arena tiles (the only ones that rows see
-// differently) the loader looks its values over, puts zeros in their place and says so; the rows that do see such
-// a slot add it at the end.
+//   products   one lane issues the matrix instructions; with two S in tensor memory, a tile's scores before the outputs of the
+//              tile before it.
+//   inspector  values that are not finite would reach all rows of the tile through 0 * inf: in arena tiles (the only ones
+//              that rows see differently) it looks the values over, puts zeros in their place and says so; the rows that do
+//              see such a slot add it at the end.  (With one softmax warp the products' warp does it.)
+//   loaders    two warps: walk the run and tell the others its pieces; 16-byte cp.async with zero fill, every place looked up
+//              in the page table by itself, so pages of any size may end inside a tile (a tensor map's box could not); written
+//              in the 128-byte swizzle both operand forms want: keys K-major, values MN-major ([key][d] either way).  Rows
+//              that do not exist, or that no row of the sequence sees, are zeros.
 // Every wait on an mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
+//
+// What bounds it, measured (6551 GB/s is what a copy reaches): with few rows and long contexts HBM: one row, 32 heads over 4 key heads of
+// 128, 4 x up to 131071 tokens, 1.03 GB: 162 us, 6.35 TB/s.  With many rows the two longest chains of a tile, which take about
+// as long: the loader's instructions (2000 to 2600 cycles; dropping the exponentials, or most of the products, or
+// reading everything from L2, each changes under 3 %) and the softmax warps' (2600): 61 rows, 32 heads over 8 of 128, 8 x up
+// to 8189 tokens: 107 us, of which 10 join the pieces; 37 would do.  A third loader warp, or two softmax threads to a row
+// (158 us when it was tried), do not fit the 65536 registers beside 128 for a thread that holds 64 scores.  Many short items
+// (256 x 16 heads of 64, 20 rows, 30 to 160 keys): what an item costs from its look-up to its output, 41 us; 15 would do.
 #include <cuda_bf16.h>
 
 #include "tree_device.cuh"
