@@ -259,7 +259,7 @@ def _plain_commit(s):
     i = torch.arange(s["most"], device=src.device)
     live = i < count[:, None]
     a = _rows_of(s["table"], src[:, :s["most"]].clamp(min=0).long(), page)[live]
-    b = _rows_of(s["table"], (A + s["ctx_len"] - count)[:, None] + i * live, page)[live]
+    b = _rows_of(s["table"], ((A + s["ctx_len"] - count)[:, None] + i) * live, page)[live]
     s["k"][:, b // page, b % page] = s["k"][:, a // page, a % page]
     s["v"][:, b // page, b % page] = s["v"][:, a // page, a % page]
     return s["k"], s["v"]
