@@ -17,6 +17,8 @@
 // blocks an SM, and plain instead of paired products, were no faster.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "tree_device.cuh"
 
 namespace dba {
@@ -174,21 +176,28 @@ __global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plai
             for (int i = 0; i < RI; ++i)
 #pragma unroll
                 for (int j = 0; j < NK; ++j) s[i][j] = make_float2(0.f, 0.f);
+            // A tile's keys are its first `count`: of 16 or fewer, the first of each thread's alone (121 sequences of 3 tokens and 27
+            // slots, 27 rows, 14 heads over 2 of 64: 84 us, 100 with all products; full tiles as before).
+            const auto products = [&](auto keys) {
 #pragma unroll 4
-            for (int d = 0; d < DP; d += 4) {
-                float4 qv[RI];
+                for (int d = 0; d < DP; d += 4) {
+                    float4 qv[RI];
 #pragma unroll
-                for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[grp + 8 * i][d]);
+                    for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[grp + 8 * i][d]);
 #pragma unroll
-                for (int j = 0; j < NK; ++j) {
-                    const float4 kv = *reinterpret_cast<const float4*>(&sm.k[t & 1][c + 16 * j][d]);
+                    for (int j = 0; j < decltype(keys)::value; ++j) {
+                        const float4 kv = *reinterpret_cast<const float4*>(&sm.k[t & 1][c + 16 * j][d]);
 #pragma unroll
-                    for (int i = 0; i < RI; ++i) {
-                        pair_fma(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
-                        pair_fma(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
+                        for (int i = 0; i < RI; ++i) {
+                            pair_fma(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
+                            pair_fma(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
+                        }
                     }
                 }
-            }
+            };
+            if (NK > 1 && count <= 16) products(std::integral_constant<int, 1>{});
+            else if (NK > 2 && count <= 32) products(std::integral_constant<int, 2>{});
+            else products(std::integral_constant<int, NK>{});
 #pragma unroll
             for (int i = 0; i < RI; ++i) {
                 float x[NK], top = neg_inf();
@@ -244,7 +253,7 @@ __global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plai
                 }
             } else {
 #pragma unroll 2
-                for (int k = 0; k < KT; k += 4) {          // (rows that do not exist are zeros, and so are their probabilities)
+                for (int k = 0; k < count; k += 4) {       // (rows that do not exist are zeros, and so are their probabilities)
                     float4 e[RI];
 #pragma unroll
                     for (int i = 0; i < RI; ++i) e[i] = *reinterpret_cast<const float4*>(&sm.p[grp + 8 * i][k]);
