@@ -292,11 +292,13 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     if (tid == 0) {
         for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kLoadThreads + kLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); if (C::inspectors) mbar_init(msmem_u32(&sm.landed[s]), kLoadThreads); }
         // (s_full counts the product and, beside it, an arrival of the issuing thread, which passes on what the loader wrote
-        // before it; `told` does that once a piece for its values.  pv_done counts products alone: the issuing thread
-        // may be a product ahead of it)
+        // before it; `told` does that once a piece for its values, and its product is the piece's last, so all its outputs are
+        // there.  pv_done, a phase to a tile, does not show that: the last two outputs may be issued together, and a wait for
+        // a phase's parity passes while the phase before it is still open.  It serves rows that raise their reference, whose
+        // tile's scores came after the outputs of two tiles before)
         for (int s = 0; s < C::s_bufs; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s]), SW); }
         for (int s = 0; s < C::q_bufs; ++s) mbar_init(msmem_u32(&sm.q_empty[s]), 1);
-        mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 1); mbar_init(msmem_u32(&sm.o_free), SW);
+        mbar_init(msmem_u32(&sm.pv_done), 1); mbar_init(msmem_u32(&sm.told), 2); mbar_init(msmem_u32(&sm.o_free), SW);
         mbar_init(msmem_u32(&sm.last), 1);
         for (int i = 0; i < kPieces; ++i) { mbar_init(msmem_u32(&sm.published[i]), 1); mbar_init(msmem_u32(&sm.released[i]), SW + 1 + C::inspectors); }
         for (int i = 0; i < kPieces; ++i) sm.bad[i] = 0;
@@ -563,7 +565,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                                 mma_ts(tmem + C::o_col, p + ks * 8, dv + (uint64_t)((w * C::head_bytes + ks * 2048) / 16), idesc_o, (of | ks) != 0, HP > 1 ? w : -1);
                         mma_commit(msmem_u32(&sm.empty[v_stage]));
                         mma_commit(msmem_u32(&sm.pv_done));
-                        if (of + 1 == n_tiles) mbar_arrive(msmem_u32(&sm.told));
+                        if (of + 1 == n_tiles) { mma_commit(msmem_u32(&sm.told)); mbar_arrive(msmem_u32(&sm.told)); }
                     }
                     __syncwarp();
                     ++n_o;
@@ -714,7 +716,6 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
             }
             if (!ok) break;
             if (!mbar_wait(msmem_u32(&sm.told), piece & 1, abort_flag, limit)) { ok = false; break; }
-            if (!mbar_wait(msmem_u32(&sm.pv_done), (g - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             if (active) {
                 tc_after();
                 const bool bad = sm.bad[piece % kPieces] == (uint32_t)piece + 1;

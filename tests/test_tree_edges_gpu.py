@@ -1,0 +1,46 @@
+"""The token tree's branches that ordinary calls seldom reach, against the plain 64-bit models (tests/tree_model.py)."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from tests import tree_model as M                                     # noqa: E402
+from tests.test_tree_gpu import DT, _cache, _check, _masks, _top, _tree  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def dba():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_1804_06609_b200 as pkg
+    pkg.lib()
+    return pkg
+
+
+@pytest.mark.parametrize("n,H,K,D", [(5, 8, 8, 64), (40, 8, 8, 64), (20, 32, 8, 128), (4, 8, 4, 128), (4, 4, 2, 64)])
+@pytest.mark.parametrize("W", [3, 8])
+def test_items_that_end_in_arena_tiles_have_all_their_outputs(dba, n, H, K, D, W):
+    """Without a context an item's last tiles are of the arena, whose values are looked over before their products: the last
+    two products of an item follow each other at once, and its output must wait for both.  Every SM is kept busy
+    by sequences that repeat three, so that each is compared with the model."""
+    B, kinds, ps = 240, 3, 16
+    rng = torch.Generator().manual_seed(20 + n + W)
+    per = 2 * W + 1
+    k, v, table = _cache(rng, kinds, per, ps, K, D, "bf16")
+    masks = _masks(rng, kinds, n, W, 0.4, closed=0.0)
+    q = torch.randn(kinds, n, H, D, generator=rng).to(torch.bfloat16)
+    c = torch.zeros(kinds, dtype=torch.int32)
+    want = M.attend(q, k, v, table, c, masks, D ** -0.5, ps, W, k.shape[0])
+    t = _tree(dba, B, n, H, K, D, ps, per, W)
+    many = lambda x: x.repeat(*([B // kinds] + [1] * (x.dim() - 1))).cuda()  # noqa: E731
+    args = (many(q), k, v, many(table), many(c), many(masks))
+    first = t.attend(*args).clone()
+    _check(first[:kinds], None, want, D, 32 * W, "bf16")
+    assert torch.equal(first, first[:kinds].repeat(B // kinds, 1, 1, 1))
+    for _ in range(40):
+        assert torch.equal(t.attend(*args), first)
+    assert t.status() == 0
