@@ -16,7 +16,6 @@ struct dba_tree {
     float *part_ml, *part_o;
     long long wait_clocks;
     int drop_item;
-    uint32_t calls;                // of the attention
     uint64_t launches;
 };
 
@@ -178,8 +177,6 @@ dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* q, const dba_kv_ca
     if (a.scale_log2e == 0.f) a.scale_log2e = 1e-37f;         // all scores alike; the kernels multiply -inf by it
     a.part_o = h->part_o; a.part_ml = h->part_ml; a.meta = h->meta; a.turns = h->turns;
     a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
-    if (++h->calls == 0) h->calls = 1;         // (0: no call has failed)
-    a.call = h->calls;
     int n = 0;
     // (planned for the configuration's rows: the workspace was sized for that)
     const TreeAttendPlan plan = plan_tree_attend(c.dtype, c.rows * a.G, c.kv_heads, c.head_dim, h->sm_count);

@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plai
 // Finishes the items that several blocks worked on.  Block c of the attention names in meta[c] the item it shares with block
 // c - 1 if that one was the item's first: those are the items there are.  Every block here lists them and takes every
 // gridDim-th row of theirs: a warp per row where few pieces meet, all eight warps on a row (each an eighth of its pieces)
-// where many do.  Pieces are added in a fixed order, so equal inputs give equal bits.
+// where many do.  Pieces are added in a fixed order, so equal inputs give equal bits.  A block that gave up says so in its entry, which
+// every launch writes anew: a call that is recorded once and run often (a graph) keeps no failure from one run to the next.
 constexpr int kCombineThreads = 256, kCombineWarps = 8, kCombineMany = 8;
 
 template <typename T>
@@ -317,17 +318,9 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     grid_dependency_wait();
     allow_dependents();
-    if (a.pages.status[1] == a.call) {       // a wait of this call ran out: nothing it wrote can be trusted
-        const int64_t rows = (int64_t)a.B * a.n * a.H;
-        for (int64_t i = (int64_t)blockIdx.x * kCombineThreads + tid; i < rows * a.D; i += (int64_t)gridDim.x * kCombineThreads) {
-            const int64_t r = i / a.D, tok = r / a.H, b = tok / a.n;
-            tree_store((T*)a.out + b * a.o_seq + (tok - b * a.n) * a.o_row + (r - tok * a.H) * a.o_head + (i - r * a.D), __int_as_float(0x7fc00000));
-            if (a.lse && i == r * a.D) a.lse[r] = __int_as_float(0x7fc00000);
-        }
-        return;
-    }
     const int M = a.n * a.G, head_rows = item_rows / a.item_heads, row_blocks = (M + head_rows - 1) / head_rows, per_head = min(M, head_rows), rows = a.item_heads * per_head;
     int n_items = 0, n_most = 0;
+    bool failed = false;
     for (int c0 = 0; c0 < blocks; c0 += kCombineThreads) {
         const int c = c0 + tid;
         const int4 meta = c < blocks ? a.meta[c] : make_int4(-1, 0, 0, 0);
@@ -344,7 +337,16 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
             n_most = max(n_most, most[w]);
         }
         if (meta.x >= 0) shared_items[before] = c;
-        __syncthreads();
+        failed = __syncthreads_or(meta.x == -2) || failed;
+    }
+    if (failed) {                            // a wait of this call ran out: nothing it wrote can be trusted
+        const int64_t all = (int64_t)a.B * a.n * a.H;
+        for (int64_t i = (int64_t)blockIdx.x * kCombineThreads + tid; i < all * a.D; i += (int64_t)gridDim.x * kCombineThreads) {
+            const int64_t r = i / a.D, tok = r / a.H, b = tok / a.n;
+            tree_store((T*)a.out + b * a.o_seq + (tok - b * a.n) * a.o_row + (r - tok * a.H) * a.o_head + (i - r * a.D), __int_as_float(0x7fc00000));
+            if (a.lse && i == r * a.D) a.lse[r] = __int_as_float(0x7fc00000);
+        }
+        return;
     }
     const bool many = n_most > kCombineMany;
     const int step = many ? gridDim.x : gridDim.x * kCombineWarps;

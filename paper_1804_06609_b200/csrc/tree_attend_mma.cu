@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
     tc_after();
     if (warp == SW) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
     if (sm.abort_flag) {
-        if (tid == 0) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.pages.status[1] = a.call; }
+        if (tid == 0) { atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT); a.meta[blockIdx.x] = make_int4(-2, 0, 0, 0); }       // (over what the loader wrote)
         if (a.whole_items) {           // (else the joining kernel sees to it)
             run = tree_run<C::threads>(a, kMKeys, groups * row_blocks, kItemUnits, 1, &sm.run);
             TreePiece pc;

@@ -41,11 +41,11 @@ struct TreeAttend {
     float* part_o;                     // [2 * grid][rows of an item][D]: unfinished first and last items of a block's run
     float* part_ml;                    // [2 * grid][rows of an item][2]: their maxima (of the scaled scores, in powers of two) and sums
     uint32_t* turns;                   // [kTreeTurns] a counter per SM, which goes on from call to call: blocks on an SM take turns by it
-    int4* meta;                        // [grid] item shared with the block before this one, if that block is the first on it
+    int4* meta;                        // [grid] item shared with the block before this one, if that block is the first on it (x = -1: none,
+                                       // -2: the block gave up)
     int whole_items;                   // items are not cut (short ones: no second kernel then)
     long long wait_clocks;
     int drop_item;
-    uint32_t call;                     // number of the call: what a failed wait leaves in the second status word
 };
 
 struct TreeAttendPlan {

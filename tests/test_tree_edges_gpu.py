@@ -44,3 +44,38 @@ def test_items_that_end_in_arena_tiles_have_all_their_outputs(dba, n, H, K, D, W
     for _ in range(40):
         assert torch.equal(t.attend(*args), first)
     assert t.status() == 0
+
+
+def test_a_failure_in_a_recorded_call_ends_with_it(dba):
+    """A graph runs one recorded call again and again.  The withheld hand-over is the seventh of a block: with long contexts the
+    call fails, with short ones no block comes that far and it must be right again."""
+    B, n, H, K, D, ps, W = 2, 3, 4, 2, 64, 16, 1
+    rng = torch.Generator().manual_seed(31)
+    per = (32 + 60000) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, "bf16")
+    masks = _masks(rng, B, n, W, 0.3, closed=0.0).cuda()
+    q = torch.randn(B, n, H, D, generator=rng).to(torch.bfloat16).cuda()
+    long, short = (torch.full((B,), x, dtype=torch.int32).cuda() for x in (60000, 2000))
+    c, side = long.clone(), torch.cuda.Stream()
+    lse = torch.zeros(B, n, H, device="cuda")
+    torch.cuda.synchronize()
+    t = _tree(dba, B, n, H, K, D, ps, per, W, stream=side)
+    with torch.cuda.stream(side):
+        want = t.attend(q, k, v, table, short, masks).clone()
+    launches = t.launch_count()
+    assert t.status() == 0 and torch.isfinite(want.float()).all()
+    t.test_hook(wait_clocks=2_000_000, drop_item=6)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        t.attend(q, k, v, table, c, masks, lse=lse)
+    assert t.launch_count() == launches + 2                           # cut, and joined by a second kernel
+    for _ in range(2):
+        with torch.cuda.stream(side):
+            c.copy_(long)
+            graph.replay()
+        assert t.status() == dba.TREE_TIMEOUT and torch.isnan(t.out.float()).all() and torch.isnan(lse).all()
+        with torch.cuda.stream(side):
+            c.copy_(short)
+            graph.replay()
+        assert t.status() == 0 and torch.equal(t.out, want) and torch.isfinite(lse).all()
+    del graph
