@@ -328,7 +328,7 @@ size_t dba_row_scan_static_max_bytes(void);
  * are of one type (dba_dtype); every sum and softmax statistic is fp32.
  *   Limits: rows <= 64, words <= 128, head_dim <= 256, head_dim and every stride a multiple of 16 bytes, pointers
  *   16-byte aligned, heads a multiple of kv_heads, max_pages * page_size < 2^31.  Other shapes: DBA_ERR_UNSUPPORTED.
- *   A layer of the cache may be larger than 2^31 elements, but spans at most 64 GiB from its first row to its last.
+ *   A layer of the cache may be larger than 2^31 elements, but its last row begins less than 64 GiB - 16 bytes after its first.
  * What only the device can see is not returned by calls that do not wait: a page number outside the cache (the place
  * counts as absent: not read, not written), an arena without a free slot, a table without room for settled tokens,
  * a place or position outside its range, a bounded wait that ran out.  Each sets a bit that dba_tree_status reports.

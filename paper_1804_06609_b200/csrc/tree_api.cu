@@ -76,9 +76,9 @@ dba_status check_cache(const dba_tree* h, const dba_kv_cache* c, const int32_t* 
     if (!aligned16(c->k) || !aligned16(c->v) || (c->page_stride * es) & 15 || (c->token_stride * es) & 15 || (c->head_stride * es) & 15 ||
         (c->layer_stride * es) & 15)
         return DBA_ERR_UNSUPPORTED;
-    // kernels count a layer's rows in 16 bytes and 32 bits
+    // kernels count a layer's rows in 16 bytes and 32 bits, of which the highest number stands for no row
     const int64_t span = ((int64_t)(c->num_pages - 1) * c->page_stride + (int64_t)(h->c.page_size - 1) * c->token_stride) * es / 16;
-    if (span > 0xffffffffLL) return DBA_ERR_UNSUPPORTED;
+    if (span >= 0xffffffffLL) return DBA_ERR_UNSUPPORTED;
     // n / d for n < 2^31: with 2^s >= d and m = ceil(2^(31+s) / d), m d - 2^(31+s) < d <= 2^s, so n m / 2^(31+s) exceeds n / d by less than 1 / d
     int s = 1;
     while ((1LL << s) < h->c.page_size) ++s;

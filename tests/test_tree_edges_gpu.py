@@ -79,3 +79,33 @@ def test_a_failure_in_a_recorded_call_ends_with_it(dba):
             graph.replay()
         assert t.status() == 0 and torch.equal(t.out, want) and torch.isfinite(lse).all()
     del graph
+
+
+def _rows_far_apart(t, T, query, k, v, table, ctx, masks, **kw):
+    """dba_tree_attend with a cache of these strides; nothing is seen, so nothing of the cache is read."""
+    import ctypes as C
+    import paper_1804_06609_b200 as pkg
+    c = T.KvCache(k=k.data_ptr(), v=v.data_ptr(), layers=1, head_stride=8, layer_stride=0, **kw)
+    return pkg.lib().dba_tree_attend(t._h, C.byref(query), C.byref(c), table.data_ptr(), table.shape[1], ctx.data_ptr(), masks.data_ptr(), None)
+
+
+@pytest.fixture
+def far(dba):
+    """A handle of rows of 16 bytes, two to a page, and a call to it that sees nothing."""
+    from paper_1804_06609_b200 import tree as T
+    t = _tree(dba, 1, 1, 1, 1, 8, 2, 16, 1)
+    k, v = (torch.zeros(4, 2, 1, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, out = (torch.zeros(1, 1, 1, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table, ctx, masks = (torch.zeros(*s, dtype=torch.int32, device="cuda") for s in ((1, 16), (1,), (1, 1, 1)))
+    query = T.TreeQuery(rows=1, q=q.data_ptr(), q_seq_stride=8, q_row_stride=8, q_head_stride=8, out=out.data_ptr(), out_seq_stride=8, out_row_stride=8,
+                        out_head_stride=8, lse=None, scale=1.0)
+    keep = (k, v, q, out, table, ctx, masks)
+    return lambda pages, page16, token16, keep=keep: _rows_far_apart(t, T, query, k, v, table, ctx, masks, num_pages=pages, page_stride=8 * page16, token_stride=8 * token16)
+
+
+def test_the_last_row_number_is_not_taken_for_none(dba, far):
+    """Rows are counted in 16 bytes; the number 2^32 - 1 stands for a place without a row, so a layer must not have it."""
+    assert far(65537, 65535, 65534) == 0                              # the last row's number: 65536 * 65535 + 65534 = 2^32 - 2
+    assert far(65537, 65535, 65535) == 2                              # 2^32 - 1
+    assert far(65537, 65535, 65536) == 2
+    torch.cuda.synchronize()
