@@ -72,13 +72,13 @@ dba_status device_of(dba_tree* h) {
 dba_status check_cache(const dba_tree* h, const dba_kv_cache* c, const int32_t* table, int64_t table_stride, TreePages* pg) {
     if (!c || !c->k || !c->v || !table || c->num_pages < 1 || c->layers < 1 || table_stride < h->c.max_pages) return DBA_ERR_INVALID_ARG;
     if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->layer_stride < 0) return DBA_ERR_INVALID_ARG;
-    const int es = elem_size(h->c.dtype);
-    if (!aligned16(c->k) || !aligned16(c->v) || (c->page_stride * es) & 15 || (c->token_stride * es) & 15 || (c->head_stride * es) & 15 ||
-        (c->layer_stride * es) & 15)
+    const int chunk = 16 / elem_size(h->c.dtype);                            // elements in 16 bytes
+    if (!aligned16(c->k) || !aligned16(c->v) || c->page_stride % chunk || c->token_stride % chunk || c->head_stride % chunk || c->layer_stride % chunk)
         return DBA_ERR_UNSUPPORTED;
     // kernels count a layer's rows in 16 bytes and 32 bits, of which the highest number stands for no row
-    const int64_t span = ((int64_t)(c->num_pages - 1) * c->page_stride + (int64_t)(h->c.page_size - 1) * c->token_stride) * es / 16;
-    if (span >= 0xffffffffLL) return DBA_ERR_UNSUPPORTED;
+    const uint64_t page16 = c->num_pages > 1 ? (uint64_t)(c->page_stride / chunk) : 0, token16 = h->c.page_size > 1 ? (uint64_t)(c->token_stride / chunk) : 0;
+    if (page16 >= 0xffffffffu || token16 >= 0xffffffffu) return DBA_ERR_UNSUPPORTED;         // (and the sum of products below 2^64)
+    if ((uint64_t)(c->num_pages - 1) * page16 + (uint64_t)(h->c.page_size - 1) * token16 >= 0xffffffffu) return DBA_ERR_UNSUPPORTED;
     // n / d for n < 2^31: with 2^s >= d and m = ceil(2^(31+s) / d), m d - 2^(31+s) < d <= 2^s, so n m / 2^(31+s) exceeds n / d by less than 1 / d
     int s = 1;
     while ((1LL << s) < h->c.page_size) ++s;

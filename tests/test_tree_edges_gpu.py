@@ -109,3 +109,11 @@ def test_the_last_row_number_is_not_taken_for_none(dba, far):
     assert far(65537, 65535, 65535) == 2                              # 2^32 - 1
     assert far(65537, 65535, 65536) == 2
     torch.cuda.synchronize()
+
+
+def test_strides_whose_span_passes_64_bits_are_refused(dba, far):
+    """16 pages at 2^60 elements end where 64 bits wrap around to 0."""
+    assert far(17, 1 << 57, 1) == 2
+    assert far(2, 1 << 59, 1) == 2 and far(2, 1, 1 << 59) == 2
+    assert far((1 << 31) - 1, (1 << 32) - 2, (1 << 32) - 2) == 2
+    torch.cuda.synchronize()
