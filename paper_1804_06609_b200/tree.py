@@ -3,6 +3,7 @@ drafted tokens, over a paged cache; appending to it; the tree after a step.  Arg
 from __future__ import annotations
 
 import ctypes as C
+import math
 
 from .binding import BF16, F32, _check, lib
 
@@ -89,6 +90,23 @@ class TokenTree:
 
     def _next_struct(self, out):
         return TreeNext(*[out[f].data_ptr() if out.get(f) is not None else None for f in self.NEXT])
+
+    def _next_views(self, out, n):
+        """out with its tensors in the shapes that n rows are written in (the front of larger ones), each looked over."""
+        B, W, dev, out = self.B, self.words, self._dev, dict(out)
+        if out.get("masks") is None:
+            raise ValueError("out: a dict with masks [B, rows, words] at least")
+        for f in self.NEXT:
+            t = out.get(f)
+            if t is None:
+                continue
+            shape = (B, n, W) if f == "masks" else (B, n) if f in ("slot", "position") else (B, 32 * W) if f == "commit_src" else (B,)
+            size = math.prod(shape)
+            if t.dtype is not self._i32t or t.get_device() != dev or not t.is_contiguous() or t.numel() < size:
+                raise ValueError(f"out: {f} int32 {shape}, contiguous, on the handle's device")
+            if t.shape != shape:
+                out[f] = t.view(-1)[:size].view(shape)
+        return out
 
     # Checks are written out in the calls and look at no more than memory safety and the argument's meaning need.
     def _cache(self, k, v, layers):
@@ -207,7 +225,8 @@ class TokenTree:
     def advance(self, backptr, masks, slot_pos, ctx_len, score=None, token=None, eos=-1, out=None):
         """The tree after a step: see dba_tree_advance.  backptr (and score, token: dba_step's outputs) [B, rows] or [B * rows];
         slot_pos [B, 32 * words] is updated in place.  Returns a dict of masks, slot, position, ctx_len, top, commit_src,
-        commit_n (default: one of two sets of the handle's own tensors, in turn) with slot_pos."""
+        commit_n (default: one of two sets of the handle's own tensors, in turn; out: a dict of such tensors, as new_next makes
+        them or larger, all but masks optional) with slot_pos."""
         B, W, dev = self.B, self.words, self._dev
         size, rows_in = backptr.numel(), masks.shape[1]
         n = size // B
@@ -219,13 +238,11 @@ class TokenTree:
                 self._turn = 1 - self._turn
             out, nx = self._next[self._turn]
             self._turn = 1 - self._turn
+            if n != self.rows:
+                out = self._next_views(out, n)
         else:
+            out = self._next_views(out, n)
             nx = self._next_struct(out)
-        if n != out["slot"].shape[1]:                       # fewer rows than the handle's: the front of its tensors
-            out = dict(out)
-            out["masks"] = out["masks"].view(-1)[:B * n * W].view(B, n, W)
-            for f in ("slot", "position"):
-                out[f] = out[f].view(-1)[:B * n].view(B, n)
         s = slot_pos.stride()
         if slot_pos.dtype is not self._i32t or slot_pos.shape != self._shape_arena or s[1] != 1 or slot_pos.get_device() != dev:
             raise ValueError("slot_pos: int32 [B, 32 * words]")

@@ -43,3 +43,57 @@ def test_calls_without_a_handle_are_refused():
     assert L.dba_tree_status(None, C.byref(bits)) == INVALID and L.dba_tree_test_hook(None, 0, -1) == INVALID
     assert L.dba_tree_launch_count(None) == 0
     L.dba_tree_destroy(None)
+
+
+# The binding's own checks, on a handle without a device: calls that pass them are noted instead of made.
+def _handle(B=2, rows=4, words=2, kv_heads=2, head_dim=64, page_size=16, max_pages=8):
+    torch = pytest.importorskip("torch")
+    t = object.__new__(tree.TokenTree)
+    t.torch, t.B, t.rows, t.heads, t.kv_heads, t.head_dim, t.page_size, t.max_pages, t.words = torch, B, rows, 4, kv_heads, head_dim, page_size, max_pages, words
+    t.device, t._dev, t.dtype, t.torch_dtype, t._i32t, t._f32t = torch.device("cpu"), -1, 1, torch.bfloat16, torch.int32, torch.float32
+    t._h, t.calls = None, []
+    note = lambda name: lambda *a: t.calls.append((name, a)) or 0  # noqa: E731
+    t._f_append, t._f_attend, t._f_advance, t._f_commit = (note(x) for x in ("append", "attend", "advance", "commit"))
+    t._next = [(x, t._next_struct(x)) for x in ([t.new_next(), t.new_next()] if words else [])]
+    t._turn = 0
+    t._kv, t._tok, t._query = tree.KvCache(), tree.TreeTokens(), tree.TreeQuery()
+    t._kv_ref, t._tok_ref, t._query_ref = (C.byref(x) for x in (t._kv, t._tok, t._query))
+    t._shape_table, t._shape_page, t._shape_arena = (B, max_pages), (page_size, kv_heads, head_dim), (B, 32 * words)
+    t._kv_last = t._tok_last = t._query_last = None
+    t._no_stride = (0, 0, 1)
+    t.out = torch.zeros(B, rows, t.heads, head_dim, dtype=torch.bfloat16)
+    return t
+
+
+def _advance(t, out, rows=None):
+    torch, n = t.torch, t.rows if rows is None else rows
+    return t.advance(torch.zeros(t.B, n, dtype=torch.int32), torch.zeros(t.B, t.rows, t.words, dtype=torch.int32),
+                     torch.zeros(t.B, 32 * t.words, dtype=torch.int32), torch.zeros(t.B, dtype=torch.int32), out=out)
+
+
+def test_advance_takes_outputs_that_hold_its_results():
+    t = _handle()
+    out = t.new_next()
+    got = _advance(t, out)
+    assert all(got[f].data_ptr() == out[f].data_ptr() and got[f].shape == out[f].shape for f in t.NEXT) and len(t.calls) == 1
+    got = _advance(t, out, rows=3)                                    # fewer rows: the front of the tensors
+    assert got["masks"].shape == (2, 3, 2) and got["slot"].shape == got["position"].shape == (2, 3) and got["masks"].is_contiguous()
+    got = _advance(t, dict(masks=out["masks"]))                       # what is not wanted is left out, or None
+    assert set(got) == {"masks", "slot_pos"}
+    assert _advance(t, dict(out, top=None, slot=None))["top"] is None and len(t.calls) == 4
+    for larger in (_handle(B=3), _handle(rows=6), _handle(words=3)):
+        got = _advance(t, larger.new_next())
+        assert all(got[f].shape == out[f].shape and got[f].is_contiguous() for f in t.NEXT)
+
+
+@pytest.mark.parametrize("change", [
+    lambda t, o: _handle(B=1).new_next(), lambda t, o: _handle(words=1).new_next(), lambda t, o: _handle(rows=3).new_next(),
+    lambda t, o: setattr(t, "_dev", 0) or o, lambda t, o: {f: x for f, x in o.items() if f != "masks"}, lambda t, o: dict(o, masks=None),
+    *[(lambda t, o, f=f: dict(o, **{f: o[f].long()})) for f in tree.TokenTree.NEXT],
+    *[(lambda t, o, f=f: dict(o, **{f: o[f].flatten()[:-1]})) for f in tree.TokenTree.NEXT],
+    *[(lambda t, o, f=f: dict(o, **{f: o[f].repeat_interleave(2, -1)[..., ::2]})) for f in tree.TokenTree.NEXT]])
+def test_advance_refuses_outputs_that_do_not_hold_its_results(change):
+    t = _handle()
+    with pytest.raises(ValueError, match="out:"):
+        _advance(t, change(t, t.new_next()))
+    assert not t.calls
