@@ -111,13 +111,13 @@ class TokenTree:
     # Checks are written out in the calls and look at no more than memory safety and the argument's meaning need.
     def _cache(self, k, v, layers):
         s, sh = k.stride(), k.shape
-        if (s, sh) != self._kv_last:
+        if (s, sh, layers) != self._kv_last:
             if s[-1] != 1 or len(s) != 4 + layers or sh[-3:] != self._shape_page:
                 raise ValueError("k and v: [pages, page_size, kv_heads, head_dim] with a unit inner stride (commit: layers in front)")
             c = self._kv
             c.num_pages, c.page_stride, c.token_stride, c.head_stride = sh[-4], s[-4], s[-3], s[-2]
             c.layers, c.layer_stride = (sh[0], s[0]) if layers else (1, 0)
-            self._kv_last = (s, sh)
+            self._kv_last = (s, sh, layers)
         dt, dev = self.torch_dtype, self._dev
         if k.dtype is not dt or v.dtype is not dt or k.get_device() != dev or v.get_device() != dev or v.stride() != s or v.shape != sh:
             raise ValueError("k and v: alike, of the handle's type and on its device")

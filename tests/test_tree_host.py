@@ -97,3 +97,22 @@ def test_advance_refuses_outputs_that_do_not_hold_its_results(change):
     with pytest.raises(ValueError, match="out:"):
         _advance(t, change(t, t.new_next()))
     assert not t.calls
+
+
+def test_a_cache_with_layers_is_refused_whatever_was_called_before():
+    t = _handle()
+    torch = t.torch
+    k, v = (torch.zeros(3, 16, 16, 2, 64, dtype=torch.bfloat16) for _ in range(2))
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    table, ctx = i32(2, 8), i32(2)
+    new, q = torch.zeros(8, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 4, 4, 64, dtype=torch.bfloat16)
+    for _ in range(2):
+        for call in (lambda: t.append(new, new, k, v, table, i32(8)), lambda: t.attend(q, k, v, table, ctx)):
+            with pytest.raises(ValueError):
+                call()
+        assert not t.calls
+        t.commit(k, v, table, ctx, i32(2, 64), i32(2))
+        assert t._kv.layers == 3 and t._kv.layer_stride == 16 * 16 * 2 * 64 and t._kv.num_pages == 16 and len(t.calls) == 1
+        t.calls.clear()
+    t.attend(q, k[1], v[1], table, ctx)
+    assert t._kv.layers == 1 and t._kv.k == k[1].data_ptr() and len(t.calls) == 1
