@@ -191,8 +191,10 @@ dba_status dba_tree_advance(dba_tree* h, int32_t rows_in, const int32_t* masks_i
                             int64_t slot_pos_stride, const int32_t* ctx_len_dev, const dba_tree_next* next) {
     if (!h || !masks_in_dev || !backptr_dev || !slot_pos_dev || !ctx_len_dev || !next || !next->masks || rows_in < 1 || rows_out < 1)
         return DBA_ERR_INVALID_ARG;
-    if (h->c.words == 0 || rows_in > h->c.rows || rows_out > h->c.rows || next->masks == masks_in_dev || slot_pos_stride < 32 * h->c.words)
-        return DBA_ERR_INVALID_ARG;
+    if (h->c.words == 0 || rows_in > h->c.rows || rows_out > h->c.rows || slot_pos_stride < 32 * h->c.words) return DBA_ERR_INVALID_ARG;
+    // one sequence's new masks must not be another's old ones
+    const uintptr_t in = (uintptr_t)masks_in_dev, out = (uintptr_t)next->masks, row = (uintptr_t)h->c.B * h->c.words * sizeof(int32_t);
+    if (in < out + rows_out * row && out < in + rows_in * row) return DBA_ERR_INVALID_ARG;
     TreeAdvance a{};
     a.B = h->c.B; a.rows_in = rows_in; a.rows_out = rows_out; a.W = h->c.words; a.ctx_cap = (int32_t)h->ctx_cap; a.eos_id = eos_id;
     a.masks_in = (const uint32_t*)masks_in_dev; a.backptr = backptr_dev; a.token = token_dev; a.ctx_len = ctx_len_dev; a.score = score_dev;

@@ -234,7 +234,8 @@ class TokenTree:
             raise ValueError("backptr: [B, rows], rows up to the handle's")
         at = masks.data_ptr()
         if out is None:
-            if at == self._next[self._turn][0]["masks"].data_ptr():
+            own = self._next[self._turn][0]["masks"]
+            if 0 <= at - own.data_ptr() < 4 * own.numel():         # (a part of it may be the old masks)
                 self._turn = 1 - self._turn
             out, nx = self._next[self._turn]
             self._turn = 1 - self._turn

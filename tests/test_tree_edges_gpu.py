@@ -117,3 +117,18 @@ def test_strides_whose_span_passes_64_bits_are_refused(dba, far):
     assert far(2, 1 << 59, 1) == 2 and far(2, 1, 1 << 59) == 2
     assert far((1 << 31) - 1, (1 << 32) - 2, (1 << 32) - 2) == 2
     torch.cuda.synchronize()
+
+
+def test_advance_refuses_new_masks_over_the_old_ones(dba):
+    import ctypes as C
+    from paper_1804_06609_b200 import tree as T
+    B, n, W = 3, 4, 2
+    t = _tree(dba, B, n, 1, 1, 64, 16, 8, W)
+    room = torch.zeros(4, B, n, W, dtype=torch.int32, device="cuda")
+    back, pos, ctx = (torch.zeros(*s, dtype=torch.int32, device="cuda") for s in ((B, n), (B, 32 * W), (B,)))
+    whole, at = 4 * B * n * W, room.data_ptr() + 4 * B * n * W
+    adv = lambda to, ni=n, no=n: dba.lib().dba_tree_advance(t._h, ni, at, no, back.data_ptr(), None, None, 0, pos.data_ptr(), 32 * W, ctx.data_ptr(), C.byref(T.TreeNext(masks=to)))  # noqa: E731
+    assert all(adv(at + by) == 1 for by in (0, 4, -4, whole - 4, 4 - whole))
+    assert adv(at + whole) == 0 and adv(at - whole) == 0
+    assert adv(at + whole - 4 * B * W, ni=n - 1) == 0 and adv(at - whole + 4 * B * W, no=n - 1) == 0       # fewer rows end earlier
+    torch.cuda.synchronize()

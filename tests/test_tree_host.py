@@ -116,3 +116,20 @@ def test_a_cache_with_layers_is_refused_whatever_was_called_before():
         t.calls.clear()
     t.attend(q, k[1], v[1], table, ctx)
     assert t._kv.layers == 1 and t._kv.k == k[1].data_ptr() and len(t.calls) == 1
+
+
+def test_advance_from_a_part_of_its_own_masks_uses_the_other_set():
+    t = _handle(B=1)
+    torch, i32 = t.torch, lambda *s: t.torch.zeros(*s, dtype=t.torch.int32)  # noqa: E731
+    masks, seen = i32(1, 4, 2), []
+    for _ in range(5):
+        got = t.advance(i32(1, 4), masks, i32(1, 64), i32(1))
+        lo, hi = got["masks"].data_ptr(), got["masks"].data_ptr() + 4 * got["masks"].numel()
+        assert masks.data_ptr() + 4 * masks.numel() <= lo or hi <= masks.data_ptr()
+        masks = got["masks"][:, 2:]
+        assert masks.is_contiguous()
+        seen.append(lo)
+    first = t.advance(i32(1, 4), i32(1, 4, 2), i32(1, 64), i32(1))["masks"]      # from others' masks: the sets in turn
+    again = t.advance(i32(1, 4), i32(1, 4, 2), i32(1, 64), i32(1))["masks"]
+    part = t.advance(i32(1, 4), first[:, 2:], i32(1, 64), i32(1))["masks"]        # its turn would be the set that is read
+    assert first.data_ptr() != again.data_ptr() == part.data_ptr()
