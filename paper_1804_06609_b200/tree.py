@@ -228,6 +228,8 @@ class TokenTree:
         commit_n (default: one of two sets of the handle's own tensors, in turn; out: a dict of such tensors, as new_next makes
         them or larger, all but masks optional) with slot_pos."""
         B, W, dev = self.B, self.words, self._dev
+        if not W:
+            raise ValueError("advance: the handle has no arena (words = 0)")
         size, rows_in = backptr.numel(), masks.shape[1]
         n = size // B
         if size != B * n or n > self.rows:

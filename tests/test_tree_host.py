@@ -133,3 +133,11 @@ def test_advance_from_a_part_of_its_own_masks_uses_the_other_set():
     again = t.advance(i32(1, 4), i32(1, 4, 2), i32(1, 64), i32(1))["masks"]
     part = t.advance(i32(1, 4), first[:, 2:], i32(1, 64), i32(1))["masks"]        # its turn would be the set that is read
     assert first.data_ptr() != again.data_ptr() == part.data_ptr()
+
+
+def test_a_handle_without_an_arena_refuses_the_tree():
+    t = _handle(words=0)
+    i32 = lambda *s: t.torch.zeros(*s, dtype=t.torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="arena"):
+        t.advance(i32(2, 4), i32(2, 4, 0), i32(2, 0), i32(2))
+    assert not t.calls
