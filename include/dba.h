@@ -395,7 +395,7 @@ typedef struct {
 enum {                          /* bits of dba_tree_status */
     DBA_TREE_TIMEOUT = 1,       /* a bounded device-side wait gave up: that call's outputs are NaN (short tables: those of the
                                    items concerned)                                                              */
-    DBA_TREE_BAD_PAGE = 2,      /* a page number outside the cache                                              */
+    DBA_TREE_BAD_PAGE = 2,      /* a page number outside the cache (an arena slot that no row sees needs no page) */
     DBA_TREE_ARENA_FULL = 4,    /* dba_tree_advance found no free slot for some row                             */
     DBA_TREE_NO_ROOM = 8,       /* settled tokens do not fit the sequence's table: none was settled             */
     DBA_TREE_BAD_INDEX = 16     /* a place, sequence or position outside its range                              */

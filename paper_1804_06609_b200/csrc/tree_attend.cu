@@ -96,6 +96,13 @@ template <> struct TreeCopied<__nv_bfloat16> : TreeCopiedN<8> {};
 __device__ __forceinline__ float g_widen(float x) { return x; }
 __device__ __forceinline__ float g_widen(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+// Whether some of a sequence's rows see an arena slot; masks: the sequence's, W words a row.
+__device__ __noinline__ bool g_seen(const uint32_t* masks, int rows, int W, int slot) {
+    for (int i = 0; i < rows; ++i)
+        if ((__ldg(masks + i * W + (slot >> 5)) >> (slot & 31)) & 1u) return true;
+    return false;
+}
+
 template <typename T, int DP, int RI>
 __global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plain_kernel(const TreeAttend a) {
     using S = GSmem<DP>;
@@ -123,7 +130,8 @@ __global__ void __launch_bounds__(kGThreads, DP <= 128 ? 3 : 2) tree_attend_plai
                 for (int i = tid; i < KT; i += kGThreads) {
                     int place, count;
                     tree_tile_span(a, pc, t, KT, &place, &count);
-                    sm.row[t & 1][i] = i < count ? tree_row(a.pages, pc.b, place + i) : -1;
+                    // (an arena slot that no row sees need not have a page)
+                    sm.row[t & 1][i] = i >= count ? -1 : tree_row(a.pages, pc.b, place + i, [&] { return place >= a.A || g_seen(a.masks + (int64_t)pc.b * a.n * a.W, a.n, a.W, place + i); });
                 }
         };
         __syncthreads();                                   // the last piece is done with

@@ -11,14 +11,19 @@ __device__ __forceinline__ uint32_t tree_page(const TreePages& pg, uint32_t plac
 }
 // Element offset of a place of sequence b in one layer's cache; -1 where there is no such row (the place is outside the
 // table, or the table names a page outside the cache: recorded in the status word).  64 bits: a cache may be longer
-// than 2^31 elements.
-__device__ __forceinline__ int64_t tree_row(const TreePages& pg, int b, int place) {
+// than 2^31 elements.  `wanted()` is asked of a page outside the cache alone: false where nobody needs the place, and nothing is recorded.
+template <typename F>
+__device__ __forceinline__ int64_t tree_row(const TreePages& pg, int b, int place, F wanted) {
     const unsigned page = tree_page(pg, (unsigned)place);
     if (place < 0 || page >= (unsigned)pg.max_pages) return -1;
     const int32_t id = __ldg(pg.table + (int64_t)b * pg.table_stride + page);
-    if ((unsigned)id >= (unsigned)pg.num_pages) { atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_PAGE); return -1; }
+    if ((unsigned)id >= (unsigned)pg.num_pages) {
+        if (wanted()) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_PAGE);
+        return -1;
+    }
     return (int64_t)id * pg.page_stride + (int64_t)((unsigned)place - page * (unsigned)pg.page_size) * pg.token_stride;
 }
+__device__ __forceinline__ int64_t tree_row(const TreePages& pg, int b, int place) { return tree_row(pg, b, place, [] { return true; }); }
 
 // Keys of a sequence are walked in tiles of `kt` places: first the arena up to the highest slot in use, then the
 // context (each starts a tile of its own).  A sequence with nothing to see has one (empty) tile, so that somebody

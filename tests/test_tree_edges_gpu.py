@@ -132,3 +132,28 @@ def test_advance_refuses_new_masks_over_the_old_ones(dba):
     assert adv(at + whole) == 0 and adv(at - whole) == 0
     assert adv(at + whole - 4 * B * W, ni=n - 1) == 0 and adv(at - whole + 4 * B * W, no=n - 1) == 0       # fewer rows end earlier
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("bf16", 192), ("f32", 64)])
+def test_pages_of_slots_no_row_sees_need_not_exist(dba, dtype, D):
+    """A table whose arena pages are handed out as slots come into use: the others' entries are -1 and nobody looks at them."""
+    B, n, H, K, ps, W = 2, 5, 8, 2, 16, 4
+    rng = torch.Generator().manual_seed(51)
+    per = (32 * W + 100) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, dtype)
+    masks = torch.zeros(B, n, W, dtype=torch.int32)
+    for b in range(B):
+        for i in range(n):
+            masks[b, i] = torch.from_numpy(M.words_of({i, 40 + i, 70, 100 + b}, W))       # of pages 0, 2, 4 and 6 of 8
+    table[:, [1, 3, 5, 7]] = -1
+    c = torch.tensor([100, 0], dtype=torch.int32)
+    q = torch.randn(B, n, H, D, generator=rng).to(DT[dtype]).cuda()
+    want = M.attend(q, k, v, table, c, masks, D ** -0.5, ps, W, k.shape[0])
+    t = _tree(dba, B, n, H, K, D, ps, per, W, dtype)
+    for top in (None, _top(masks).cuda()):
+        _check(t.attend(q, k, v, table, c.cuda(), masks.cuda(), top), None, want, D, 300, dtype)
+        assert t.status() == 0
+    table[1, 4] = -1                                                  # slot 70: seen, and without a page
+    want = M.attend(q, k, v, table, c, masks, D ** -0.5, ps, W, k.shape[0])
+    _check(t.attend(q, k, v, table, c.cuda(), masks.cuda()), None, want, D, 300, dtype)
+    assert t.status() == dba.TREE_BAD_PAGE
