@@ -157,3 +157,128 @@ def test_pages_of_slots_no_row_sees_need_not_exist(dba, dtype, D):
     want = M.attend(q, k, v, table, c, masks, D ** -0.5, ps, W, k.shape[0])
     _check(t.attend(q, k, v, table, c.cuda(), masks.cuda()), None, want, D, 300, dtype)
     assert t.status() == dba.TREE_BAD_PAGE
+
+
+VARIANTS = [  # n, H, K, D, dtype: a case for each kernel a call can come to
+    (5, 8, 8, 64, "bf16"), (40, 8, 8, 64, "bf16"), (20, 32, 8, 128, "bf16"), (4, 8, 4, 128, "bf16"), (4, 4, 2, 64, "bf16"), (6, 8, 2, 192, "bf16"),
+    (4, 4, 2, 64, "f32"), (20, 8, 2, 128, "f32")]
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0])
+@pytest.mark.parametrize("n,H,K,D,dtype", VARIANTS)
+def test_scales_below_zero_and_of_zero(dba, n, H, K, D, dtype, scale):
+    """The sign is the matrix instruction's, the size the softmax's; with a scale of zero every place counts alike."""
+    B, ps, W, ctx = 2, 16, 2, [300, 9]
+    rng = torch.Generator().manual_seed(61 + n + D)
+    per = (32 * W + max(ctx)) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, dtype)
+    masks = _masks(rng, B, n, W, 0.3)
+    c = torch.tensor(ctx, dtype=torch.int32)
+    q = (torch.randn(B, n, H, D, generator=rng) * 1.5).to(DT[dtype]).cuda()
+    lse = torch.zeros(B, n, H, device="cuda")
+    t = _tree(dba, B, n, H, K, D, ps, per, W, dtype)
+    want = M.attend(q, k, v, table, c, masks, scale, ps, W, k.shape[0])
+    _check(t.attend(q, k, v, table, c.cuda(), masks.cuda(), scale=scale, lse=lse), lse, want, D, 32 * W + 300, dtype)
+    assert t.status() == 0
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("n,H,K,D,dtype", VARIANTS)
+def test_values_that_are_not_finite_in_every_kernel_and_in_cut_items(dba, n, H, K, D, dtype, cut):
+    """inf seen by row 1, NaN by row 2, inf and -inf in tiles far apart by row 3: theirs alone, whether an item is one block's or is
+    joined from pieces that begin inside its arena tiles."""
+    B, ps, W, ctx = 2, 16, 40 if cut else 3, [1500, 30] if cut else [100, 0]
+    A = 32 * W
+    rng = torch.Generator().manual_seed(71 + n + D)
+    per = (A + max(ctx)) // ps + 1
+    k, v, table = _cache(rng, B, per, ps, K, D, dtype)
+    slots = [2, A // 2 + 5, A - 7, 9]                                  # inf, NaN, -inf and inf
+    masks = _masks(rng, B, n, W, 0.2, closed=0.0)
+    for b in range(B):
+        for i in range(n):
+            own = set(M.bits_of(masks[b, i].numpy())) - set(slots) | {20}
+            own |= {1: {slots[0]}, 2: {slots[1]}, 3: {slots[2], slots[3]}}.get(i, set())
+            masks[b, i] = torch.from_numpy(M.words_of(own, W))
+    c = torch.tensor(ctx, dtype=torch.int32)
+    q = torch.randn(B, n, H, D, generator=rng).to(DT[dtype]).cuda()
+    want = M.attend(q, k, v, table, c, masks, D ** -0.5, ps, W, k.shape[0])
+    v2, h, last = v.clone(), K - 1, D - 1
+    for slot, head, d, x in ((slots[0], h, 3, math.inf), (slots[1], 0, last, math.nan), (slots[2], h, 5, -math.inf), (slots[3], h, 5, math.inf)):
+        v2[int(table[0, slot // ps]), slot % ps, head, d] = x           # of sequence 0 alone
+    t = _tree(dba, B, n, H, K, D, ps, per, W, dtype)
+    launches = t.launch_count()
+    for top in (None, _top(masks).cuda()):
+        got = t.attend(q, k, v2, table, c.cuda(), masks.cuda(), top).double().cpu()
+        G, hit = H // K, torch.zeros(B, n, H, D, dtype=torch.bool)
+        assert (got[0, 1, h * G:, 3] == math.inf).all() and torch.isnan(got[0, 2, :G, last]).all() and torch.isnan(got[0, 3, h * G:, 5]).all()
+        hit[0, 1, h * G:, 3] = hit[0, 2, :G, last] = hit[0, 3, h * G:, 5] = True
+        out, _, spread, reach = want
+        tol = M.attend_tolerance(out, spread, reach, D, A + max(ctx), DT[dtype])
+        assert torch.isfinite(got[~hit]).all() and ((got - out).abs() <= tol)[~hit].all()
+    assert t.launch_count() == launches + (4 if cut else 2) and t.status() == 0
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("n,H,K,D,dtype", [(1, 2, 2, 64, "bf16"), (2, 4, 4, 64, "bf16"), (1, 2, 1, 64, "f32")])
+def test_more_sequences_than_a_block_has_threads(dba, n, H, K, D, dtype, cut):
+    """The lengths are scanned by blocks of 128 to 256 threads: each has several sequences, and the last ones none."""
+    B, ps, W = 1000, 16, 1
+    rng = torch.Generator().manual_seed(81 + n)
+    ctx = (torch.rand(B, generator=rng) ** 3 * 60).int()
+    ctx[0], ctx[500], ctx[B - 1] = 0, 61, 60
+    per = (32 + 61) // ps + 1
+    long = per if not cut else 50                                     # a table that could hold more: its items may be cut
+    k, v, table = _cache(rng, B, per, ps, K, D, dtype)
+    wide = torch.full((B, long), -1, dtype=torch.int32)
+    wide[:, :per] = table.cpu()
+    masks = _masks(rng, B, n, W, 0.1)
+    q = torch.randn(B, n, H, D, generator=rng).to(DT[dtype]).cuda()
+    want = M.attend(q, k, v, table, ctx, masks, D ** -0.5, ps, W, k.shape[0])
+    t = _tree(dba, B, n, H, K, D, ps, long, W, dtype)
+    launches, lse = t.launch_count(), torch.zeros(B, n, H, device="cuda")
+    _check(t.attend(q, k, v, wide.cuda(), ctx.cuda(), masks.cuda(), lse=lse), lse, want, D, 93, dtype)
+    assert t.launch_count() == launches + (2 if cut else 1) and t.status() == 0
+
+
+@pytest.mark.parametrize("dtype,hnd", [("bf16", False), ("f32", True)])
+def test_commit_of_more_tokens_than_a_block_has_threads(dba, dtype, hnd):
+    """A block looks 256 places up at a time."""
+    B, layers, K, D, ps, W = 5, 3, 2, 64, 24, 17
+    A, rng = 32 * W, torch.Generator().manual_seed(91)
+    n = torch.tensor([257, A, 0, 256, 512], dtype=torch.int32)
+    ctx = n + torch.tensor([5, 0, 3, 40, 1], dtype=torch.int32)
+    per = (A + int(ctx.max())) // ps + 1
+    shape = (layers, B * per, K, ps, D) if hnd else (layers, B * per, ps, K, D)
+    k, v = (torch.randn(shape, generator=rng).to(DT[dtype]).cuda() for _ in range(2))
+    if hnd:
+        k, v = k.transpose(2, 3), v.transpose(2, 3)
+    table = torch.randperm(B * per, generator=rng).int().view(B, per)
+    src = torch.full((B, A), -1, dtype=torch.int32)
+    want_k, want_v = k.clone(), v.clone()
+    for b in range(B):
+        m = int(n[b])
+        src[b, :m] = torch.randperm(A, generator=rng)[:m].int()
+        s, d = src[b, :m].long(), A + int(ctx[b]) - m + torch.arange(m)
+        at, to = (table[b].long()[x // ps].cuda() for x in (s, d))
+        for x, w in ((k, want_k), (v, want_v)):
+            w[:, to, d.cuda() % ps] = x[:, at, s.cuda() % ps]
+    t = _tree(dba, B, 4, K, K, D, ps, per, W, dtype)
+    t.commit(k, v, table.cuda(), ctx.cuda(), src.cuda(), n.cuda())
+    assert torch.equal(k, want_k) and torch.equal(v, want_v) and t.status() == 0
+
+
+def test_advance_into_tensors_of_the_callers(dba):
+    B, n, W, per = 3, 6, 2, 30
+    rng = torch.Generator().manual_seed(95)
+    t = _tree(dba, B, n, 1, 1, 64, 16, per, W)
+    masks = _masks(rng, B, n, W, 0.1, closed=0.0).cuda()
+    ctx = torch.tensor([4, 0, 9], dtype=torch.int32).cuda()
+    for rows in (n, 4):
+        back = (torch.rand(B, rows, generator=rng) * n).int().cuda()
+        pos = [torch.arange(64, dtype=torch.int32).repeat(B, 1).cuda() for _ in range(2)]
+        want = {f: x.clone() for f, x in t.advance(back, masks, pos[0], ctx).items()}
+        room = {f: torch.full((x.numel() + 40,), -7, dtype=torch.int32, device="cuda") for f, x in t.new_next().items()}
+        got = t.advance(back, masks, pos[1], ctx, out=room)
+        assert set(got) == set(want) and all(torch.equal(got[f], want[f]) for f in want)
+        assert all((room[f][want[f].numel():] == -7).all() and got[f].data_ptr() == room[f].data_ptr() for f in room)
+    assert t.status() == 0
