@@ -325,7 +325,9 @@ size_t dba_row_scan_static_max_bytes(void);
  *
  * Conventions are the step's: nothing throws; argument errors are found on the host; calls only enqueue work on the
  * handle's stream; the caller owns all device memory; calls on one handle must not overlap.  Keys, values and queries
- * are of one type (dba_dtype); every sum and softmax statistic is fp32.
+ * are of one type (dba_dtype); every sum and softmax statistic is fp32.  bf16 with heads of up to 128 has its products on the tensor
+ * cores, whose operands are bf16: there the probabilities, relative to the row's reference, are rounded to bf16 (half a unit in the 8th
+ * bit each) before they meet the values; elsewhere they stay fp32.
  *   Limits: rows <= 64, words <= 128, head_dim <= 256, head_dim and every stride a multiple of 16 bytes, pointers
  *   16-byte aligned, heads a multiple of kv_heads, max_pages * page_size < 2^31.  Other shapes: DBA_ERR_UNSUPPORTED.
  *   A layer of the cache may be larger than 2^31 elements, but its last row begins less than 64 GiB - 16 bytes after its first.
