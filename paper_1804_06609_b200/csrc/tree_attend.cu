@@ -11,10 +11,13 @@
 // at a time (fma.rn.f32x2), which leaves issue slots to the loads from shared memory that feed them.
 // The keys of the next tile and the values of this one are on their way (cp.async) while the scores are computed.
 //
-// What bounds it: the loads from shared memory that feed the products.  16 sequences of up to 1000 tokens, 16 heads of 64, 20 rows,
-// fp32: 75 us for 104 MB read (1.5 TB/s; dram 19 % busy) and 1 GFLOP a direction; warps wait for shared memory (short scoreboard 1.9 and
-// fixed latencies 1.8 of 7 cycles an instruction), 12 warps an SM is what 65 KB of tiles a block leave.  Half the tile and four
-// blocks an SM, and plain instead of paired products, were no faster.
+// What bounds it: latency.  16 sequences of up to 1000 tokens, 16 heads of 64, 20 rows, fp32: 82 to 85 us for 104 MB read (1.3 TB/s) and
+// 1 GFLOP; no unit is full (instructions issued in 39 % of the cycles, loads and stores 28 %, fma 21 %, dram 19 %): a thread's products
+// follow right after the loads from shared memory that feed them (short scoreboard 1.9 and fixed latencies 1.8 of 7 cycles
+// an instruction), and the 12 warps that 71 KB a block leave an SM do not cover that.  Half the tile and four blocks an SM, and
+// plain instead of paired products, were no faster; more products to a load has not been tried.  bf16 heads over 128 come here
+// too, widened through registers into tiles of 16 keys: 16 sequences of up to 1000 tokens, 16 heads over 4 of 256, 20 rows: 364 us, where
+// their 56 MB take 9.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -409,6 +412,7 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
 
 template <typename T, int DP, int RI>
 cudaError_t configure_plain() {
+    static_assert((DP <= 128 ? 3 : 2) * (sizeof(GSmem<DP>) + 1024) <= 228 * 1024, "blocks of the grid that an SM holds");
     return cudaFuncSetAttribute(tree_attend_plain_kernel<T, DP, RI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GSmem<DP>));
 }
 template <typename T, int DP>
@@ -442,7 +446,7 @@ TreeAttendPlan plan_tree_attend(int dtype, int M, int K, int D, int sm_count) {
     const int blocks = (M + kGRows - 1) / kGRows;
     p.rows = ((M + blocks - 1) / blocks + 7) / 8 * 8;
     p.item_heads = 1;
-    p.grid = (D <= 128 ? 3 : 2) * sm_count;         // blocks that an SM's shared memory holds (65, 75 and 88 KB each)
+    p.grid = (D <= 128 ? 3 : 2) * sm_count;         // blocks that an SM's shared memory holds (71, 73 and 86 KB each)
     return p;
 }
 
@@ -458,11 +462,13 @@ cudaError_t configure_tree_attend() {
     return e;
 }
 
-// Whether items are left whole, each to one block: without pieces there is nothing to join, and no second kernel.  By the most
-// keys that a table holds, in 64: up to 5 always (one sequence of 250 tokens, 8 heads of 128: 11.2 us whole, 13.6 cut; of 440,
-// 16 heads of 64: 16.9 whole, 14.0 cut); with at least a third as many items as there are blocks, up to 8 (64 sequences of 440,
-// one row: 30.7 whole, 32.3 cut; 256 of 1200: 139 whole, 130 cut), and up to 24 where an item has more than 32 rows,
-// whose pieces are long to write and to join (64 sequences of 1100, 80 rows: 66 whole, 77 cut; of 2400: 120 whole, 116 cut).
+// Whether items are left whole, each to one block: without pieces there is nothing to join, and no second kernel.  The lengths are on the
+// device, so it goes by the most keys that a table holds (short contexts in long tables are cut: 256 x 20 rows, 16 heads of
+// 64, 30 to 120 tokens and 256 slots: 40 us with tables of up to 256 context places, 51 with longer ones), in 64: up to 5
+// always (one sequence of 250 tokens, 8 heads of 128: 11.2 us whole, 13.6 cut; of 440, 16 heads of 64: 16.9 whole, 14.0 cut); with
+// at least a third as many items as there are blocks, up to 8 (64 sequences of 440, one row: 30.7 whole, 32.3 cut; 256 of 1200: 139
+// whole, 130 cut), and up to 24 where an item has more than 32 rows, whose pieces are long to write and to join (64 sequences
+// of 1100, 80 rows: 66 whole, 77 cut; of 2400: 120 whole, 116 cut).
 bool stays_whole(const TreeAttend& a, const TreeAttendPlan& plan) {
     const int64_t most = ((a.masks ? a.A : 0) + 63) / 64 + ((int64_t)a.ctx_cap + 63) / 64;
     const int rows = plan.rows / plan.item_heads;

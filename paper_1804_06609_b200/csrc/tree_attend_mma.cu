@@ -22,13 +22,14 @@
 //              that do not exist, or that no row of the sequence sees, are zeros.
 // Every wait on an mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
 //
-// What bounds it, measured (6551 GB/s is what a copy reaches): with few rows and long contexts HBM: one row, 32 heads over 4 key heads of
-// 128, 4 x up to 131071 tokens, 1.03 GB: 162 us, 6.35 TB/s.  With many rows the two longest chains of a tile, which take about
-// as long: the loader's instructions (2000 to 2600 cycles; dropping the exponentials, or most of the products, or
-// reading everything from L2, each changes under 3 %) and the softmax warps' (2600): 61 rows, 32 heads over 8 of 128, 8 x up
-// to 8189 tokens: 107 us, of which 10 join the pieces; 37 would do.  A third loader warp, or two softmax threads to a row
-// (158 us when it was tried), do not fit the 65536 registers beside 128 for a thread that holds 64 scores.  Many short items
-// (256 x 16 heads of 64, 20 rows, 30 to 160 keys): what an item costs from its look-up to its output, 41 us; 15 would do.
+// What bounds it, measured (6551 GB/s is what a copy reaches; times of calls among others, then of six calls at a time, whose clocks
+// are higher): with few rows and long contexts HBM: one row, 32 heads over 4 key heads of 128, 4 x up to 131071 tokens, 1.03 GB:
+// 176 to 186 us (5.5 to 5.9 TB/s), 168.  With many rows the two longest chains of a tile, which take about as long: the loader's
+// instructions (2000 to 2600 cycles; dropping the exponentials, or most of the products, or reading everything from L2,
+// each changes under 3 %) and the softmax warps' (2600): 61 rows, 32 heads over 8 of 128, 8 x up to 8189 tokens: 122 us, 110, of
+// which 10 join the pieces; 37 would do.  Two softmax threads to a row were 158 us when they were tried: a thread that holds
+// 64 scores takes 128 registers, and the SM has 65536.  Many short items (256 x 16 heads of 64, 20 rows, 30 to 160 keys):
+// what an item costs from its look-up to its output, 41 us; 15 would do.
 #include <cuda_bf16.h>
 
 #include "tree_device.cuh"
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
                 for (int j = 0; j < NJ; ++j) at[j] = rows[j * RW];
                 const int64_t head_at = pc.h * HP * head2 + (ch_in ? ch * 16 : 0);
                 // With one head the two go side by side, so that a warp waits for the steps of one address at a time half as
-                // often (a tree of 61 rows over 8189 tokens, heads of 128: 107 us, one after the other 114); with four, one
+                // often (a tree of 61 rows over 8189 tokens, heads of 128, in short runs: 107 us, one after the other 114); with four, one
                 // after the other, as either may begin when its own stage is free and there are only three.
                 constexpr int SIDE = HP == 1 ? 2 : 1;
 #pragma unroll 1
@@ -786,6 +787,7 @@ __global__ void __launch_bounds__(MConf<DP, SW, HP>::threads, MConf<DP, SW, HP>:
 
 template <int DP, int SW, int HP>
 cudaError_t configure_mma() {
+    static_assert(MConf<DP, SW, HP>::blocks_per_sm * (sizeof(MSmem<DP, SW, HP>) + 1024) <= 228 * 1024, "blocks of the grid that an SM holds");
     return cudaFuncSetAttribute(tree_attend_mma_kernel<DP, SW, HP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MSmem<DP, SW, HP>));
 }
 template <int DP, int SW, int HP>
