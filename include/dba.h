@@ -452,6 +452,93 @@ dba_status dba_tree_advance(dba_tree* h, int32_t rows_in, const int32_t* masks_i
 dba_status dba_tree_commit(dba_tree* h, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride,
                            const int32_t* ctx_len_dev, const int32_t* src_dev, const int32_t* n_dev);
 
+/*
+ * Long and shared texts.
+ *
+ * Several sequences that begin with the same tokens (an instruction, examples, a document) need them in the cache once.  Prefix g is
+ * len[g] tokens at places 0 .. len[g] - 1 of its own table row, pages of the same cache; it stands before the sequences first[g] ..
+ * first[g + 1] - 1, which lie next to one another.  Sequences below first[0] or from first[groups] on have no prefix.  What belongs to a sequence alone,
+ * its context and arena, stays as it is; the prefix' tokens come before them, so positions count on from it (dba_tree_norm.offset).
+ */
+typedef struct {
+    int32_t groups;            /* prefixes                                                                        */
+    int32_t max_pages;         /* pages per prefix: entries of a table row                                        */
+    const int32_t* first;      /* [groups + 1] not decreasing, within 0 .. B                                      */
+    const int32_t* len;        /* [groups] within 0 .. max_pages * page_size                                      */
+    const int32_t* table;      /* [groups] rows of max_pages page numbers, table_stride apart                     */
+    int64_t table_stride;
+} dba_tree_prefix;
+
+/*
+ * dba_tree_attend where every open row also sees the prefix of its sequence, if it has one:  out = sum_p softmax_p(scale <q, k_p>) v_p over
+ * prefix, context and the arena slots of its mask; lse likewise.  The prefix is read once for all rows of its sequences (once for 256
+ * of them on the tensor cores) and not once for each sequence.  A row's two parts, what is its own and the prefix, are joined by their
+ * log-sum-exps; its own part is rounded to the output's type before (half a unit of its share; the prefix' part and fp32 are not).
+ * scratch_dev: dba_tree_shared_bytes, 256-byte aligned, used until the call's work is done.  Calls that follow one another on the handle's
+ * stream may have the same; calls (or replays of graphs they were recorded into) that can overlap may not, nor may they the handle.
+ * first that decreases or leaves its range, or a length outside it, sets DBA_TREE_BAD_INDEX; the rows concerned are unspecified.
+ */
+dba_status dba_tree_shared_bytes(const dba_tree* h, size_t* bytes);
+dba_status dba_tree_attend_shared(dba_tree* h, const dba_tree_query* query, const dba_kv_cache* cache, const int32_t* table_dev,
+                                  int64_t table_stride, const int32_t* ctx_len_dev, const int32_t* masks_dev, const int32_t* top_dev,
+                                  const dba_tree_prefix* prefix, void* scratch_dev, size_t scratch_bytes);
+
+/* Norms of queries and keys.  Arrays of head_dim fp32; NULL: that side is not normed. */
+typedef struct {
+    const float* q_weight;
+    const float* k_weight;
+    float eps;
+    const int32_t* offset;     /* optional, [B]: added to the positions (those >= 0) of the sequence's tokens: a prefix' length,
+                                  or how many tokens of it have been evicted                                     */
+} dba_tree_norm;
+
+/*
+ * dba_tree_append for decoders that norm every head's queries and keys before the rotation:  x <- x / sqrt(mean(x^2) + eps) * weight over
+ * the head's dimensions, then the rotation, then the cache (keys) or q_out (queries): one pass, in fp32, rounded once at the end.
+ */
+dba_status dba_tree_append_norm(dba_tree* h, const dba_tree_tokens* tokens, const dba_tree_norm* norm, const dba_kv_cache* cache,
+                                const int32_t* table_dev, int64_t table_stride);
+
+/*
+ * The weight that context tokens receive from attention, one layer:
+ *     weight_out[b, kh, p] = decay * weight_in[b, kh, p] + sum exp(scale <q, k_p> - lse)     for p < ctx_len[b]
+ * over the open rows of the sequence and the query heads of key head kh.  lse is dba_tree_attend's (or ..._shared's) of the same
+ * queries; a row whose lse is -inf is closed and counts nothing, whatever its query holds.  query->out and query->lse are not used.
+ * weight_in may be NULL (zeros) and may be weight_out; element (b, kh, p) at base + b * seq_stride + kh * head_stride + p; places from
+ * ctx_len on are left as they are.  A place on a page outside the cache receives nothing.
+ */
+dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float* lse_dev, const dba_kv_cache* cache, const int32_t* table_dev,
+                          int64_t table_stride, const int32_t* ctx_len_dev, const float* weight_in, float* weight_out, int64_t seq_stride,
+                          int64_t head_stride, float decay);
+
+/*
+ * Eviction: of a sequence whose context is longer than `keep`, every layer's every key head keeps its last `recent` tokens and, of the
+ * others, the keep - recent of the largest weight (of equal ones the earlier; NaN is less than any number), in their order, at
+ * context places 0 .. keep - 1; the rest is gone, and its pages are free from ceil((A + keep) / page_size) on.  A sequence that is not longer
+ * keeps its tokens.  Keys carry their rotation with them, so what is kept goes on having its position.
+ *   to_table: where what is kept goes: the sequence's own table (in place), or one whose entries are each either the own table's
+ *   entry at the same index or a page that no table of this call names otherwise.  In place the copies of a (layer, sequence, key head)
+ *   are made one after the other by one thread block; to other pages they spread over the machine.
+ *   weight, weight_out: [layers, B, kv_heads] rows, layer_stride, seq_stride and head_stride apart (alike in both); may be the same.
+ *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0.
+ *   kept: scratch and result, [layers, B, kv_heads, keep]: the old context places of what is kept, -1 beyond.
+ *   ctx_len_out, dropped: [B] optional: the new length, and the old less the new.  (ctx_len_out may be ctx_len.)
+ * 0 <= recent <= keep, keep >= 1.  A place on a page outside the cache is not copied (DBA_TREE_BAD_PAGE).
+ */
+typedef struct {
+    const float* weight;
+    float* weight_out;
+    int64_t layer_stride, seq_stride, head_stride;
+    int32_t keep, recent;
+    const int32_t* to_table;
+    int64_t to_table_stride;
+    int32_t* kept;
+    int32_t* ctx_len_out;
+    int32_t* dropped;
+} dba_tree_evicted;
+dba_status dba_tree_evict(dba_tree* h, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride, const int32_t* ctx_len_dev,
+                          const dba_tree_evicted* evict);
+
 /* The bits set since the last call (cleared by it).  Synchronises the stream. */
 dba_status dba_tree_status(dba_tree* h, uint32_t* bits);
 uint64_t dba_tree_launch_count(const dba_tree* h);

@@ -18,6 +18,7 @@ EXPORTS = ["dba_workspace_bytes", "dba_init", "dba_reset", "dba_step", "dba_step
            "dba_timing_enable", "dba_timing_read", "dba_counters", "dba_launch_count", "dba_test_hook", "dba_destroy", "dba_status_string", "dba_row_scan_scratch_bytes", "dba_row_scan",
            "dba_row_scan_static", "dba_row_scan_static_max_bytes", "dba_project_scan_scratch_bytes", "dba_project_scan",
            "dba_tree_workspace_bytes", "dba_tree_init", "dba_tree_append", "dba_tree_attend", "dba_tree_advance", "dba_tree_commit",
+           "dba_tree_shared_bytes", "dba_tree_attend_shared", "dba_tree_append_norm", "dba_tree_weigh", "dba_tree_evict",
            "dba_tree_status", "dba_tree_launch_count", "dba_tree_test_hook", "dba_tree_destroy"]
 
 
@@ -81,6 +82,11 @@ def lib():
         L.dba_tree_attend.argtypes = [vp, vp, vp, vp, C.c_int64, vp, vp, vp]
         L.dba_tree_advance.argtypes = [vp, C.c_int32, vp, C.c_int32, vp, vp, vp, C.c_int32, vp, C.c_int64, vp, vp]
         L.dba_tree_commit.argtypes = [vp, vp, vp, C.c_int64, vp, vp, vp]
+        L.dba_tree_shared_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+        L.dba_tree_attend_shared.argtypes = [vp, vp, vp, vp, C.c_int64, vp, vp, vp, vp, vp, C.c_size_t]
+        L.dba_tree_append_norm.argtypes = [vp, vp, vp, vp, vp, C.c_int64]
+        L.dba_tree_weigh.argtypes = [vp, vp, vp, vp, vp, C.c_int64, vp, vp, vp, C.c_int64, C.c_int64, C.c_float]
+        L.dba_tree_evict.argtypes = [vp, vp, vp, C.c_int64, vp, vp]
         L.dba_tree_status.argtypes = [vp, C.POINTER(C.c_uint32)]
         L.dba_tree_launch_count.argtypes = [vp]
         L.dba_tree_launch_count.restype = C.c_uint64

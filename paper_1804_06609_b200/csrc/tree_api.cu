@@ -88,9 +88,58 @@ dba_status check_cache(const dba_tree* h, const dba_kv_cache* c, const int32_t* 
     return DBA_OK;
 }
 
+// The handle's device for as long as a call takes, whichever is current.
+struct OnDevice {
+    int before = -1;
+    bool ok;
+    explicit OnDevice(int device) {
+        int now = -1;
+        ok = cudaGetDevice(&now) == cudaSuccess;
+        if (ok && now != device) {
+            ok = cudaSetDevice(device) == cudaSuccess;
+            before = now;
+        }
+    }
+    ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
 inline bool strides_ok(const dba_tree* h, int64_t a, int64_t b, int64_t c) {
     const int es = elem_size(h->c.dtype);
     return !((a * es) & 15) && !((b * es) & 15) && !((c * es) & 15);
+}
+
+// The scale in powers of two; 0 (all scores alike) as a number so small that the kernels may multiply -inf by it.
+inline float softmax_scale(float scale) {
+    const float x = (float)((double)scale * 1.4426950408889634);
+    return x == 0.f ? 1e-37f : x;
+}
+
+// The scratch of attention over shared prefixes; returns its size.
+size_t carve_prefix(const dba_tree* h, void* base, TreePrefix* a) {
+    TreeCarver cv{(char*)base};
+    const dba_tree_config& c = h->c;
+    const TreePrefixPlan p = plan_tree_prefix(c.dtype, c.head_dim, h->sm_count);
+    a->own_lse = cv.take<float>((size_t)c.B * c.rows * c.heads);
+    a->meta = cv.take<int4>((size_t)2 * p.grid);
+    a->part_ml = cv.take<float>((size_t)2 * p.grid * p.rows * 2);
+    a->part_o = cv.take<float>((size_t)2 * p.grid * p.rows * c.head_dim);
+    return (cv.off + 255) / 256 * 256;
+}
+
+// What dba_tree_append and dba_tree_append_norm look over, and the tokens as the kernels want them.
+dba_status check_tokens(const dba_tree* h, const dba_tree_tokens* t, dba_tree_tokens* out) {
+    if (!t->seq && t->N % h->c.B) return DBA_ERR_INVALID_ARG;
+    if (t->rot_dim < 0 || t->rot_dim > h->c.head_dim || (t->rot_dim & 1)) return DBA_ERR_INVALID_ARG;
+    if (t->position && t->rot_dim > 0 && (!t->cos || !t->sin || t->positions < 1)) return DBA_ERR_INVALID_ARG;
+    if (!aligned16(t->k) || !aligned16(t->v) || !strides_ok(h, t->k_token_stride, t->k_head_stride, 0) ||
+        !strides_ok(h, t->v_token_stride, t->v_head_stride, 0))
+        return DBA_ERR_UNSUPPORTED;
+    if (t->q && (!aligned16(t->q) || !aligned16(t->q_out) || !strides_ok(h, t->q_token_stride, t->q_head_stride, 0) ||
+                 !strides_ok(h, t->qo_token_stride, t->qo_head_stride, 0)))
+        return DBA_ERR_UNSUPPORTED;
+    *out = *t;
+    if (!out->position || out->rot_dim == 0) { out->position = nullptr; out->rot_dim = 0; out->cos = out->sin = nullptr; out->positions = 0; }
+    return DBA_OK;
 }
 
 inline dba_status launched(cudaError_t e) { return e == cudaSuccess ? DBA_OK : DBA_ERR_CUDA; }
@@ -126,6 +175,8 @@ dba_status dba_tree_init(const dba_tree_config* cfg, void* workspace_dev, size_t
     h->stream = (cudaStream_t)cuda_stream;
     cudaError_t e = configure_tree_attend();
     if (e == cudaSuccess) e = configure_tree_advance();
+    if (e == cudaSuccess) e = configure_tree_prefix();
+    if (e == cudaSuccess) e = configure_tree_weigh();
     if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 256 + 4 * kTreeTurns, h->stream);     // (the turns lie behind it)
     if (e != cudaSuccess) { delete h; return DBA_ERR_CUDA; }
     *out = h;
@@ -139,18 +190,9 @@ dba_status dba_tree_append(dba_tree* h, const dba_tree_tokens* t, const dba_kv_c
     TreePages pg;
     dba_status st = check_cache(h, cache, table_dev, table_stride, &pg);
     if (st != DBA_OK) return st;
-    if (!t->seq && t->N % h->c.B) return DBA_ERR_INVALID_ARG;
-    if (t->rot_dim < 0 || t->rot_dim > h->c.head_dim || (t->rot_dim & 1)) return DBA_ERR_INVALID_ARG;
-    if (t->position && t->rot_dim > 0 && (!t->cos || !t->sin || t->positions < 1)) return DBA_ERR_INVALID_ARG;
-    if (!aligned16(t->k) || !aligned16(t->v) || !strides_ok(h, t->k_token_stride, t->k_head_stride, 0) ||
-        !strides_ok(h, t->v_token_stride, t->v_head_stride, 0))
-        return DBA_ERR_UNSUPPORTED;
-    if (t->q && (!aligned16(t->q) || !aligned16(t->q_out) || !strides_ok(h, t->q_token_stride, t->q_head_stride, 0) ||
-                 !strides_ok(h, t->qo_token_stride, t->qo_head_stride, 0)))
-        return DBA_ERR_UNSUPPORTED;
+    dba_tree_tokens tt;
+    if ((st = check_tokens(h, t, &tt)) != DBA_OK) return st;
     int n = 0;
-    dba_tree_tokens tt = *t;
-    if (!tt.position || tt.rot_dim == 0) { tt.position = nullptr; tt.rot_dim = 0; tt.cos = tt.sin = nullptr; tt.positions = 0; }
     const cudaError_t e = launch_tree_append(tt, pg, cache->k, cache->v, h->c.B, h->c.heads, h->c.kv_heads, h->c.head_dim, h->c.dtype, h->stream, &n);
     h->launches += n;
     return launched(e);
@@ -173,8 +215,7 @@ dba_status dba_tree_attend(dba_tree* h, const dba_tree_query* q, const dba_kv_ca
     a.W = c.words; a.A = 32 * c.words; a.ctx_cap = (int32_t)h->ctx_cap;
     a.q_seq = q->q_seq_stride; a.q_row = q->q_row_stride; a.q_head = q->q_head_stride;
     a.o_seq = q->out_seq_stride; a.o_row = q->out_row_stride; a.o_head = q->out_head_stride;
-    a.scale_log2e = (float)((double)q->scale * 1.4426950408889634);
-    if (a.scale_log2e == 0.f) a.scale_log2e = 1e-37f;         // all scores alike; the kernels multiply -inf by it
+    a.scale_log2e = softmax_scale(q->scale);
     a.part_o = h->part_o; a.part_ml = h->part_ml; a.meta = h->meta; a.turns = h->turns;
     a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
     int n = 0;
@@ -215,6 +256,112 @@ dba_status dba_tree_commit(dba_tree* h, const dba_kv_cache* cache, const int32_t
     int n = 0;
     const cudaError_t e = launch_tree_commit(*cache, pg, h->c.B, h->c.kv_heads, h->c.head_dim, 32 * h->c.words, h->c.dtype, ctx_len_dev, src_dev,
                                              n_dev, h->stream, &n);
+    h->launches += n;
+    return launched(e);
+}
+
+dba_status dba_tree_append_norm(dba_tree* h, const dba_tree_tokens* t, const dba_tree_norm* norm, const dba_kv_cache* cache, const int32_t* table_dev,
+                                int64_t table_stride) {
+    if (!h || !t || !norm || t->N < 0 || !(norm->eps >= 0.f)) return DBA_ERR_INVALID_ARG;
+    if (t->N == 0) return DBA_OK;                              // (an empty array has no address)
+    if (!t->k || !t->v || !t->place || (t->q && !t->q_out)) return DBA_ERR_INVALID_ARG;
+    TreePages pg;
+    dba_status st = check_cache(h, cache, table_dev, table_stride, &pg);
+    if (st != DBA_OK) return st;
+    dba_tree_tokens tt;
+    if ((st = check_tokens(h, t, &tt)) != DBA_OK) return st;
+    const OnDevice on(h->device);
+    if (!on.ok) return DBA_ERR_CUDA;
+    int n = 0;
+    const cudaError_t e = launch_tree_append_norm(tt, *norm, pg, cache->k, cache->v, h->c.B, h->c.heads, h->c.kv_heads, h->c.head_dim, h->c.dtype, h->stream, &n);
+    h->launches += n;
+    return launched(e);
+}
+
+dba_status dba_tree_shared_bytes(const dba_tree* h, size_t* bytes) {
+    if (!h || !bytes) return DBA_ERR_INVALID_ARG;
+    TreePrefix a;
+    *bytes = carve_prefix(h, nullptr, &a);
+    return DBA_OK;
+}
+
+dba_status dba_tree_attend_shared(dba_tree* h, const dba_tree_query* q, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride,
+                                  const int32_t* ctx_len_dev, const int32_t* masks_dev, const int32_t* top_dev, const dba_tree_prefix* prefix,
+                                  void* scratch_dev, size_t scratch_bytes) {
+    if (!h || !q || !prefix || !prefix->first || !prefix->len || !prefix->table || prefix->groups < 1 || prefix->max_pages < 1 ||
+        prefix->table_stride < prefix->max_pages)
+        return DBA_ERR_INVALID_ARG;
+    if (prefix->groups > 1 << 20 || (int64_t)prefix->max_pages * h->c.page_size >= (int64_t)1 << 31) return DBA_ERR_UNSUPPORTED;
+    if (!scratch_dev || ((uintptr_t)scratch_dev & 255u)) return DBA_ERR_WORKSPACE;
+    TreePrefix a{};
+    if (scratch_bytes < carve_prefix(h, scratch_dev, &a)) return DBA_ERR_WORKSPACE;
+    const OnDevice on(h->device);
+    if (!on.ok) return DBA_ERR_CUDA;
+    dba_tree_query own = *q;
+    if (own.lse) a.own_lse = own.lse;
+    else own.lse = a.own_lse;
+    dba_status st = dba_tree_attend(h, &own, cache, table_dev, table_stride, ctx_len_dev, masks_dev, top_dev);      // (looks the arguments over)
+    if (st != DBA_OK) return st;
+    if ((st = check_cache(h, cache, prefix->table, h->c.max_pages, &a.pages)) != DBA_OK) return st;
+    const dba_tree_config& c = h->c;
+    a.pages.table_stride = prefix->table_stride; a.pages.max_pages = prefix->max_pages;
+    a.first = prefix->first; a.len = prefix->len; a.groups = prefix->groups; a.cap = prefix->max_pages * c.page_size;
+    a.k = cache->k; a.v = cache->v; a.q = q->q; a.out = q->out; a.masks = (const uint32_t*)masks_dev;
+    a.B = c.B; a.n = q->rows; a.H = c.heads; a.K = c.kv_heads; a.G = c.heads / c.kv_heads; a.D = c.head_dim; a.W = c.words;
+    a.q_seq = q->q_seq_stride; a.q_row = q->q_row_stride; a.q_head = q->q_head_stride;
+    a.o_seq = q->out_seq_stride; a.o_row = q->out_row_stride; a.o_head = q->out_head_stride;
+    a.scale_log2e = softmax_scale(q->scale);
+    a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
+    int n = 0;
+    const cudaError_t e = launch_tree_prefix(a, plan_tree_prefix(c.dtype, c.head_dim, h->sm_count), c.dtype, h->stream, &n);
+    h->launches += n;
+    return launched(e);
+}
+
+dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* q, const float* lse_dev, const dba_kv_cache* cache, const int32_t* table_dev,
+                          int64_t table_stride, const int32_t* ctx_len_dev, const float* weight_in, float* weight_out, int64_t seq_stride,
+                          int64_t head_stride, float decay) {
+    if (!h || !q || !q->q || !lse_dev || !ctx_len_dev || !weight_out || q->rows < 1 || q->rows > h->c.rows || q->scale != q->scale || decay != decay)
+        return DBA_ERR_INVALID_ARG;
+    if (seq_stride < 0 || head_stride < 0) return DBA_ERR_INVALID_ARG;
+    TreeWeigh a{};
+    const dba_status st = check_cache(h, cache, table_dev, table_stride, &a.pages);
+    if (st != DBA_OK) return st;
+    if (!aligned16(q->q) || !strides_ok(h, q->q_seq_stride, q->q_row_stride, q->q_head_stride)) return DBA_ERR_UNSUPPORTED;
+    const OnDevice on(h->device);
+    if (!on.ok) return DBA_ERR_CUDA;
+    const dba_tree_config& c = h->c;
+    a.k = cache->k; a.q = q->q; a.lse = lse_dev; a.in = weight_in; a.out = weight_out; a.ctx_len = ctx_len_dev;
+    a.B = c.B; a.n = q->rows; a.H = c.heads; a.K = c.kv_heads; a.G = c.heads / c.kv_heads; a.D = c.head_dim; a.A = 32 * c.words;
+    a.ctx_cap = (int32_t)h->ctx_cap;
+    a.q_seq = q->q_seq_stride; a.q_row = q->q_row_stride; a.q_head = q->q_head_stride; a.w_seq = seq_stride; a.w_head = head_stride;
+    a.scale_log2e = softmax_scale(q->scale); a.decay = decay;
+    a.wait_clocks = h->wait_clocks; a.drop_item = h->drop_item;
+    int n = 0;
+    const cudaError_t e = launch_tree_weigh(a, c.dtype, h->sm_count, h->stream, &n);
+    h->launches += n;
+    return launched(e);
+}
+
+dba_status dba_tree_evict(dba_tree* h, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride, const int32_t* ctx_len_dev,
+                          const dba_tree_evicted* ev) {
+    if (!h || !ctx_len_dev || !ev || !ev->weight || !ev->weight_out || !ev->to_table || !ev->kept || ev->keep < 1 || ev->recent < 0 || ev->recent > ev->keep)
+        return DBA_ERR_INVALID_ARG;
+    if (ev->layer_stride < 0 || ev->seq_stride < 0 || ev->head_stride < 0) return DBA_ERR_INVALID_ARG;
+    TreeEvict a{};
+    dba_status st = check_cache(h, cache, table_dev, table_stride, &a.from);
+    if (st == DBA_OK) st = check_cache(h, cache, ev->to_table, ev->to_table_stride, &a.to);
+    if (st != DBA_OK) return st;
+    if ((int64_t)cache->layers * h->c.B * h->c.kv_heads >= (int64_t)1 << 27) return DBA_ERR_UNSUPPORTED;       // (blocks of a grid)
+    const OnDevice on(h->device);
+    if (!on.ok) return DBA_ERR_CUDA;
+    a.k = (char*)cache->k; a.v = (char*)cache->v;
+    a.es = elem_size(h->c.dtype);
+    a.layer_bytes = cache->layer_stride * a.es;
+    a.layers = cache->layers; a.B = h->c.B; a.K = h->c.kv_heads; a.D = h->c.head_dim; a.A = 32 * h->c.words; a.ctx_cap = (int32_t)h->ctx_cap;
+    a.sm_count = h->sm_count; a.ctx_len = ctx_len_dev; a.e = *ev;
+    int n = 0;
+    const cudaError_t e = launch_tree_evict(a, h->stream, &n);
     h->launches += n;
     return launched(e);
 }

@@ -87,6 +87,113 @@ __global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_t
     }
 }
 
+// The same for decoders that norm queries and keys: y = x / sqrt(mean(x^2) + eps) * weight per head, then the rotation.  A head is
+// the work of L lanes next to one another (the power of two from D/(2 VEC) up, 32 at most), which hold its UNITS units each in registers between
+// the sum of squares and the turn; a thread keeps the same dimensions from head to head, so weights, cosines and sines are read once a token.
+// Sum, norm and turn are fp32; the one rounding is the store's.
+template <typename T, int VEC, bool PAIRS, int UNITS>
+__global__ void __launch_bounds__(kAThreads) tree_append_norm_kernel(const dba_tree_tokens t, const dba_tree_norm nm, const TreePages pg, T* ck, T* cv, int B,
+                                                                     int H, int K, int D, int lanes) {
+    using P = TreePack<T, VEC>;
+    grid_dependency_wait();
+    allow_dependents();
+    const int tok = blockIdx.x;
+    const int b = t.seq ? __ldg(t.seq + tok) : tok / (t.N / B);
+    const int place = __ldg(t.place + tok);
+    int pos = t.position ? __ldg(t.position + tok) : -1;
+    int64_t row = -1;
+    bool bad = false;
+    if ((unsigned)b < (unsigned)B) {
+        if (place >= 0) {
+            row = tree_row(pg, b, place);
+            bad = row < 0;
+        }
+        if (pos >= 0 && nm.offset) {
+            const int64_t moved = (int64_t)pos + __ldg(nm.offset + b);
+            if (moved < 0 || moved >= t.positions) bad = true;
+            pos = moved < 0 || moved >= t.positions ? -1 : (int)moved;
+        }
+    } else bad = true;
+    if (pos >= t.positions) { bad = bad || t.cos; pos = -1; }
+    if (bad && threadIdx.x == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
+    const int half = t.rot_dim / 2, per = D / (2 * VEC), turned = half / VEC;
+    const int sub = threadIdx.x / lanes, lane = threadIdx.x - sub * lanes, heads_at = blockDim.x / lanes;
+    int d0[UNITS], d1[UNITS];
+    float cs[UNITS][VEC], sn[UNITS][VEC];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const int j = lane + u * lanes;
+        d0[u] = j < turned ? (PAIRS ? 2 * j * VEC : j * VEC) : t.rot_dim + 2 * (j - turned) * VEC;
+        d1[u] = j < turned && !PAIRS ? d0[u] + half : d0[u] + VEC;
+        const bool turn = pos >= 0 && j < turned;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            cs[u][i] = turn ? __ldg(t.cos + (int64_t)pos * half + j * VEC + i) : 1.f;
+            sn[u][i] = turn ? __ldg(t.sin + (int64_t)pos * half + j * VEC + i) : 0.f;
+        }
+        if (j >= per) d0[u] = -1;
+    }
+    // the heads of one kind: queries, keys
+    const auto heads = [&](const T* src, int64_t src_head, T* dst, int64_t dst_head, int n, const float* weight) {
+        float w0[UNITS][VEC], w1[UNITS][VEC];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                w0[u][i] = weight && d0[u] >= 0 ? __ldg(weight + d0[u] + i) : 1.f;
+                w1[u][i] = weight && d0[u] >= 0 ? __ldg(weight + d1[u] + i) : 1.f;
+            }
+        const float inv_d = 1.f / (float)D;
+#pragma unroll 1
+        for (int h0 = 0; h0 < n; h0 += heads_at) {
+            const int h = h0 + sub;
+            P x[UNITS], y[UNITS];
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                if (h >= n || d0[u] < 0) continue;
+                x[u] = *reinterpret_cast<const P*>(src + (int64_t)h * src_head + d0[u]);
+                y[u] = *reinterpret_cast<const P*>(src + (int64_t)h * src_head + d1[u]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float p = tree_widen(x[u].x[i]), q = tree_widen(y[u].x[i]);
+                    sum = fmaf(p, p, sum); sum = fmaf(q, q, sum);
+                }
+            }
+            for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
+            const float r = weight ? rsqrtf(fmaf(sum, inv_d, nm.eps)) : 1.f;
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                if (h >= n || d0[u] < 0) continue;
+                float e[2 * VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) { e[i] = tree_widen(x[u].x[i]) * r * w0[u][i]; e[VEC + i] = tree_widen(y[u].x[i]) * r * w1[u][i]; }
+                float f[2 * VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    // PAIRS: elements 2i, 2i+1 of the 2 VEC neighbours; else element i of either pack
+                    const int k0 = PAIRS ? 2 * i : i, k1 = PAIRS ? 2 * i + 1 : VEC + i;
+                    f[k0] = fmaf(e[k0], cs[u][i], -(e[k1] * sn[u][i]));
+                    f[k1] = fmaf(e[k1], cs[u][i], e[k0] * sn[u][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) { tree_narrow(f[i], &x[u].x[i]); tree_narrow(f[VEC + i], &y[u].x[i]); }
+                *reinterpret_cast<P*>(dst + (int64_t)h * dst_head + d0[u]) = x[u];
+                *reinterpret_cast<P*>(dst + (int64_t)h * dst_head + d1[u]) = y[u];
+            }
+        }
+    };
+    if (t.q) heads((const T*)t.q + (int64_t)tok * t.q_token_stride, t.q_head_stride, (T*)t.q_out + (int64_t)tok * t.qo_token_stride, t.qo_head_stride, H, nm.q_weight);
+    if (row < 0) return;
+    heads((const T*)t.k + (int64_t)tok * t.k_token_stride, t.k_head_stride, ck + row, pg.head_stride, K, nm.k_weight);
+    const int chunks = D * (int)sizeof(T) / 16;
+    for (int u = threadIdx.x; u < K * chunks; u += blockDim.x) {
+        const int h = u / chunks, ch = u - h * chunks;
+        *reinterpret_cast<uint4*>((char*)(cv + row + (int64_t)h * pg.head_stride) + ch * 16) =
+            *reinterpret_cast<const uint4*>((const char*)((const T*)t.v + (int64_t)tok * t.v_token_stride + (int64_t)h * t.v_head_stride) + ch * 16);
+    }
+}
+
 // A block per (sequence, layer, keys or values).  The places of up to kCThreads tokens are looked up first, one to a thread,
 // so that the chain of loads to a place (slot, page) is gone through once and not for every 16 bytes; then a thread has
 // kCopies copies of 16 bytes in the air.
@@ -159,6 +266,43 @@ cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, vo
            : vec == 4 ? launch_append_v<__nv_bfloat16, 4>(t, pg, k, v, B, H, K, D, st)
            : vec == 2 ? launch_append_v<__nv_bfloat16, 2>(t, pg, k, v, B, H, K, D, st)
                       : launch_append_v<__nv_bfloat16, 1>(t, pg, k, v, B, H, K, D, st);
+}
+
+namespace {
+template <typename T, int VEC, int UNITS>
+cudaError_t launch_norm_u(const dba_tree_tokens& t, const dba_tree_norm& nm, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, int lanes, cudaStream_t st) {
+    const int threads = t.N >= 2048 ? 64 : kAThreads;
+    return t.pairs ? launch_after(tree_append_norm_kernel<T, VEC, true, UNITS>, dim3(t.N), dim3(threads), 0, st, t, nm, pg, (T*)k, (T*)v, B, H, K, D, lanes)
+                   : launch_after(tree_append_norm_kernel<T, VEC, false, UNITS>, dim3(t.N), dim3(threads), 0, st, t, nm, pg, (T*)k, (T*)v, B, H, K, D, lanes);
+}
+template <typename T, int VEC>
+cudaError_t launch_norm_v(const dba_tree_tokens& t, const dba_tree_norm& nm, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, cudaStream_t st) {
+    const int per = D / (2 * VEC);
+    int lanes = 1;
+    while (lanes < 32 && lanes < per) lanes *= 2;
+    // (a head of 256 in units of 2 VEC: up to 128 / VEC units)
+    if (per <= 32) return launch_norm_u<T, VEC, 1>(t, nm, pg, k, v, B, H, K, D, lanes, st);
+    if constexpr (VEC <= 2) {
+        if (per <= 64) return launch_norm_u<T, VEC, 2>(t, nm, pg, k, v, B, H, K, D, lanes, st);
+        if constexpr (VEC == 1) return launch_norm_u<T, VEC, 4>(t, nm, pg, k, v, B, H, K, D, lanes, st);
+    }
+    return cudaErrorInvalidValue;
+}
+}  // namespace
+
+cudaError_t launch_tree_append_norm(const dba_tree_tokens& t, const dba_tree_norm& norm, const TreePages& pg, void* k, void* v, int32_t B, int32_t H,
+                                    int32_t K, int32_t D, int dtype, cudaStream_t st, int* launches) {
+    *launches += 1;
+    const int half = t.rot_dim / 2, rest = (D - t.rot_dim) / 2;       // (packs as above)
+    int vec = dtype == DBA_F32 ? 4 : 8;
+    while (half % vec || rest % vec) vec >>= 1;
+    if (dtype == DBA_F32)
+        return vec == 4 ? launch_norm_v<float, 4>(t, norm, pg, k, v, B, H, K, D, st) : vec == 2 ? launch_norm_v<float, 2>(t, norm, pg, k, v, B, H, K, D, st)
+                                                                                              : launch_norm_v<float, 1>(t, norm, pg, k, v, B, H, K, D, st);
+    return vec == 8   ? launch_norm_v<__nv_bfloat16, 8>(t, norm, pg, k, v, B, H, K, D, st)
+           : vec == 4 ? launch_norm_v<__nv_bfloat16, 4>(t, norm, pg, k, v, B, H, K, D, st)
+           : vec == 2 ? launch_norm_v<__nv_bfloat16, 2>(t, norm, pg, k, v, B, H, K, D, st)
+                      : launch_norm_v<__nv_bfloat16, 1>(t, norm, pg, k, v, B, H, K, D, st);
 }
 
 cudaError_t launch_tree_commit(const dba_kv_cache& c, const TreePages& pg, int32_t B, int32_t K, int32_t D, int32_t A, int dtype,

@@ -1,0 +1,205 @@
+// Eviction of context tokens by the weight they have received: which ones stay, and their keys and values to the front.
+//
+// For every (layer, sequence, key head) with L > keep tokens: the last `recent` of them and, of the others, the m = keep - recent of the
+// largest weight.  Weights become whole numbers in the same order (ord32; NaN: 0); the m-th largest is found by its digits, the
+// highest first, from histograms in shared memory; a last pass keeps what is above it and the first ones at it, in order, by a
+// prefix sum.  Everything is decided by counts, so equal inputs give equal results.
+//
+// Copies: row i of what is kept comes from place kept[i] >= i.  Other pages: any order.  The same pages: rows in ascending order, each
+// batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.
+#include "tree_device.cuh"
+
+namespace dba {
+
+namespace {
+
+constexpr int kEThreads = 512, kEWarps = kEThreads / 32, kEBins = 2048;
+constexpr int kMThreads = 256, kMRowsAt = 256, kMCopies = 8;
+
+// larger weight, larger number; NaN is less than any
+__device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : ord32(w); }
+
+struct ESmem {
+    uint32_t bins[kEBins];
+    int sums[2][kEWarps];
+    int digit, above;
+};
+
+// A block per (layer, sequence, key head), the last counting fastest.
+__global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a) {
+    __shared__ ESmem sm;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int h = (int)(blockIdx.x % a.K), b = (int)(blockIdx.x / a.K % a.B), l = (int)(blockIdx.x / a.K / a.B);
+    grid_dependency_wait();
+    allow_dependents();
+    const int L = min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap), keep = a.e.keep, n = min(L, keep);
+    const int64_t row = (int64_t)l * a.e.layer_stride + (int64_t)b * a.e.seq_stride + (int64_t)h * a.e.head_stride;
+    const float* w = a.e.weight + row;
+    float* out = a.e.weight_out + row;
+    int32_t* kept = a.e.kept + (((int64_t)l * a.B + b) * a.K + h) * keep;
+    for (int i = n + tid; i < keep; i += kEThreads) kept[i] = -1;
+    if (L <= keep) {
+        for (int i = tid; i < L; i += kEThreads) {
+            kept[i] = i;
+            out[i] = w[i];
+        }
+        return;
+    }
+    const int old = L - min(a.e.recent, keep);               // places that have to earn it
+    int m = keep - (L - old);                              // how many of them stay: less than there are
+    uint32_t bar = 0xffffffffu;
+    if (m > 0) {
+        uint32_t prefix = 0;                               // the digits found, and how many of those with them stay
+        int shift = 32;
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) {
+            const int bits = pass == 2 ? 10 : 11;
+            const uint32_t known = shift == 32 ? 0u : ~0u << shift;
+            shift -= bits;
+            for (int i = tid; i < kEBins; i += kEThreads) sm.bins[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < old; i += kEThreads) {
+                const uint32_t key = weight_key(w[i]);
+                if ((key & known) == prefix) atomicAdd(&sm.bins[(key >> shift) & ((1u << bits) - 1u)], 1u);
+            }
+            __syncthreads();
+            // from the largest digit down: a thread has bins 4 tid' .. 4 tid' + 3, tid' counted from the top
+            constexpr int per = kEBins / kEThreads;
+            const int top = kEBins - 1 - per * tid;
+            int c[per], sum = 0;
+#pragma unroll
+            for (int i = 0; i < per; ++i) { c[i] = (int)sm.bins[top - i]; sum += c[i]; }
+            int pre = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(kFullMask, pre, o);
+                if (lane >= o) pre += v;
+            }
+            if (lane == 31) sm.sums[0][warp] = pre;
+            __syncthreads();
+            int before = pre - sum;
+            for (int i = 0; i < warp; ++i) before += sm.sums[0][i];
+#pragma unroll
+            for (int i = 0; i < per; ++i) {
+                if (before < m && before + c[i] >= m) { sm.digit = top - i; sm.above = before; }
+                before += c[i];
+            }
+            __syncthreads();
+            prefix |= (uint32_t)sm.digit << shift;
+            m -= sm.above;                                 // of those with this digit, m stay
+            __syncthreads();
+        }
+        bar = prefix;
+    }
+    // m of the keys at the bar stay, the first ones
+    int n_above = 0, n_at = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < L; i0 += kEThreads) {
+        const int i = i0 + tid;
+        const float x = i < L ? w[i] : 0.f;
+        const uint32_t key = weight_key(x);
+        const bool above = i < L && (i >= old || (bar != 0xffffffffu && key > bar)), at = i < old && bar != 0xffffffffu && key == bar;
+        const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at);
+        if (lane == 0) { sm.sums[0][warp] = __popc(u); sm.sums[1][warp] = __popc(e); }
+        __syncthreads();                                   // (and the weights of this batch have been read)
+        int before_u = n_above + __popc(u & ((1u << lane) - 1u)), before_e = n_at + __popc(e & ((1u << lane) - 1u));
+#pragma unroll
+        for (int j = 0; j < kEWarps; ++j) {
+            if (j < warp) { before_u += sm.sums[0][j]; before_e += sm.sums[1][j]; }
+            n_above += sm.sums[0][j]; n_at += sm.sums[1][j];
+        }
+        if (above || (at && before_e < m)) {
+            const int to = before_u + min(before_e, m);
+            kept[to] = i;
+            out[to] = x;
+        }
+        __syncthreads();
+    }
+    for (int i = n + tid; i < L; i += kEThreads) out[i] = 0.f;
+}
+
+// Blocks: keys or values, layer, sequence, key head, split, the last counting fastest.
+__global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a, int splits) {
+    __shared__ int64_t from_at[kMRowsAt], to_at[kMRowsAt];
+    const int tid = threadIdx.x, split = (int)(blockIdx.x % splits);
+    unsigned at = blockIdx.x / splits;
+    const int h = (int)(at % a.K);
+    at /= a.K;
+    const int b = (int)(at % a.B);
+    at /= a.B;
+    const int l = (int)(at % a.layers);
+    const bool values = at >= (unsigned)a.layers;
+    grid_dependency_wait();
+    allow_dependents();
+    const int keep = a.e.keep;
+    if (split == 0 && h == 0 && l == 0 && !values && tid == 0) {
+        const int L = min(max(a.ctx_len[b], 0), a.ctx_cap);
+        if (a.e.dropped) a.e.dropped[b] = L - min(L, keep);
+        if (a.e.ctx_len_out) a.e.ctx_len_out[b] = min(L, keep);
+    }
+    // pages that stay the same: one block, in order
+    const unsigned first_page = tree_page(a.from, (unsigned)a.A), pages = tree_page(a.from, (unsigned)(a.A + min(keep, a.ctx_cap) - 1)) + 1;
+    bool same = false;
+    for (unsigned i = first_page + tid; i < pages; i += kMThreads)
+        same = same || __ldg(a.to.table + (int64_t)b * a.to.table_stride + i) == __ldg(a.from.table + (int64_t)b * a.from.table_stride + i);
+    same = __syncthreads_or(same);
+    if (same && split > 0) return;
+    const int chunks = a.D * a.es / 16;
+    const int32_t* kept = a.e.kept + (((int64_t)l * a.B + b) * a.K + h) * keep;
+    char* base = (values ? a.v : a.k) + l * a.layer_bytes + (int64_t)h * a.from.head_stride * a.es;
+    const int step = same ? kMRowsAt : kMRowsAt * splits;
+    for (int i0 = split * kMRowsAt; i0 < keep; i0 += step) {
+        const int rows = min(kMRowsAt, keep - i0);
+        __syncthreads();
+        bool any = false;
+        if (tid < rows) {
+            const int src = __ldg(kept + i0 + tid);
+            int64_t r0 = -1, r1 = -1;
+            if (src >= 0) {
+                r0 = tree_row(a.from, b, a.A + src);
+                r1 = tree_row(a.to, b, a.A + i0 + tid);
+                any = true;
+            }
+            const bool skip = r0 < 0 || r1 < 0 || r0 == r1;
+            from_at[tid] = skip ? -1 : r0 * a.es; to_at[tid] = r1 * a.es;
+        }
+        if (!__syncthreads_or(any)) break;                 // (what is kept is at the front)
+        const int units = rows * chunks;
+        for (int u0 = 0; u0 < units; u0 += kMCopies * kMThreads) {
+            uint4 x[kMCopies];
+            char* to[kMCopies];
+#pragma unroll
+            for (int c = 0; c < kMCopies; ++c) {
+                const int u = u0 + tid + c * kMThreads;
+                to[c] = nullptr;
+                if (u < units) {
+                    const int i = u / chunks, ch = u - i * chunks;
+                    if (from_at[i] >= 0) {
+                        x[c] = *reinterpret_cast<const uint4*>(base + from_at[i] + ch * 16);
+                        to[c] = base + to_at[i] + ch * 16;
+                    }
+                }
+            }
+            if (same) __syncthreads();                     // the batch has been read
+#pragma unroll
+            for (int c = 0; c < kMCopies; ++c)
+                if (to[c]) *reinterpret_cast<uint4*>(to[c]) = x[c];
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches) {
+    cudaError_t e = launch_after(tree_keep_kernel, dim3((unsigned)(a.K * a.B * a.layers)), dim3(kEThreads), 0, st, a);
+    *launches += 1;
+    if (e != cudaSuccess) return e;
+    // some eight blocks an SM, none without a batch of rows
+    const int64_t rows = (int64_t)a.K * a.B * a.layers * 2;
+    const int most = (a.e.keep + kMRowsAt - 1) / kMRowsAt, want = (int)((8LL * a.sm_count + rows - 1) / rows), splits = want < most ? want : most;
+    e = launch_after(tree_move_kernel, dim3((unsigned)(rows * splits)), dim3(kMThreads), 0, st, a, splits);
+    *launches += 1;
+    return e;
+}
+
+}  // namespace dba

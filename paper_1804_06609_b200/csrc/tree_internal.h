@@ -77,6 +77,55 @@ struct TreeAdvance {
     dba_tree_next next;
     uint32_t* status;
 };
+// Attention over prefixes that sequences share, joined with the rows' own part.
+struct TreePrefix {
+    TreePages pages;                   // of the prefixes' table
+    const int32_t *first, *len;
+    int32_t groups, cap;               // prefixes, places that a table row holds
+    const void *k, *v, *q;
+    void* out;                         // the rows' own part, and then their whole
+    float* own_lse;                    // [B, n, H] of the own part, and then of the whole
+    const uint32_t* masks;             // null: every row is open
+    int32_t B, n, H, K, G, D, W;       // G = H / K query heads per key head
+    int64_t q_seq, q_row, q_head, o_seq, o_row, o_head;
+    float scale_log2e;
+    float* part_o;                     // [2 * grid][item rows][D]: first and last pieces of a block's run that are part of an item
+    float* part_ml;                    // [2 * grid][item rows][2]: maximum (powers of two) and sum
+    int4* meta;                        // [2 * grid] prefix, key head and block of rows of the piece there (x = -1: none, -2: the block gave up)
+    long long wait_clocks;
+    int drop_item;
+};
+struct TreePrefixPlan { int grid, rows; bool tensor; };        // blocks of the kernel, rows of an item
+TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count);
+cudaError_t configure_tree_prefix();
+cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches);
+
+// The weight that context tokens receive.
+struct TreeWeigh {
+    TreePages pages;
+    const void *k, *q;
+    const float *lse, *in;
+    float* out;
+    const int32_t* ctx_len;
+    int32_t B, n, H, K, G, D, A, ctx_cap;
+    int64_t q_seq, q_row, q_head, w_seq, w_head;
+    float scale_log2e, decay;
+    long long wait_clocks;
+    int drop_item;
+};
+cudaError_t configure_tree_weigh();
+cudaError_t launch_tree_weigh(const TreeWeigh& a, int dtype, int sm_count, cudaStream_t st, int* launches);
+struct TreeEvict {
+    TreePages from, to;
+    char *k, *v;
+    int64_t layer_bytes;
+    int32_t es, layers, B, K, D, A, ctx_cap, sm_count;
+    const int32_t* ctx_len;
+    dba_tree_evicted e;
+};
+cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches);
+cudaError_t launch_tree_append_norm(const dba_tree_tokens& t, const dba_tree_norm& norm, const TreePages& pg, void* k, void* v, int32_t B, int32_t H,
+                                    int32_t K, int32_t D, int dtype, cudaStream_t st, int* launches);
 cudaError_t configure_tree_advance();
 cudaError_t launch_tree_advance(const TreeAdvance& a, cudaStream_t st, int* launches);
 

@@ -37,17 +37,34 @@ class TreeNext(C.Structure):
     _fields_ = [(f, C.c_void_p) for f in ("masks", "slot", "position", "ctx_len", "top", "commit_src", "commit_n")]
 
 
+class TreePrefix(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("max_pages", C.c_int32), ("first", C.c_void_p), ("len", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64)]
+
+
+class TreeNorm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("offset", C.c_void_p)]
+
+
+class TreeEvicted(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("weight_out", C.c_void_p), ("layer_stride", C.c_int64), ("seq_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("keep", C.c_int32), ("recent", C.c_int32), ("to_table", C.c_void_p), ("to_table_stride", C.c_int64), ("kept", C.c_void_p),
+                ("ctx_len_out", C.c_void_p), ("dropped", C.c_void_p)]
+
+
 class TokenTree:
     """Owns a dba_tree handle and its workspace.  Caches, tables, masks and lengths are the caller's tensors:
-    k, v [pages, page_size, kv_heads, head_dim] (any strides with a unit inner one; both alike; commit: a leading layer
+    k, v [pages, page_size, kv_heads, head_dim] (any strides with a unit inner one; both alike; commit and evict: a leading layer
     dimension), table [B, max_pages] int32, masks [B, rows, words] int32, ctx_len [B] int32.
+
+    prefixes: the most prefixes a call of attend_shared may have; 0: none, and the handle holds no scratch for it.
 
     Calls are short (a few microseconds of work each at the smallest sizes), so the argument structures are made once and
     filled in by each call; calls on one handle must not overlap."""
 
-    def __init__(self, B, rows, heads, kv_heads, head_dim, page_size, max_pages, words, dtype=BF16, device="cuda:0", stream=None):
+    def __init__(self, B, rows, heads, kv_heads, head_dim, page_size, max_pages, words, dtype=BF16, device="cuda:0", stream=None, prefixes=0):
         import torch
         self.torch = torch
+        self.prefixes = prefixes
         self.B, self.rows, self.heads, self.kv_heads, self.head_dim = B, rows, heads, kv_heads, head_dim
         self.page_size, self.max_pages, self.words, self.dtype = page_size, max_pages, words, dtype
         self.torch_dtype = torch.float32 if dtype == F32 else torch.bfloat16
@@ -70,6 +87,13 @@ class TokenTree:
                 self.out = torch.empty(B, rows, heads, head_dim, dtype=self.torch_dtype, device=self.device)
                 self.q_out = torch.empty(B * rows, heads, head_dim, dtype=self.torch_dtype, device=self.device)
                 self._next = [self.new_next(), self.new_next()] if words else []
+                if prefixes:
+                    _check(L.dba_tree_shared_bytes(h, C.byref(n)), "dba_tree_shared_bytes")
+                    self._scratch_bytes = n.value
+                    self.scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+                    self._scratch_at = (self.scratch.data_ptr() + 255) // 256 * 256
+        self._prefix, self._norm = TreePrefix(), TreeNorm()
+        self._prefix_ref, self._norm_ref = C.byref(self._prefix), C.byref(self._norm)
         self._next = [(x, self._next_struct(x)) for x in self._next]
         self._turn = 0
         self._f_append, self._f_attend, self._f_advance, self._f_commit = L.dba_tree_append, L.dba_tree_attend, L.dba_tree_advance, L.dba_tree_commit
@@ -137,11 +161,13 @@ class TokenTree:
             raise ValueError("table: rows of a unit stride")
         return s[0] if self.B > 1 else self.max_pages
 
-    def append(self, new_k, new_v, k, v, table, place, position=None, rotary=None, pairs=False, q=None, seq=None, q_out=None):
+    def append(self, new_k, new_v, k, v, table, place, position=None, rotary=None, pairs=False, q=None, seq=None, q_out=None, norm=None, offset=None):
         """new_k, new_v [N, kv_heads, head_dim] into the cache at `place` [N] of sequence `seq` [N] (None: N / B tokens to a
         sequence, in order), keys rotated by `position` [N] with rotary = (cos, sin) [positions, rot / 2] fp32.  Rotates
         q [N, heads, head_dim] too and returns it (q_out: where to; may be q; default: the handle's own buffer for up to
-        B * rows tokens, overwritten by the next call, or a new tensor)."""
+        B * rows tokens, overwritten by the next call, or a new tensor).
+        norm = (q_weight, k_weight, eps), weights [head_dim] fp32 or None: every head's queries and keys are normed before the rotation
+        (root mean square).  offset [B] int32: added to the positions of the sequence's tokens."""
         dt, dev, t, shape = self.torch_dtype, self._dev, self._tok, new_k.shape
         N, _, D = shape
         sk, sv = new_k.stride(), new_v.stride()
@@ -180,10 +206,25 @@ class TokenTree:
             t.position = t.cos = t.sin = None
             t.positions = t.rot_dim = t.pairs = 0
         stride = self._table(table)
-        code = self._f_append(self._h, self._tok_ref, self._cache(k, v, 0), table.data_ptr(), stride)
+        if norm is None and offset is None:
+            code = self._f_append(self._h, self._tok_ref, self._cache(k, v, 0), table.data_ptr(), stride)
+            if code:
+                _check(code, "dba_tree_append")
+            return q_out
+        nm = self._norm
+        nm.q_weight, nm.k_weight, nm.eps = (self._weight(norm[0]), self._weight(norm[1]), norm[2]) if norm is not None else (None, None, 0.0)
+        nm.offset = None if offset is None else self._i32(offset, self.B, "offset: int32 [B]")
+        code = lib().dba_tree_append_norm(self._h, self._tok_ref, self._norm_ref, self._cache(k, v, 0), table.data_ptr(), stride)
         if code:
-            _check(code, "dba_tree_append")
+            _check(code, "dba_tree_append_norm")
         return q_out
+
+    def _weight(self, w):
+        if w is None:
+            return None
+        if w.dtype is not self._f32t or w.get_device() != self._dev or w.shape != (self.head_dim,) or not w.is_contiguous():
+            raise ValueError("norm: (q_weight, k_weight, eps), weights [head_dim] fp32 on the handle's device or None")
+        return w.data_ptr()
 
     def _q_out(self, N):
         if N <= self.B * self.rows:
@@ -192,7 +233,7 @@ class TokenTree:
         with torch.cuda.stream(self.stream):         # (the allocator gives freed memory out by stream)
             return torch.empty(N, self.heads, self.head_dim, dtype=self.torch_dtype, device=self.device)
 
-    def attend(self, q, k, v, table, ctx_len, masks=None, top=None, scale=None, out=None, lse=None):
+    def attend(self, q, k, v, table, ctx_len, masks=None, top=None, scale=None, out=None, lse=None, _shared=None):
         """q [B, rows, heads, head_dim] (rows up to the handle's) over the context and the arena slots of `masks`; returns out
         (default: the handle's own buffer, overwritten by the next call)."""
         B, d, dt, dev, shape, sq = self.B, self._query, self.torch_dtype, self._dev, q.shape, q.stride()
@@ -215,12 +256,36 @@ class TokenTree:
             d.lse = lse.data_ptr()
         d.q, d.out, d.scale = q.data_ptr(), out.data_ptr(), self.head_dim ** -0.5 if scale is None else scale
         stride = self._table(table)
-        code = self._f_attend(self._h, self._query_ref, self._cache(k, v, 0), table.data_ptr(), stride, self._i32(ctx_len, B, "ctx_len: int32 [B]"),
-                              None if masks is None else self._i32(masks, B * n * self.words, "masks: int32 [B, rows, words]"),
-                              None if top is None else self._i32(top, B, "top: int32 [B]"))
+        code = (self._f_attend if _shared is None else _shared)(
+            self._h, self._query_ref, self._cache(k, v, 0), table.data_ptr(), stride, self._i32(ctx_len, B, "ctx_len: int32 [B]"),
+            None if masks is None else self._i32(masks, B * n * self.words, "masks: int32 [B, rows, words]"),
+            None if top is None else self._i32(top, B, "top: int32 [B]"))
         if code:
-            _check(code, "dba_tree_attend")
+            _check(code, "dba_tree_attend" if _shared is None else "dba_tree_attend_shared")
         return out
+
+    def attend_shared(self, q, k, v, table, ctx_len, prefix, masks=None, top=None, scale=None, out=None, lse=None):
+        """attend where the sequences also see a prefix that several of them share, gone through once for all: prefix = (first, length,
+        table).  Prefix g, length[g] tokens at the places of table[g], stands before sequences first[g] .. first[g + 1] - 1:
+        first int32 [groups + 1], length int32 [groups], table int32 [groups, pages], pages of the same cache.  See dba_tree_attend_shared."""
+        first, length, ptable = prefix
+        groups, dev, p = length.numel(), self._dev, self._prefix
+        if not self.prefixes:
+            raise ValueError("attend_shared: the handle was made without prefixes=")
+        if groups < 1 or groups > self.prefixes:
+            raise ValueError("prefix: between 1 and the handle's `prefixes` of them")
+        if ptable.dtype is not self._i32t or ptable.get_device() != dev or ptable.dim() != 2 or ptable.shape[0] != groups or ptable.shape[1] < 1:
+            raise ValueError("prefix table: int32 [groups, pages] on the handle's device")
+        s = ptable.stride()
+        if s[1] != 1 and ptable.shape[1] > 1:
+            raise ValueError("prefix table: rows of a unit stride")
+        p.groups, p.max_pages = groups, ptable.shape[1]
+        p.first, p.len = self._i32(first, groups + 1, "prefix first: int32 [groups + 1]"), self._i32(length, groups, "prefix length: int32 [groups]")
+        p.table, p.table_stride = ptable.data_ptr(), s[0] if groups > 1 else ptable.shape[1]
+        return self.attend(q, k, v, table, ctx_len, masks, top, scale, out, lse, _shared=self._call_shared)
+
+    def _call_shared(self, *args):
+        return lib().dba_tree_attend_shared(*args, self._prefix_ref, self._scratch_at, self._scratch_bytes)
 
     def advance(self, backptr, masks, slot_pos, ctx_len, score=None, token=None, eos=-1, out=None):
         """The tree after a step: see dba_tree_advance.  backptr (and score, token: dba_step's outputs) [B, rows] or [B * rows];
@@ -267,6 +332,67 @@ class TokenTree:
                               self._i32(commit_src, B * 32 * self.words, "commit_src: int32 [B, 32 * words]"), self._i32(commit_n, B, "commit_n: int32 [B]"))
         if code:
             _check(code, "dba_tree_commit")
+
+    # [B, kv_heads, places] (evict: layers in front) fp32 with a unit inner stride: at least the places a table leaves the context
+    def _weights(self, w, lead, what):
+        B, sh, s = self.B, w.shape, w.stride()
+        if (w.dtype is not self._f32t or w.get_device() != self._dev or len(sh) != len(lead) + 3 or sh[:-1] != (*lead, B, self.kv_heads)
+                or sh[-1] < self.max_pages * self.page_size - 32 * self.words or s[-1] != 1):
+            raise ValueError(f"{what}: fp32 [{'layers, ' if lead else ''}B, kv_heads, context places], unit inner stride")
+        return s
+
+    def weigh(self, q, k, table, ctx_len, lse, weight=None, decay=1.0, scale=None, out=None):
+        """The attention that context tokens receive from the rows of q [B, rows, heads, head_dim], whose log-sum-exps lse [B, rows, heads]
+        attend (or attend_shared) has written:  out = decay * weight + sum of the probabilities, [B, kv_heads, context places] fp32,
+        for places below ctx_len; the others are left as they are.  out: default weight itself, in place; weight None: zeros.  Returns out."""
+        B, d, dev, shape, sq = self.B, self._query, self._dev, q.shape, q.stride()
+        if out is None:
+            out = weight
+        if out is None:
+            raise ValueError("weigh: weight or out")
+        s = self._weights(out, (), "out")
+        if weight is not None and weight is not out and self._weights(weight, (), "weight") != s:
+            raise ValueError("weight and out: of the same strides")
+        if (q.dtype is not self.torch_dtype or q.get_device() != dev or len(shape) != 4 or shape[0] != B or shape[2] != self.heads
+                or shape[3] != self.head_dim or sq[3] != 1):
+            raise ValueError("q: [B, rows, heads, head_dim] of the handle's type and on its device")
+        if lse.dtype is not self._f32t or lse.get_device() != dev or lse.shape != shape[:3] or not lse.is_contiguous():
+            raise ValueError("lse: [B, rows, heads] fp32")
+        d.rows, d.q_seq_stride, d.q_row_stride, d.q_head_stride = shape[1], sq[0], sq[1], sq[2]
+        d.q, d.scale = q.data_ptr(), self.head_dim ** -0.5 if scale is None else scale
+        self._query_last = None
+        code = lib().dba_tree_weigh(self._h, self._query_ref, lse.data_ptr(), self._cache(k, k, 0), table.data_ptr(), self._table(table),
+                                    self._i32(ctx_len, B, "ctx_len: int32 [B]"), None if weight is None else weight.data_ptr(), out.data_ptr(), s[0], s[1], decay)
+        if code:
+            _check(code, "dba_tree_weigh")
+        return out
+
+    def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None):
+        """Keeps `keep` tokens of every longer context: the last `recent` and, of the others, those of the largest weight, in their order,
+        at the front.  weight [layers, B, kv_heads, context places] fp32 (without layers where k, v have none).  table_out, weight_out:
+        where to; default the same, in place.  Returns a dict of ctx_len and dropped [B] (new tensors), kept [(layers,) B, kv_heads, keep]
+        (the old context places, -1 beyond) and weight (weight_out).  See dba_tree_evict."""
+        torch, B, layers = self.torch, self.B, k.shape[:-4]
+        if len(layers) > 1:
+            raise ValueError("k and v: [pages, page_size, kv_heads, head_dim], or layers in front")
+        if keep < 1 or not 0 <= recent <= keep:
+            raise ValueError("evict: 0 <= recent <= keep, keep >= 1")
+        table_out = table if table_out is None else table_out
+        weight_out = weight if weight_out is None else weight_out
+        s = self._weights(weight, tuple(layers), "weight")
+        if weight_out is not weight and self._weights(weight_out, tuple(layers), "weight_out") != s:
+            raise ValueError("weight and weight_out: of the same strides")
+        cache, n = self._cache(k, v, len(layers)), self._i32(ctx_len, B, "ctx_len: int32 [B]")
+        stride, stride_out = self._table(table), self._table(table_out)
+        with torch.cuda.stream(self.stream):             # (the allocator gives freed memory out by stream)
+            ints = torch.empty(2 * B + math.prod(layers) * B * self.kv_heads * keep, dtype=self._i32t, device=self.device)
+        new_len, dropped, kept = ints[:B], ints[B:2 * B], ints[2 * B:].view(*layers, B, self.kv_heads, keep)
+        e = TreeEvicted(weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2], keep, recent, table_out.data_ptr(), stride_out,
+                        kept.data_ptr(), new_len.data_ptr(), dropped.data_ptr())
+        code = lib().dba_tree_evict(self._h, cache, table.data_ptr(), stride, n, C.byref(e))
+        if code:
+            _check(code, "dba_tree_evict")
+        return {"ctx_len": new_len, "dropped": dropped, "kept": kept, "weight": weight_out}
 
     def status(self):
         """TREE_* bits since the last call.  Waits for the handle's stream."""
