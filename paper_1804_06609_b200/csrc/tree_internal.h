@@ -98,6 +98,10 @@ struct TreePrefix {
 struct TreePrefixPlan { int grid, rows; bool tensor; };        // blocks of the kernel, rows of an item
 TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count);
 cudaError_t configure_tree_prefix();
+// the tensor-core kernel (tree_prefix_mma.cu); usable where tree_mma_usable
+int tree_prefix_mma_rows();
+cudaError_t configure_tree_prefix_mma();
+cudaError_t launch_tree_prefix_mma(const TreePrefix& a, int grid, cudaStream_t st);
 cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches);
 
 // The weight that context tokens receive.

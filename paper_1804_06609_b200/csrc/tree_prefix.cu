@@ -342,6 +342,12 @@ cudaError_t launch_prefix(const TreePrefix& a, int grid, cudaStream_t st) {
 
 TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count) {
     TreePrefixPlan p{};
+    if (tree_mma_usable(dtype, D)) {
+        p.tensor = true;
+        p.grid = sm_count;
+        p.rows = tree_prefix_mma_rows();
+        return p;
+    }
     p.grid = (D <= 128 ? 2 : 1) * sm_count;
     p.rows = kPRows;
     return p;
@@ -351,19 +357,15 @@ cudaError_t configure_tree_prefix() {
     cudaError_t e = configure_prefix<float, 64>();
     if (e == cudaSuccess) e = configure_prefix<float, 128>();
     if (e == cudaSuccess) e = configure_prefix<float, 256>();
-    if (e == cudaSuccess) e = configure_prefix<__nv_bfloat16, 64>();
-    if (e == cudaSuccess) e = configure_prefix<__nv_bfloat16, 128>();
     if (e == cudaSuccess) e = configure_prefix<__nv_bfloat16, 256>();
-    return e;
+    return e == cudaSuccess ? configure_tree_prefix_mma() : e;
 }
 
 cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches) {
     cudaError_t e;
-    if (dtype == DBA_F32)
-        e = a.D <= 64 ? launch_prefix<float, 64>(a, plan.grid, st) : a.D <= 128 ? launch_prefix<float, 128>(a, plan.grid, st) : launch_prefix<float, 256>(a, plan.grid, st);
-    else
-        e = a.D <= 64 ? launch_prefix<__nv_bfloat16, 64>(a, plan.grid, st) : a.D <= 128 ? launch_prefix<__nv_bfloat16, 128>(a, plan.grid, st)
-                                                                          : launch_prefix<__nv_bfloat16, 256>(a, plan.grid, st);
+    if (plan.tensor) e = launch_tree_prefix_mma(a, plan.grid, st);
+    else if (dtype == DBA_BF16) e = launch_prefix<__nv_bfloat16, 256>(a, plan.grid, st);
+    else e = a.D <= 64 ? launch_prefix<float, 64>(a, plan.grid, st) : a.D <= 128 ? launch_prefix<float, 128>(a, plan.grid, st) : launch_prefix<float, 256>(a, plan.grid, st);
     *launches += 1;
     if (e != cudaSuccess) return e;
     const size_t list = (size_t)2 * plan.grid * (sizeof(int4) + sizeof(int32_t));
