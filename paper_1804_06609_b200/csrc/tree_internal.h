@@ -95,7 +95,7 @@ struct TreePrefix {
     long long wait_clocks;
     int drop_item;
 };
-struct TreePrefixPlan { int grid, rows; bool tensor; };        // blocks of the kernel, rows of an item
+struct TreePrefixPlan { int grid, rows, sm_count; bool tensor; };      // blocks of the kernel, rows of an item
 TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count);
 cudaError_t configure_tree_prefix();
 // the tensor-core kernel (tree_prefix_mma.cu); usable where tree_mma_usable

@@ -240,16 +240,21 @@ __global__ void __launch_bounds__(kPThreads, DP <= 128 ? 2 : 1) tree_prefix_kern
 
 // Finishes the items that several blocks worked on.  A block's run leaves at most two pieces of such items, in the order of the
 // units, so the pieces of an item are neighbours in the list of all blocks' pieces.  Every block here reads the list and takes every
-// gridDim-th row of the items on it, a warp to a row.  Pieces are added in their order: equal inputs give equal bits.  A block that gave
-// up says so in its entry, which every launch writes anew.
-constexpr int kPJoinThreads = 256, kPJoinWarps = kPJoinThreads / 32;
+// gridDim-th stretch of the items' rows: 32 rows where no item has more than kPJoinFew pieces, 8 elsewhere.  First the rows' weights for
+// each piece, a thread to a piece, then the outputs, four columns to a thread, all loads of which are in the air together.  Pieces are
+// added in their order: equal inputs give equal bits.  A block that gave up says so in its entry, which every launch writes anew.
+constexpr int kPJoinThreads = 256, kPJoinWarps = kPJoinThreads / 32, kPJoinFew = 8, kPJoinRows = kPJoinThreads / kPJoinFew, kPJoinManyRows = kPJoinWarps;
 
 template <typename T>
 __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const TreePrefix a, int item_rows, int blocks) {
-    extern __shared__ int4 pieces[];                       // [2 * blocks], then [2 * blocks] places of items' first pieces
-    int32_t* const items = reinterpret_cast<int32_t*>(pieces + 2 * blocks);
-    __shared__ int counts[kPJoinWarps];
+    extern __shared__ int4 pieces[];                       // [2 * blocks]; places of the pieces there are; of items' first ones among them; weights
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = 2 * blocks;
+    int32_t* const list = reinterpret_cast<int32_t*>(pieces + n);
+    int32_t* const items = list + n;
+    float* const weights = reinterpret_cast<float*>(items + n);      // [rows][pieces]
+    __shared__ int counts[kPJoinWarps];
+    __shared__ int64_t out_at[kPJoinRows];                 // -1: the row stays as it is
+    __shared__ float own_weight[kPJoinRows];
     grid_dependency_wait();
     allow_dependents();
     bool failed = false;
@@ -267,64 +272,92 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
         }
         return;
     }
-    const auto same = [&](const int4& x, const int4& y) { return x.x == y.x && x.y == y.y && x.z == y.z; };
-    int n_items = 0;
-    for (int i0 = 0; i0 < n; i0 += kPJoinThreads) {
-        const int i = i0 + tid;
-        bool first = i < n && pieces[i].x >= 0;
-        if (first) {
-            int j = i - 1;
-            while (j >= 0 && pieces[j].x < 0) --j;
-            first = j < 0 || !same(pieces[j], pieces[i]);
+    // the numbers of those for which `is` holds, in order, to `to`; returns how many
+    const auto compact = [&](int32_t* to, int count, auto is) {
+        int total = 0;
+        for (int i0 = 0; i0 < count; i0 += kPJoinThreads) {
+            const bool mine = i0 + tid < count && is(i0 + tid);
+            const uint32_t votes = __ballot_sync(kFullMask, mine);
+            if (lane == 0) counts[warp] = __popc(votes);
+            __syncthreads();
+            int before = total + __popc(votes & ((1u << lane) - 1u));
+#pragma unroll
+            for (int w = 0; w < kPJoinWarps; ++w) {
+                if (w < warp) before += counts[w];
+                total += counts[w];
+            }
+            if (mine) to[before] = i0 + tid;
+            __syncthreads();
         }
-        const uint32_t mine = __ballot_sync(kFullMask, first);
-        if (lane == 0) counts[warp] = __popc(mine);
-        __syncthreads();
-        int before = n_items + __popc(mine & ((1u << lane) - 1u));
-        for (int w = 0; w < kPJoinWarps; ++w) {
-            if (w < warp) before += counts[w];
-            n_items += counts[w];
-        }
-        if (first) items[before] = i;
-        __syncthreads();
-    }
-    for (int task = blockIdx.x * kPJoinWarps + warp; task < n_items * item_rows; task += gridDim.x * kPJoinWarps) {
-        const int item = task / item_rows, r = task - item * item_rows, first = items[item];
-        const int4 id = pieces[first];
+        return total;
+    };
+    const int n_pieces = compact(list, n, [&](int i) { return pieces[i].x >= 0; });
+    if (n_pieces == 0) return;
+    const int n_items = compact(items, n_pieces, [&](int i) {
+        if (i == 0) return true;
+        const int4 x = pieces[list[i]], y = pieces[list[i - 1]];
+        return x.x != y.x || x.y != y.y || x.z != y.z;
+    });
+    bool more = false;
+    for (int i = tid; i < n_items; i += kPJoinThreads) more = more || (i + 1 < n_items ? items[i + 1] : n_pieces) - items[i] > kPJoinFew;
+    const bool many = __syncthreads_or(more);
+    const int rows = many ? kPJoinManyRows : kPJoinRows, per_item = item_rows / rows, vecs = a.D / 4;
+    for (int task = blockIdx.x; task < n_items * per_item; task += gridDim.x) {
+        const int item = task / per_item, r0 = (task - item * per_item) * rows, first = items[item];
+        const int count = (item + 1 < n_items ? items[item + 1] : n_pieces) - first;
+        const int4 id = pieces[list[first]];
         const PrefixGroup pg = prefix_group(a, id.x);
-        const int row = id.z * item_rows + r;
-        if (row >= (pg.hi - pg.lo) * a.n * a.G) continue;
-        const int last = item + 1 < n_items ? items[item + 1] : n;
-        const PrefixRow w = prefix_row(a, pg.lo, id.y, row);
-        float own, w_own, w_pre, lse;
-        if (!prefix_own(a, w, &own)) continue;
-        float m = neg_inf();
-        for (int i = first + lane; i < last; i += 32)
-            if (pieces[i].x >= 0) m = fmaxf(m, a.part_ml[2 * ((int64_t)i * item_rows + r)]);
-        m = warp_max(m);
+        const int left = (pg.hi - pg.lo) * a.n * a.G - (id.z * item_rows + r0);       // rows from here on
+        if (left <= 0) continue;
+        // --- weights: a warp to a row, or eight lanes
+        const int lanes = many ? 32 : kPJoinFew, r = tid / lanes, l0 = tid - r * lanes;
+        const bool in = r < left;
+        const PrefixRow w = prefix_row(a, pg.lo, id.y, id.z * item_rows + r0 + (in ? r : 0));
+        float own, w_own = 0.f, w_pre, lse, m = neg_inf(), l = 0.f;
+        const bool is_open = prefix_own(a, w, &own) && in;
+        for (int i = l0; i < count; i += lanes) {
+            const int64_t at = (int64_t)list[first + i] * item_rows + r0 + r;
+            if (in) m = fmaxf(m, a.part_ml[2 * at]);
+        }
+        for (int o = lanes >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFullMask, m, o));
         const float ref = m == neg_inf() ? 0.f : m;
-        float l = 0.f;
-        for (int i = first + lane; i < last; i += 32)
-            if (pieces[i].x >= 0) l += a.part_ml[2 * ((int64_t)i * item_rows + r) + 1] * exp2f(a.part_ml[2 * ((int64_t)i * item_rows + r)] - ref);
-        l = warp_sum(l);
-        if (!prefix_join(own, ref, l, &w_own, &w_pre, &lse)) continue;
-        T* out = (T*)a.out + (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head;
-        for (int d = 4 * lane; d < a.D; d += 128) {
+        for (int i = l0; i < count; i += lanes) {
+            const int64_t at = (int64_t)list[first + i] * item_rows + r0 + r;
+            float e = 0.f;
+            if (in) {
+                const float sum = a.part_ml[2 * at + 1];
+                e = sum == 0.f ? 0.f : exp2f(a.part_ml[2 * at] - ref);
+                l += sum * e;
+            }
+            weights[r * count + i] = e;
+        }
+        for (int o = lanes >> 1; o; o >>= 1) l += __shfl_xor_sync(kFullMask, l, o);
+        const bool write = prefix_join(own, ref, l, &w_own, &w_pre, &lse) && is_open;
+        if (write)
+            for (int i = l0; i < count; i += lanes) weights[r * count + i] *= w_pre;
+        if (l0 == 0) {
+            out_at[r] = write ? (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head : -1;
+            own_weight[r] = w_own;
+        }
+        __syncthreads();                                   // (and every lane has read what one of the row's writes)
+        if (write && l0 == 0) a.own_lse[((int64_t)w.b * a.n + w.i) * a.H + w.head] = lse;
+        // --- outputs
+        for (int u = tid; u < rows * vecs; u += kPJoinThreads) {
+            const int row = u / vecs, d = (u - row * vecs) * 4;
+            if (row >= left || out_at[row] < 0) continue;
+            T* out = (T*)a.out + out_at[row] + d;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int i = first; i < last; ++i) {
-                if (pieces[i].x < 0) continue;
-                const int64_t at = (int64_t)i * item_rows + r;
-                const float e = exp2f(a.part_ml[2 * at] - ref);
-                const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * a.D + d);
+#pragma unroll 8
+            for (int i = 0; i < count; ++i) {
+                const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((int64_t)list[first + i] * item_rows + r0 + row) * a.D + d);
+                const float e = weights[row * count + i];
                 o.x = fmaf(e, v.x, o.x); o.y = fmaf(e, v.y, o.y); o.z = fmaf(e, v.z, o.z); o.w = fmaf(e, v.w, o.w);
             }
-            const float y[4] = {o.x, o.y, o.z, o.w};
+            const float y[4] = {o.x, o.y, o.z, o.w}, wo = own_weight[row];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p_store(out + d + j, fmaf(w_own, p_widen(out[d + j]), w_pre * y[j]));
+            for (int j = 0; j < 4; ++j) p_store(out + j, fmaf(wo, p_widen(out[j]), y[j]));
         }
-        __syncwarp();                                      // (all lanes have read what one writes)
-        if (lane == 0) a.own_lse[((int64_t)w.b * a.n + w.i) * a.H + w.head] = lse;
+        __syncthreads();
     }
 }
 
@@ -342,6 +375,7 @@ cudaError_t launch_prefix(const TreePrefix& a, int grid, cudaStream_t st) {
 
 TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count) {
     TreePrefixPlan p{};
+    p.sm_count = sm_count;
     if (tree_mma_usable(dtype, D)) {
         p.tensor = true;
         p.grid = sm_count;
@@ -358,6 +392,9 @@ cudaError_t configure_tree_prefix() {
     if (e == cudaSuccess) e = configure_prefix<float, 128>();
     if (e == cudaSuccess) e = configure_prefix<float, 256>();
     if (e == cudaSuccess) e = configure_prefix<__nv_bfloat16, 256>();
+    // the same division of shared memory and L1 as the kernel before, or the SMs change over between the two
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_prefix_join_kernel<float>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_prefix_join_kernel<__nv_bfloat16>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     return e == cudaSuccess ? configure_tree_prefix_mma() : e;
 }
 
@@ -368,8 +405,10 @@ cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, 
     else e = a.D <= 64 ? launch_prefix<float, 64>(a, plan.grid, st) : a.D <= 128 ? launch_prefix<float, 128>(a, plan.grid, st) : launch_prefix<float, 256>(a, plan.grid, st);
     *launches += 1;
     if (e != cudaSuccess) return e;
-    const size_t list = (size_t)2 * plan.grid * (sizeof(int4) + sizeof(int32_t));
-    const int grid = plan.grid * 2;
+    // (an item has at most one piece from each block)
+    const size_t n = (size_t)2 * plan.grid, most = (size_t)plan.grid * kPJoinManyRows, few = kPJoinRows * kPJoinFew;
+    const size_t list = n * (sizeof(int4) + 2 * sizeof(int32_t)) + (most > few ? most : few) * sizeof(float);
+    const int grid = plan.sm_count * 4;
     e = dtype == DBA_F32 ? launch_after(tree_prefix_join_kernel<float>, dim3(grid), dim3(kPJoinThreads), list, st, a, plan.rows, plan.grid)
                          : launch_after(tree_prefix_join_kernel<__nv_bfloat16>, dim3(grid), dim3(kPJoinThreads), list, st, a, plan.rows, plan.grid);
     *launches += 1;

@@ -29,16 +29,18 @@ constexpr int kXWarpRows = 44;         // rows of a tile that a loader copies: 4
 
 template <int DP> struct XConf {
     static constexpr int tile_bytes = kXKeys * DP * 2, q_half = 128 * DP * 2, q_bytes = 2 * q_half;
-    static constexpr int stages = DP == 128 ? 5 : 10;
+    static constexpr int stages = DP == 128 ? 4 : 8, q_bufs = DP == 128 ? 1 : 2;
     static constexpr int s_col = 0, o_col = 256, tmem_cols = 512;
 };
 template <int DP> struct XSmem {
     using C = XConf<DP>;
-    alignas(1024) unsigned char q[C::q_bytes];
+    alignas(1024) unsigned char q[C::q_bufs][C::q_bytes];
     unsigned char kv[C::stages][C::tile_bytes];
+    float4 turn[8][32][8];                      // by softmax warp: 32 columns of its rows, on their way to memory
     uint64_t full[C::stages], empty[C::stages];
-    uint64_t s_full[2], p_ready[2], o_done[2];
-    uint64_t o_free, q_full, q_empty, ml_ready, last;
+    uint64_t s_full[2], p_ready[2][2], half_done[2], o_done[2];
+    uint64_t q_full[C::q_bufs], q_empty[C::q_bufs];
+    uint64_t o_free, ml_ready, last;
     float ml[2][128][2];
     uint32_t seen[kXSeen][kXLoadWarps][2];      // (by tile, in turn) which rows of a loader's there are
     uint32_t tmem_base;
@@ -49,6 +51,7 @@ template <int DP> struct XSmem {
     };
 };
 constexpr uint32_t kXNoRow = 0xffffffffu;
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 using XCut = PrefixCut<kXKeys, kXRows, 128>;
 
 template <int DP>
@@ -62,8 +65,10 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
     if (tid == 0) {
         for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kXLoadThreads + kXLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
         // (s_full: the products, and an arrival of the issuing thread, which passes on what the loaders wrote before it)
-        for (int s = 0; s < 2; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s]), 4); mbar_init(msmem_u32(&sm.o_done[s]), 1); }
-        mbar_init(msmem_u32(&sm.o_free), 8); mbar_init(msmem_u32(&sm.q_full), kXLoadThreads); mbar_init(msmem_u32(&sm.q_empty), 1);
+        for (int s = 0; s < 2; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s][0]), 4); mbar_init(msmem_u32(&sm.p_ready[s][1]), 4);
+                                      mbar_init(msmem_u32(&sm.half_done[s]), 1); mbar_init(msmem_u32(&sm.o_done[s]), 1); }
+        for (int i = 0; i < C::q_bufs; ++i) { mbar_init(msmem_u32(&sm.q_full[i]), kXLoadThreads); mbar_init(msmem_u32(&sm.q_empty[i]), 1); }
+        mbar_init(msmem_u32(&sm.o_free), 8);
         mbar_init(msmem_u32(&sm.ml_ready), 8); mbar_init(msmem_u32(&sm.last), 1);
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -74,10 +79,11 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_before();
-    grid_dependency_wait();
+    // Nothing but the rows' own part comes from the kernel before this one, and that kernel has waited for what came before it: the wait
+    // is the epilogue's.
     allow_dependents();
     if (blockIdx.x == 0) prefix_check(a);
-    SpanRun run = span_run<kXThreads>(a.groups, 8, &sm.span, [&](int g) { return XCut::units(a, g); });      // (has the block's barriers)
+    SpanRun run = span_run<kXThreads>(a.groups, 3, &sm.span, [&](int g) { return XCut::units(a, g); });      // (has the block's barriers)
     __syncthreads();           // its numbers have been read: their place is used again
     tc_after();
     const uint32_t tmem = sm.tmem_base;
@@ -90,7 +96,9 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
         const int lw = warp - 9, ch = lane % CH, sub = lane / CH, base = lw * kXWarpRows, mine = lw < 2 ? kXWarpRows : kXKeys - 2 * kXWarpRows;
         const bool ch_in = ch * 8 < a.D;
         const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;
-        const uint32_t q_at = msmem_u32(sm.q), kv_at = msmem_u32(sm.kv);
+        const uint32_t q_at = msmem_u32(sm.q), kv_at = msmem_u32(sm.kv) + (uint32_t)(ch >> 3) * (kXKeys * 128) + (uint32_t)(base + sub) * 128;
+        // the swizzle moves a chunk by its row's last three bits (of the queries' rows, and of a tile's: base is 0 or 4 of 8)
+        const uint32_t swz = (uint32_t)((ch & 7) ^ sub) << 4, kv_swz = swz ^ (uint32_t)((base & 7) << 4);
         uint32_t* const rows = sm.rows + base;
         uint32_t copy = 0;
         int cut = 0;
@@ -98,25 +106,8 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
         bool ok = true;
         while (ok && XCut::next(a, run, &pc)) {
             if (!pc.whole()) { if (cut == 0) meta[0] = make_int4(pc.g, pc.h, pc.rb, 0); else meta[1] = make_int4(pc.g, pc.h, pc.rb, 0); ++cut; }
-            if (piece > 0 && !mbar_wait(msmem_u32(&sm.q_empty), (piece - 1) & 1, abort_flag, limit)) { ok = false; break; }
-            // queries, zeros beyond the rows and the head size
-            const char* q = (const char*)a.q + (ch_in ? ch * 16 : 0);
-#pragma unroll 1
-            for (int r0 = lw * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * kXLoadWarps) {        // a lane finds one row, and every lane copies chunks of all
-                int64_t at = -1;
-                if (r0 + lane < pc.rows) {
-                    const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
-                    at = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
-                }
-#pragma unroll 4
-                for (int j = 0; j < 32; j += RW) {
-                    const int64_t from = __shfl_sync(kFullMask, at, j + sub);
-                    const uint32_t r = (uint32_t)(r0 + j + sub) & 127u;
-                    const uint32_t to = q_at + (r0 >= 128 ? C::q_half : 0) + (uint32_t)(ch >> 3) * (128 * 128) + r * 128 + ((((uint32_t)ch ^ r) & 7u) << 4);
-                    cp_async16(to, from >= 0 ? q + from : q, from >= 0 && ch_in ? 16u : 0u);
-                }
-            }
-            cp_arrive(msmem_u32(&sm.q_full));
+            const uint32_t qb = (uint32_t)piece % C::q_bufs;
+            if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
             // where a tile's rows are, looked up one tile ahead
             const int64_t head_at = 2 * (int64_t)pc.h * a.pages.head_stride + (ch_in ? ch * 16 : 0);
             uint32_t at[2];
@@ -135,6 +126,28 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                 }
             };
             look_up(pc.tile);
+            // queries, zeros beyond the rows and the head size
+            const char* q = (const char*)a.q + (ch_in ? ch * 16 : 0);
+#pragma unroll 1
+            for (int r0 = lw * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * kXLoadWarps) {        // a lane finds one row, and every lane copies chunks of all
+                int64_t q_row = -1;
+                if (r0 + lane < pc.rows) {
+                    const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
+                    q_row = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
+                }
+                const uint32_t to = q_at + qb * C::q_bytes + (r0 >= 128 ? C::q_half : 0) + (uint32_t)(ch >> 3) * (128 * 128) + (uint32_t)((r0 & 127) + sub) * 128;
+#pragma unroll 1
+                for (int j0 = 0; j0 < 32; j0 += 8 * RW) {
+                    int64_t from[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) from[j] = j0 + j * RW < 32 ? __shfl_sync(kFullMask, q_row, j0 + j * RW + sub) : -1;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j0 + j * RW < 32)
+                            cp_async16(to + (j0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[j] >= 0 ? q + from[j] : q, from[j] >= 0 && ch_in ? 16u : 0u);
+                }
+            }
+            cp_arrive(msmem_u32(&sm.q_full[qb]));
 #pragma unroll 1
             for (int t = pc.tile; t < pc.tile_end; ++t) {
                 const uint32_t seen0 = __ballot_sync(kFullMask, at[0] != kXNoRow), seen1 = __ballot_sync(kFullMask, at[1] != kXNoRow);
@@ -144,17 +157,21 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                 if (lane < 2) sm.seen[(tiles0 + t - pc.tile) % kXSeen][lw][lane] = lane ? seen1 : seen0;
                 __syncwarp();
                 look_up(t + 1);
+                constexpr int NJ = kXWarpRows / RW;
+                uint32_t row[NJ];                          // (read before the copies: they are not reordered)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) row[j] = rows[j * RW + sub];
 #pragma unroll 1
                 for (int k = 0; k < 2; ++k, ++copy) {
                     const uint32_t stage = copy % C::stages, use = copy / C::stages;
                     if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[stage]), (use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
                     const char* from = (const char*)(k ? a.v : a.k) + head_at;
-                    const uint32_t to = kv_at + stage * C::tile_bytes + (uint32_t)(ch >> 3) * (kXKeys * 128);
-#pragma unroll 11
-                    for (int j = 0; j < mine; j += RW) {
-                        const uint32_t row = rows[j + sub], r = (uint32_t)(base + j + sub);
-                        const bool in = row != kXNoRow && ch_in;
-                        cp_async16(to + r * 128 + ((((uint32_t)ch ^ r) & 7u) << 4), in ? from + (uint64_t)row * 16 : from, in ? 16u : 0u);
+                    const uint32_t to = kv_at + stage * C::tile_bytes;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        if (j * RW >= mine) break;
+                        const bool in = row[j] != kXNoRow && ch_in;
+                        cp_async16(to + j * RW * 128 + (kv_swz ^ (uint32_t)((j * RW & 7) << 4)), from + (uint64_t)(in ? row[j] : 0u) * 16, in ? 16u : 0u);
                     }
                     if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));
                     if ((int)copy != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
@@ -176,7 +193,8 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
         while (ok && XCut::next(a, run, &pc)) {
             const bool two = pc.rows > 128;
             const int n = (pc.tile_end - pc.tile) * (two ? 2 : 1);
-            if (!(ok = mbar_wait(msmem_u32(&sm.q_full), piece & 1, abort_flag, limit))) break;
+            const uint32_t qb = (uint32_t)piece % C::q_bufs;
+            if (!(ok = mbar_wait(msmem_u32(&sm.q_full[qb]), ((uint32_t)piece / C::q_bufs) & 1u, abort_flag, limit))) break;
 #pragma unroll 1
             for (int i = 0; i < n + 2; ++i) {
                 const uint32_t s = i & 1;
@@ -184,26 +202,33 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                     const int j = i - 2;
                     const uint32_t copy = 2 * (tiles0 + (two ? j >> 1 : j)) + 1, stage = copy % C::stages;
                     if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), (copy / C::stages) & 1u, abort_flag, limit))) break;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[s]), done[s] & 1u, abort_flag, limit))) break;
                     if (j == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1, abort_flag, limit))) break;
                     const uint64_t dv = sw128_desc(kv_at + stage * C::tile_bytes, kXKeys * 128);
-                    const uint32_t p = tmem + C::s_col + s * kXKeys, d = tmem + C::o_col + s * DP;
-                    if (elect_one()) {
-                        fence_async_proxy();               // the copies' writes (generic) before the products' reads
-                        tc_after();
+                    const uint32_t p = tmem + C::s_col + s * kXKeys, d = tmem + C::o_col + s * DP, parity = (s ? done[1] : done[0]) & 1u;
 #pragma unroll
-                        for (int ks = 0; ks < kXKeys / 16; ++ks) mma_ts(d, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, j >= 2 || ks != 0, -1);
-                        if (!two || s == 1) mma_commit(msmem_u32(&sm.empty[stage]));
-                        if (j + 2 >= n) mma_commit(msmem_u32(&sm.o_done[s]));
-                        if (n == 1) mma_commit(msmem_u32(&sm.o_done[1]));
+                    for (int h = 0; h < 2; ++h) {
+                        if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[s][h]), parity, abort_flag, limit))) break;
+                        if (elect_one()) {
+                            fence_async_proxy();           // the copies' writes (generic) before the products' reads
+                            tc_after();
+#pragma unroll
+                            for (int ks = 4 * h; ks < 4 * h + 4; ++ks) mma_ts(d, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, j >= 2 || ks != 0, -1);
+                            if (h == 0) mma_commit(msmem_u32(&sm.half_done[s]));
+                            else {
+                                if (!two || s == 1) mma_commit(msmem_u32(&sm.empty[stage]));
+                                if (j + 2 >= n) mma_commit(msmem_u32(&sm.o_done[s]));
+                                if (n == 1) mma_commit(msmem_u32(&sm.o_done[1]));
+                            }
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (!ok) break;
                     if (s) ++done[1]; else ++done[0];
                 }
                 if (i < n) {
                     const uint32_t copy = 2 * (tiles0 + (two ? i >> 1 : i)), stage = copy % C::stages;
                     if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), (copy / C::stages) & 1u, abort_flag, limit))) break;
-                    const uint64_t dq = sw128_desc(q_at + (two ? s * C::q_half : 0), 16), dk = sw128_desc(kv_at + stage * C::tile_bytes, 16);
+                    const uint64_t dq = sw128_desc(q_at + qb * C::q_bytes + (two ? s * C::q_half : 0), 16), dk = sw128_desc(kv_at + stage * C::tile_bytes, 16);
                     const uint32_t d = tmem + C::s_col + s * kXKeys;
                     if (elect_one()) {
                         fence_async_proxy();
@@ -216,7 +241,7 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                         if (!two || s == 1) mma_commit(msmem_u32(&sm.empty[stage]));
                         mma_commit(msmem_u32(&sm.s_full[s]));
                         mbar_arrive(msmem_u32(&sm.s_full[s]));
-                        if (i + 1 == n) mma_commit(msmem_u32(&sm.q_empty));
+                        if (i + 1 == n) mma_commit(msmem_u32(&sm.q_empty[qb]));
                     }
                     __syncwarp();
                 }
@@ -245,72 +270,99 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
             for (int t = first; t < pc.tile_end; t += by, ++steps) {
                 if (!mbar_wait(msmem_u32(&sm.s_full[s]), steps & 1u, abort_flag, limit)) { ok = false; break; }
                 tc_after();
-                uint32_t x[kXKeys];
-                tm_ld64(s_at, x);
-                tm_ld64(s_at + 64, x + 64);
                 const uint32_t (*seen)[2] = sm.seen[(tiles0 + t - pc.tile) % kXSeen];
-                if ((seen[0][0] & seen[1][0] & seen[2][0]) != 0xffffffffu || seen[0][1] != 0xfffu || seen[1][1] != 0xfffu || seen[2][1] != 0xffu) {
-                    // the end of the prefix, or a page that there is not
-                    const uint64_t m0 = (uint64_t)seen[0][1] << 32 | seen[0][0], m1 = (uint64_t)seen[1][1] << 32 | seen[1][0], m2 = (uint64_t)seen[2][1] << 32 | seen[2][0];
-                    const uint64_t lo = m0 | m1 << 44, hi = m1 >> 20 | m2 << 24;
-                    const uint32_t see[4] = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-#pragma unroll
-                    for (int j = 0; j < kXKeys; ++j) if (!((see[j >> 5] >> (j & 31)) & 1u)) x[j] = 0xff800000u;
-                }
-                float m0 = neg_inf(), m1 = m0, m2 = m0, m3 = m0;
-#pragma unroll
-                for (int j = 0; j < kXKeys; j += 4) {
-                    m0 = fmaxf(m0, __uint_as_float(x[j])); m1 = fmaxf(m1, __uint_as_float(x[j + 1]));
-                    m2 = fmaxf(m2, __uint_as_float(x[j + 2])); m3 = fmaxf(m3, __uint_as_float(x[j + 3]));
-                }
-                const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
-                const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
-                if (__any_sync(kFullMask, raise)) {
-                    const float factor = raise ? ex2(ref - top) : 1.f;             // 0 where nothing has been seen before
-                    if (raise) { ref = top; sum *= factor; }
-                    if (t > first) {                       // (these scores came behind the outputs of all steps before)
+                const bool all = (seen[0][0] & seen[1][0] & seen[2][0]) == 0xffffffffu && seen[0][1] == 0xfffu && seen[1][1] == 0xfffu && seen[2][1] == 0xffu;
+                // Half a tile at a time: the first half's outputs are under way while the second goes through here, and 64 scores fit
+                // the registers.
 #pragma unroll 1
-                        for (int c = 0; c < DP; c += 16) {
-                            uint32_t o[16];
-                            tm_ld16(o_at + s * DP + c, o);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[64];
+                    tm_ld64(s_at + 64 * h, x);
+                    if (!all) {                            // the end of the prefix, or a page that there is not
+                        const uint64_t m0 = (uint64_t)seen[0][1] << 32 | seen[0][0], m1 = (uint64_t)seen[1][1] << 32 | seen[1][0], m2 = (uint64_t)seen[2][1] << 32 | seen[2][0];
+                        const uint64_t see = h ? m1 >> 20 | m2 << 24 : m0 | m1 << 44;
+                        const uint32_t see0 = (uint32_t)see, see1 = (uint32_t)(see >> 32);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
-                            tm_st16(o_at + s * DP + c, o);
+                        for (int j = 0; j < 32; ++j) {
+                            if (!((see0 >> j) & 1u)) x[j] = 0xff800000u;
+                            if (!((see1 >> j) & 1u)) x[32 + j] = 0xff800000u;
                         }
                     }
-                }
-                const float shift = ref == neg_inf() ? 0.f : -ref;
-                float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                    float m0 = neg_inf(), m1 = m0;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        float e0, e1, e2, e3;
-                        fma2(e0, e1, __uint_as_float(x[32 * h + j]), __uint_as_float(x[32 * h + j + 1]), scale, shift);
-                        fma2(e2, e3, __uint_as_float(x[32 * h + j + 2]), __uint_as_float(x[32 * h + j + 3]), scale, shift);
-                        e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
-                        add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
-                        p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
+                    for (int j = 0; j < 64; j += 4) {
+                        m0 = max3(m0, __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+                        m1 = max3(m1, __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]));
                     }
-                    tm_st16(s_at + 16 * h, p);
+                    const float top = fmaxf(m0, m1) * scale;
+                    const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
+                    if (__any_sync(kFullMask, raise)) {
+                        const float factor = raise ? ex2(ref - top) : 1.f;         // 0 where nothing has been seen before
+                        if (raise) { ref = top; sum *= factor; }
+                        if (h && !mbar_wait(msmem_u32(&sm.half_done[s]), steps & 1u, abort_flag, limit)) { ok = false; break; }
+                        if (t > first || h) {              // (these scores came behind the outputs of all steps before)
+                            tc_after();
+#pragma unroll 1
+                            for (int c = 0; c < DP; c += 16) {
+                                uint32_t o[16];
+                                tm_ld16(o_at + s * DP + c, o);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * factor);
+                                tm_st16(o_at + s * DP + c, o);
+                            }
+                        }
+                    }
+                    const float shift = ref == neg_inf() ? 0.f : -ref;
+                    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            float e0, e1, e2, e3;
+                            fma2(e0, e1, __uint_as_float(x[32 * q + j]), __uint_as_float(x[32 * q + j + 1]), scale, shift);
+                            fma2(e2, e3, __uint_as_float(x[32 * q + j + 2]), __uint_as_float(x[32 * q + j + 3]), scale, shift);
+                            e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
+                            add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
+                            p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
+                        }
+                        tm_st16(s_at + 32 * h + 16 * q, p);
+                    }
+                    sum += (s0 + s1) + (s2 + s3);
+                    tm_wait_st();
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(msmem_u32(&sm.p_ready[s][h]));
                 }
-                sum += (s0 + s1) + (s2 + s3);
-                tm_wait_st();
-                tc_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(msmem_u32(&sm.p_ready[s]));
+                if (!ok) break;
             }
             if (!ok) break;
-            // --- the item's outputs
+            // --- the item's outputs.  A thread has a row's, and memory wants rows' neighbours: 32 columns at a time go through shared memory, and
+            // four lanes (a piece of an item: eight) have a row.
             const int64_t part = pc.whole() ? -1 : (int64_t)(2 * blockIdx.x + cut) * kXRows;
             if (part >= 0) ++cut;
-            const int row = two ? s * 128 + in_stream : in_stream;
+            const int row0 = (two ? s * 128 : 0) + (warp & 3) * 32, row = row0 + lane;
             const bool in = row < pc.rows;
             const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + (in ? row : 0));
+            const int64_t out_at = (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head;
+            grid_dependency_wait();                        // the rows' own part
             float own = neg_inf();
             bool write = in;
             if (part < 0) write = prefix_own(a, w, &own) && in;
+            const int c0 = two ? 0 : s * (DP / 2), c1 = two ? DP : c0 + DP / 2;
+            uint4 old[4];                                  // what the rows that this lane will write have of their own, one block of columns ahead
+            const auto fetch = [&](int c) {
+                const int col = c + (lane & 3) * 8;
+                const uint32_t rows_in = __ballot_sync(kFullMask, write);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i * 8 + (lane >> 2);
+                    const int64_t at = __shfl_sync(kFullMask, out_at, r);
+                    if (((rows_in >> r) & 1u) && col < a.D) old[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out + at + col);
+                    else old[i] = make_uint4(0, 0, 0, 0);
+                }
+            };
+            if (part < 0) fetch(c0);
             if (!mbar_wait(msmem_u32(&sm.o_done[s]), piece & 1, abort_flag, limit)) { ok = false; break; }
             float f = 1.f, g = 0.f;                        // factors of this stream's output, and of the other's
             if (!two) {
@@ -328,11 +380,12 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
             } else if (sum == 0.f) f = 0.f;
             float w_own = 0.f, w_pre = 1.f, lse = 0.f;
             if (part < 0) write = prefix_join(own, ref, sum, &w_own, &w_pre, &lse) && write;
+            const uint32_t rows_in = __ballot_sync(kFullMask, write);
             tc_after();
-            __nv_bfloat16* out = (__nv_bfloat16*)a.out + (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head;
-            const int c0 = two ? 0 : s * (DP / 2), c1 = two ? DP : c0 + DP / 2;
+            float4 (*turn)[8] = sm.turn[warp];
 #pragma unroll 1
             for (int c = c0; c < c1; c += 32) {
+                if (c >= a.D) break;
                 uint32_t u[32];
                 float y[32];
                 tm_ld32(o_at + s * DP + c, u);
@@ -343,26 +396,39 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
 #pragma unroll
                     for (int j = 0; j < 32; ++j) y[j] += g == 0.f ? 0.f : __uint_as_float(u[j]) * g;
                 }
+                __syncwarp();                              // the last block of columns has been read
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    if (!write || c + j >= a.D) continue;
-                    if (part >= 0) {
-                        float4* po = reinterpret_cast<float4*>(a.part_o + (part + row) * a.D + c + j);
-                        po[0] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
-                        po[1] = make_float4(y[j + 4], y[j + 5], y[j + 6], y[j + 7]);
-                    } else {
-                        uint4* at = reinterpret_cast<uint4*>(out + c + j);
-                        const uint4 o = *at;
-                        const uint32_t old[4] = {o.x, o.y, o.z, o.w};
-                        uint32_t v[4];
+                for (int j = 0; j < 8; ++j) turn[lane][j ^ (lane & 7)] = make_float4(y[4 * j] * w_pre, y[4 * j + 1] * w_pre, y[4 * j + 2] * w_pre, y[4 * j + 3] * w_pre);
+                __syncwarp();
+                if (part >= 0) {
+                    const int col = c + (lane & 7) * 4;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[i] = pack_bf16(fmaf(w_own, __uint_as_float(old[i] << 16), w_pre * y[j + 2 * i]),
-                                             fmaf(w_own, __uint_as_float(old[i] & 0xffff0000u), w_pre * y[j + 2 * i + 1]));
-                        *at = make_uint4(v[0], v[1], v[2], v[3]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + (lane >> 3);
+                        const float4 v = turn[r][(lane & 7) ^ (r & 7)];
+                        if (((rows_in >> r) & 1u) && col < a.D) *reinterpret_cast<float4*>(a.part_o + (part + row0 + r) * a.D + col) = v;
+                    }
+                } else {
+                    const int col = c + (lane & 3) * 8;
+                    uint4 now[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) now[i] = old[i];
+                    if (c + 32 < c1 && c + 32 < a.D) fetch(c + 32);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 8 + (lane >> 2);
+                        const int64_t at = __shfl_sync(kFullMask, out_at, r);
+                        const float wo = __shfl_sync(kFullMask, w_own, r);
+                        const float4 v0 = turn[r][((lane & 3) * 2) ^ (r & 7)], v1 = turn[r][((lane & 3) * 2 + 1) ^ (r & 7)];
+                        const uint32_t o[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+                        const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+                        uint32_t z[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            z[k] = pack_bf16(fmaf(wo, __uint_as_float(o[k] << 16), v[2 * k]), fmaf(wo, __uint_as_float(o[k] & 0xffff0000u), v[2 * k + 1]));
+                        if (((rows_in >> r) & 1u) && col < a.D) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at + col) = make_uint4(z[0], z[1], z[2], z[3]);
                     }
                 }
-                __syncwarp();
             }
             if (write && (two || s == 0)) {
                 if (part >= 0) { a.part_ml[2 * (part + row)] = ref; a.part_ml[2 * (part + row) + 1] = sum; }
@@ -378,6 +444,7 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
     tc_before();
     __syncthreads();
     tc_after();
+    grid_dependency_wait();                                // (a block without work too: what follows this kernel follows the one before it)
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
     if (sm.abort_flag && tid == 0) {
         atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT);
