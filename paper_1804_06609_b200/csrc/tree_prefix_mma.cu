@@ -14,6 +14,7 @@
 //              may end inside a tile; keys K-major, values MN-major, both [key][d] in the 128-byte swizzle.
 // The epilogue joins a whole item with the rows' own part and writes the result; pieces of an item go to scratch, and to the joining
 // kernel (tree_prefix.cu).  Every wait on an mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "tree_mma.cuh"
@@ -23,53 +24,98 @@ namespace dba {
 
 namespace {
 
-constexpr int kXKeys = 128, kXRows = 256, kXThreads = 384, kXLoadWarps = 3, kXLoadThreads = 32 * kXLoadWarps;
-constexpr int kXSeen = 8;              // more than the tiles the loaders may be ahead by
-constexpr int kXWarpRows = 44;         // rows of a tile that a loader copies: 44, 44, 40
+constexpr int kXKeys = 128, kXRows = 256;
+constexpr int kXSeen = 8;              // more than the tiles the loader may be ahead by
 
-template <int DP> struct XConf {
+// Keys and values as tensors of (head dimension, place in a page, page, head), for copies of `rows` places of a page at a time.
+struct XMaps { CUtensorMap k, v; int32_t rows; };
+template <int DP, bool TMA> struct XConf {
+    static constexpr int load_warps = TMA ? 2 : 4, threads = 32 * (10 + load_warps);
+    static constexpr int q_warps = TMA ? 1 : load_warps;               // of them, those that load queries
     static constexpr int tile_bytes = kXKeys * DP * 2, q_half = 128 * DP * 2, q_bytes = 2 * q_half;
     static constexpr int stages = DP == 128 ? 4 : 8, q_bufs = DP == 128 ? 1 : 2;
     static constexpr int s_col = 0, o_col = 256, tmem_cols = 512;
 };
-template <int DP> struct XSmem {
-    using C = XConf<DP>;
+template <int DP, bool TMA> struct XSmem {
+    using C = XConf<DP, TMA>;
     alignas(1024) unsigned char q[C::q_bufs][C::q_bytes];
     unsigned char kv[C::stages][C::tile_bytes];
     float4 turn[8][32][8];                      // by softmax warp: 32 columns of its rows, on their way to memory
     uint64_t full[C::stages], empty[C::stages];
-    uint64_t s_full[2], p_ready[2][2], half_done[2], o_done[2];
+    uint64_t s_full[2][2], p_ready[2][2], pv_done[2], o_done[2];
     uint64_t q_full[C::q_bufs], q_empty[C::q_bufs];
-    uint64_t o_free, ml_ready, last;
+    uint64_t o_free, ml_ready, last[2];
     float ml[2][128][2];
-    uint32_t seen[kXSeen][kXLoadWarps][2];      // (by tile, in turn) which rows of a loader's there are
+    uint32_t seen[kXSeen][4];                   // (by tile, in turn) which of its rows there are
     uint32_t tmem_base;
     int abort_flag;
     union {
         SpanShared span;                        // (until the roles begin)
-        uint32_t rows[kXLoadWarps * kXWarpRows];       // a tile's rows in the cache, in 16 bytes; kXNoRow: none
+        alignas(16) uint32_t rows[kXKeys];      // a tile's rows in the cache, in 16 bytes; kXNoRow: none
     };
 };
 constexpr uint32_t kXNoRow = 0xffffffffu;
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+// (x, y) = (a0, a1) * b + (c0, c1), and (x, y) = (x, y) * (a0, a1) + c
+__device__ __forceinline__ void fma2v(float& x, float& y, float a0, float a1, float b, float c0, float c1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %6};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(x), "=f"(y) : "f"(a0), "f"(a1), "f"(b), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void fma2v2(float& x, float& y, float a0, float a1, float c) {
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tmov.b64 c, {%4, %4};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x), "+f"(y) : "f"(a0), "f"(a1), "f"(c));
+}
+// 2^x of two numbers on the fused multiply-add pipes, x up to some 2^7: the whole number next to x by adding and taking away 1.5 2^23, a polynomial of
+// degree 4 for the rest f in -1/2 .. 1/2 (least largest relative error, fitted by reweighted least squares with 1 at 0: 2.9e-6), the whole
+// number into the exponent.  Below -126 it goes to 0 through subnormals, and is 0 from -127 on.
+__device__ __forceinline__ void ex2_pair(float& x, float& y) {
+    float tx = fmaxf(x, -127.f), ty = fmaxf(y, -127.f), fx = tx, fy = ty, nx, ny, px, py;
+    add2(tx, ty, 12582912.f, 12582912.f);
+    nx = tx; ny = ty;
+    add2(nx, ny, -12582912.f, -12582912.f);
+    fma2v(fx, fy, nx, ny, -1.f, fx, fy);
+    px = py = 0.009582852944731712f;
+    fma2v2(px, py, fx, fy, 0.055906426161527634f);
+    fma2v2(px, py, fx, fy, 0.24024099111557007f);
+    fma2v2(px, py, fx, fy, 0.6931241750717163f);
+    fma2v2(px, py, fx, fy, 1.f);
+    x = __uint_as_float(__float_as_uint(px) + (__float_as_uint(tx) << 23));
+    y = __uint_as_float(__float_as_uint(py) + (__float_as_uint(ty) << 23));
+}
+// 64 columns from x on of neighbouring places of a page; what lies outside is zeros.
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int token, int page, int head, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(token), "r"(page), "r"(head), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      // (does not wait)
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 using XCut = PrefixCut<kXKeys, kXRows, 128>;
 
-template <int DP>
-__global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __grid_constant__ TreePrefix a, const uint32_t negate) {
-    using C = XConf<DP>;
+template <int DP, bool TMA>
+__global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_kernel(const __grid_constant__ TreePrefix a, const __grid_constant__ XMaps maps,
+                                                                        const uint32_t negate) {
+    using C = XConf<DP, TMA>;
     extern __shared__ __align__(1024) unsigned char xraw[];
-    XSmem<DP>& sm = *reinterpret_cast<XSmem<DP>*>(xraw);
+    XSmem<DP, TMA>& sm = *reinterpret_cast<XSmem<DP, TMA>*>(xraw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     volatile int* abort_flag = &sm.abort_flag;
     const long long limit = a.wait_clocks > 0 ? a.wait_clocks : kMWaitClocks;
     if (tid == 0) {
-        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), kXLoadThreads + kXLoadWarps); mbar_init(msmem_u32(&sm.empty[s]), 1); }
-        // (s_full: the products, and an arrival of the issuing thread, which passes on what the loaders wrote before it)
-        for (int s = 0; s < 2; ++s) { mbar_init(msmem_u32(&sm.s_full[s]), 2); mbar_init(msmem_u32(&sm.p_ready[s][0]), 4); mbar_init(msmem_u32(&sm.p_ready[s][1]), 4);
-                                      mbar_init(msmem_u32(&sm.half_done[s]), 1); mbar_init(msmem_u32(&sm.o_done[s]), 1); }
-        for (int i = 0; i < C::q_bufs; ++i) { mbar_init(msmem_u32(&sm.q_full[i]), kXLoadThreads); mbar_init(msmem_u32(&sm.q_empty[i]), 1); }
+        for (int s = 0; s < C::stages; ++s) { mbar_init(msmem_u32(&sm.full[s]), TMA ? 1 : 33 * C::load_warps); mbar_init(msmem_u32(&sm.empty[s]), 2); }
+        // (s_full: the products, and an arrival of the issuing thread, which passes on what the loader wrote before it)
+        for (int s = 0; s < 2; ++s) {
+            for (int h = 0; h < 2; ++h) { mbar_init(msmem_u32(&sm.s_full[s][h]), 2); mbar_init(msmem_u32(&sm.p_ready[s][h]), 4); }
+            mbar_init(msmem_u32(&sm.pv_done[s]), 1); mbar_init(msmem_u32(&sm.o_done[s]), 1); mbar_init(msmem_u32(&sm.last[s]), 1);
+        }
+        for (int i = 0; i < C::q_bufs; ++i) { mbar_init(msmem_u32(&sm.q_full[i]), 32 * C::q_warps); mbar_init(msmem_u32(&sm.q_empty[i]), 2); }
         mbar_init(msmem_u32(&sm.o_free), 8);
-        mbar_init(msmem_u32(&sm.ml_ready), 8); mbar_init(msmem_u32(&sm.last), 1);
+        mbar_init(msmem_u32(&sm.ml_ready), 8);
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -83,176 +129,239 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
     // is the epilogue's.
     allow_dependents();
     if (blockIdx.x == 0) prefix_check(a);
-    SpanRun run = span_run<kXThreads>(a.groups, 3, &sm.span, [&](int g) { return XCut::units(a, g); });      // (has the block's barriers)
+    SpanRun run = span_run<C::threads>(a.groups, 3, &sm.span, [&](int g) { return XCut::units(a, g); });      // (has the block's barriers)
     __syncthreads();           // its numbers have been read: their place is used again
     tc_after();
     const uint32_t tmem = sm.tmem_base;
     XCut::Piece pc;
     int piece = 0;
     uint32_t tiles0 = 0;                                   // tiles before this piece
-    if (warp > 8) {
-        // ------------------------------------------------------------------ loaders
-        constexpr int CH = DP / 8, RW = 32 / CH;           // 16-byte chunks of a row, rows a warp copies at a time
-        const int lw = warp - 9, ch = lane % CH, sub = lane / CH, base = lw * kXWarpRows, mine = lw < 2 ? kXWarpRows : kXKeys - 2 * kXWarpRows;
+    if (warp > 9) {
+        // ------------------------------------------------------------------ loaders.  TMA: one warp for keys and values, a lane to a box, one for queries.
+        // Else all of them for everything, warp lw rows 32 lw .. 32 lw + 31 of a tile.
+        constexpr int CH = DP / 8, RW = 32 / CH, NJ = 32 / RW;         // 16-byte chunks of a row, rows a warp copies at a time, and how often
+        const int lw = warp - 10, ch = lane % CH, sub = lane / CH, q_warp = TMA ? lw - 1 : lw;
         const bool ch_in = ch * 8 < a.D;
-        const int64_t page16 = a.pages.page_stride / 8, token16 = a.pages.token_stride / 8;
-        const uint32_t q_at = msmem_u32(sm.q), kv_at = msmem_u32(sm.kv) + (uint32_t)(ch >> 3) * (kXKeys * 128) + (uint32_t)(base + sub) * 128;
-        // the swizzle moves a chunk by its row's last three bits (of the queries' rows, and of a tile's: base is 0 or 4 of 8)
-        const uint32_t swz = (uint32_t)((ch & 7) ^ sub) << 4, kv_swz = swz ^ (uint32_t)((base & 7) << 4);
-        uint32_t* const rows = sm.rows + base;
+        const uint32_t q_at = msmem_u32(sm.q), kv_at = msmem_u32(sm.kv);
+        const uint32_t swz = (uint32_t)((ch & 7) ^ sub) << 4;          // the swizzle moves a chunk by its row's last three bits
+        const uint32_t page16 = (uint32_t)(a.pages.page_stride / 8), token16 = (uint32_t)(a.pages.token_stride / 8);
+        const int box_lane = TMA ? min(lane, kXKeys / maps.rows - 1) * maps.rows : lw * 32 + lane;       // the lane's (first) place in a tile
+        uint32_t* const rows = sm.rows + lw * 32;
         uint32_t copy = 0;
         int cut = 0;
         int4 meta[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
         bool ok = true;
+        if (TMA && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.v : &maps.k) : "memory");
         while (ok && XCut::next(a, run, &pc)) {
             if (!pc.whole()) { if (cut == 0) meta[0] = make_int4(pc.g, pc.h, pc.rb, 0); else meta[1] = make_int4(pc.g, pc.h, pc.rb, 0); ++cut; }
-            const uint32_t qb = (uint32_t)piece % C::q_bufs;
-            if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
-            // where a tile's rows are, looked up one tile ahead
-            const int64_t head_at = 2 * (int64_t)pc.h * a.pages.head_stride + (ch_in ? ch * 16 : 0);
-            uint32_t at[2];
-            auto look_up = [&](int t) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = lane + 32 * i, place = t * kXKeys + base + r;
-                    at[i] = kXNoRow;
-                    if (r < mine && place < pc.len && t < pc.tile_end) {
-                        const uint32_t page = tree_page(a.pages, (uint32_t)place);       // (below the table's entries: len is)
-                        const int32_t id = __ldg(a.pages.table + (int64_t)pc.g * a.pages.table_stride + page);
-                        if ((uint32_t)id < (uint32_t)a.pages.num_pages)
-                            at[i] = (uint32_t)((int64_t)id * page16 + (int64_t)((uint32_t)place - page * (uint32_t)a.pages.page_size) * token16);
-                        else atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
-                    }
-                }
+            // where a tile's rows are: page numbers are fetched a tile ahead and not looked at before their turn
+            const int32_t* const table = a.pages.table + (int64_t)pc.g * a.pages.table_stride;
+            int32_t id = 0;
+            const auto fetch = [&](int t) {
+                const int place = t * kXKeys + box_lane;
+                id = place < pc.len ? __ldg(table + tree_page(a.pages, (uint32_t)place)) : -1;       // (below the table's entries: len is)
             };
-            look_up(pc.tile);
-            // queries, zeros beyond the rows and the head size
-            const char* q = (const char*)a.q + (ch_in ? ch * 16 : 0);
+            if (!TMA || lw == 0) fetch(pc.tile);
+            if (q_warp >= 0) {                             // queries, zeros beyond the rows and the head size
+                const uint32_t qb = (uint32_t)piece % C::q_bufs;
+                if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                const char* q = (const char*)a.q + (ch_in ? ch * 16 : 0);
 #pragma unroll 1
-            for (int r0 = lw * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * kXLoadWarps) {        // a lane finds one row, and every lane copies chunks of all
-                int64_t q_row = -1;
-                if (r0 + lane < pc.rows) {
-                    const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
-                    q_row = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
-                }
-                const uint32_t to = q_at + qb * C::q_bytes + (r0 >= 128 ? C::q_half : 0) + (uint32_t)(ch >> 3) * (128 * 128) + (uint32_t)((r0 & 127) + sub) * 128;
-#pragma unroll 1
-                for (int j0 = 0; j0 < 32; j0 += 8 * RW) {
-                    int64_t from[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) from[j] = j0 + j * RW < 32 ? __shfl_sync(kFullMask, q_row, j0 + j * RW + sub) : -1;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j0 + j * RW < 32)
-                            cp_async16(to + (j0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[j] >= 0 ? q + from[j] : q, from[j] >= 0 && ch_in ? 16u : 0u);
-                }
-            }
-            cp_arrive(msmem_u32(&sm.q_full[qb]));
-#pragma unroll 1
-            for (int t = pc.tile; t < pc.tile_end; ++t) {
-                const uint32_t seen0 = __ballot_sync(kFullMask, at[0] != kXNoRow), seen1 = __ballot_sync(kFullMask, at[1] != kXNoRow);
-                __syncwarp();                              // the last tile's rows have been read
-                rows[lane] = at[0];
-                if (lane + 32 < mine) rows[lane + 32] = at[1];
-                if (lane < 2) sm.seen[(tiles0 + t - pc.tile) % kXSeen][lw][lane] = lane ? seen1 : seen0;
-                __syncwarp();
-                look_up(t + 1);
-                constexpr int NJ = kXWarpRows / RW;
-                uint32_t row[NJ];                          // (read before the copies: they are not reordered)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) row[j] = rows[j * RW + sub];
-#pragma unroll 1
-                for (int k = 0; k < 2; ++k, ++copy) {
-                    const uint32_t stage = copy % C::stages, use = copy / C::stages;
-                    if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[stage]), (use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
-                    const char* from = (const char*)(k ? a.v : a.k) + head_at;
-                    const uint32_t to = kv_at + stage * C::tile_bytes;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        if (j * RW >= mine) break;
-                        const bool in = row[j] != kXNoRow && ch_in;
-                        cp_async16(to + j * RW * 128 + (kv_swz ^ (uint32_t)((j * RW & 7) << 4)), from + (uint64_t)(in ? row[j] : 0u) * 16, in ? 16u : 0u);
+                for (int r0 = q_warp * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * C::q_warps) {         // a lane finds one row, and every lane copies chunks of all
+                    int64_t q_row = -1;
+                    if (r0 + lane < pc.rows) {
+                        const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
+                        q_row = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
                     }
-                    if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));
-                    if ((int)copy != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
+                    const uint32_t to = q_at + qb * C::q_bytes + (r0 >= 128 ? C::q_half : 0) + (uint32_t)(ch >> 3) * (128 * 128) + (uint32_t)((r0 & 127) + sub) * 128;
+#pragma unroll 1
+                    for (int j0 = 0; j0 < 32; j0 += 8 * RW) {
+                        int64_t from[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) from[j] = __shfl_sync(kFullMask, q_row, j0 + j * RW + sub);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            cp_async16(to + (j0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[j] >= 0 ? q + from[j] : q, from[j] >= 0 && ch_in ? 16u : 0u);
+                    }
+                }
+                cp_arrive(msmem_u32(&sm.q_full[qb]));
+            }
+            const int64_t head_at = 2 * (int64_t)pc.h * a.pages.head_stride + (ch_in ? ch * 16 : 0);
+#pragma unroll 1
+            for (int t = pc.tile; t < (TMA && lw > 0 ? 0 : pc.tile_end); ++t) {
+                const int place = t * kXKeys + box_lane;
+                const uint32_t in_page = (uint32_t)place - tree_page(a.pages, (uint32_t)place) * (uint32_t)a.pages.page_size;
+                const bool there = (uint32_t)id < (uint32_t)a.pages.num_pages;
+                if (!there && place < pc.len) atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
+                const int page = there ? id : a.pages.num_pages;       // (a page that there is not: zeros)
+                if (TMA) {
+                    // a lane finds the word of the mask that is its own, of four: the boxes' last places on this side of the prefix' end
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t mine = 0;
+                        if (there && lane * maps.rows < kXKeys) {
+                            const int lo = max(box_lane - 32 * w, 0), hi = min(min(box_lane + maps.rows, pc.len - t * kXKeys) - 32 * w, 32);
+                            if (hi > lo) mine = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+                        }
+                        mine = __reduce_or_sync(kFullMask, mine);
+                        if (lane == 0) sm.seen[(tiles0 + t - pc.tile) % kXSeen][w] = mine;
+                    }
+                    __syncwarp();
+                    if (t + 1 < pc.tile_end) fetch(t + 1);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k, ++copy) {
+                        const uint32_t stage = copy % C::stages, use = copy / C::stages, full = msmem_u32(&sm.full[stage]);
+                        if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[stage]), (use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                        if (lane == 0) mbar_expect(full, C::tile_bytes);
+                        __syncwarp();
+                        if ((int)copy != a.drop_item && lane * maps.rows < kXKeys) {
+#pragma unroll
+                            for (int c = 0; c < DP / 64; ++c)
+                                copy_box(kv_at + stage * C::tile_bytes + c * (kXKeys * 128) + box_lane * 128, k ? &maps.v : &maps.k, 64 * c, (int)in_page, page, pc.h, full);
+                        }
+                    }
+                } else {
+                    const uint32_t at = there ? (uint32_t)id * page16 + in_page * token16 : kXNoRow, seen = __ballot_sync(kFullMask, there);     // (the host has seen to it that 32 bits are enough)
+                    __syncwarp();                          // the last tile's rows have been read
+                    rows[(lane % RW) * NJ + lane / RW] = at;           // a lane will copy rows sub, sub + RW, ..: its numbers lie side by side
+                    if (lane == 0) sm.seen[(tiles0 + t - pc.tile) % kXSeen][lw] = seen;
+                    __syncwarp();
+                    if (t + 1 < pc.tile_end) fetch(t + 1);
+                    uint32_t row[NJ];                      // (read before the copies: they are not reordered)
+#pragma unroll
+                    for (int j = 0; j < NJ; j += 4) {
+                        const uint4 r4 = *reinterpret_cast<const uint4*>(rows + sub * NJ + j);
+                        row[j] = r4.x; row[j + 1] = r4.y; row[j + 2] = r4.z; row[j + 3] = r4.w;
+                    }
+#pragma unroll 1
+                    for (int k = 0; k < 2; ++k, ++copy) {
+                        const uint32_t stage = copy % C::stages, use = copy / C::stages;
+                        if (use > 0 && !mbar_wait(msmem_u32(&sm.empty[stage]), (use - 1) & 1u, abort_flag, limit)) { ok = false; break; }
+                        const char* from = (const char*)(k ? a.v : a.k) + head_at;
+                        const uint32_t to = kv_at + stage * C::tile_bytes + (uint32_t)(ch >> 3) * (kXKeys * 128) + (uint32_t)(lw * 32 + sub) * 128;
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) {
+                            const bool in = row[j] != kXNoRow && ch_in;
+                            cp_async16(to + j * RW * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from + (uint64_t)(in ? row[j] : 0u) * 16, in ? 16u : 0u);
+                        }
+                        if (lane == 0) mbar_arrive(msmem_u32(&sm.full[stage]));
+                        if ((int)copy != a.drop_item) cp_arrive(msmem_u32(&sm.full[stage]));
+                    }
                 }
                 if (!ok) break;
             }
             tiles0 += pc.tile_end - pc.tile;
             ++piece;
         }
-        cp_wait_all();
         if (lw == 0 && lane < 2) a.meta[2 * blockIdx.x + lane] = lane ? meta[1] : meta[0];
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------ matrix products: the warp walks in step, one lane issues
-        const int steps16 = (a.D + 15) / 16;
-        const uint32_t idesc_s = mma_idesc(kXKeys, false) | negate, idesc_o = mma_idesc(steps16 * 16, true);
-        const uint32_t q_at = msmem_u32(sm.q), kv_at = msmem_u32(sm.kv);
-        uint32_t done[2] = {0, 0};                         // outputs issued for each stream
+        // nothing of this block is in flight when it leaves (where nobody gave up, all boxes have been waited for)
+        cp_wait_all();
+        if (TMA && lw == 0 && *abort_flag)
+            for (uint32_t c = copy > C::stages ? copy - C::stages : 0; c < copy; ++c)
+                for (int i = 0; i < 100000 && (int)c != a.drop_item && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.full[c % C::stages]), (c / C::stages) & 1u)); ++i) {}
+    } else if (warp > 7) {
+        // ------------------------------------------------------------------ matrix products of stream s: the warp walks in step, one lane issues
+        const int s = warp - 8, steps16 = (a.D + 15) / 16;
+        const uint32_t idesc_s = mma_idesc(kXKeys / 2, false) | negate, idesc_o = mma_idesc(steps16 * 16, true);
+        const uint32_t p_at = tmem + C::s_col + s * kXKeys, o_at = tmem + C::o_col + s * DP;
+        const uint32_t s_full = msmem_u32(&sm.s_full[s][0]), p_ready = msmem_u32(&sm.p_ready[s][0]), pv_done = msmem_u32(&sm.pv_done[s]);
+        const uint64_t k_desc = sw128_desc(msmem_u32(sm.kv), 16), v_desc = sw128_desc(msmem_u32(sm.kv), kXKeys * 128);
+        uint32_t done = 0;                                 // outputs issued
         bool ok = true;
         while (ok && XCut::next(a, run, &pc)) {
             const bool two = pc.rows > 128;
-            const int n = (pc.tile_end - pc.tile) * (two ? 2 : 1);
+            const int tiles = pc.tile_end - pc.tile, by = two ? 1 : 2, n = two ? tiles : (tiles + 1 - s) / 2;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
             if (!(ok = mbar_wait(msmem_u32(&sm.q_full[qb]), ((uint32_t)piece / C::q_bufs) & 1u, abort_flag, limit))) break;
+            const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]) + (two ? s * C::q_half : 0), 16);
+            // rows of this stream's last tile behind the prefix' end
+            const int n_tail = pc.tile_end == pc.tiles && (pc.tiles - 1 - pc.tile) % by == (two ? 0 : s) ? pc.tiles * kXKeys - pc.len : 0;
+            uint32_t k_copy = 2 * (tiles0 + (two ? 0 : s)), v_copy = k_copy + 1;
 #pragma unroll 1
-            for (int i = 0; i < n + 2; ++i) {
-                const uint32_t s = i & 1;
-                if (i >= 2) {                              // outputs of step i - 2
-                    const int j = i - 2;
-                    const uint32_t copy = 2 * (tiles0 + (two ? j >> 1 : j)) + 1, stage = copy % C::stages;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), (copy / C::stages) & 1u, abort_flag, limit))) break;
-                    if (j == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1, abort_flag, limit))) break;
-                    const uint64_t dv = sw128_desc(kv_at + stage * C::tile_bytes, kXKeys * 128);
-                    const uint32_t p = tmem + C::s_col + s * kXKeys, d = tmem + C::o_col + s * DP, parity = (s ? done[1] : done[0]) & 1u;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (!(ok = mbar_wait(msmem_u32(&sm.p_ready[s][h]), parity, abort_flag, limit))) break;
-                        if (elect_one()) {
-                            fence_async_proxy();           // the copies' writes (generic) before the products' reads
-                            tc_after();
-#pragma unroll
-                            for (int ks = 4 * h; ks < 4 * h + 4; ++ks) mma_ts(d, p + ks * 8, dv + (uint64_t)(ks * 2048 / 16), idesc_o, j >= 2 || ks != 0, -1);
-                            if (h == 0) mma_commit(msmem_u32(&sm.half_done[s]));
-                            else {
-                                if (!two || s == 1) mma_commit(msmem_u32(&sm.empty[stage]));
-                                if (j + 2 >= n) mma_commit(msmem_u32(&sm.o_done[s]));
-                                if (n == 1) mma_commit(msmem_u32(&sm.o_done[1]));
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    if (!ok) break;
-                    if (s) ++done[1]; else ++done[0];
-                }
-                if (i < n) {
-                    const uint32_t copy = 2 * (tiles0 + (two ? i >> 1 : i)), stage = copy % C::stages;
-                    if (!(ok = mbar_wait(msmem_u32(&sm.full[stage]), (copy / C::stages) & 1u, abort_flag, limit))) break;
-                    const uint64_t dq = sw128_desc(q_at + qb * C::q_bytes + (two ? s * C::q_half : 0), 16), dk = sw128_desc(kv_at + stage * C::tile_bytes, 16);
-                    const uint32_t d = tmem + C::s_col + s * kXKeys;
+            for (int g = n ? -1 : 0; g < n; ++g) {
+                const uint32_t v_stage = v_copy % C::stages, k_stage = k_copy % C::stages;
+                const uint64_t dv = v_desc + (uint64_t)(v_stage * (C::tile_bytes / 16)), dk = k_desc + (uint64_t)(k_stage * (C::tile_bytes / 16));
+                if (g >= 0 && !(ok = mbar_wait(msmem_u32(&sm.full[v_stage]), (v_copy / C::stages) & 1u, abort_flag, limit))) break;
+                if (g == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1, abort_flag, limit))) break;      // (the outputs' place)
+                // the scores of half a tile, over the probabilities of the same half of the one before
+                const auto scores = [&](int h) {
                     if (elect_one()) {
-                        fence_async_proxy();
+                        if (!TMA || g < 0) fence_async_proxy();        // the copies' writes (generic) before the products' reads
                         tc_after();
 #pragma unroll
                         for (int ks = 0; ks < DP / 16; ++ks)       // 16 dimensions = 32 bytes along a swizzled row; 64 to a block of columns
                             if (ks < steps16)
-                                mma_ss(d, dq + (uint64_t)((ks >> 2) * (128 * 128 / 16) + (ks & 3) * 2), dk + (uint64_t)((ks >> 2) * (kXKeys * 128 / 16) + (ks & 3) * 2),
-                                       idesc_s, ks != 0, -1);
-                        if (!two || s == 1) mma_commit(msmem_u32(&sm.empty[stage]));
-                        mma_commit(msmem_u32(&sm.s_full[s]));
-                        mbar_arrive(msmem_u32(&sm.s_full[s]));
-                        if (i + 1 == n) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                                mma_ss(p_at + 64 * h, dq + (uint64_t)((ks >> 2) * (128 * 128 / 16) + (ks & 3) * 2),
+                                       dk + (uint64_t)(h * (64 * 128 / 16) + (ks >> 2) * (kXKeys * 128 / 16) + (ks & 3) * 2), idesc_s, ks != 0, -1);
+                        mma_commit(s_full + 8 * h);
+                        mbar_arrive(s_full + 8 * h);
+                        if (h) {
+                            mma_commit(msmem_u32(&sm.empty[k_stage]));
+                            if (!two) mma_commit(msmem_u32(&sm.empty[k_stage]));       // (for the other stream too)
+                            if (g + 2 == n) mma_commit(msmem_u32(&sm.q_empty[qb]));    // the queries have been used
+                        }
                     }
                     __syncwarp();
+                };
+                const uint32_t k_full = msmem_u32(&sm.full[k_stage]), k_parity = (k_copy / C::stages) & 1u;
+                bool early = false;                        // the next keys are there before these values are done with
+                if (g >= 0) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {          // outputs of half a tile
+                        if (!(ok = mbar_wait(p_ready + 8 * h, done & 1u, abort_flag, limit))) break;
+                        if (TMA && h == 0 && n_tail && g + 1 == n) {       // (places behind the prefix hold anything, and 0 times it may be anything)
+                            for (int i = lane; i < n_tail * (DP / 8); i += 32) {
+                                const int r = kXKeys - 1 - i / (DP / 8), c = i % (DP / 8);
+                                *reinterpret_cast<uint4*>(&sm.kv[v_stage][(c >> 3) * (kXKeys * 128) + r * 128 + (c & 7) * 16]) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_proxy();
+                            __syncwarp();
+                        }
+                        if (elect_one()) {
+                            if (!TMA) fence_async_proxy();
+                            tc_after();
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks)
+                                mma_ts(o_at, p_at + 64 * h + ks * 8, dv + (uint64_t)((4 * h + ks) * 2048 / 16), idesc_o, g > 0 || h > 0 || ks > 0, -1);
+                            mma_commit(pv_done);
+                            if (h) {
+                                mma_commit(msmem_u32(&sm.empty[v_stage]));
+                                if (!two) mma_commit(msmem_u32(&sm.empty[v_stage]));
+                            }
+                        }
+                        __syncwarp();
+                        if (h == 0 && g + 1 < n && __all_sync(kFullMask, mbar_test(k_full, k_parity))) {
+                            early = true;
+                            scores(0);
+                        }
+                    }
+                    if (!ok) break;
                 }
+                if (g + 1 < n) {
+                    if (!early) {
+                        if (!(ok = mbar_wait(k_full, k_parity, abort_flag, limit))) break;
+                        scores(0);
+                    }
+                    scores(1);
+                }
+                if (!ok) break;
+                if (g >= 0) { ++done; v_copy += 2 * by; }
+                k_copy += 2 * by;
             }
             if (!ok) break;
-            tiles0 += pc.tile_end - pc.tile;
+            if (n == 0) {                                  // (one tile for both streams)
+                if (elect_one()) mma_commit(msmem_u32(&sm.q_empty[qb]));
+                __syncwarp();
+                if (piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1, abort_flag, limit))) break;
+            }
+            if (elect_one()) mma_commit(msmem_u32(&sm.o_done[s]));
+            __syncwarp();
+            tiles0 += tiles;
             ++piece;
         }
         // nothing of this block is in flight when it leaves, whatever happened
-        if (elect_one()) mma_commit(msmem_u32(&sm.last));
-        for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last), 0)); ++i) {}
+        if (elect_one()) mma_commit(msmem_u32(&sm.last[s]));
+        for (int i = 0; i < 1000000 && !__all_sync(kFullMask, mbar_try(msmem_u32(&sm.last[s]), 0)); ++i) {}
     } else {
         // ------------------------------------------------------------------ softmax: stream s, a row per thread
         const int s = warp >> 2, in_stream = tid & 127;
@@ -268,20 +377,15 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
             const int first = pc.tile + (two ? 0 : s), by = two ? 1 : 2;
 #pragma unroll 1
             for (int t = first; t < pc.tile_end; t += by, ++steps) {
-                if (!mbar_wait(msmem_u32(&sm.s_full[s]), steps & 1u, abort_flag, limit)) { ok = false; break; }
-                tc_after();
-                const uint32_t (*seen)[2] = sm.seen[(tiles0 + t - pc.tile) % kXSeen];
-                const bool all = (seen[0][0] & seen[1][0] & seen[2][0]) == 0xffffffffu && seen[0][1] == 0xfffu && seen[1][1] == 0xfffu && seen[2][1] == 0xffu;
-                // Half a tile at a time: the first half's outputs are under way while the second goes through here, and 64 scores fit
-                // the registers.
+                const uint32_t* seen = sm.seen[(tiles0 + t - pc.tile) % kXSeen];
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 2; ++h) {              // half a tile at a time
+                    if (!mbar_wait(msmem_u32(&sm.s_full[s][h]), steps & 1u, abort_flag, limit)) { ok = false; break; }
+                    tc_after();
                     uint32_t x[64];
                     tm_ld64(s_at + 64 * h, x);
-                    if (!all) {                            // the end of the prefix, or a page that there is not
-                        const uint64_t m0 = (uint64_t)seen[0][1] << 32 | seen[0][0], m1 = (uint64_t)seen[1][1] << 32 | seen[1][0], m2 = (uint64_t)seen[2][1] << 32 | seen[2][0];
-                        const uint64_t see = h ? m1 >> 20 | m2 << 24 : m0 | m1 << 44;
-                        const uint32_t see0 = (uint32_t)see, see1 = (uint32_t)(see >> 32);
+                    const uint32_t see0 = seen[2 * h], see1 = seen[2 * h + 1];
+                    if ((see0 & see1) != 0xffffffffu) {    // the end of the prefix, or a page that there is not
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
                             if (!((see0 >> j) & 1u)) x[j] = 0xff800000u;
@@ -299,8 +403,9 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                     if (__any_sync(kFullMask, raise)) {
                         const float factor = raise ? ex2(ref - top) : 1.f;         // 0 where nothing has been seen before
                         if (raise) { ref = top; sum *= factor; }
-                        if (h && !mbar_wait(msmem_u32(&sm.half_done[s]), steps & 1u, abort_flag, limit)) { ok = false; break; }
-                        if (t > first || h) {              // (these scores came behind the outputs of all steps before)
+                        if (t > first || h) {
+                            // the outputs before this half (those before them came before these scores, so the parity cannot be an older phase's)
+                            if (!mbar_wait(msmem_u32(&sm.pv_done[s]), (2 * steps + h - 1) & 1u, abort_flag, limit)) { ok = false; break; }
                             tc_after();
 #pragma unroll 1
                             for (int c = 0; c < DP; c += 16) {
@@ -322,11 +427,13 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
                             float e0, e1, e2, e3;
                             fma2(e0, e1, __uint_as_float(x[32 * q + j]), __uint_as_float(x[32 * q + j + 1]), scale, shift);
                             fma2(e2, e3, __uint_as_float(x[32 * q + j + 2]), __uint_as_float(x[32 * q + j + 3]), scale, shift);
-                            e0 = ex2(e0); e1 = ex2(e1); e2 = ex2(e2); e3 = ex2(e3);
+                            e0 = ex2(e0); e1 = ex2(e1);
+                            if (j % 8 == 8 - 4) ex2_pair(e2, e3);
+                            else { e2 = ex2(e2); e3 = ex2(e3); }
                             add2(s0, s1, e0, e1); add2(s2, s3, e2, e3);
                             p[j / 2] = pack_bf16(e0, e1); p[j / 2 + 1] = pack_bf16(e2, e3);
                         }
-                        tm_st16(s_at + 32 * h + 16 * q, p);
+                        tm_st16(s_at + 64 * h + 16 * q, p);
                     }
                     sum += (s0 + s1) + (s2 + s3);
                     tm_wait_st();
@@ -452,26 +559,58 @@ __global__ void __launch_bounds__(kXThreads, 1) tree_prefix_mma_kernel(const __g
     }
 }
 
-template <int DP>
+template <int DP, bool TMA>
 cudaError_t configure_prefix_mma() {
-    static_assert(sizeof(XSmem<DP>) <= 227 * 1024, "a block's shared memory");
-    return cudaFuncSetAttribute(tree_prefix_mma_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(XSmem<DP>));
+    static_assert(sizeof(XSmem<DP, TMA>) <= 227 * 1024, "a block's shared memory");
+    return cudaFuncSetAttribute(tree_prefix_mma_kernel<DP, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(XSmem<DP, TMA>));
 }
-template <int DP>
-cudaError_t launch_prefix_mma(const TreePrefix& a, int grid, cudaStream_t st) {
+typedef CUresult (*XEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                            CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+XEncode encode_fn() {
+    static const XEncode fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess ? (XEncode)f : nullptr;
+    }();
+    return fn;
+}
+bool make_map(CUtensorMap* map, const void* base, const TreePrefix& a, int rows) {
+    const TreePages& pg = a.pages;
+    // (a dimension of one has any stride)
+    const auto bytes = [&](int64_t n, int64_t stride) { return (cuuint64_t)(n > 1 ? 2 * stride : 16); };
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)pg.page_size, (cuuint64_t)pg.num_pages, (cuuint64_t)a.K};
+    const cuuint64_t strides[3] = {bytes(pg.page_size, pg.token_stride), bytes(pg.num_pages, pg.page_stride), bytes(a.K, pg.head_stride)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+    const XEncode fn = encode_fn();
+    return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <int DP, bool TMA>
+cudaError_t launch_prefix_mma(const TreePrefix& a, const XMaps& m, int grid, cudaStream_t st) {
     const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
-    return launch_after(tree_prefix_mma_kernel<DP>, dim3(grid), dim3(kXThreads), sizeof(XSmem<DP>), st, a, negate);
+    return launch_after(tree_prefix_mma_kernel<DP, TMA>, dim3(grid), dim3(XConf<DP, TMA>::threads), sizeof(XSmem<DP, TMA>), st, a, m, negate);
 }
 
 }  // namespace
 
 int tree_prefix_mma_rows() { return kXRows; }
 cudaError_t configure_tree_prefix_mma() {
-    const cudaError_t e = configure_prefix_mma<64>();
-    return e == cudaSuccess ? configure_prefix_mma<128>() : e;
+    cudaError_t e = configure_prefix_mma<64, true>();
+    if (e == cudaSuccess) e = configure_prefix_mma<128, true>();
+    if (e == cudaSuccess) e = configure_prefix_mma<64, false>();
+    return e == cudaSuccess ? configure_prefix_mma<128, false>() : e;
 }
+// Boxes of 8 to 128 places, the most that divide both a page and a tile; pages that are not made of eights, and strides that no tensor map has
+// (there are few), by copies of 16 bytes.
 cudaError_t launch_tree_prefix_mma(const TreePrefix& a, int grid, cudaStream_t st) {
-    return a.D <= 64 ? launch_prefix_mma<64>(a, grid, st) : launch_prefix_mma<128>(a, grid, st);
+    XMaps m;
+    m.rows = 128;
+    while (a.pages.page_size % m.rows) m.rows /= 2;
+    if (m.rows >= 8 && make_map(&m.k, a.k, a, m.rows) && make_map(&m.v, a.v, a, m.rows))
+        return a.D <= 64 ? launch_prefix_mma<64, true>(a, m, grid, st) : launch_prefix_mma<128, true>(a, m, grid, st);
+    m = XMaps{};
+    m.rows = kXKeys;
+    return a.D <= 64 ? launch_prefix_mma<64, false>(a, m, grid, st) : launch_prefix_mma<128, false>(a, m, grid, st);
 }
 
 }  // namespace dba
