@@ -118,6 +118,9 @@ struct TreeWeigh {
     int drop_item;
 };
 cudaError_t configure_tree_weigh();
+// the tensor-core kernel (tree_weigh_mma.cu); usable where tree_mma_usable
+cudaError_t configure_tree_weigh_mma();
+cudaError_t launch_tree_weigh_mma(const TreeWeigh& a, int grid, cudaStream_t st);
 cudaError_t launch_tree_weigh(const TreeWeigh& a, int dtype, int sm_count, cudaStream_t st, int* launches);
 struct TreeEvict {
     TreePages from, to;

@@ -14,10 +14,9 @@
 //              may end inside a tile; keys K-major, values MN-major, both [key][d] in the 128-byte swizzle.
 // The epilogue joins a whole item with the rows' own part and writes the result; pieces of an item go to scratch, and to the joining
 // kernel (tree_prefix.cu).  Every wait on an mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
-#include <cuda.h>
 #include <cuda_bf16.h>
 
-#include "tree_mma.cuh"
+#include "tree_boxes.cuh"
 #include "tree_span.cuh"
 
 namespace dba {
@@ -27,8 +26,6 @@ namespace {
 constexpr int kXKeys = 128, kXRows = 256;
 constexpr int kXSeen = 8;              // more than the tiles the loader may be ahead by
 
-// Keys and values as tensors of (head dimension, place in a page, page, head), for copies of `rows` places of a page at a time.
-struct XMaps { CUtensorMap k, v; int32_t rows; };
 template <int DP, bool TMA> struct XConf {
     static constexpr int load_warps = TMA ? 2 : 4, threads = 32 * (10 + load_warps);
     static constexpr int q_warps = TMA ? 1 : load_warps;               // of them, those that load queries
@@ -82,23 +79,10 @@ __device__ __forceinline__ void ex2_pair(float& x, float& y) {
     x = __uint_as_float(__float_as_uint(px) + (__float_as_uint(tx) << 23));
     y = __uint_as_float(__float_as_uint(py) + (__float_as_uint(ty) << 23));
 }
-// 64 columns from x on of neighbouring places of a page; what lies outside is zeros.
-__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int token, int page, int head, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(token), "r"(page), "r"(head), "r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      // (does not wait)
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 using XCut = PrefixCut<kXKeys, kXRows, 128>;
 
 template <int DP, bool TMA>
-__global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_kernel(const __grid_constant__ TreePrefix a, const __grid_constant__ XMaps maps,
+__global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_kernel(const __grid_constant__ TreePrefix a, const __grid_constant__ TreeBoxes maps,
                                                                         const uint32_t negate) {
     using C = XConf<DP, TMA>;
     extern __shared__ __align__(1024) unsigned char xraw[];
@@ -195,17 +179,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
                 if (!there && place < pc.len) atomicOr(a.pages.status, (uint32_t)DBA_TREE_BAD_PAGE);
                 const int page = there ? id : a.pages.num_pages;       // (a page that there is not: zeros)
                 if (TMA) {
-                    // a lane finds the word of the mask that is its own, of four: the boxes' last places on this side of the prefix' end
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        uint32_t mine = 0;
-                        if (there && lane * maps.rows < kXKeys) {
-                            const int lo = max(box_lane - 32 * w, 0), hi = min(min(box_lane + maps.rows, pc.len - t * kXKeys) - 32 * w, 32);
-                            if (hi > lo) mine = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
-                        }
-                        mine = __reduce_or_sync(kFullMask, mine);
-                        if (lane == 0) sm.seen[(tiles0 + t - pc.tile) % kXSeen][w] = mine;
-                    }
+                    boxes_seen(sm.seen[(tiles0 + t - pc.tile) % kXSeen], maps.rows, box_lane, there, pc.len - t * kXKeys);
                     __syncwarp();
                     if (t + 1 < pc.tile_end) fetch(t + 1);
 #pragma unroll
@@ -564,29 +538,8 @@ cudaError_t configure_prefix_mma() {
     static_assert(sizeof(XSmem<DP, TMA>) <= 227 * 1024, "a block's shared memory");
     return cudaFuncSetAttribute(tree_prefix_mma_kernel<DP, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(XSmem<DP, TMA>));
 }
-typedef CUresult (*XEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                            CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-XEncode encode_fn() {
-    static const XEncode fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess ? (XEncode)f : nullptr;
-    }();
-    return fn;
-}
-bool make_map(CUtensorMap* map, const void* base, const TreePrefix& a, int rows) {
-    const TreePages& pg = a.pages;
-    // (a dimension of one has any stride)
-    const auto bytes = [&](int64_t n, int64_t stride) { return (cuuint64_t)(n > 1 ? 2 * stride : 16); };
-    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)pg.page_size, (cuuint64_t)pg.num_pages, (cuuint64_t)a.K};
-    const cuuint64_t strides[3] = {bytes(pg.page_size, pg.token_stride), bytes(pg.num_pages, pg.page_stride), bytes(a.K, pg.head_stride)};
-    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
-    const XEncode fn = encode_fn();
-    return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 template <int DP, bool TMA>
-cudaError_t launch_prefix_mma(const TreePrefix& a, const XMaps& m, int grid, cudaStream_t st) {
+cudaError_t launch_prefix_mma(const TreePrefix& a, const TreeBoxes& m, int grid, cudaStream_t st) {
     const uint32_t negate = a.scale_log2e < 0.f ? 1u << 13 : 0u;       // the scores' sign by the instruction, their size by the softmax
     return launch_after(tree_prefix_mma_kernel<DP, TMA>, dim3(grid), dim3(XConf<DP, TMA>::threads), sizeof(XSmem<DP, TMA>), st, a, m, negate);
 }
@@ -600,16 +553,10 @@ cudaError_t configure_tree_prefix_mma() {
     if (e == cudaSuccess) e = configure_prefix_mma<64, false>();
     return e == cudaSuccess ? configure_prefix_mma<128, false>() : e;
 }
-// Boxes of 8 to 128 places, the most that divide both a page and a tile; pages that are not made of eights, and strides that no tensor map has
-// (there are few), by copies of 16 bytes.
 cudaError_t launch_tree_prefix_mma(const TreePrefix& a, int grid, cudaStream_t st) {
-    XMaps m;
-    m.rows = 128;
-    while (a.pages.page_size % m.rows) m.rows /= 2;
-    if (m.rows >= 8 && make_map(&m.k, a.k, a, m.rows) && make_map(&m.v, a.v, a, m.rows))
+    TreeBoxes m{};
+    if (tree_boxes(&m, a.k, a.v, a.pages, a.K, a.D, 0))
         return a.D <= 64 ? launch_prefix_mma<64, true>(a, m, grid, st) : launch_prefix_mma<128, true>(a, m, grid, st);
-    m = XMaps{};
-    m.rows = kXKeys;
     return a.D <= 64 ? launch_prefix_mma<64, false>(a, m, grid, st) : launch_prefix_mma<128, false>(a, m, grid, st);
 }
 

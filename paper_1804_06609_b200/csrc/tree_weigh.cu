@@ -150,18 +150,16 @@ cudaError_t configure_tree_weigh() {
     cudaError_t e = configure_weigh<float, 64>();
     if (e == cudaSuccess) e = configure_weigh<float, 128>();
     if (e == cudaSuccess) e = configure_weigh<float, 256>();
-    if (e == cudaSuccess) e = configure_weigh<__nv_bfloat16, 64>();
-    if (e == cudaSuccess) e = configure_weigh<__nv_bfloat16, 128>();
     if (e == cudaSuccess) e = configure_weigh<__nv_bfloat16, 256>();
-    return e;
+    return e == cudaSuccess ? configure_tree_weigh_mma() : e;
 }
 
 cudaError_t launch_tree_weigh(const TreeWeigh& a, int dtype, int sm_count, cudaStream_t st, int* launches) {
     *launches += 1;
+    if (tree_mma_usable(dtype, a.D)) return launch_tree_weigh_mma(a, sm_count, st);
     if (dtype == DBA_F32)
         return a.D <= 64 ? launch_weigh<float, 64>(a, sm_count, st) : a.D <= 128 ? launch_weigh<float, 128>(a, sm_count, st) : launch_weigh<float, 256>(a, sm_count, st);
-    return a.D <= 64 ? launch_weigh<__nv_bfloat16, 64>(a, sm_count, st) : a.D <= 128 ? launch_weigh<__nv_bfloat16, 128>(a, sm_count, st)
-                                                                                  : launch_weigh<__nv_bfloat16, 256>(a, sm_count, st);
+    return launch_weigh<__nv_bfloat16, 256>(a, sm_count, st);
 }
 
 }  // namespace dba
