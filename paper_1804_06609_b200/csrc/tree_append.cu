@@ -87,17 +87,30 @@ __global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_t
     }
 }
 
-// The same for decoders that norm queries and keys: y = x / sqrt(mean(x^2) + eps) * weight per head, then the rotation.  A head is
-// the work of L lanes next to one another (the power of two from D/(2 VEC) up, 32 at most), which hold its UNITS units each in registers between
-// the sum of squares and the turn; a thread keeps the same dimensions from head to head, so weights, cosines and sines are read once a token.
-// Sum, norm and turn are fp32; the one rounding is the store's.
-template <typename T, int VEC, bool PAIRS, int UNITS>
-__global__ void __launch_bounds__(kAThreads) tree_append_norm_kernel(const dba_tree_tokens t, const dba_tree_norm nm, const TreePages pg, T* ck, T* cv, int B,
-                                                                     int H, int K, int D, int lanes) {
+// (x, y) = (a0, a1) * (b0, b1) [+ (x, y)]
+__device__ __forceinline__ void norm_mul2(float& x, float& y, float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "=f"(x), "=f"(y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void norm_fma2(float& x, float& y, float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%0, %1};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x), "+f"(y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// The same for decoders that norm queries and keys: y = x / sqrt(mean(x^2) + eps) * weight per head, then the rotation.  A block per token;
+// a head is the work of `lanes` lanes next to one another (the power of two from D/(2 VEC) up, 32 at most), each with UNITS units of
+// it.  With r the root's inverse, a pair of dimensions (a, b) becomes
+//     y_a = r (x_a w_a cos - x_b w_b sin),  y_b = r (x_b w_b cos + x_a w_a sin),
+// whose four products of weights and cosines are the same for all heads of a kind: they are made once a token, in shared memory.  All of it is fp32; the
+// one rounding is the store's.
+
+template <typename T, int VEC, bool PAIRS, int UNITS, int NT>
+__global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_append_norm_kernel(const dba_tree_tokens t, const dba_tree_norm nm, const TreePages pg, T* ck,
+                                                                                                T* cv, int B, int H, int K, int D, int lanes) {
     using P = TreePack<T, VEC>;
+    __shared__ alignas(16) float factor[2][4][kTreeMaxDim / 2];        // of queries, of keys: x_a to y_a, x_b to y_a, x_b to y_b, x_a to y_b, by pair
     grid_dependency_wait();
     allow_dependents();
-    const int tok = blockIdx.x;
+    const int tok = blockIdx.x, tid = threadIdx.x;
     const int b = t.seq ? __ldg(t.seq + tok) : tok / (t.N / B);
     const int place = __ldg(t.place + tok);
     int pos = t.position ? __ldg(t.position + tok) : -1;
@@ -110,87 +123,95 @@ __global__ void __launch_bounds__(kAThreads) tree_append_norm_kernel(const dba_t
         }
         if (pos >= 0 && nm.offset) {
             const int64_t moved = (int64_t)pos + __ldg(nm.offset + b);
-            if (moved < 0 || moved >= t.positions) bad = true;
+            bad = bad || moved < 0 || moved >= t.positions;
             pos = moved < 0 || moved >= t.positions ? -1 : (int)moved;
         }
     } else bad = true;
     if (pos >= t.positions) { bad = bad || t.cos; pos = -1; }
-    if (bad && threadIdx.x == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
-    const int half = t.rot_dim / 2, per = D / (2 * VEC), turned = half / VEC;
-    const int sub = threadIdx.x / lanes, lane = threadIdx.x - sub * lanes, heads_at = blockDim.x / lanes;
+    if (bad && tid == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
+    const int half = t.rot_dim / 2, turned = half / VEC;
+    for (int i = tid; i < D; i += NT) {
+        const int side = i >= D / 2, p = i - side * (D / 2), j = p / VEC;
+        // the pair's dimensions: of unit j, element p % VEC of either pack, or two neighbours
+        const int da = PAIRS ? 2 * p : j < turned ? p : p + j * VEC, db = PAIRS ? da + 1 : j < turned ? p + half : da + VEC;
+        const float* const w = side ? nm.k_weight : nm.q_weight;
+        const float wa = w ? __ldg(w + da) : 1.f, wb = w ? __ldg(w + db) : 1.f;
+        const bool turn = pos >= 0 && j < turned;
+        const float c = turn ? __ldg(t.cos + (int64_t)pos * half + p) : 1.f, s = turn ? __ldg(t.sin + (int64_t)pos * half + p) : 0.f;
+        factor[side][0][p] = wa * c; factor[side][1][p] = -(wb * s); factor[side][2][p] = wb * c; factor[side][3][p] = wa * s;
+    }
+    __syncthreads();
+    const int per = D / (2 * VEC), sub = tid / lanes, lane = tid - sub * lanes, heads_at = NT / lanes;
     int d0[UNITS], d1[UNITS];
-    float cs[UNITS][VEC], sn[UNITS][VEC];
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         const int j = lane + u * lanes;
-        d0[u] = j < turned ? (PAIRS ? 2 * j * VEC : j * VEC) : t.rot_dim + 2 * (j - turned) * VEC;
+        d0[u] = PAIRS || j >= turned ? 2 * j * VEC : j * VEC;
         d1[u] = j < turned && !PAIRS ? d0[u] + half : d0[u] + VEC;
-        const bool turn = pos >= 0 && j < turned;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            cs[u][i] = turn ? __ldg(t.cos + (int64_t)pos * half + j * VEC + i) : 1.f;
-            sn[u][i] = turn ? __ldg(t.sin + (int64_t)pos * half + j * VEC + i) : 0.f;
-        }
         if (j >= per) d0[u] = -1;
     }
-    // the heads of one kind: queries, keys
-    const auto heads = [&](const T* src, int64_t src_head, T* dst, int64_t dst_head, int n, const float* weight) {
-        float w0[UNITS][VEC], w1[UNITS][VEC];
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                w0[u][i] = weight && d0[u] >= 0 ? __ldg(weight + d0[u] + i) : 1.f;
-                w1[u][i] = weight && d0[u] >= 0 ? __ldg(weight + d1[u] + i) : 1.f;
-            }
-        const float inv_d = 1.f / (float)D;
+    // heads: the queries' (where there are any), then the keys'
+    const int q_heads = t.q ? H : 0, n = q_heads + (row >= 0 ? K : 0);
+    const float inv_d = 1.f / (float)D;
 #pragma unroll 1
-        for (int h0 = 0; h0 < n; h0 += heads_at) {
-            const int h = h0 + sub;
-            P x[UNITS], y[UNITS];
-            float sum = 0.f;
+    for (int h0 = 0; h0 < n; h0 += heads_at) {
+        const int h = h0 + sub;
+        const bool is_q = h < q_heads;
+        const T* const src = is_q ? (const T*)t.q + (int64_t)tok * t.q_token_stride + (int64_t)h * t.q_head_stride
+                                  : (const T*)t.k + (int64_t)tok * t.k_token_stride + (int64_t)(h - q_heads) * t.k_head_stride;
+        float e[UNITS][2 * VEC], sum = 0.f, sum2 = 0.f;
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u) {
-                if (h >= n || d0[u] < 0) continue;
-                x[u] = *reinterpret_cast<const P*>(src + (int64_t)h * src_head + d0[u]);
-                y[u] = *reinterpret_cast<const P*>(src + (int64_t)h * src_head + d1[u]);
+        for (int u = 0; u < UNITS; ++u) {
+            if (h >= n || d0[u] < 0) continue;
+            const P x = *reinterpret_cast<const P*>(src + d0[u]), y = *reinterpret_cast<const P*>(src + d1[u]);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float p = tree_widen(x[u].x[i]), q = tree_widen(y[u].x[i]);
-                    sum = fmaf(p, p, sum); sum = fmaf(q, q, sum);
-                }
-            }
-            for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
-            const float r = weight ? rsqrtf(fmaf(sum, inv_d, nm.eps)) : 1.f;
+            for (int i = 0; i < VEC; ++i) { e[u][i] = tree_widen(x.x[i]); e[u][VEC + i] = tree_widen(y.x[i]); }
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u) {
-                if (h >= n || d0[u] < 0) continue;
-                float e[2 * VEC];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) { e[i] = tree_widen(x[u].x[i]) * r * w0[u][i]; e[VEC + i] = tree_widen(y[u].x[i]) * r * w1[u][i]; }
-                float f[2 * VEC];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    // PAIRS: elements 2i, 2i+1 of the 2 VEC neighbours; else element i of either pack
-                    const int k0 = PAIRS ? 2 * i : i, k1 = PAIRS ? 2 * i + 1 : VEC + i;
-                    f[k0] = fmaf(e[k0], cs[u][i], -(e[k1] * sn[u][i]));
-                    f[k1] = fmaf(e[k1], cs[u][i], e[k0] * sn[u][i]);
-                }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) { tree_narrow(f[i], &x[u].x[i]); tree_narrow(f[VEC + i], &y[u].x[i]); }
-                *reinterpret_cast<P*>(dst + (int64_t)h * dst_head + d0[u]) = x[u];
-                *reinterpret_cast<P*>(dst + (int64_t)h * dst_head + d1[u]) = y[u];
-            }
+            for (int i = 0; i < 2 * VEC; i += 2) norm_fma2(sum, sum2, e[u][i], e[u][i + 1], e[u][i], e[u][i + 1]);
         }
-    };
-    if (t.q) heads((const T*)t.q + (int64_t)tok * t.q_token_stride, t.q_head_stride, (T*)t.q_out + (int64_t)tok * t.qo_token_stride, t.qo_head_stride, H, nm.q_weight);
+        sum += sum2;
+        for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
+        const float r = (is_q ? nm.q_weight : nm.k_weight) ? rsqrtf(fmaf(sum, inv_d, nm.eps)) : 1.f;
+        T* const dst = is_q ? (T*)t.q_out + (int64_t)tok * t.qo_token_stride + (int64_t)h * t.qo_head_stride : ck + row + (int64_t)(h - q_heads) * pg.head_stride;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            if (h >= n || d0[u] < 0) continue;
+            const float* const f = factor[is_q ? 0 : 1][0] + (lane + u * lanes) * VEC;
+            constexpr int to = kTreeMaxDim / 2;            // the next of the four
+            P ya, yb;
+            const auto put = [&](int i, float va, float vb) {
+                if (PAIRS) { tree_narrow(va, 2 * i < VEC ? &ya.x[2 * i % VEC] : &yb.x[2 * i % VEC]); tree_narrow(vb, 2 * i + 1 < VEC ? &ya.x[(2 * i + 1) % VEC] : &yb.x[(2 * i + 1) % VEC]); }
+                else { tree_narrow(va, &ya.x[i]); tree_narrow(vb, &yb.x[i]); }
+            };
+            if constexpr (VEC >= 2) {
+                constexpr int FN = VEC < 4 ? VEC : 4;      // what shared memory gives at a time
+                using F = TreePack<float, FN>;
+#pragma unroll
+                for (int i0 = 0; i0 < VEC; i0 += FN) {
+                    const F aa = *reinterpret_cast<const F*>(f + i0), ba = *reinterpret_cast<const F*>(f + to + i0), bb = *reinterpret_cast<const F*>(f + 2 * to + i0),
+                            ab = *reinterpret_cast<const F*>(f + 3 * to + i0);
+#pragma unroll
+                    for (int k = 0; k < FN; k += 2) {
+                        const int i = i0 + k;
+                        const float a0 = e[u][PAIRS ? 2 * i : i], a1 = e[u][PAIRS ? 2 * i + 2 : i + 1], b0 = e[u][PAIRS ? 2 * i + 1 : VEC + i], b1 = e[u][PAIRS ? 2 * i + 3 : VEC + i + 1];
+                        float p0, p1, q0, q1;
+                        norm_mul2(p0, p1, b0, b1, ba.x[k], ba.x[k + 1]); norm_fma2(p0, p1, a0, a1, aa.x[k], aa.x[k + 1]);
+                        norm_mul2(q0, q1, a0, a1, ab.x[k], ab.x[k + 1]); norm_fma2(q0, q1, b0, b1, bb.x[k], bb.x[k + 1]);
+                        norm_mul2(p0, p1, p0, p1, r, r); norm_mul2(q0, q1, q0, q1, r, r);
+                        put(i, p0, q0); put(i + 1, p1, q1);
+                    }
+                }
+            } else put(0, r * fmaf(e[u][0], f[0], e[u][1] * f[to]), r * fmaf(e[u][1], f[2 * to], e[u][0] * f[3 * to]));
+            *reinterpret_cast<P*>(dst + d0[u]) = ya;
+            *reinterpret_cast<P*>(dst + d1[u]) = yb;
+        }
+    }
     if (row < 0) return;
-    heads((const T*)t.k + (int64_t)tok * t.k_token_stride, t.k_head_stride, ck + row, pg.head_stride, K, nm.k_weight);
     const int chunks = D * (int)sizeof(T) / 16;
-    for (int u = threadIdx.x; u < K * chunks; u += blockDim.x) {
-        const int h = u / chunks, ch = u - h * chunks;
-        *reinterpret_cast<uint4*>((char*)(cv + row + (int64_t)h * pg.head_stride) + ch * 16) =
-            *reinterpret_cast<const uint4*>((const char*)((const T*)t.v + (int64_t)tok * t.v_token_stride + (int64_t)h * t.v_head_stride) + ch * 16);
+    for (int u = tid; u < K * chunks; u += NT) {
+        const int h = u / chunks, at = (u - h * chunks) * 16;
+        *reinterpret_cast<uint4*>((char*)(cv + row + (int64_t)h * pg.head_stride) + at) =
+            *reinterpret_cast<const uint4*>((const char*)((const T*)t.v + (int64_t)tok * t.v_token_stride + (int64_t)h * t.v_head_stride) + at);
     }
 }
 
@@ -271,9 +292,10 @@ cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, vo
 namespace {
 template <typename T, int VEC, int UNITS>
 cudaError_t launch_norm_u(const dba_tree_tokens& t, const dba_tree_norm& nm, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, int lanes, cudaStream_t st) {
-    const int threads = t.N >= 2048 ? 64 : kAThreads;
-    return t.pairs ? launch_after(tree_append_norm_kernel<T, VEC, true, UNITS>, dim3(t.N), dim3(threads), 0, st, t, nm, pg, (T*)k, (T*)v, B, H, K, D, lanes)
-                   : launch_after(tree_append_norm_kernel<T, VEC, false, UNITS>, dim3(t.N), dim3(threads), 0, st, t, nm, pg, (T*)k, (T*)v, B, H, K, D, lanes);
+    // (blocks of 64 or of 128 threads as above: 8 x 2039 tokens of 48 heads of 128 78 us, with 128 threads 87; 16 x 20 tokens 6.9 and 5.8)
+    const auto go = [&](auto* kernel, int threads) { return launch_after(kernel, dim3(t.N), dim3(threads), 0, st, t, nm, pg, (T*)k, (T*)v, B, H, K, D, lanes); };
+    if (t.N >= 2048) return t.pairs ? go(tree_append_norm_kernel<T, VEC, true, UNITS, 64>, 64) : go(tree_append_norm_kernel<T, VEC, false, UNITS, 64>, 64);
+    return t.pairs ? go(tree_append_norm_kernel<T, VEC, true, UNITS, 128>, 128) : go(tree_append_norm_kernel<T, VEC, false, UNITS, 128>, 128);
 }
 template <typename T, int VEC>
 cudaError_t launch_norm_v(const dba_tree_tokens& t, const dba_tree_norm& nm, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, cudaStream_t st) {
