@@ -177,6 +177,7 @@ dba_status dba_tree_init(const dba_tree_config* cfg, void* workspace_dev, size_t
     if (e == cudaSuccess) e = configure_tree_advance();
     if (e == cudaSuccess) e = configure_tree_prefix();
     if (e == cudaSuccess) e = configure_tree_weigh();
+    if (e == cudaSuccess) e = configure_tree_evict();
     if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 256 + 4 * kTreeTurns, h->stream);     // (the turns lie behind it)
     if (e != cudaSuccess) { delete h; return DBA_ERR_CUDA; }
     *out = h;

@@ -13,21 +13,19 @@ namespace dba {
 
 namespace {
 
-constexpr int kEThreads = 512, kEWarps = kEThreads / 32, kEBins = 2048;
+constexpr int kEBins = 2048, kEShared = 48 * 1024;         // weights of a row that shared memory takes
 constexpr int kMThreads = 256, kMRowsAt = 256, kMCopies = 8;
 
 // larger weight, larger number; NaN is less than any
 __device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : ord32(w); }
 
-struct ESmem {
-    uint32_t bins[kEBins];
-    int sums[2][kEWarps];
-    int digit, above;
-};
-
-// A block per (layer, sequence, key head), the last counting fastest.
-__global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a) {
-    __shared__ ESmem sm;
+// A block per (layer, sequence, key head), the last counting fastest.  A row of up to `room` weights is read once, into shared memory.
+template <int NT>
+__global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int room) {
+    constexpr int warps = NT / 32;
+    extern __shared__ float held[];
+    __shared__ uint32_t bins[kEBins];
+    __shared__ int sums[2][warps], digit, above_digit;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = (int)(blockIdx.x % a.K), b = (int)(blockIdx.x / a.K % a.B), l = (int)(blockIdx.x / a.K / a.B);
     grid_dependency_wait();
@@ -37,13 +35,19 @@ __global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a)
     const float* w = a.e.weight + row;
     float* out = a.e.weight_out + row;
     int32_t* kept = a.e.kept + (((int64_t)l * a.B + b) * a.K + h) * keep;
-    for (int i = n + tid; i < keep; i += kEThreads) kept[i] = -1;
+    for (int i = n + tid; i < keep; i += NT) kept[i] = -1;
     if (L <= keep) {
-        for (int i = tid; i < L; i += kEThreads) {
+        for (int i = tid; i < L; i += NT) {
             kept[i] = i;
             out[i] = w[i];
         }
         return;
+    }
+    if (L <= room) {
+#pragma unroll 8
+        for (int i = tid; i < L; i += NT) held[i] = w[i];
+        w = held;
+        __syncthreads();
     }
     const int old = L - min(a.e.recent, keep);               // places that have to earn it
     int m = keep - (L - old);                              // how many of them stay: less than there are
@@ -56,37 +60,48 @@ __global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a)
             const int bits = pass == 2 ? 10 : 11;
             const uint32_t known = shift == 32 ? 0u : ~0u << shift;
             shift -= bits;
-            for (int i = tid; i < kEBins; i += kEThreads) sm.bins[i] = 0;
+            for (int i = tid; i < kEBins; i += NT) bins[i] = 0;
             __syncthreads();
-            for (int i = tid; i < old; i += kEThreads) {
-                const uint32_t key = weight_key(w[i]);
-                if ((key & known) == prefix) atomicAdd(&sm.bins[(key >> shift) & ((1u << bits) - 1u)], 1u);
+            // (a warp counts those with its first one's digit together: rows whose weights are alike, or nothing, would wait for one another's additions)
+#pragma unroll 4
+            for (int i0 = 0; i0 < old; i0 += NT) {
+                const int i = i0 + tid;
+                const uint32_t key = i < old ? weight_key(w[i]) : 0u;
+                const bool in = i < old && (key & known) == prefix;
+                const uint32_t mine = (key >> shift) & ((1u << bits) - 1u), who = __ballot_sync(kFullMask, in);
+                if (who == 0) continue;
+                const int leader = __ffs(who) - 1;
+                const uint32_t leaders = __shfl_sync(kFullMask, mine, leader);       // (by all lanes)
+                const bool same = in && mine == leaders;
+                const uint32_t together = __ballot_sync(kFullMask, same);
+                if (lane == leader) atomicAdd(&bins[mine], (uint32_t)__popc(together));
+                else if (in && !same) atomicAdd(&bins[mine], 1u);
             }
             __syncthreads();
-            // from the largest digit down: a thread has bins 4 tid' .. 4 tid' + 3, tid' counted from the top
-            constexpr int per = kEBins / kEThreads;
+            // from the largest digit down: thread tid has bins per tid .. per tid + per - 1, counted from the top
+            constexpr int per = kEBins / NT;
             const int top = kEBins - 1 - per * tid;
             int c[per], sum = 0;
 #pragma unroll
-            for (int i = 0; i < per; ++i) { c[i] = (int)sm.bins[top - i]; sum += c[i]; }
+            for (int i = 0; i < per; ++i) { c[i] = (int)bins[top - i]; sum += c[i]; }
             int pre = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int v = __shfl_up_sync(kFullMask, pre, o);
                 if (lane >= o) pre += v;
             }
-            if (lane == 31) sm.sums[0][warp] = pre;
+            if (lane == 31) sums[0][warp] = pre;
             __syncthreads();
             int before = pre - sum;
-            for (int i = 0; i < warp; ++i) before += sm.sums[0][i];
+            for (int i = 0; i < warp; ++i) before += sums[0][i];
 #pragma unroll
             for (int i = 0; i < per; ++i) {
-                if (before < m && before + c[i] >= m) { sm.digit = top - i; sm.above = before; }
+                if (before < m && before + c[i] >= m) { digit = top - i; above_digit = before; }
                 before += c[i];
             }
             __syncthreads();
-            prefix |= (uint32_t)sm.digit << shift;
-            m -= sm.above;                                 // of those with this digit, m stay
+            prefix |= (uint32_t)digit << shift;
+            m -= above_digit;                              // of those with this digit, m stay
             __syncthreads();
         }
         bar = prefix;
@@ -94,20 +109,19 @@ __global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a)
     // m of the keys at the bar stay, the first ones
     int n_above = 0, n_at = 0;
 #pragma unroll 1
-    for (int i0 = 0; i0 < L; i0 += kEThreads) {
+    for (int i0 = 0; i0 < L; i0 += NT) {
         const int i = i0 + tid;
         const float x = i < L ? w[i] : 0.f;
         const uint32_t key = weight_key(x);
         const bool above = i < L && (i >= old || (bar != 0xffffffffu && key > bar)), at = i < old && bar != 0xffffffffu && key == bar;
         const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at);
-        if (lane == 0) { sm.sums[0][warp] = __popc(u); sm.sums[1][warp] = __popc(e); }
+        if (lane == 0) { sums[0][warp] = __popc(u); sums[1][warp] = __popc(e); }
         __syncthreads();                                   // (and the weights of this batch have been read)
-        int before_u = n_above + __popc(u & ((1u << lane) - 1u)), before_e = n_at + __popc(e & ((1u << lane) - 1u));
-#pragma unroll
-        for (int j = 0; j < kEWarps; ++j) {
-            if (j < warp) { before_u += sm.sums[0][j]; before_e += sm.sums[1][j]; }
-            n_above += sm.sums[0][j]; n_at += sm.sums[1][j];
-        }
+        // the warps' counts: lane j has warp j's
+        const int cu = lane < warps ? sums[0][lane] : 0, ce = lane < warps ? sums[1][lane] : 0;
+        const int before_u = n_above + __reduce_add_sync(kFullMask, lane < warp ? cu : 0) + __popc(u & ((1u << lane) - 1u));
+        const int before_e = n_at + __reduce_add_sync(kFullMask, lane < warp ? ce : 0) + __popc(e & ((1u << lane) - 1u));
+        n_above += __reduce_add_sync(kFullMask, cu); n_at += __reduce_add_sync(kFullMask, ce);
         if (above || (at && before_e < m)) {
             const int to = before_u + min(before_e, m);
             kept[to] = i;
@@ -115,7 +129,7 @@ __global__ void __launch_bounds__(kEThreads) tree_keep_kernel(const TreeEvict a)
         }
         __syncthreads();
     }
-    for (int i = n + tid; i < L; i += kEThreads) out[i] = 0.f;
+    for (int i = n + tid; i < L; i += NT) out[i] = 0.f;
 }
 
 // Blocks: keys or values, layer, sequence, key head, split, the last counting fastest.
@@ -190,8 +204,18 @@ __global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a,
 
 }  // namespace
 
+cudaError_t configure_tree_evict() {
+    return cudaFuncSetAttribute(tree_keep_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEShared * (int)sizeof(float));
+}
+
 cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches) {
-    cudaError_t e = launch_after(tree_keep_kernel, dim3((unsigned)(a.K * a.B * a.layers)), dim3(kEThreads), 0, st, a);
+    // (by the most tokens that a table holds: the lengths are on the device)
+    const unsigned rows_keep = (unsigned)(a.K * a.B * a.layers);
+    const int room = a.ctx_cap < kEShared ? a.ctx_cap : kEShared;
+    const size_t bytes = (size_t)room * sizeof(float);
+    cudaError_t e = a.ctx_cap <= 2048 ? launch_after(tree_keep_kernel<256>, dim3(rows_keep), dim3(256), bytes, st, a, room)
+                    : a.ctx_cap <= 8192 ? launch_after(tree_keep_kernel<512>, dim3(rows_keep), dim3(512), bytes, st, a, room)
+                                        : launch_after(tree_keep_kernel<1024>, dim3(rows_keep), dim3(1024), bytes, st, a, room);
     *launches += 1;
     if (e != cudaSuccess) return e;
     // some eight blocks an SM, none without a batch of rows

@@ -130,6 +130,7 @@ struct TreeEvict {
     const int32_t* ctx_len;
     dba_tree_evicted e;
 };
+cudaError_t configure_tree_evict();
 cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches);
 cudaError_t launch_tree_append_norm(const dba_tree_tokens& t, const dba_tree_norm& norm, const TreePages& pg, void* k, void* v, int32_t B, int32_t H,
                                     int32_t K, int32_t D, int dtype, cudaStream_t st, int* launches);

@@ -384,9 +384,13 @@ class TokenTree:
             raise ValueError("weight and weight_out: of the same strides")
         cache, n = self._cache(k, v, len(layers)), self._i32(ctx_len, B, "ctx_len: int32 [B]")
         stride, stride_out = self._table(table), self._table(table_out)
-        with torch.cuda.stream(self.stream):             # (the allocator gives freed memory out by stream)
-            ints = torch.empty(2 * B + math.prod(layers) * B * self.kv_heads * keep, dtype=self._i32t, device=self.device)
-        new_len, dropped, kept = ints[:B], ints[B:2 * B], ints[2 * B:].view(*layers, B, self.kv_heads, keep)
+        shape = (*layers, B, self.kv_heads, keep)
+        if torch.cuda.current_stream(self.device) == self.stream:
+            lens, kept = ctx_len.new_empty((2, B)), ctx_len.new_empty(shape)
+        else:
+            with torch.cuda.stream(self.stream):         # (the allocator gives freed memory out by stream)
+                lens, kept = ctx_len.new_empty((2, B)), ctx_len.new_empty(shape)
+        new_len, dropped = lens.unbind()
         e = TreeEvicted(weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2], keep, recent, table_out.data_ptr(), stride_out,
                         kept.data_ptr(), new_len.data_ptr(), dropped.data_ptr())
         code = lib().dba_tree_evict(self._h, cache, table.data_ptr(), stride, n, C.byref(e))
