@@ -92,17 +92,19 @@ struct TreePrefix {
     float* part_o;                     // [2 * grid][item rows][D]: first and last pieces of a block's run that are part of an item
     float* part_ml;                    // [2 * grid][item rows][2]: maximum (powers of two) and sum
     int4* meta;                        // [2 * grid] prefix, key head and block of rows of the piece there (x = -1: none, -2: the block gave up)
+    bool joined;                       // the joining kernel follows (prefixes of one tile cannot be cut)
     long long wait_clocks;
     int drop_item;
 };
-struct TreePrefixPlan { int grid, rows, sm_count; bool tensor; };      // blocks of the kernel, rows of an item
+struct TreePrefixPlan { int grid, rows, keys, sm_count; bool tensor; };        // blocks of the kernel, rows of an item, keys of a tile (tensor)
 TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count);
 cudaError_t configure_tree_prefix();
 // the tensor-core kernel (tree_prefix_mma.cu); usable where tree_mma_usable
 int tree_prefix_mma_rows();
+int tree_prefix_mma_keys();
 cudaError_t configure_tree_prefix_mma();
 cudaError_t launch_tree_prefix_mma(const TreePrefix& a, int grid, cudaStream_t st);
-cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches);
+cudaError_t launch_tree_prefix(TreePrefix a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches);
 
 // The weight that context tokens receive.
 struct TreeWeigh {

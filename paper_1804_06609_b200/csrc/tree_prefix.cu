@@ -81,14 +81,18 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
     };
     __syncthreads();                                       // the last piece is done with
     find_rows(pc.tile);
-    for (int i = tid; i < 16 * RI * DP; i += kPThreads) {  // queries, zero beyond the rows and the head size
-        const int r = i / DP, d = i - r * DP;
-        float x = 0.f;
+    constexpr int VEC = 16 / (int)sizeof(T);
+#pragma unroll 4
+    for (int i = tid; i < 16 * RI * (DP / VEC); i += kPThreads) {       // queries, zero beyond the rows and the head size
+        const int r = i / (DP / VEC), d = (i - r * (DP / VEC)) * VEC;
+        alignas(16) T x[VEC];
+        *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
         if (r < pc.rows && d < a.D) {
             const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r);
-            x = p_widen(((const T*)a.q)[(int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head + d]);
+            *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head + d);
         }
-        sm.q[r][d] = x;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sm.q[r][d + j] = p_widen(x[j]);
     }
     __syncthreads();
     p_load<DP>(a.D, kb, sm.row[pc.tile & 1], sm.k[pc.tile & 1]);
@@ -221,7 +225,7 @@ __global__ void __launch_bounds__(kPThreads, DP <= 128 ? 2 : 1) tree_prefix_kern
     grid_dependency_wait();
     allow_dependents();
     if (blockIdx.x == 0) prefix_check(a);
-    SpanRun run = span_run<kPThreads>(a.groups, 4, &sm.span, [&](int g) { return Cut::units(a, g); });
+    SpanRun run = Cut::template run<kPThreads>(a, 4, &sm.span);
     typename Cut::Piece pc;
     int cut = 0;
     int4 meta[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
@@ -380,6 +384,7 @@ TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count) {
         p.tensor = true;
         p.grid = sm_count;
         p.rows = tree_prefix_mma_rows();
+        p.keys = tree_prefix_mma_keys();
         return p;
     }
     p.grid = (D <= 128 ? 2 : 1) * sm_count;
@@ -398,13 +403,14 @@ cudaError_t configure_tree_prefix() {
     return e == cudaSuccess ? configure_tree_prefix_mma() : e;
 }
 
-cudaError_t launch_tree_prefix(const TreePrefix& a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches) {
+cudaError_t launch_tree_prefix(TreePrefix a, const TreePrefixPlan& plan, int dtype, cudaStream_t st, int* launches) {
     cudaError_t e;
+    a.joined = !plan.tensor || a.cap > plan.keys;
     if (plan.tensor) e = launch_tree_prefix_mma(a, plan.grid, st);
     else if (dtype == DBA_BF16) e = launch_prefix<__nv_bfloat16, 256>(a, plan.grid, st);
     else e = a.D <= 64 ? launch_prefix<float, 64>(a, plan.grid, st) : a.D <= 128 ? launch_prefix<float, 128>(a, plan.grid, st) : launch_prefix<float, 256>(a, plan.grid, st);
     *launches += 1;
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || !a.joined) return e;
     // (an item has at most one piece from each block)
     const size_t n = (size_t)2 * plan.grid, most = (size_t)plan.grid * kPJoinManyRows, few = kPJoinRows * kPJoinFew;
     const size_t list = n * (sizeof(int4) + 2 * sizeof(int32_t)) + (most > few ? most : few) * sizeof(float);

@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
     // is the epilogue's.
     allow_dependents();
     if (blockIdx.x == 0) prefix_check(a);
-    SpanRun run = span_run<C::threads>(a.groups, 3, &sm.span, [&](int g) { return XCut::units(a, g); });      // (has the block's barriers)
+    SpanRun run = XCut::run<C::threads>(a, 3, &sm.span);
     __syncthreads();           // its numbers have been read: their place is used again
     tc_after();
     const uint32_t tmem = sm.tmem_base;
@@ -527,9 +527,21 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
     tc_after();
     grid_dependency_wait();                                // (a block without work too: what follows this kernel follows the one before it)
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::tmem_cols) : "memory");
-    if (sm.abort_flag && tid == 0) {
-        atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT);
-        a.meta[2 * blockIdx.x] = make_int4(-2, 0, 0, 0);   // (over what the loader wrote)
+    if (sm.abort_flag) {
+        if (tid == 0) {
+            atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT);
+            a.meta[2 * blockIdx.x] = make_int4(-2, 0, 0, 0);           // (over what the loader wrote)
+        }
+        if (!a.joined) {               // (else the joining kernel sees to it)
+            run = XCut::run<C::threads>(a, 3, &sm.span);
+            while (XCut::next(a, run, &pc))
+                for (int i = tid; i < pc.rows * a.D; i += C::threads) {
+                    const int r = i / a.D, d = i - r * a.D;
+                    const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r);
+                    ((__nv_bfloat16*)a.out)[(int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head + d] = __float2bfloat16_rn(__int_as_float(0x7fc00000));
+                    if (d == 0) a.own_lse[((int64_t)w.b * a.n + w.i) * a.H + w.head] = __int_as_float(0x7fc00000);
+                }
+        }
     }
 }
 
@@ -547,6 +559,7 @@ cudaError_t launch_prefix_mma(const TreePrefix& a, const TreeBoxes& m, int grid,
 }  // namespace
 
 int tree_prefix_mma_rows() { return kXRows; }
+int tree_prefix_mma_keys() { return kXKeys; }
 cudaError_t configure_tree_prefix_mma() {
     cudaError_t e = configure_prefix_mma<64, true>();
     if (e == cudaSuccess) e = configure_prefix_mma<128, true>();

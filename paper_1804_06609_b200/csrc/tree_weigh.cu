@@ -8,6 +8,8 @@
 // the order of anything.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "tree_span.cuh"
 
 namespace dba {
@@ -56,6 +58,7 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
         __syncthreads();                                   // the last tile is done with
         if (tid < KT) sm.row[tid] = tid < count ? tree_row(a.pages, b, a.A + p0 + tid) : -1;
         __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < KT * (DP / VEC); i += kWThreads) {
             const int r = i / (DP / VEC), d = (i - r * (DP / VEC)) * VEC;
             alignas(16) T x[VEC];
@@ -70,15 +73,19 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
         for (int r0 = 0; r0 < M; r0 += kWRows) {
             if (M > kWRows || b != have_b || h != have_h) {
                 if (r0) __syncthreads();
-                for (int i = tid; i < kWRows * DP; i += kWThreads) {
-                    const int r = i / DP, d = i - r * DP, rr = r0 + r;
-                    float x = 0.f;
+                const int rows16 = M - r0 <= 16 ? 16 : M - r0 <= 32 ? 32 : kWRows;       // (those that are looked at)
+#pragma unroll 4
+                for (int i = tid; i < rows16 * (DP / VEC); i += kWThreads) {
+                    const int r = i / (DP / VEC), d = (i - r * (DP / VEC)) * VEC, rr = r0 + r;
+                    alignas(16) T x[VEC];
+                    *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
                     if (rr < M && d < a.D) {
                         const int tok = rr / a.G, head = h * a.G + rr - tok * a.G;
                         const bool is_open = a.lse[((int64_t)b * a.n + tok) * a.H + head] != neg_inf();      // (else the query may hold anything)
-                        if (is_open) x = w_widen(((const T*)a.q)[(int64_t)b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d]);
+                        if (is_open) *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d);
                     }
-                    sm.q[r][d] = x;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) sm.q[r][d + j] = w_widen(x[j]);
                 }
                 if (tid < kWRows) {
                     float z = __int_as_float(0x7f800000);
@@ -93,32 +100,39 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                 have_b = b; have_h = h;
             }
             __syncthreads();
-            float2 s[4][NK];
+            // sixteen rows for each that a thread has: no more of them than there are rows
+            const auto products = [&](auto rows) {
+                constexpr int RI = decltype(rows)::value;
+                float2 s[RI][NK];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RI; ++i)
 #pragma unroll
-                for (int j = 0; j < NK; ++j) s[i][j] = make_float2(0.f, 0.f);
+                    for (int j = 0; j < NK; ++j) s[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
-            for (int d = 0; d < DP; d += 4) {
-                float4 qv[4];
+                for (int d = 0; d < DP; d += 4) {
+                    float4 qv[RI];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][d]);
+                    for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][d]);
 #pragma unroll
-                for (int j = 0; j < NK; ++j) {
-                    const float4 kv = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+                    for (int j = 0; j < NK; ++j) {
+                        const float4 kv = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w_fma2(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
-                        w_fma2(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
+                        for (int i = 0; i < RI; ++i) {
+                            w_fma2(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
+                            w_fma2(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float z = sm.lse[ty + 16 * i];
+                for (int i = 0; i < RI; ++i) {
+                    const float z = sm.lse[ty + 16 * i];
 #pragma unroll
-                for (int j = 0; j < NK; ++j) sum[j] += w_ex2(fmaf(s[i][j].x + s[i][j].y, a.scale_log2e, -z));
-            }
+                    for (int j = 0; j < NK; ++j) sum[j] += w_ex2(fmaf(s[i][j].x + s[i][j].y, a.scale_log2e, -z));
+                }
+            };
+            if (M - r0 <= 16) products(std::integral_constant<int, 1>{});
+            else if (M - r0 <= 32) products(std::integral_constant<int, 2>{});
+            else products(std::integral_constant<int, 4>{});
         }
 #pragma unroll
         for (int j = 0; j < NK; ++j) sm.sum[ty][tx + 16 * j] = sum[j];
