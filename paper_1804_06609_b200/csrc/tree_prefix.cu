@@ -244,10 +244,10 @@ __global__ void __launch_bounds__(kPThreads, DP <= 128 ? 2 : 1) tree_prefix_kern
 
 // Finishes the items that several blocks worked on.  A block's run leaves at most two pieces of such items, in the order of the
 // units, so the pieces of an item are neighbours in the list of all blocks' pieces.  Every block here reads the list and takes every
-// gridDim-th stretch of the items' rows: 32 rows where no item has more than kPJoinFew pieces, 8 elsewhere.  First the rows' weights for
-// each piece, a thread to a piece, then the outputs, four columns to a thread, all loads of which are in the air together.  Pieces are
-// added in their order: equal inputs give equal bits.  A block that gave up says so in its entry, which every launch writes anew.
-constexpr int kPJoinThreads = 256, kPJoinWarps = kPJoinThreads / 32, kPJoinFew = 8, kPJoinRows = kPJoinThreads / kPJoinFew, kPJoinManyRows = kPJoinWarps;
+// gridDim-th stretch of the items' rows: 32 rows where no item has more than kPJoinFew pieces, 8 up to twice as many, 2 beyond.  First the rows'
+// weights for each piece, a thread to a piece, then the outputs, four columns to a thread, all loads of which are in the air together; of two rows
+// the pieces are shared among threads, too, and their sums added.  Pieces are added in a fixed order: equal inputs give equal bits.  A block that gave up says so in its entry, which every launch writes anew.
+constexpr int kPJoinThreads = 256, kPJoinWarps = kPJoinThreads / 32, kPJoinFew = 8, kPJoinRows = kPJoinThreads / kPJoinFew, kPJoinSomeRows = kPJoinWarps, kPJoinManyRows = 2;
 
 template <typename T>
 __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const TreePrefix a, int item_rows, int blocks) {
@@ -259,6 +259,7 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
     __shared__ int counts[kPJoinWarps];
     __shared__ int64_t out_at[kPJoinRows];                 // -1: the row stays as it is
     __shared__ float own_weight[kPJoinRows];
+    __shared__ float4 sums[kPJoinThreads];
     grid_dependency_wait();
     allow_dependents();
     bool failed = false;
@@ -302,10 +303,11 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
         const int4 x = pieces[list[i]], y = pieces[list[i - 1]];
         return x.x != y.x || x.y != y.y || x.z != y.z;
     });
-    bool more = false;
-    for (int i = tid; i < n_items; i += kPJoinThreads) more = more || (i + 1 < n_items ? items[i + 1] : n_pieces) - items[i] > kPJoinFew;
-    const bool many = __syncthreads_or(more);
-    const int rows = many ? kPJoinManyRows : kPJoinRows, per_item = item_rows / rows, vecs = a.D / 4;
+    int most = 0;
+    for (int i = tid; i < n_items; i += kPJoinThreads) most = max(most, (i + 1 < n_items ? items[i + 1] : n_pieces) - items[i]);
+    const bool some = __syncthreads_or(most > kPJoinFew), many = __syncthreads_or(most > 2 * kPJoinFew);
+    const int rows = many ? kPJoinManyRows : some ? kPJoinSomeRows : kPJoinRows, per_item = item_rows / rows, vecs = a.D / 4;
+    const int shares = many ? min(8, kPJoinThreads / (rows * vecs)) : 1;         // threads that the pieces of an output are shared among
     for (int task = blockIdx.x; task < n_items * per_item; task += gridDim.x) {
         const int item = task / per_item, r0 = (task - item * per_item) * rows, first = items[item];
         const int count = (item + 1 < n_items ? items[item + 1] : n_pieces) - first;
@@ -314,8 +316,8 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
         const int left = (pg.hi - pg.lo) * a.n * a.G - (id.z * item_rows + r0);       // rows from here on
         if (left <= 0) continue;
         // --- weights: a warp to a row, or eight lanes
-        const int lanes = many ? 32 : kPJoinFew, r = tid / lanes, l0 = tid - r * lanes;
-        const bool in = r < left;
+        const int lanes = some ? 32 : kPJoinFew, r = tid / lanes, l0 = tid - r * lanes;
+        const bool in = r < left && r < rows;
         const PrefixRow w = prefix_row(a, pg.lo, id.y, id.z * item_rows + r0 + (in ? r : 0));
         float own, w_own = 0.f, w_pre, lse, m = neg_inf(), l = 0.f;
         const bool is_open = prefix_own(a, w, &own) && in;
@@ -333,30 +335,42 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
                 e = sum == 0.f ? 0.f : exp2f(a.part_ml[2 * at] - ref);
                 l += sum * e;
             }
-            weights[r * count + i] = e;
+            if (r < rows) weights[r * count + i] = e;
         }
         for (int o = lanes >> 1; o; o >>= 1) l += __shfl_xor_sync(kFullMask, l, o);
         const bool write = prefix_join(own, ref, l, &w_own, &w_pre, &lse) && is_open;
         if (write)
             for (int i = l0; i < count; i += lanes) weights[r * count + i] *= w_pre;
-        if (l0 == 0) {
+        if (l0 == 0 && r < rows) {
             out_at[r] = write ? (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head : -1;
             own_weight[r] = w_own;
         }
         __syncthreads();                                   // (and every lane has read what one of the row's writes)
         if (write && l0 == 0) a.own_lse[((int64_t)w.b * a.n + w.i) * a.H + w.head] = lse;
         // --- outputs
-        for (int u = tid; u < rows * vecs; u += kPJoinThreads) {
-            const int row = u / vecs, d = (u - row * vecs) * 4;
-            if (row >= left || out_at[row] < 0) continue;
-            T* out = (T*)a.out + out_at[row] + d;
+        for (int u0 = 0; u0 < rows * vecs * shares; u0 += kPJoinThreads) {
+            const int u = u0 + tid, share = u / (rows * vecs), in_share = u - share * (rows * vecs), row = in_share / vecs, d = (in_share - row * vecs) * 4;
+            const bool here = share < shares && row < left && out_at[row] >= 0;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (here) {
 #pragma unroll 8
-            for (int i = 0; i < count; ++i) {
-                const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((int64_t)list[first + i] * item_rows + r0 + row) * a.D + d);
-                const float e = weights[row * count + i];
-                o.x = fmaf(e, v.x, o.x); o.y = fmaf(e, v.y, o.y); o.z = fmaf(e, v.z, o.z); o.w = fmaf(e, v.w, o.w);
+                for (int i = share; i < count; i += shares) {
+                    const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((int64_t)list[first + i] * item_rows + r0 + row) * a.D + d);
+                    const float e = weights[row * count + i];
+                    o.x = fmaf(e, v.x, o.x); o.y = fmaf(e, v.y, o.y); o.z = fmaf(e, v.z, o.z); o.w = fmaf(e, v.w, o.w);
+                }
             }
+            if (shares > 1) {                              // (all of them are in one round)
+                sums[tid] = o;
+                __syncthreads();
+                if (share == 0)
+                    for (int k = 1; k < shares; ++k) {
+                        const float4 v = sums[tid + k * rows * vecs];
+                        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+                    }
+            }
+            if (!here || share > 0) continue;
+            T* out = (T*)a.out + out_at[row] + d;
             const float y[4] = {o.x, o.y, o.z, o.w}, wo = own_weight[row];
 #pragma unroll
             for (int j = 0; j < 4; ++j) p_store(out + j, fmaf(wo, p_widen(out[j]), y[j]));
@@ -412,7 +426,7 @@ cudaError_t launch_tree_prefix(TreePrefix a, const TreePrefixPlan& plan, int dty
     *launches += 1;
     if (e != cudaSuccess || !a.joined) return e;
     // (an item has at most one piece from each block)
-    const size_t n = (size_t)2 * plan.grid, most = (size_t)plan.grid * kPJoinManyRows, few = kPJoinRows * kPJoinFew;
+    const size_t n = (size_t)2 * plan.grid, most = (size_t)plan.grid * kPJoinManyRows, few = 2 * kPJoinRows * kPJoinFew;
     const size_t list = n * (sizeof(int4) + 2 * sizeof(int32_t)) + (most > few ? most : few) * sizeof(float);
     const int grid = plan.sm_count * 4;
     e = dtype == DBA_F32 ? launch_after(tree_prefix_join_kernel<float>, dim3(grid), dim3(kPJoinThreads), list, st, a, plan.rows, plan.grid)
