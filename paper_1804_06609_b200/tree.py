@@ -92,8 +92,9 @@ class TokenTree:
                     self._scratch_bytes = n.value
                     self.scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
                     self._scratch_at = (self.scratch.data_ptr() + 255) // 256 * 256
-        self._prefix, self._norm = TreePrefix(), TreeNorm()
-        self._prefix_ref, self._norm_ref = C.byref(self._prefix), C.byref(self._norm)
+        self._prefix, self._norm, self._evict = TreePrefix(), TreeNorm(), TreeEvicted()
+        self._prefix_ref, self._norm_ref, self._evict_ref = (C.byref(x) for x in (self._prefix, self._norm, self._evict))
+        self._evicted = self._evicted_key = None
         self._next = [(x, self._next_struct(x)) for x in self._next]
         self._turn = 0
         self._f_append, self._f_attend, self._f_advance, self._f_commit = L.dba_tree_append, L.dba_tree_attend, L.dba_tree_advance, L.dba_tree_commit
@@ -370,8 +371,9 @@ class TokenTree:
     def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None):
         """Keeps `keep` tokens of every longer context: the last `recent` and, of the others, those of the largest weight, in their order,
         at the front.  weight [layers, B, kv_heads, context places] fp32 (without layers where k, v have none).  table_out, weight_out:
-        where to; default the same, in place.  Returns a dict of ctx_len and dropped [B] (new tensors), kept [(layers,) B, kv_heads, keep]
-        (the old context places, -1 beyond) and weight (weight_out).  See dba_tree_evict."""
+        where to; default the same, in place.  Returns a dict of ctx_len and dropped [B], kept [(layers,) B, kv_heads, keep] (the old context
+        places, -1 beyond) and weight (weight_out); the first three are one of two sets of the handle's own tensors, in turn.  See
+        dba_tree_evict."""
         torch, B, layers = self.torch, self.B, k.shape[:-4]
         if len(layers) > 1:
             raise ValueError("k and v: [pages, page_size, kv_heads, head_dim], or layers in front")
@@ -384,16 +386,18 @@ class TokenTree:
             raise ValueError("weight and weight_out: of the same strides")
         cache, n = self._cache(k, v, len(layers)), self._i32(ctx_len, B, "ctx_len: int32 [B]")
         stride, stride_out = self._table(table), self._table(table_out)
-        shape = (*layers, B, self.kv_heads, keep)
-        if torch.cuda.current_stream(self.device) == self.stream:
-            lens, kept = ctx_len.new_empty((2, B)), ctx_len.new_empty(shape)
-        else:
+        key = (*layers, keep)
+        if key != self._evicted_key:                     # (two sets in turn, as advance's)
             with torch.cuda.stream(self.stream):         # (the allocator gives freed memory out by stream)
-                lens, kept = ctx_len.new_empty((2, B)), ctx_len.new_empty(shape)
-        new_len, dropped = lens.unbind()
-        e = TreeEvicted(weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2], keep, recent, table_out.data_ptr(), stride_out,
-                        kept.data_ptr(), new_len.data_ptr(), dropped.data_ptr())
-        code = lib().dba_tree_evict(self._h, cache, table.data_ptr(), stride, n, C.byref(e))
+                lens, kept = torch.empty(2, 2, B, dtype=self._i32t, device=self.device), torch.empty(2, *layers, B, self.kv_heads, keep, dtype=self._i32t, device=self.device)
+            self._evicted, self._evicted_key = [(lens[i, 0], lens[i, 1], kept[i]) for i in (0, 1)], key
+        new_len, dropped, kept = self._evicted[0]
+        self._evicted.reverse()
+        e = self._evict
+        e.weight, e.weight_out, e.layer_stride, e.seq_stride, e.head_stride = weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2]
+        e.keep, e.recent, e.to_table, e.to_table_stride = keep, recent, table_out.data_ptr(), stride_out
+        e.kept, e.ctx_len_out, e.dropped = kept.data_ptr(), new_len.data_ptr(), dropped.data_ptr()
+        code = lib().dba_tree_evict(self._h, cache, table.data_ptr(), stride, n, self._evict_ref)
         if code:
             _check(code, "dba_tree_evict")
         return {"ctx_len": new_len, "dropped": dropped, "kept": kept, "weight": weight_out}
