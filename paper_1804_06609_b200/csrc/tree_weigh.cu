@@ -5,7 +5,8 @@
 // for every context place of a (sequence, key head): the attention's own probabilities, once its log-sum-exps are known, so keys are
 // read and values are not.  A block of 256 threads works on a tile of keys and 64 rows at a time: thread (ty, tx) rows ty, ty+16, .. and
 // keys tx, tx+16, ..; a key's sum goes over the rows of a thread, then over the 16 ty in their order, so no sum depends on
-// the order of anything.
+// the order of anything.  The next tile's keys are on their way (cp.async; bf16, which is widened, comes through registers) while this one is
+// worked on, and the page numbers of the one after it.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -27,15 +28,40 @@ __device__ __forceinline__ float w_widen(float x) { return x; }
 __device__ __forceinline__ float w_widen(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 template <int DP> struct WSmem {
-    static constexpr int kt = DP == 64 ? 64 : DP == 128 ? 64 : 32;
+    static constexpr int kt = DP <= 128 ? 64 : 32;
     static constexpr int pitch = DP + 4;
     float q[kWRows][pitch];
-    float k[kt][pitch];
+    float k[2][kt][pitch];
     float sum[16][kt];
     float lse[kWRows];                 // in powers of two; +inf: the row counts nothing
-    int64_t row[kt];
+    int64_t row[2][kt];
     SpanShared span;
 };
+
+// One tile of keys; rows at -1 and what lies beyond the head size are zeros.
+template <int DP>
+__device__ __forceinline__ void w_load(int D, const float* base, const int64_t* row, float (*dst)[DP + 4]) {
+    constexpr int CH = DP / 4;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < WSmem<DP>::kt * CH; i += kWThreads) {
+        const int r = i / CH, d = (i - r * CH) * 4;
+        const bool in = row[r] >= 0 && d < D;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(&dst[r][d])), "l"(in ? base + row[r] + d : base), "r"(in ? 16u : 0u) : "memory");
+    }
+}
+template <int DP>
+__device__ __forceinline__ void w_load(int D, const __nv_bfloat16* base, const int64_t* row, float (*dst)[DP + 4]) {
+    constexpr int CH = DP / 8;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < WSmem<DP>::kt * CH; i += kWThreads) {
+        const int r = i / CH, d = (i - r * CH) * 8;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (row[r] >= 0 && d < D) x = *reinterpret_cast<const uint4*>(base + row[r] + d);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { dst[r][d + 2 * j] = __uint_as_float(u[j] << 16); dst[r][d + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
+    }
+}
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) tree_weigh_kernel(const TreeWeigh a) {
@@ -46,32 +72,47 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, M = a.n * a.G;
     grid_dependency_wait();
     allow_dependents();
-    const auto tiles_of = [&](int b) { return (min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap) + KT - 1) / KT; };
-    SpanRun run = span_run<kWThreads>(a.B, 1, &sm.span, [&](int b) { return (long long)a.K * tiles_of(b); });
-    int have_b = -1, have_h = -1;                          // whose queries (all of them) are in shared memory
+    const auto length_of = [&](int b) { return min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap); };
+    SpanRun run = span_run<kWThreads>(a.B, 1, &sm.span, [&](int b) { return (long long)a.K * ((length_of(b) + KT - 1) / KT); });
+    if (run.t >= run.t_end) return;
+    // a tile: its sequence and key head, where it begins, how many keys it has
+    struct Tile { int b, h, p0, count; };
+    const auto tile_of = [&](long long t) {                // (in ascending order)
+        int L = length_of(run.g), tiles = (L + KT - 1) / KT;
+        while (t - run.at >= (long long)a.K * tiles) { run.at += (long long)a.K * tiles; L = length_of(++run.g); tiles = (L + KT - 1) / KT; }
+        const int h = (int)((t - run.at) / tiles), p0 = (int)((t - run.at) - (long long)h * tiles) * KT;
+        return Tile{run.g, h, p0, min(KT, L - p0)};
+    };
+    const auto find = [&](const Tile& u) { return tid < u.count ? tree_row(a.pages, u.b, a.A + u.p0 + tid) : (int64_t)-1; };
+    const auto load = [&](const Tile& u, int buf) {
+        w_load<DP>(a.D, (const T*)a.k + (int64_t)u.h * a.pages.head_stride, sm.row[buf], sm.k[buf]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    Tile cur = tile_of(run.t), next = cur;
+    if (tid < KT) sm.row[0][tid] = find(cur);
+    if (run.t + 1 < run.t_end) {
+        next = tile_of(run.t + 1);
+        if (tid < KT) sm.row[1][tid] = find(next);
+    }
+    __syncthreads();
+    load(cur, 0);
+    int have_b = -1, have_h = -1, buf = 0;                 // whose queries (all of them) are in shared memory
 #pragma unroll 1
-    for (; run.t < run.t_end; ++run.t) {
-        int tiles = tiles_of(run.g);
-        while (run.t - run.at >= (long long)a.K * tiles) { run.at += (long long)a.K * tiles; tiles = tiles_of(++run.g); }
-        const int b = run.g, h = (int)((run.t - run.at) / tiles), t = (int)((run.t - run.at) - (long long)h * tiles);
-        const int L = min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap), p0 = t * KT, count = min(KT, L - p0);
-        __syncthreads();                                   // the last tile is done with
-        if (tid < KT) sm.row[tid] = tid < count ? tree_row(a.pages, b, a.A + p0 + tid) : -1;
-        __syncthreads();
-#pragma unroll 4
-        for (int i = tid; i < KT * (DP / VEC); i += kWThreads) {
-            const int r = i / (DP / VEC), d = (i - r * (DP / VEC)) * VEC;
-            alignas(16) T x[VEC];
-            if (sm.row[r] >= 0 && d < a.D) *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>((const T*)a.k + sm.row[r] + (int64_t)h * a.pages.head_stride + d);
-            else *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) sm.k[r][d + j] = w_widen(x[j]);
+    for (long long t = run.t, end = run.t_end; t < end; ++t, buf ^= 1) {
+        // (both tiles' rows are there, and the buffer of the next one's keys is free)
+        if (t + 1 < end) load(next, buf ^ 1);
+        else asm volatile("cp.async.commit_group;" ::: "memory");
+        Tile after = next;
+        int64_t after_row = -1;
+        if (t + 2 < end) {
+            after = tile_of(t + 2);
+            if (tid < KT) after_row = find(after);
         }
         float sum[NK];
 #pragma unroll
         for (int j = 0; j < NK; ++j) sum[j] = 0.f;
         for (int r0 = 0; r0 < M; r0 += kWRows) {
-            if (M > kWRows || b != have_b || h != have_h) {
+            if (M > kWRows || cur.b != have_b || cur.h != have_h) {
                 if (r0) __syncthreads();
                 const int rows16 = M - r0 <= 16 ? 16 : M - r0 <= 32 ? 32 : kWRows;       // (those that are looked at)
 #pragma unroll 4
@@ -80,9 +121,9 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                     alignas(16) T x[VEC];
                     *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
                     if (rr < M && d < a.D) {
-                        const int tok = rr / a.G, head = h * a.G + rr - tok * a.G;
-                        const bool is_open = a.lse[((int64_t)b * a.n + tok) * a.H + head] != neg_inf();      // (else the query may hold anything)
-                        if (is_open) *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d);
+                        const int tok = rr / a.G, head = cur.h * a.G + rr - tok * a.G;
+                        const bool is_open = a.lse[((int64_t)cur.b * a.n + tok) * a.H + head] != neg_inf();      // (else the query may hold anything)
+                        if (is_open) *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)cur.b * a.q_seq + (int64_t)tok * a.q_row + (int64_t)head * a.q_head + d);
                     }
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) sm.q[r][d + j] = w_widen(x[j]);
@@ -92,13 +133,14 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                     const int rr = r0 + tid;
                     if (rr < M) {
                         const int tok = rr / a.G;
-                        const float lse = a.lse[((int64_t)b * a.n + tok) * a.H + h * a.G + rr - tok * a.G];
+                        const float lse = a.lse[((int64_t)cur.b * a.n + tok) * a.H + cur.h * a.G + rr - tok * a.G];
                         if (lse != neg_inf()) z = lse * 1.4426950408889634f;
                     }
                     sm.lse[tid] = z;
                 }
-                have_b = b; have_h = h;
+                have_b = cur.b; have_h = cur.h;
             }
+            if (r0 == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");      // this tile's keys (the next one's may still be on their way)
             __syncthreads();
             // sixteen rows for each that a thread has: no more of them than there are rows
             const auto products = [&](auto rows) {
@@ -115,7 +157,7 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                     for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][d]);
 #pragma unroll
                     for (int j = 0; j < NK; ++j) {
-                        const float4 kv = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+                        const float4 kv = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][d]);
 #pragma unroll
                         for (int i = 0; i < RI; ++i) {
                             w_fma2(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
@@ -137,14 +179,19 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
 #pragma unroll
         for (int j = 0; j < NK; ++j) sm.sum[ty][tx + 16 * j] = sum[j];
         __syncthreads();
-        if (tid < count) {
-            float x = 0.f;
+        if (tid < KT) {
+            if (tid < cur.count) {
+                float x = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x += sm.sum[i][tid];
-            if (sm.row[tid] < 0) x = 0.f;
-            const int64_t at = (int64_t)b * a.w_seq + (int64_t)h * a.w_head + p0 + tid;
-            a.out[at] = a.in ? fmaf(a.decay, a.in[at], x) : x;
+                for (int i = 0; i < 16; ++i) x += sm.sum[i][tid];
+                if (sm.row[buf][tid] < 0) x = 0.f;
+                const int64_t at = (int64_t)cur.b * a.w_seq + (int64_t)cur.h * a.w_head + cur.p0 + tid;
+                a.out[at] = a.in ? fmaf(a.decay, a.in[at], x) : x;
+            }
+            sm.row[buf][tid] = after_row;
         }
+        cur = next; next = after;
+        __syncthreads();                                   // (the rows, and the sums have been read)
     }
 }
 
