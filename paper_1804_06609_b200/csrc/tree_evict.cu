@@ -13,7 +13,7 @@ namespace dba {
 
 namespace {
 
-constexpr int kEBins = 2048, kEShared = 48 * 1024;         // weights of a row that shared memory takes
+constexpr int kEBins = 2048, kEShared = 48 * 1024, kEFew = 128;      // kEShared: weights of a row that shared memory takes
 constexpr int kMThreads = 256, kMRowsAt = 256, kMCopies = 8;
 
 // larger weight, larger number; NaN is less than any
@@ -25,7 +25,8 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
     constexpr int warps = NT / 32;
     extern __shared__ float held[];
     __shared__ uint32_t bins[kEBins];
-    __shared__ int sums[2][warps], digit, above_digit;
+    __shared__ int sums[2][warps], digit, above_digit, n_few;
+    __shared__ uint32_t few[kEFew], few_bar;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = (int)(blockIdx.x % a.K), b = (int)(blockIdx.x / a.K % a.B), l = (int)(blockIdx.x / a.K / a.B);
     grid_dependency_wait();
@@ -92,16 +93,35 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
             }
             if (lane == 31) sums[0][warp] = pre;
             __syncthreads();
-            int before = pre - sum;
-            for (int i = 0; i < warp; ++i) before += sums[0][i];
+            int before = pre - sum + __reduce_add_sync(kFullMask, lane < warp ? sums[0][lane] : 0);
 #pragma unroll
             for (int i = 0; i < per; ++i) {
                 if (before < m && before + c[i] >= m) { digit = top - i; above_digit = before; }
                 before += c[i];
             }
+            if (tid == 0) n_few = 0;
             __syncthreads();
             prefix |= (uint32_t)digit << shift;
             m -= above_digit;                              // of those with this digit, m stay
+            const int left = (int)bins[digit];
+            if (pass < 2 && left <= kEFew) {               // few have it: ranked among one another
+                const uint32_t same = ~0u << shift;
+                for (int i = tid; i < old; i += NT) {
+                    const uint32_t key = weight_key(w[i]);
+                    if ((key & same) == prefix) few[atomicAdd(&n_few, 1)] = key;         // (in any order: only their number and size count)
+                }
+                __syncthreads();
+                if (tid < left) {
+                    const uint32_t key = few[tid];
+                    int greater = 0, equal = 0;
+                    for (int i = 0; i < left; ++i) { greater += few[i] > key; equal += few[i] == key; }
+                    if (greater < m && greater + equal >= m) { few_bar = key; above_digit = greater; }
+                }
+                __syncthreads();
+                prefix = few_bar;
+                m -= above_digit;
+                break;
+            }
             __syncthreads();
         }
         bar = prefix;
@@ -213,9 +233,8 @@ cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches
     const unsigned rows_keep = (unsigned)(a.K * a.B * a.layers);
     const int room = a.ctx_cap < kEShared ? a.ctx_cap : kEShared;
     const size_t bytes = (size_t)room * sizeof(float);
-    cudaError_t e = a.ctx_cap <= 2048 ? launch_after(tree_keep_kernel<256>, dim3(rows_keep), dim3(256), bytes, st, a, room)
-                    : a.ctx_cap <= 8192 ? launch_after(tree_keep_kernel<512>, dim3(rows_keep), dim3(512), bytes, st, a, room)
-                                        : launch_after(tree_keep_kernel<1024>, dim3(rows_keep), dim3(1024), bytes, st, a, room);
+    cudaError_t e = a.ctx_cap <= 2048 ? launch_after(tree_keep_kernel<512>, dim3(rows_keep), dim3(512), bytes, st, a, room)
+                                      : launch_after(tree_keep_kernel<1024>, dim3(rows_keep), dim3(1024), bytes, st, a, room);
     *launches += 1;
     if (e != cudaSuccess) return e;
     // some eight blocks an SM, none without a batch of rows
