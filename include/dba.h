@@ -476,6 +476,7 @@ typedef struct {
  * log-sum-exps; its own part is rounded to the output's type before (half a unit of its share; the prefix' part and fp32 are not).
  * query->out must not overlap query->q.  scratch_dev: dba_tree_shared_bytes, 256-byte aligned, used until the call's work is done.  Calls that follow one another on the handle's
  * stream may have the same; calls (or replays of graphs they were recorded into) that can overlap may not, nor may they the handle.
+ * Limits: groups <= 2^20, max_pages * page_size < 2^31, B * rows * heads < 2^31 (the configuration's); else DBA_ERR_UNSUPPORTED.
  * first that decreases or leaves its range, or a length outside it, sets DBA_TREE_BAD_INDEX; the rows concerned are unspecified.
  */
 dba_status dba_tree_shared_bytes(const dba_tree* h, size_t* bytes);

@@ -294,6 +294,7 @@ dba_status dba_tree_attend_shared(dba_tree* h, const dba_tree_query* q, const db
         return DBA_ERR_INVALID_ARG;
     if (q->q == q->out) return DBA_ERR_INVALID_ARG;           // (the prefix' part needs the queries after the own part is written)
     if (prefix->groups > 1 << 20 || (int64_t)prefix->max_pages * h->c.page_size >= (int64_t)1 << 31) return DBA_ERR_UNSUPPORTED;
+    if ((int64_t)h->c.B * h->c.rows * h->c.heads >= (int64_t)1 << 31) return DBA_ERR_UNSUPPORTED;      // (rows of a prefix are counted in 32 bits)
     if (!scratch_dev || ((uintptr_t)scratch_dev & 255u)) return DBA_ERR_WORKSPACE;
     TreePrefix a{};
     if (scratch_bytes < carve_prefix(h, scratch_dev, &a)) return DBA_ERR_WORKSPACE;
