@@ -326,7 +326,7 @@ dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* q, const float* lse
                           int64_t head_stride, float decay) {
     if (!h || !q || !q->q || !lse_dev || !ctx_len_dev || !weight_out || q->rows < 1 || q->rows > h->c.rows || q->scale != q->scale || decay != decay)
         return DBA_ERR_INVALID_ARG;
-    if (seq_stride < 0 || head_stride < 0) return DBA_ERR_INVALID_ARG;
+    if (seq_stride < (h->c.B > 1) || head_stride < (h->c.kv_heads > 1)) return DBA_ERR_INVALID_ARG;        // (rows of their own)
     TreeWeigh a{};
     const dba_status st = check_cache(h, cache, table_dev, table_stride, &a.pages);
     if (st != DBA_OK) return st;
@@ -350,7 +350,7 @@ dba_status dba_tree_evict(dba_tree* h, const dba_kv_cache* cache, const int32_t*
                           const dba_tree_evicted* ev) {
     if (!h || !ctx_len_dev || !ev || !ev->weight || !ev->weight_out || !ev->to_table || !ev->kept || ev->keep < 1 || ev->recent < 0 || ev->recent > ev->keep)
         return DBA_ERR_INVALID_ARG;
-    if (ev->layer_stride < 0 || ev->seq_stride < 0 || ev->head_stride < 0) return DBA_ERR_INVALID_ARG;
+    if (!cache || ev->layer_stride < (cache->layers > 1) || ev->seq_stride < (h->c.B > 1) || ev->head_stride < (h->c.kv_heads > 1)) return DBA_ERR_INVALID_ARG;
     TreeEvict a{};
     dba_status st = check_cache(h, cache, table_dev, table_stride, &a.from);
     if (st == DBA_OK) st = check_cache(h, cache, ev->to_table, ev->to_table_stride, &a.to);

@@ -169,7 +169,8 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                 for (int i = 0; i < RI; ++i) {
                     const float z = sm.lse[ty + 16 * i];
 #pragma unroll
-                    for (int j = 0; j < NK; ++j) sum[j] += w_ex2(fmaf(s[i][j].x + s[i][j].y, a.scale_log2e, -z));
+                    for (int j = 0; j < NK; ++j)           // (zeros times keys that are not finite are not zero)
+                        if (z != __int_as_float(0x7f800000)) sum[j] += w_ex2(fmaf(s[i][j].x + s[i][j].y, a.scale_log2e, -z));
                 }
             };
             if (M - r0 <= 16) products(std::integral_constant<int, 1>{});
