@@ -2,11 +2,15 @@
 //
 // For every (layer, sequence, key head) with L > keep tokens: the last `recent` of them and, of the others, the m = keep - recent of the
 // largest weight.  Weights become whole numbers in the same order (ord32; NaN: 0); the m-th largest is found by its digits, the
-// highest first, from histograms in shared memory; a last pass keeps what is above it and the first ones at it, in order, by a
-// prefix sum.  Everything is decided by counts, so equal inputs give equal results.
+// highest first, from histograms in shared memory, until at most 128 are in question, which are ranked among one another; a last pass keeps
+// what is above it and the first ones at it, in order, by a prefix sum.  Everything is decided by counts, so equal inputs give equal results.
 //
 // Copies: row i of what is kept comes from place kept[i] >= i.  Other pages: any order.  The same pages: rows in ascending order, each
 // batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.
+//
+// Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: the choice 45 us (128 rows, a block each, of 65 KB to 130 KB
+// of weights: the passes' steps one after the other), the copies 183 us, 1.07 GB, 5.9 TB/s: HBM.  256 of some 300 tokens, one layer of four
+// sequences: 8 us, launches and dependent loads.
 #include "tree_device.cuh"
 
 namespace dba {
@@ -233,6 +237,7 @@ cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches
     const unsigned rows_keep = (unsigned)(a.K * a.B * a.layers);
     const int room = a.ctx_cap < kEShared ? a.ctx_cap : kEShared;
     const size_t bytes = (size_t)room * sizeof(float);
+    // 512 rows of 1000 places: 29 us with 512 threads, 38 with 256; 128 rows of 4000 27.7 with 1024, 32.8 with 512; of 32768 51 and 64
     cudaError_t e = a.ctx_cap <= 2048 ? launch_after(tree_keep_kernel<512>, dim3(rows_keep), dim3(512), bytes, st, a, room)
                                       : launch_after(tree_keep_kernel<1024>, dim3(rows_keep), dim3(1024), bytes, st, a, room);
     *launches += 1;
