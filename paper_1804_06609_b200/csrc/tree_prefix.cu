@@ -6,14 +6,16 @@
 // m the running maximum, so that the prefix is gone through once for 64 rows and not once for each sequence.  The rows' own
 // part (context and arena) comes out of dba_tree_attend's kernels before, with its log-sum-exp; out = w_own o + w_pre O.
 //
-// A block of 256 threads has 64 rows: thread (ty, tx) the scores of rows ty, ty+16, .. with keys tx, tx+16, .. and the outputs of the
-// same rows x columns 4 tx .. 4 tx + 3 (+64, ..); a row's statistics stay in the 16 threads that use them.  Sixteen bytes of
-// queries and keys feed 4 x 4 products of pairs (fma.rn.f32x2).  The keys of the next tile and the values of this one are on their way
-// (cp.async) while the scores are computed.  Two blocks an SM (one for head sizes over 128).
+// A block has 64 rows: thread (ty, tx) the scores of rows ty, ty+16, .. with keys tx, tx+TX, .. and the outputs of the same rows x columns
+// 4 tx .. 4 tx + 3 (+ 4 TX, ..); a row's statistics stay in the TX threads that use them.  Sixteen bytes of queries and keys feed products of
+// pairs (fma.rn.f32x2): 4 x 8 of them where eight threads have a row (head sizes to 64, three blocks of 128 threads an SM), else 4 x 4 or
+// less.  The keys of the next tile and the values of this one are on their way (cp.async) while the scores are computed.  Only the epilogue needs
+// the kernel before this one, so the rest runs beside its last blocks.
 //
-// Measured, fp32, beams of 20 on 16 sentences, three prefixes of up to 700 tokens, 16 heads of 64: 47 us, beside 27 of the rows' own part: 16 MB and 0.8
-// GFLOP, neither near what the machine has.  It is bound by the way from shared memory into the products (issue 35 %) and by the
-// few tiles that each of 296 blocks has.
+// Measured, fp32, beams of 20 on 16 sentences, three prefixes of up to 700 tokens, 16 heads (16 MB and 0.8 GFLOP with heads of 64), the whole call with the
+// rows' own part of 27 us: heads of 64 73 us (81 with sixteen threads to a row, two blocks of 256), of 128 125, of 256 233; waiting for the kernel before
+// at once 76, 133 and 237.  A block's chain bounds it: queries 5 us, then 6 us a tile with two others on the SM, of which the products of the scores
+// are half (their operands come through shared memory), those of the outputs a third, near the rate of the fma pipes.
 #include <cuda_bf16.h>
 
 #include "tree_span.cuh"
@@ -22,7 +24,7 @@ namespace dba {
 
 namespace {
 
-constexpr int kPThreads = 256, kPRows = 64;
+constexpr int kPRows = 64;
 
 __device__ __forceinline__ float p_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }     // (within 2^-22)
 // (a0, a1) += (b0, b1) * (c0, c1)
@@ -34,14 +36,31 @@ __device__ __forceinline__ float p_widen(float x) { return x; }
 __device__ __forceinline__ float p_widen(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void p_store(float* p, float x) { *p = x; }
 __device__ __forceinline__ void p_store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+// four neighbours, all of them there (a head's size and the strides are multiples of 16 bytes)
+__device__ __forceinline__ float4 p_load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 p_load4(const __nv_bfloat16* p) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+}
+__device__ __forceinline__ void p_store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void p_store4(__nv_bfloat16* p, float4 x) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+// w o + y
+__device__ __forceinline__ float4 p_mix(float w, float4 o, float4 y) { return make_float4(fmaf(w, o.x, y.x), fmaf(w, o.y, y.y), fmaf(w, o.z, y.z), fmaf(w, o.w, y.w)); }
 
 template <int DP> struct PSmem {
+    static constexpr int tx = DP == 64 ? 8 : 16, threads = 16 * tx;    // threads to a row
     static constexpr int kt = DP == 64 ? 64 : DP == 128 ? 32 : 16;     // keys per tile: 16 KB of fp32
-    static constexpr int pitch = DP + 4;
+    static constexpr int blocks = DP == 64 ? 3 : DP == 128 ? 2 : 1;    // an SM's
+    static constexpr int half = DP == 64 ? 32 : 0, least = DP == 64 ? 4 : 2;       // of PrefixCut and of its runs: 16 rows cost less than 64 where eight threads have a row
+    static constexpr bool over = DP == 64;                             // probabilities come over the keys: a third block has room
+    static constexpr int pitch = DP + 4, p_pitch = over ? kt + 8 : kt + 4;
     float q[kPRows][pitch];
-    float k[2][kt][pitch];
+    float k[2][over ? kt + 4 : kt][pitch];
     float v[kt][pitch];
-    float p[kPRows][kt + 4];
+    float p[over ? 1 : kPRows][p_pitch];
     int64_t row[2][kt];
     SpanShared span;
 };
@@ -51,7 +70,7 @@ template <int DP>
 __device__ __forceinline__ void p_load(int D, const float* base, const int64_t* row, float (*dst)[DP + 4]) {
     constexpr int CH = DP / 4;
 #pragma unroll
-    for (int i = threadIdx.x; i < PSmem<DP>::kt * CH; i += kPThreads) {
+    for (int i = threadIdx.x; i < PSmem<DP>::kt * CH; i += PSmem<DP>::threads) {
         const int r = i / CH, d = (i - r * CH) * 4;
         const bool in = row[r] >= 0 && d < D;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(&dst[r][d])), "l"(in ? base + row[r] + d : base), "r"(in ? 16u : 0u) : "memory");
@@ -61,7 +80,7 @@ template <int DP>
 __device__ __forceinline__ void p_load(int D, const __nv_bfloat16* base, const int64_t* row, float (*dst)[DP + 4]) {
     constexpr int CH = DP / 8;
 #pragma unroll
-    for (int i = threadIdx.x; i < PSmem<DP>::kt * CH; i += kPThreads) {
+    for (int i = threadIdx.x; i < PSmem<DP>::kt * CH; i += PSmem<DP>::threads) {
         const int r = i / CH, d = (i - r * CH) * 8;
         uint4 x = make_uint4(0, 0, 0, 0);
         if (row[r] >= 0 && d < D) x = *reinterpret_cast<const uint4*>(base + row[r] + d);
@@ -75,9 +94,9 @@ template <int N> __device__ __forceinline__ void p_wait() { asm volatile("cp.asy
 
 // A piece with at most 16 RI rows.
 template <typename T, int DP, int RI>
-__device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm, const typename PrefixCut<PSmem<DP>::kt, kPRows, 0>::Piece& pc, int64_t part) {
-    constexpr int KT = PSmem<DP>::kt, NK = KT / 16, NC = DP / 64;
-    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+__device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm, const typename PrefixCut<PSmem<DP>::kt, kPRows, PSmem<DP>::half>::Piece& pc, int64_t part) {
+    constexpr int KT = PSmem<DP>::kt, TX = PSmem<DP>::tx, NK = KT / TX, NC = DP / (4 * TX);
+    const int tid = threadIdx.x, ty = tid / TX, tx = tid % TX;
     const T* const kb = (const T*)a.k + (int64_t)pc.h * a.pages.head_stride;
     const T* const vb = (const T*)a.v + (int64_t)pc.h * a.pages.head_stride;
     auto find_rows = [&](int t) {
@@ -87,7 +106,7 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
     find_rows(pc.tile);
     constexpr int VEC = 16 / (int)sizeof(T);
 #pragma unroll 4
-    for (int i = tid; i < 16 * RI * (DP / VEC); i += kPThreads) {       // queries, zero beyond the rows and the head size
+    for (int i = tid; i < 16 * RI * (DP / VEC); i += PSmem<DP>::threads) {       // queries, zero beyond the rows and the head size
         const int r = i / (DP / VEC), d = (i - r * (DP / VEC)) * VEC;
         alignas(16) T x[VEC];
         *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
@@ -119,6 +138,8 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
         p_commit();
         if (t + 1 < pc.tile_end) p_load<DP>(a.D, kb, sm.row[(t + 1) & 1], sm.k[(t + 1) & 1]);
         p_commit();
+        const float (*const keys)[DP + 4] = sm.k[t & 1];
+        float (*const p)[PSmem<DP>::p_pitch] = PSmem<DP>::over ? reinterpret_cast<float (*)[PSmem<DP>::p_pitch]>(&sm.k[t & 1][0][0]) : sm.p;
         float2 s[RI][NK];
 #pragma unroll
         for (int i = 0; i < RI; ++i)
@@ -131,35 +152,35 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
             for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][d]);
 #pragma unroll
             for (int j = 0; j < NK; ++j) {
-                const float4 kv = *reinterpret_cast<const float4*>(&sm.k[t & 1][tx + 16 * j][d]);
+                const float4 kv = *reinterpret_cast<const float4*>(&keys[tx + TX * j][d]);
 #pragma unroll
-                for (int i = 0; i < RI; ++i) {
-                    p_fma2(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
-                    p_fma2(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
-                }
+                for (int i = 0; i < RI; ++i) p_fma2(s[i][j], qv[i].x, qv[i].y, kv.x, kv.y);
+#pragma unroll
+                for (int i = 0; i < RI; ++i) p_fma2(s[i][j], qv[i].z, qv[i].w, kv.z, kv.w);
             }
         }
+        if (PSmem<DP>::over) __syncthreads();              // the keys have been used
 #pragma unroll
         for (int i = 0; i < RI; ++i) {
             float x[NK], top = neg_inf();
 #pragma unroll
             for (int j = 0; j < NK; ++j) {
-                const int kk = tx + 16 * j;
+                const int kk = tx + TX * j;
                 x[j] = sm.row[t & 1][kk] >= 0 ? (s[i][j].x + s[i][j].y) * a.scale_log2e : neg_inf();
                 top = fmaxf(top, x[j]);
             }
 #pragma unroll
-            for (int k = 8; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, k));
+            for (int k = TX / 2; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, k));
             const float mn = fmaxf(m[i], top), ref = mn == neg_inf() ? 0.f : mn, corr = p_ex2(m[i] - ref);      // 0 while nothing has been seen
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < NK; ++j) {
                 const float e = p_ex2(x[j] - ref);
-                sm.p[ty + 16 * i][tx + 16 * j] = e;
+                p[ty + 16 * i][tx + TX * j] = e;
                 sum += e;
             }
 #pragma unroll
-            for (int k = 8; k; k >>= 1) sum += __shfl_xor_sync(kFullMask, sum, k);
+            for (int k = TX / 2; k; k >>= 1) sum += __shfl_xor_sync(kFullMask, sum, k);
             l[i] = fmaf(l[i], corr, sum);
             m[i] = mn;
 #pragma unroll
@@ -171,12 +192,12 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
         for (int k = 0; k < count; k += 4) {               // (rows that do not exist are zeros, and so are their probabilities)
             float4 e[RI];
 #pragma unroll
-            for (int i = 0; i < RI; ++i) e[i] = *reinterpret_cast<const float4*>(&sm.p[ty + 16 * i][k]);
+            for (int i = 0; i < RI; ++i) e[i] = *reinterpret_cast<const float4*>(&p[ty + 16 * i][k]);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    const float4 vv = *reinterpret_cast<const float4*>(&sm.v[k + kk][c * 64 + 4 * tx]);
+                    const float4 vv = *reinterpret_cast<const float4*>(&sm.v[k + kk][c * (4 * TX) + 4 * tx]);
 #pragma unroll
                     for (int i = 0; i < RI; ++i) {
                         const float w = kk == 0 ? e[i].x : kk == 1 ? e[i].y : kk == 2 ? e[i].z : e[i].w;
@@ -186,50 +207,55 @@ __device__ __forceinline__ void prefix_piece(const TreePrefix& a, PSmem<DP>& sm,
         }
         find_rows(t + 2);
     }
+    if (part >= 0) {
 #pragma unroll
-    for (int i = 0; i < RI; ++i) {
-        const int r = ty + 16 * i;
-        const bool in = r < pc.rows;
-        if (part >= 0) {
-            if (!in) continue;
+        for (int i = 0; i < RI; ++i) {
+            const int r = ty + 16 * i;
+            if (r >= pc.rows) continue;
             const int64_t at = part + r;
             if (tx == 0) { a.part_ml[2 * at] = m[i]; a.part_ml[2 * at + 1] = l[i]; }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const int d = c * 64 + 4 * tx;
+                const int d = c * (4 * TX) + 4 * tx;
                 if (d < a.D) *reinterpret_cast<float4*>(a.part_o + at * a.D + d) = make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
             }
-            continue;
         }
-        const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + (in ? r : 0));
+        return;
+    }
+    grid_dependency_wait();
+#pragma unroll
+    for (int i = 0; i < RI; ++i) {
+        const int r = ty + 16 * i;
+        const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + (r < pc.rows ? r : 0));
+        T* const out = (T*)a.out + (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head + 4 * tx;
+        float4 old[NC];                                    // what the row has of its own: all of it on its way before anything is written
         float own, w_own, w_pre, lse;
-        const bool is_open = prefix_own(a, w, &own) && in;
-        __syncwarp();                                      // (the row's 16 threads have read what one of them writes)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (c * (4 * TX) + 4 * tx < a.D) old[c] = p_load4(out + c * (4 * TX));
+        const bool is_open = prefix_own(a, w, &own) && r < pc.rows;
+        __syncwarp();                                      // (the row's threads have read what one of them writes)
         if (!is_open || !prefix_join(own, m[i], l[i], &w_own, &w_pre, &lse)) continue;
-        T* out = (T*)a.out + (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const float y[4] = {o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = c * 64 + 4 * tx + j;
-                if (d < a.D) p_store(out + d, fmaf(w_own, p_widen(out[d]), w_pre * y[j]));
-            }
+            const float2 y0 = o[i][2 * c], y1 = o[i][2 * c + 1];
+            if (c * (4 * TX) + 4 * tx < a.D) p_store4(out + c * (4 * TX), p_mix(w_own, old[c], make_float4(w_pre * y0.x, w_pre * y0.y, w_pre * y1.x, w_pre * y1.y)));
         }
         if (tx == 0) a.own_lse[((int64_t)w.b * a.n + w.i) * a.H + w.head] = lse;
     }
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kPThreads, DP <= 128 ? 2 : 1) tree_prefix_kernel(const TreePrefix a) {
+__global__ void __launch_bounds__(PSmem<DP>::threads, PSmem<DP>::blocks) tree_prefix_kernel(const TreePrefix a) {
     using S = PSmem<DP>;
-    using Cut = PrefixCut<S::kt, kPRows, 0>;
+    using Cut = PrefixCut<S::kt, kPRows, S::half>;
     extern __shared__ __align__(16) unsigned char praw[];
     S& sm = *reinterpret_cast<S*>(praw);
-    grid_dependency_wait();
+    // Nothing but the rows' own part comes from the kernel before this one, and that kernel has waited for what came before it: the wait
+    // is the epilogue's.
     allow_dependents();
     if (blockIdx.x == 0) prefix_check(a);
-    SpanRun run = Cut::template run<kPThreads>(a, 4, &sm.span);
+    SpanRun run = Cut::template run<S::threads>(a, S::least, &sm.span);
     typename Cut::Piece pc;
     int cut = 0;
     int4 meta[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
@@ -244,6 +270,7 @@ __global__ void __launch_bounds__(kPThreads, DP <= 128 ? 2 : 1) tree_prefix_kern
         else prefix_piece<T, DP, 4>(a, sm, pc, part);
     }
     if (threadIdx.x < 2) a.meta[2 * blockIdx.x + threadIdx.x] = meta[threadIdx.x];
+    grid_dependency_wait();            // (a block without work too: what follows this kernel follows the one before it)
 }
 
 // Finishes the items that several blocks worked on.  A block's run leaves at most two pieces of such items, in the order of the
@@ -356,8 +383,9 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
         for (int u0 = 0; u0 < rows * vecs * shares; u0 += kPJoinThreads) {
             const int u = u0 + tid, share = u / (rows * vecs), in_share = u - share * (rows * vecs), row = in_share / vecs, d = (in_share - row * vecs) * 4;
             const bool here = share < shares && row < left && out_at[row] >= 0;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f), old = o;
             if (here) {
+                if (share == 0) old = p_load4((const T*)a.out + out_at[row] + d);
 #pragma unroll 8
                 for (int i = share; i < count; i += shares) {
                     const float4 v = *reinterpret_cast<const float4*>(a.part_o + ((int64_t)list[first + i] * item_rows + r0 + row) * a.D + d);
@@ -375,10 +403,7 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
                     }
             }
             if (!here || share > 0) continue;
-            T* out = (T*)a.out + out_at[row] + d;
-            const float y[4] = {o.x, o.y, o.z, o.w}, wo = own_weight[row];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p_store(out + j, fmaf(wo, p_widen(out[j]), y[j]));
+            p_store4((T*)a.out + out_at[row] + d, p_mix(own_weight[row], old, o));
         }
         __syncthreads();
     }
@@ -386,12 +411,12 @@ __global__ void __launch_bounds__(kPJoinThreads) tree_prefix_join_kernel(const T
 
 template <typename T, int DP>
 cudaError_t configure_prefix() {
-    static_assert((DP <= 128 ? 2 : 1) * (sizeof(PSmem<DP>) + 1024) <= 228 * 1024, "blocks of the grid that an SM holds");
+    static_assert(PSmem<DP>::blocks * (sizeof(PSmem<DP>) + 1024) <= 228 * 1024, "blocks of the grid that an SM holds");
     return cudaFuncSetAttribute(tree_prefix_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PSmem<DP>));
 }
 template <typename T, int DP>
 cudaError_t launch_prefix(const TreePrefix& a, int grid, cudaStream_t st) {
-    return launch_after(tree_prefix_kernel<T, DP>, dim3(grid), dim3(kPThreads), sizeof(PSmem<DP>), st, a);
+    return launch_after(tree_prefix_kernel<T, DP>, dim3(grid), dim3(PSmem<DP>::threads), sizeof(PSmem<DP>), st, a);
 }
 
 }  // namespace
@@ -406,7 +431,7 @@ TreePrefixPlan plan_tree_prefix(int dtype, int D, int sm_count) {
         p.keys = tree_prefix_mma_keys();
         return p;
     }
-    p.grid = (D <= 128 ? 2 : 1) * sm_count;
+    p.grid = (D <= 64 ? PSmem<64>::blocks : D <= 128 ? PSmem<128>::blocks : PSmem<256>::blocks) * sm_count;
     p.rows = kPRows;
     return p;
 }

@@ -12,18 +12,19 @@
 //   products   one lane of a stream's warp issues, a half at a time: P V of half h, then the next tile's scores into the half that P has left.
 //              A stream's next scores come behind its outputs, so their completion shows that of the outputs before.
 //   loaders    keys and values K-major and MN-major, both [key][d] in the 128-byte swizzle.  Pages made of eights of places: one warp sends
-//              tensor-map boxes, a lane to a stretch of a page, another one fetches queries (16-byte cp.async); places of a box that lie
+//              tensor-map boxes, a lane to a stretch of a page, another one fetches queries (16-byte cp.async; a block's first ones the
+//              softmax warps, which have nothing to do yet); places of a box that lie
 //              behind the prefix are hidden from the scores, and their values made zeros.  Other pages, and strides that no tensor map has: four
 //              warps of cp.async with zero fill, every place looked up by itself, so pages of any size may end inside a tile.
 // The epilogue joins a whole item with the rows' own part and writes the result; pieces of an item go to scratch, and to the joining
 // kernel (tree_prefix.cu).  Only the epilogue needs the kernel before this one, so the rest runs beside its last blocks.  Every wait on an
 // mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
 //
-// Measured: beams of 20 on 64 sentences, 32 heads over 8 of 128, 6007 tokens (126 GFLOP, 40960 rows) 126 us beside 30 of the rows' own part: 1.0
+// Measured: beams of 20 on 64 sentences, 32 heads over 8 of 128, 6007 tokens (126 GFLOP, 40960 rows) 124 us beside 30 of the rows' own part: 1.0
 // PFLOP/s, 62 % of the rate of a large matrix product.  What bounds it is the softmax: a tile of 128 keys takes a stream's warps some 3500 cycles, of
 // which exponentials, sums and packing 2000, and the tensor cores, at 50 to 60 %, wait for them.  Eight rows on 100003 tokens (205 MB): 54 us,
 // 3.8 TB/s.  Both sides of what was chosen, the document's call in us: half tiles 157, whole ones 170; a quarter of the exponentials as
-// polynomials 157, none 162, half of them 164; the few rows' call with boxes 73, with cp.async 92.
+// polynomials 157, none 162, half of them 164; the first queries by one warp 156, by eight 154; the few rows' call with boxes 73, with cp.async 92.
 #include <cuda_bf16.h>
 
 #include "tree_boxes.cuh"
@@ -51,7 +52,7 @@ template <int DP, bool TMA> struct XSmem {
     uint64_t full[C::stages], empty[C::stages];
     uint64_t s_full[2][2], p_ready[2][2], pv_done[2], o_done[2];
     uint64_t q_full[C::q_bufs], q_empty[C::q_bufs];
-    uint64_t o_free, ml_ready, last[2];
+    uint64_t q_first, o_free, ml_ready, last[2];
     float ml[2][128][2];
     uint32_t seen[kXSeen][4];                   // (by tile, in turn) which of its rows there are
     uint32_t tmem_base;
@@ -91,6 +92,32 @@ __device__ __forceinline__ void ex2_pair(float& x, float& y) {
 }
 using XCut = PrefixCut<kXKeys, kXRows, 128>;
 
+// 32 queries of an item from its row r0 on into their place in shared memory (both halves begin at q_at), zeros beyond the rows and the head size: a lane finds
+// one row, and every lane copies chunks of all.
+template <int DP>
+__device__ __forceinline__ void copy_queries(const TreePrefix& a, const XCut::Piece& pc, uint32_t q_at, int r0, int lane) {
+    constexpr int CH = DP / 8, RW = 32 / CH, NJ = 32 / RW;             // 16-byte chunks of a row, rows a warp copies at a time, and how often
+    const int ch = lane % CH, sub = lane / CH;
+    const bool ch_in = ch * 8 < a.D;
+    const uint32_t swz = (uint32_t)((ch & 7) ^ sub) << 4;              // the swizzle moves a chunk by its row's last three bits
+    const char* const q = (const char*)a.q + (ch_in ? ch * 16 : 0);
+    int64_t q_row = -1;
+    if (r0 + lane < pc.rows) {
+        const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
+        q_row = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
+    }
+    const uint32_t to = q_at + (r0 >= 128 ? 128 * DP * 2 : 0) + (uint32_t)(ch >> 3) * (128 * 128) + (uint32_t)((r0 & 127) + sub) * 128;
+#pragma unroll
+    for (int j0 = 0; j0 < NJ; j0 += 8) {
+        int64_t from[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) from[j] = __shfl_sync(kFullMask, q_row, (j0 + j) * RW + sub);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            cp_async16(to + (j0 + j) * RW * 128 + (swz ^ (uint32_t)(((j0 + j) * RW & 7) << 4)), from[j] >= 0 ? q + from[j] : q, from[j] >= 0 && ch_in ? 16u : 0u);
+    }
+}
+
 template <int DP, bool TMA>
 __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_kernel(const __grid_constant__ TreePrefix a, const __grid_constant__ TreeBoxes maps,
                                                                         const uint32_t negate) {
@@ -108,6 +135,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             mbar_init(msmem_u32(&sm.pv_done[s]), 1); mbar_init(msmem_u32(&sm.o_done[s]), 1); mbar_init(msmem_u32(&sm.last[s]), 1);
         }
         for (int i = 0; i < C::q_bufs; ++i) { mbar_init(msmem_u32(&sm.q_full[i]), 32 * C::q_warps); mbar_init(msmem_u32(&sm.q_empty[i]), 2); }
+        mbar_init(msmem_u32(&sm.q_first), 256);
         mbar_init(msmem_u32(&sm.o_free), 8);
         mbar_init(msmem_u32(&sm.ml_ready), 8);
         sm.abort_flag = 0;
@@ -156,28 +184,12 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
                 id = place < pc.len ? __ldg(table + tree_page(a.pages, (uint32_t)place)) : -1;       // (below the table's entries: len is)
             };
             if (!TMA || lw == 0) fetch(pc.tile);
-            if (q_warp >= 0) {                             // queries, zeros beyond the rows and the head size
+            if (q_warp >= 0) {                             // queries
                 const uint32_t qb = (uint32_t)piece % C::q_bufs;
                 if (piece >= C::q_bufs && !mbar_wait(msmem_u32(&sm.q_empty[qb]), ((uint32_t)piece / C::q_bufs - 1) & 1u, abort_flag, limit)) { ok = false; break; }
-                const char* q = (const char*)a.q + (ch_in ? ch * 16 : 0);
+                if (piece > 0)                             // (the first ones are the softmax warps' to copy, which have nothing to do yet)
 #pragma unroll 1
-                for (int r0 = q_warp * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * C::q_warps) {         // a lane finds one row, and every lane copies chunks of all
-                    int64_t q_row = -1;
-                    if (r0 + lane < pc.rows) {
-                        const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + r0 + lane);
-                        q_row = 2 * ((int64_t)w.b * a.q_seq + (int64_t)w.i * a.q_row + (int64_t)w.head * a.q_head);
-                    }
-                    const uint32_t to = q_at + qb * C::q_bytes + (r0 >= 128 ? C::q_half : 0) + (uint32_t)(ch >> 3) * (128 * 128) + (uint32_t)((r0 & 127) + sub) * 128;
-#pragma unroll 1
-                    for (int j0 = 0; j0 < 32; j0 += 8 * RW) {
-                        int64_t from[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) from[j] = __shfl_sync(kFullMask, q_row, j0 + j * RW + sub);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            cp_async16(to + (j0 + j * RW) * 128 + (swz ^ (uint32_t)((j * RW & 7) << 4)), from[j] >= 0 ? q + from[j] : q, from[j] >= 0 && ch_in ? 16u : 0u);
-                    }
-                }
+                    for (int r0 = q_warp * 32; r0 < (pc.rows > 128 ? kXRows : 128); r0 += 32 * C::q_warps) copy_queries<DP>(a, pc, q_at + qb * C::q_bytes, r0, lane);
                 cp_arrive(msmem_u32(&sm.q_full[qb]));
             }
             const int64_t head_at = 2 * (int64_t)pc.h * a.pages.head_stride + (ch_in ? ch * 16 : 0);
@@ -257,6 +269,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             const int tiles = pc.tile_end - pc.tile, by = two ? 1 : 2, n = two ? tiles : (tiles + 1 - s) / 2;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
             if (!(ok = mbar_wait(msmem_u32(&sm.q_full[qb]), ((uint32_t)piece / C::q_bufs) & 1u, abort_flag, limit))) break;
+            if (piece == 0 && !(ok = mbar_wait(msmem_u32(&sm.q_first), 0, abort_flag, limit))) break;
             const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]) + (two ? s * C::q_half : 0), 16);
             // rows of this stream's last tile behind the prefix' end
             const int n_tail = pc.tile_end == pc.tiles && (pc.tiles - 1 - pc.tile) % by == (two ? 0 : s) ? pc.tiles * kXKeys - pc.len : 0;
@@ -357,6 +370,10 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
         bool ok = true;
         while (ok && XCut::next(a, run, &pc)) {
             const bool two = pc.rows > 128;
+            if (piece == 0) {
+                if (two || warp < 4) copy_queries<DP>(a, pc, msmem_u32(sm.q), 32 * warp, lane);
+                cp_arrive(msmem_u32(&sm.q_first));
+            }
             float ref = neg_inf(), sum = 0.f;
             const int first = pc.tile + (two ? 0 : s), by = two ? 1 : 2;
 #pragma unroll 1
@@ -437,23 +454,26 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             const PrefixRow w = prefix_row(a, pc.lo, pc.h, pc.row0 + (in ? row : 0));
             const int64_t out_at = (int64_t)w.b * a.o_seq + (int64_t)w.i * a.o_row + (int64_t)w.head * a.o_head;
             grid_dependency_wait();                        // the rows' own part
-            float own = neg_inf();
-            bool write = in;
-            if (part < 0) write = prefix_own(a, w, &own) && in;
             const int c0 = two ? 0 : s * (DP / 2), c1 = two ? DP : c0 + DP / 2;
-            uint4 old[4];                                  // what the rows that this lane will write have of their own, one block of columns ahead
-            const auto fetch = [&](int c) {
+            uint4 old[4], next[4];                               // what the rows that this lane will write have of their own, two blocks of columns ahead
+            const uint32_t rows_here = __ballot_sync(kFullMask, in);
+            const auto fetch = [&](int c, uint4* to) {
                 const int col = c + (lane & 3) * 8;
-                const uint32_t rows_in = __ballot_sync(kFullMask, write);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = i * 8 + (lane >> 2);
                     const int64_t at = __shfl_sync(kFullMask, out_at, r);
-                    if (((rows_in >> r) & 1u) && col < a.D) old[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out + at + col);
-                    else old[i] = make_uint4(0, 0, 0, 0);
+                    if (((rows_here >> r) & 1u) && col < a.D && c < c1) to[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out + at + col);
+                    else to[i] = make_uint4(0, 0, 0, 0);
                 }
             };
-            if (part < 0) fetch(c0);
+            float own = neg_inf();
+            bool write = in;
+            if (part < 0) {
+                fetch(c0, old);
+                fetch(c0 + 32, next);
+                write = prefix_own(a, w, &own) && in;
+            }
             if (!mbar_wait(msmem_u32(&sm.o_done[s]), piece & 1, abort_flag, limit)) { ok = false; break; }
             float f = 1.f, g = 0.f;                        // factors of this stream's output, and of the other's
             if (!two) {
@@ -475,8 +495,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             tc_after();
             float4 (*turn)[8] = sm.turn[warp];
 #pragma unroll 1
-            for (int c = c0; c < c1; c += 32) {
-                if (c >= a.D) break;
+            for (int c = c0; c < c1 && c < a.D; c += 32) {
                 uint32_t u[32];
                 float y[32];
                 tm_ld32(o_at + s * DP + c, u);
@@ -503,8 +522,8 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
                     const int col = c + (lane & 3) * 8;
                     uint4 now[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) now[i] = old[i];
-                    if (c + 32 < c1 && c + 32 < a.D) fetch(c + 32);
+                    for (int i = 0; i < 4; ++i) { now[i] = old[i]; old[i] = next[i]; }
+                    fetch(c + 64, next);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = i * 8 + (lane >> 2);
@@ -531,6 +550,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             tiles0 += pc.tile_end - pc.tile;
             ++piece;
         }
+        cp_wait_all();
     }
     tc_before();
     __syncthreads();

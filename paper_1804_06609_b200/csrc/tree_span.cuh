@@ -154,14 +154,20 @@ __device__ __forceinline__ PrefixRow prefix_row(const TreePrefix& a, int lo, int
     return {lo + seq, i, h * a.G + in - i * a.G};
 }
 
-// What a row's own part says of it: its log-sum-exp in powers of two (-inf: nothing seen of its own); false: the row is closed.
-__device__ __forceinline__ bool prefix_own(const TreePrefix& a, const PrefixRow& r, float* own) {
-    *own = a.own_lse[((int64_t)r.b * a.n + r.i) * a.H + r.head] * 1.4426950408889634f;
-    if (*own != neg_inf() || !a.masks) return true;
+// What a row's own part says of it: its log-sum-exp in powers of two (-inf: nothing seen of its own); whether the row is open.
+__device__ __forceinline__ float prefix_own_lse(const TreePrefix& a, const PrefixRow& r) {
+    return a.own_lse[((int64_t)r.b * a.n + r.i) * a.H + r.head] * 1.4426950408889634f;
+}
+__device__ __forceinline__ bool prefix_open(const TreePrefix& a, const PrefixRow& r, float own) {
+    if (own != neg_inf() || !a.masks) return true;
     uint32_t any = 0;
     const uint32_t* m = a.masks + ((int64_t)r.b * a.n + r.i) * a.W;
     for (int w = 0; w < a.W; ++w) any |= __ldg(m + w);
     return any != 0;
+}
+__device__ __forceinline__ bool prefix_own(const TreePrefix& a, const PrefixRow& r, float* own) {
+    *own = prefix_own_lse(a, r);
+    return prefix_open(a, r, *own);
 }
 
 // A row's whole from its own part (log-sum-exp in powers of two `own`, output o) and the prefix' (reference m, sum l, products O):
