@@ -2,14 +2,15 @@
 //
 // For every (layer, sequence, key head) with L > keep tokens: the last `recent` of them and, of the others, the m = keep - recent of the
 // largest weight.  Weights become whole numbers in the same order (ord32; NaN: 0); the m-th largest is found by its digits, the
-// highest first, from histograms in shared memory, until at most 128 are in question, which are ranked among one another; a last pass keeps
-// what is above it and the first ones at it, in order, by a prefix sum.  Everything is decided by counts, so equal inputs give equal results.
+// highest first, from histograms in shared memory, until at most 128 are in question, which are ranked among one another; a last pass counts,
+// and then keeps, what is above it and the first ones at it, in order, a stretch of the row to a warp.  Everything is decided by counts, so equal inputs give equal results.
 //
 // Copies: row i of what is kept comes from place kept[i] >= i.  Other pages: any order.  The same pages: rows in ascending order, each
 // batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.
 //
-// Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: the choice 45 us (128 rows, a block each, of 65 KB to 130 KB
-// of weights: the passes' steps one after the other), the copies 183 us, 1.07 GB, 5.9 TB/s: HBM.  256 of some 300 tokens, one layer of four
+// Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: the choice 33 us (128 rows, a block each, of up to 130 KB
+// of weights: the passes one after the other; 45 with the last one all over the row between barriers and the first digits counted after the load),
+// the copies 183 us, 1.07 GB, 5.9 TB/s: HBM.  256 of some 300 tokens, one layer of four
 // sequences: 8 us, launches and dependent loads.
 #include "tree_device.cuh"
 
@@ -23,7 +24,7 @@ constexpr int kMThreads = 256, kMRowsAt = 256, kMCopies = 8;
 // larger weight, larger number; NaN is less than any
 __device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : ord32(w); }
 
-// A block per (layer, sequence, key head), the last counting fastest.  A row of up to `room` weights is read once, into shared memory.
+// A block per (layer, sequence, key head), the last counting fastest.  A row of up to `room` weights is read once, into shared memory; a longer one by every pass.
 template <int NT>
 __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int room) {
     constexpr int warps = NT / 32;
@@ -48,15 +49,40 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
         }
         return;
     }
-    if (L <= room) {
-#pragma unroll 8
-        for (int i = tid; i < L; i += NT) held[i] = w[i];
-        w = held;
-        __syncthreads();
-    }
     const int old = L - min(a.e.recent, keep);               // places that have to earn it
     int m = keep - (L - old);                              // how many of them stay: less than there are
     uint32_t bar = 0xffffffffu;
+    // Counts a digit (of all lanes that are `in`).  A warp counts those with its first one's digit together: rows whose weights are alike, or nothing, would
+    // wait for one another's additions.
+    const auto count = [&](bool in, uint32_t mine) {
+        const uint32_t who = __ballot_sync(kFullMask, in);
+        if (who == 0) return;
+        const int leader = __ffs(who) - 1;
+        const uint32_t leaders = __shfl_sync(kFullMask, mine, leader);       // (by all lanes)
+        const bool same = in && mine == leaders;
+        const uint32_t together = __ballot_sync(kFullMask, same);
+        if (lane == leader) atomicAdd(&bins[mine], (uint32_t)__popc(together));
+        else if (in && !same) atomicAdd(&bins[mine], 1u);
+    };
+    const bool fits = L <= room;
+    if (fits) {                                            // with the first digits counted on the way
+        for (int i = tid; i < kEBins; i += NT) bins[i] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i0 = 0; i0 < L; i0 += 8 * NT) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = i0 + j * NT + tid < L ? w[i0 + j * NT + tid] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + j * NT + tid;
+                if (i0 + j * NT >= L) break;
+                if (i < L) held[i] = x[j];
+                count(i < old, weight_key(x[j]) >> 21);
+            }
+        }
+        w = held;
+    }
     if (m > 0) {
         uint32_t prefix = 0;                               // the digits found, and how many of those with them stay
         int shift = 32;
@@ -65,22 +91,15 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
             const int bits = pass == 2 ? 10 : 11;
             const uint32_t known = shift == 32 ? 0u : ~0u << shift;
             shift -= bits;
-            for (int i = tid; i < kEBins; i += NT) bins[i] = 0;
-            __syncthreads();
-            // (a warp counts those with its first one's digit together: rows whose weights are alike, or nothing, would wait for one another's additions)
+            if (pass > 0 || !fits) {
+                for (int i = tid; i < kEBins; i += NT) bins[i] = 0;
+                __syncthreads();
 #pragma unroll 4
-            for (int i0 = 0; i0 < old; i0 += NT) {
-                const int i = i0 + tid;
-                const uint32_t key = i < old ? weight_key(w[i]) : 0u;
-                const bool in = i < old && (key & known) == prefix;
-                const uint32_t mine = (key >> shift) & ((1u << bits) - 1u), who = __ballot_sync(kFullMask, in);
-                if (who == 0) continue;
-                const int leader = __ffs(who) - 1;
-                const uint32_t leaders = __shfl_sync(kFullMask, mine, leader);       // (by all lanes)
-                const bool same = in && mine == leaders;
-                const uint32_t together = __ballot_sync(kFullMask, same);
-                if (lane == leader) atomicAdd(&bins[mine], (uint32_t)__popc(together));
-                else if (in && !same) atomicAdd(&bins[mine], 1u);
+                for (int i0 = 0; i0 < old; i0 += NT) {
+                    const int i = i0 + tid;
+                    const uint32_t key = i < old ? weight_key(w[i]) : 0u;
+                    count(i < old && (key & known) == prefix, (key >> shift) & ((1u << bits) - 1u));
+                }
             }
             __syncthreads();
             // from the largest digit down: thread tid has bins per tid .. per tid + per - 1, counted from the top
@@ -130,28 +149,57 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
         }
         bar = prefix;
     }
-    // m of the keys at the bar stay, the first ones
+    // Those above the bar stay, and m of those at it, the first ones; then the last tokens.  As many places at a time as shared memory holds, a stretch of
+    // them to a warp, which first counts what stays of it.  (Where weights go over themselves, what is written lies in front of what has not been read.)
+    const bool none = bar == 0xffffffffu, nan_at = bar == 0u;           // (NaN is less than any)
+    const float at_least = none ? __int_as_float(0x7fc00000) : nan_at ? neg_inf() : unord32(bar), more = none ? at_least : nan_at ? neg_inf() : unord32(bar + 1u);
     int n_above = 0, n_at = 0;
 #pragma unroll 1
-    for (int i0 = 0; i0 < L; i0 += NT) {
-        const int i = i0 + tid;
-        const float x = i < L ? w[i] : 0.f;
-        const uint32_t key = weight_key(x);
-        const bool above = i < L && (i >= old || (bar != 0xffffffffu && key > bar)), at = i < old && bar != 0xffffffffu && key == bar;
-        const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at);
-        if (lane == 0) { sums[0][warp] = __popc(u); sums[1][warp] = __popc(e); }
-        __syncthreads();                                   // (and the weights of this batch have been read)
+    for (int at0 = 0; at0 < L; at0 += room) {
+        const int here = min(room, L - at0), choose = min(max(old - at0, 0), here);
+        const int stretch = (choose + 32 * warps - 1) / (32 * warps) * 32, lo = warp * stretch, hi = min(lo + stretch, choose);
+        __syncthreads();                                   // (the last ones have been written, the counts read)
+        if (!fits) {
+#pragma unroll 8
+            for (int i = tid; i < here; i += NT) held[i] = w[at0 + i];
+            __syncthreads();
+        }
+        int cu = 0, ce = 0;
+#pragma unroll 4
+        for (int i = lo + lane; i < hi; i += 32) {
+            const float x = held[i];
+            const bool above = x >= more;
+            cu += above;
+            ce += !above && (x >= at_least || nan_at);
+        }
+        cu = __reduce_add_sync(kFullMask, cu); ce = __reduce_add_sync(kFullMask, ce);
+        if (lane == 0) { sums[0][warp] = cu; sums[1][warp] = ce; }
+        __syncthreads();
         // the warps' counts: lane j has warp j's
-        const int cu = lane < warps ? sums[0][lane] : 0, ce = lane < warps ? sums[1][lane] : 0;
-        const int before_u = n_above + __reduce_add_sync(kFullMask, lane < warp ? cu : 0) + __popc(u & ((1u << lane) - 1u));
-        const int before_e = n_at + __reduce_add_sync(kFullMask, lane < warp ? ce : 0) + __popc(e & ((1u << lane) - 1u));
-        n_above += __reduce_add_sync(kFullMask, cu); n_at += __reduce_add_sync(kFullMask, ce);
-        if (above || (at && before_e < m)) {
-            const int to = before_u + min(before_e, m);
-            kept[to] = i;
+        const int all_u = lane < warps ? sums[0][lane] : 0, all_e = lane < warps ? sums[1][lane] : 0;
+        int before_u = n_above + __reduce_add_sync(kFullMask, lane < warp ? all_u : 0), before_e = n_at + __reduce_add_sync(kFullMask, lane < warp ? all_e : 0);
+        n_above += __reduce_add_sync(kFullMask, all_u); n_at += __reduce_add_sync(kFullMask, all_e);
+        const uint32_t below = (1u << lane) - 1u;
+#pragma unroll 2
+        for (int i0 = lo; i0 < hi; i0 += 32) {
+            const int i = i0 + lane;
+            const float x = i < hi ? held[i] : 0.f;
+            const bool above = i < hi && x >= more, at = i < hi && !above && (x >= at_least || nan_at);
+            const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at);
+            const int mine_e = before_e + __popc(e & below);
+            if (above || (at && mine_e < m)) {
+                const int to = before_u + __popc(u & below) + min(mine_e, m);
+                kept[to] = at0 + i;
+                out[to] = x;
+            }
+            before_u += __popc(u); before_e += __popc(e);
+        }
+        for (int i = choose + tid; i < here; i += NT) {    // (what is before them: all that stays of the others)
+            const int to = keep - L + at0 + i;
+            const float x = held[i];
+            kept[to] = at0 + i;
             out[to] = x;
         }
-        __syncthreads();
     }
     for (int i = n + tid; i < L; i += NT) out[i] = 0.f;
 }
@@ -237,7 +285,7 @@ cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches
     const unsigned rows_keep = (unsigned)(a.K * a.B * a.layers);
     const int room = a.ctx_cap < kEShared ? a.ctx_cap : kEShared;
     const size_t bytes = (size_t)room * sizeof(float);
-    // 512 rows of 1000 places: 29 us with 512 threads, 38 with 256; 128 rows of 4000 27.7 with 1024, 32.8 with 512; of 32768 51 and 64
+    // Both kernels, 512 rows of 1000 places: 26 us with 512 threads, 30 with 256, 31 with 1024; 256 rows of 4000 22 with 1024, 25 with 512
     cudaError_t e = a.ctx_cap <= 2048 ? launch_after(tree_keep_kernel<512>, dim3(rows_keep), dim3(512), bytes, st, a, room)
                                       : launch_after(tree_keep_kernel<1024>, dim3(rows_keep), dim3(1024), bytes, st, a, room);
     *launches += 1;
