@@ -7,9 +7,12 @@
 // keys tx, tx+16, ..; a key's sum goes over the rows of a thread, then over the 16 ty in their order, so no sum depends on
 // the order of anything.  The next tile's keys are on their way (cp.async; bf16, which is widened, comes through registers) while this one is
 // worked on, and the page numbers of the one after it.
+// Up to eight rows (a beam or one token, a query head to a key head): four or eight threads have a key, its dimensions in registers, and rows go by, so
+// that keys come out of shared memory once and not once for every two rows.
 //
-// Measured, fp32, five rows on 8 sequences of up to 1000 tokens, 16 heads of 64: 24 us for 27 MB; bound by loads from shared memory (five of the 16 rows
-// that a tile of products has are there).  Without the copies ahead 29.
+// Measured, fp32, 8 sequences of up to 1000 tokens, 16 heads of 64 (27 MB): one row 14 us, five 17 (24 by the way of many rows), 20 rows 27, 64 rows 35; five
+// rows of heads of 256 71 (101).  A tile's chain bounds few rows (some three tiles a block: page numbers, keys, products, sums), loads from shared
+// memory many.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -20,7 +23,7 @@ namespace dba {
 
 namespace {
 
-constexpr int kWThreads = 256, kWRows = 64;
+constexpr int kWThreads = 256, kWRows = 64, kWFew = 8;
 
 __device__ __forceinline__ float w_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }     // (within 2^-22)
 __device__ __forceinline__ void w_fma2(float2& a, float b0, float b1, float c0, float c1) {
@@ -35,7 +38,7 @@ template <int DP> struct WSmem {
     static constexpr int pitch = DP + 4;
     float q[kWRows][pitch];
     float k[2][kt][pitch];
-    float sum[16][kt];
+    float sum[16][kt];                 // of a key, by rows' threads; few rows: the first is all
     float lse[kWRows];                 // in powers of two; +inf: the row counts nothing
     int64_t row[2][kt];
     SpanShared span;
@@ -66,10 +69,11 @@ __device__ __forceinline__ void w_load(int D, const __nv_bfloat16* base, const i
     }
 }
 
-template <typename T, int DP>
+// FEW: up to kWFew rows to a key.
+template <typename T, int DP, bool FEW>
 __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) tree_weigh_kernel(const TreeWeigh a) {
     using S = WSmem<DP>;
-    constexpr int KT = S::kt, NK = KT / 16, VEC = 16 / (int)sizeof(T);
+    constexpr int KT = S::kt, NK = KT / 16, VEC = 16 / (int)sizeof(T), PT = kWThreads / KT, PV = DP / (4 * PT);
     extern __shared__ __align__(16) unsigned char wraw[];
     S& sm = *reinterpret_cast<S*>(wraw);
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, M = a.n * a.G;
@@ -176,18 +180,57 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
                         if (z != __int_as_float(0x7f800000)) sum[j] += w_ex2(fmaf(s[i][j].x + s[i][j].y, a.scale_log2e, -z));
                 }
             };
-            if (M - r0 <= 16) products(std::integral_constant<int, 1>{});
+            // few rows: PT threads have a key, whose dimensions stay in their registers while the rows go by.  Eight neighbours read 128 bytes of shared memory
+            // without a conflict (a row is 16 bytes longer than a multiple of 128, so four rows on it is 64 bytes further).
+            const auto few = [&]() {
+                const int in_key = tid % PT, key = PT == 8 ? tid / 8 : (tid >> 5) * 8 + ((tid >> 3) & 3) + (tid & 4);
+                float few_sum = 0.f;
+                float4 kv[PV];
+#pragma unroll
+                for (int c = 0; c < PV; ++c) kv[c] = *reinterpret_cast<const float4*>(&sm.k[buf][key][4 * (c * PT + in_key)]);
+#pragma unroll 1
+                for (int r = 0; r < M; r += PT) {     // PT rows: at last each thread has one of them
+                    float x[PT];
+#pragma unroll
+                    for (int i = 0; i < PT; ++i) {
+                        float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int c = 0; c < PV; ++c) {
+                            const float4 qv = *reinterpret_cast<const float4*>(&sm.q[r + i][4 * (c * PT + in_key)]);
+                            w_fma2(s, qv.x, qv.y, kv[c].x, kv[c].y);
+                            w_fma2(s, qv.z, qv.w, kv[c].z, kv[c].w);
+                        }
+                        x[i] = s.x + s.y;
+                    }
+#pragma unroll
+                    for (int o = PT / 2; o; o >>= 1)       // half of the rows stay, the other half's sums go to the thread that keeps those
+#pragma unroll
+                        for (int i = 0; i < o; ++i) {
+                            const float mine = in_key & o ? x[i + o] : x[i], other = in_key & o ? x[i] : x[i + o];
+                            x[i] = mine + __shfl_xor_sync(kFullMask, other, o);
+                        }
+                    const float z = sm.lse[r + in_key];
+                    if (z != __int_as_float(0x7f800000)) few_sum += w_ex2(fmaf(x[0], a.scale_log2e, -z));
+                }
+#pragma unroll
+                for (int o = PT / 2; o; o >>= 1) few_sum += __shfl_xor_sync(kFullMask, few_sum, o);
+                if (in_key == 0) sm.sum[0][key] = few_sum;
+            };
+            if constexpr (FEW) few();
+            else if (M - r0 <= 16) products(std::integral_constant<int, 1>{});
             else if (M - r0 <= 32) products(std::integral_constant<int, 2>{});
             else products(std::integral_constant<int, 4>{});
         }
+        if (!FEW)
 #pragma unroll
-        for (int j = 0; j < NK; ++j) sm.sum[ty][tx + 16 * j] = sum[j];
+            for (int j = 0; j < NK; ++j) sm.sum[ty][tx + 16 * j] = sum[j];
         __syncthreads();
         if (tid < KT) {
             if (tid < cur.count) {
-                float x = 0.f;
+                float x = sm.sum[0][tid];
+                if (!FEW)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x += sm.sum[i][tid];
+                    for (int i = 1; i < 16; ++i) x += sm.sum[i][tid];
                 if (sm.row[buf][tid] < 0) x = 0.f;
                 const int64_t at = (int64_t)cur.b * a.w_seq + (int64_t)cur.h * a.w_head + cur.p0 + tid;
                 a.out[at] = a.in ? fmaf(a.decay, a.in[at], x) : x;
@@ -202,11 +245,15 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
 template <typename T, int DP>
 cudaError_t configure_weigh() {
     static_assert((DP <= 64 ? 3 : DP <= 128 ? 2 : 1) * (sizeof(WSmem<DP>) + 1024) <= 228 * 1024, "blocks of the grid that an SM holds");
-    return cudaFuncSetAttribute(tree_weigh_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WSmem<DP>));
+    const cudaError_t e = cudaFuncSetAttribute(tree_weigh_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WSmem<DP>));
+    return e == cudaSuccess ? cudaFuncSetAttribute(tree_weigh_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WSmem<DP>)) : e;
 }
 template <typename T, int DP>
 cudaError_t launch_weigh(const TreeWeigh& a, int sm_count, cudaStream_t st) {
-    return launch_after(tree_weigh_kernel<T, DP>, dim3((DP <= 64 ? 3 : DP <= 128 ? 2 : 1) * sm_count), dim3(kWThreads), sizeof(WSmem<DP>), st, a);
+    const dim3 grid((DP <= 64 ? 3 : DP <= 128 ? 2 : 1) * sm_count);
+    // (fp32, 8 sequences of up to 1000 tokens, 16 heads of 64: five rows 20 us, as 16 rows 24; sixteen rows 24.6, as few 28)
+    return a.n * a.G <= kWFew ? launch_after(tree_weigh_kernel<T, DP, true>, grid, dim3(kWThreads), sizeof(WSmem<DP>), st, a)
+                              : launch_after(tree_weigh_kernel<T, DP, false>, grid, dim3(kWThreads), sizeof(WSmem<DP>), st, a);
 }
 
 }  // namespace

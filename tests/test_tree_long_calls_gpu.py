@@ -13,11 +13,12 @@ from tests.test_tree_gpu import DT, _cache, _tree, dba                          
 from tests.test_tree_long_gpu import _attend, _compare, _i32, _setup                    # noqa: E402
 
 
-@pytest.mark.parametrize("dtype,D,ps,rows", [("bf16", 64, 16, 3), ("bf16", 128, 5, 3), ("bf16", 128, 8, 50), ("bf16", 256, 16, 3), ("f32", 64, 16, 3), ("f32", 128, 7, 50)])
-def test_weights_of_keys_that_are_not_finite(dba, dtype, D, ps, rows):
+@pytest.mark.parametrize("dtype,D,ps,rows,G", [("bf16", 64, 16, 3, 6), ("bf16", 128, 5, 3, 6), ("bf16", 128, 8, 50, 6), ("bf16", 256, 16, 3, 6), ("bf16", 256, 16, 4, 2), ("f32", 64, 16, 3, 6),
+                                               ("f32", 128, 7, 50, 6), ("f32", 64, 16, 2, 1), ("f32", 64, 5, 4, 2), ("f32", 128, 7, 7, 1), ("f32", 256, 16, 2, 3), ("f32", 40, 9, 5, 1)])
+def test_weights_of_keys_that_are_not_finite(dba, dtype, D, ps, rows, G):
     """An infinite element of a key whose scores are -inf receives nothing, whatever rows that are closed or not there would make of it."""
     rng = torch.Generator().manual_seed(1)
-    B, K, G, n = 2, 2, 6, 150
+    B, K, n = 2, 2, 150
     k, v, table = _cache(rng, B, -(-n // ps), ps, K, D, dtype)
     q = torch.randn(B, rows, K * G, D, generator=rng).to(DT[dtype])
     q[..., 3] = -q[..., 3].abs() - 0.5                                  # all see a key with +inf there from the other side
