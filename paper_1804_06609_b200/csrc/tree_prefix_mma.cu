@@ -491,6 +491,10 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             } else if (sum == 0.f) f = 0.f;
             float w_own = 0.f, w_pre = 1.f, lse = 0.f;
             if (part < 0) write = prefix_join(own, ref, sum, &w_own, &w_pre, &lse) && write;
+            f *= w_pre; g *= w_pre;
+            // (of an item of one tile the second stream has no outputs: their place may hold anything, and 0 times it may be anything)
+            const bool lone = !two && pc.tile_end - pc.tile == 1;
+            const uint32_t o_mine = o_at + (lone ? 0 : s * DP), o_other = o_at + (lone ? 0 : (s ^ 1) * DP);
             const uint32_t rows_in = __ballot_sync(kFullMask, write);
             tc_after();
             float4 (*turn)[8] = sm.turn[warp];
@@ -498,17 +502,17 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             for (int c = c0; c < c1 && c < a.D; c += 32) {
                 uint32_t u[32];
                 float y[32];
-                tm_ld32(o_at + s * DP + c, u);
+                tm_ld32(o_mine + c, u);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) y[j] = f == 0.f ? 0.f : __uint_as_float(u[j]) * f;      // (where nothing was seen O may hold anything)
+                for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(u[j]) * f;
                 if (!two) {
-                    tm_ld32(o_at + (s ^ 1) * DP + c, u);
+                    tm_ld32(o_other + c, u);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) y[j] += g == 0.f ? 0.f : __uint_as_float(u[j]) * g;
+                    for (int j = 0; j < 32; ++j) y[j] = fmaf(__uint_as_float(u[j]), g, y[j]);
                 }
                 __syncwarp();                              // the last block of columns has been read
 #pragma unroll
-                for (int j = 0; j < 8; ++j) turn[lane][j ^ (lane & 7)] = make_float4(y[4 * j] * w_pre, y[4 * j + 1] * w_pre, y[4 * j + 2] * w_pre, y[4 * j + 3] * w_pre);
+                for (int j = 0; j < 8; ++j) turn[lane][j ^ (lane & 7)] = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
                 __syncwarp();
                 if (part >= 0) {
                     const int col = c + (lane & 7) * 4;
