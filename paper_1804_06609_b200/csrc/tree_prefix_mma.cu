@@ -23,7 +23,7 @@
 // Measured: beams of 20 on 64 sentences, 32 heads over 8 of 128, 6007 tokens (126 GFLOP, 40960 rows) 124 us beside 30 of the rows' own part: 1.0
 // PFLOP/s, 62 % of the rate of a large matrix product.  What bounds it is the softmax: a tile of 128 keys takes a stream's warps some 3500 cycles, of
 // which exponentials, sums and packing 2000, and the tensor cores, at 50 to 60 %, wait for them.  Eight rows on 100003 tokens (205 MB): 54 us,
-// 3.8 TB/s.  Both sides of what was chosen, the document's call in us: half tiles 157, whole ones 170; a quarter of the exponentials as
+// of which the main loop 29, at HBM's rate.  Both sides of what was chosen, the document's call in us: half tiles 157, whole ones 170; a quarter of the exponentials as
 // polynomials 157, none 162, half of them 164; the first queries by one warp 156, by eight 154; the few rows' call with boxes 73, with cp.async 92.
 #include <cuda_bf16.h>
 
