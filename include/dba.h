@@ -474,6 +474,7 @@ typedef struct {
  * prefix, context and the arena slots of its mask; lse likewise.  The prefix is read once for all rows of its sequences (once for 256
  * of them on the tensor cores) and not once for each sequence.  A row's two parts, what is its own and the prefix, are joined by their
  * log-sum-exps; its own part is rounded to the output's type before (half a unit of its share; the prefix' part and fp32 are not).
+ * A score of NaN or +inf with a key of the prefix makes NaN of its row's output and log-sum-exp; a key whose score is -inf counts nothing.
  * query->out must not overlap query->q.  scratch_dev: dba_tree_shared_bytes, 256-byte aligned, used until the call's work is done.  Calls that follow one another on the handle's
  * stream may have the same; calls (or replays of graphs they were recorded into) that can overlap may not, nor may they the handle.
  * Limits: groups <= 2^20, max_pages * page_size < 2^31, B * rows * heads < 2^31 (the configuration's); else DBA_ERR_UNSUPPORTED.

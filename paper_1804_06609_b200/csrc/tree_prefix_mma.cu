@@ -63,7 +63,8 @@ template <int DP, bool TMA> struct XSmem {
     };
 };
 constexpr uint32_t kXNoRow = 0xffffffffu;
-__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+// NaN where one of them is
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // (x, y) = (a0, a1) * b + (c0, c1), and (x, y) = (x, y) * (a0, a1) + c
 __device__ __forceinline__ void fma2v(float& x, float& y, float a0, float a1, float b, float c0, float c1) {
     asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %6};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
@@ -75,7 +76,8 @@ __device__ __forceinline__ void fma2v2(float& x, float& y, float a0, float a1, f
 }
 // 2^x of two numbers on the fused multiply-add pipes, x up to some 2^7: the whole number next to x by adding and taking away 1.5 2^23, a polynomial of
 // degree 4 for the rest f in -1/2 .. 1/2 (least largest relative error, fitted by reweighted least squares with 1 at 0: 2.9e-6), the whole
-// number into the exponent.  Below -126 it goes to 0 through subnormals, and is 0 from -127 on.
+// number into the exponent.  Below -126 it goes to 0 through subnormals, and is 0 from -127 on.  NaN gives 0 too: the softmax sees to it that a row with such
+// a score has a reference of NaN, and with it the exponentials beside these.
 __device__ __forceinline__ void ex2_pair(float& x, float& y) {
     float tx = fmaxf(x, -127.f), ty = fmaxf(y, -127.f), fx = tx, fy = ty, nx, ny, px, py;
     add2(tx, ty, 12582912.f, 12582912.f);
@@ -399,11 +401,14 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
                         m0 = max3(m0, __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
                         m1 = max3(m1, __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]));
                     }
-                    const float top = fmaxf(m0, m1) * scale;
-                    const bool raise = top > (ref == neg_inf() ? ref : ref + kRaise);
+                    const float top = max3(m0, m1, m1) * scale;
+                    const bool raise = !(top <= (ref == neg_inf() ? ref : ref + kRaise));
                     if (__any_sync(kFullMask, raise)) {
                         const float factor = raise ? ex2(ref - top) : 1.f;         // 0 where nothing has been seen before
-                        if (raise) { ref = top; sum *= factor; }
+                        if (raise) {           // (a score of NaN or +inf makes NaN of the sum, which it stays, and so of the row)
+                            ref = top < -neg_inf() ? top : __int_as_float(0x7fc00000);
+                            sum *= factor;
+                        }
                         if (t > first || h) {
                             // the outputs before this half (those before them came before these scores, so the parity cannot be an older phase's)
                             if (!mbar_wait(msmem_u32(&sm.pv_done[s]), (2 * steps + h - 1) & 1u, abort_flag, limit)) { ok = false; break; }
