@@ -265,13 +265,19 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
         const uint32_t s_full = msmem_u32(&sm.s_full[s][0]), p_ready = msmem_u32(&sm.p_ready[s][0]), pv_done = msmem_u32(&sm.pv_done[s]);
         const uint64_t k_desc = sw128_desc(msmem_u32(sm.kv), 16), v_desc = sw128_desc(msmem_u32(sm.kv), kXKeys * 128);
         uint32_t done = 0;                                 // outputs issued
-        bool ok = true;
+        bool ok = true, shared_before = false;             // the last piece's tiles went to the two streams in turn
         while (ok && XCut::next(a, run, &pc)) {
             const bool two = pc.rows > 128;
             const int tiles = pc.tile_end - pc.tile, by = two ? 1 : 2, n = two ? tiles : (tiles + 1 - s) / 2;
             const uint32_t qb = (uint32_t)piece % C::q_bufs;
             if (!(ok = mbar_wait(msmem_u32(&sm.q_full[qb]), ((uint32_t)piece / C::q_bufs) & 1u, abort_flag, limit))) break;
             if (piece == 0 && !(ok = mbar_wait(msmem_u32(&sm.q_first), 0, abort_flag, limit))) break;
+            // A stage's wait tells a phase from the one before it alone, so what was there before has to have come.  This stream has waited for its own tiles; the
+            // other one's keys of the last piece have come when its scores are done (one buffer of queries: their wait has shown it), and all the rest
+            // before this piece by the wait for the outputs' place below.
+            if (C::q_bufs > 1 && shared_before &&
+                !(ok = mbar_wait(msmem_u32(&sm.q_empty[(uint32_t)(piece - 1) % C::q_bufs]), ((uint32_t)(piece - 1) / C::q_bufs) & 1u, abort_flag, limit))) break;
+            shared_before = !two;
             const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]) + (two ? s * C::q_half : 0), 16);
             // rows of this stream's last tile behind the prefix' end
             const int n_tail = pc.tile_end == pc.tiles && (pc.tiles - 1 - pc.tile) % by == (two ? 0 : s) ? pc.tiles * kXKeys - pc.len : 0;
@@ -280,8 +286,8 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             for (int g = n ? -1 : 0; g < n; ++g) {
                 const uint32_t v_stage = v_copy % C::stages, k_stage = k_copy % C::stages;
                 const uint64_t dv = v_desc + (uint64_t)(v_stage * (C::tile_bytes / 16)), dk = k_desc + (uint64_t)(k_stage * (C::tile_bytes / 16));
-                if (g >= 0 && !(ok = mbar_wait(msmem_u32(&sm.full[v_stage]), (v_copy / C::stages) & 1u, abort_flag, limit))) break;
                 if (g == 0 && piece > 0 && !(ok = mbar_wait(msmem_u32(&sm.o_free), (piece - 1) & 1, abort_flag, limit))) break;      // (the outputs' place)
+                if (g >= 0 && !(ok = mbar_wait(msmem_u32(&sm.full[v_stage]), (v_copy / C::stages) & 1u, abort_flag, limit))) break;
                 // the scores of half a tile, over the probabilities of the same half of the one before
                 const auto scores = [&](int h) {
                     if (elect_one()) {
