@@ -496,7 +496,9 @@ typedef struct {
 
 /*
  * dba_tree_append for decoders that norm every head's queries and keys before the rotation:  x <- x / sqrt(mean(x^2) + eps) * weight over
- * the head's dimensions, then the rotation, then the cache (keys) or q_out (queries): one pass, in fp32, rounded once at the end.
+ * the head's dimensions, then the rotation, then the cache (keys) or q_out (queries): one pass, in fp32, rounded once at the end.  Dimensions that
+ * are not rotated (or all, of tokens without a position) are the side's own without a norm: copies, bit for bit.  Without any norm, and an offset, it
+ * is dba_tree_append at the moved positions.
  */
 dba_status dba_tree_append_norm(dba_tree* h, const dba_tree_tokens* tokens, const dba_tree_norm* norm, const dba_kv_cache* cache,
                                 const int32_t* table_dev, int64_t table_stride);

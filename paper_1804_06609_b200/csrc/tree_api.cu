@@ -194,7 +194,7 @@ dba_status dba_tree_append(dba_tree* h, const dba_tree_tokens* t, const dba_kv_c
     dba_tree_tokens tt;
     if ((st = check_tokens(h, t, &tt)) != DBA_OK) return st;
     int n = 0;
-    const cudaError_t e = launch_tree_append(tt, pg, cache->k, cache->v, h->c.B, h->c.heads, h->c.kv_heads, h->c.head_dim, h->c.dtype, h->stream, &n);
+    const cudaError_t e = launch_tree_append(tt, nullptr, pg, cache->k, cache->v, h->c.B, h->c.heads, h->c.kv_heads, h->c.head_dim, h->c.dtype, h->stream, &n);
     h->launches += n;
     return launched(e);
 }

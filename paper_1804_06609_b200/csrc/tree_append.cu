@@ -22,9 +22,9 @@ __device__ __forceinline__ void tree_narrow(float v, __nv_bfloat16* x) { *x = __
 
 // A block per token.  A rotated head is cut into rot/2/VEC units of two packs (dimensions d.. and d + rot/2.., or 2 VEC
 // neighbouring ones) and (D - rot)/(2 VEC) units that are copied; a value head into D/(2 VEC) copied units.  A unit is
-// read whole before it is written, so q_out may be q.
+// read whole before it is written, so q_out may be q.  offset (may be null): of the sequences' positions.
 template <typename T, int VEC, bool PAIRS>
-__global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_tokens t, const TreePages pg, T* ck, T* cv, int B, int H, int K, int D) {
+__global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_tokens t, const int32_t* offset, const TreePages pg, T* ck, T* cv, int B, int H, int K, int D) {
     using P = TreePack<T, VEC>;
     grid_dependency_wait();
     allow_dependents();
@@ -37,6 +37,10 @@ __global__ void __launch_bounds__(kAThreads) tree_append_kernel(const dba_tree_t
         if (place >= 0) {
             row = tree_row(pg, b, place);
             if (row < 0 && threadIdx.x == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
+        }
+        if (offset && pos >= 0) {
+            const int64_t moved = (int64_t)pos + __ldg(offset + b);
+            pos = moved < 0 || moved > 0x7fffffff ? 0x7fffffff : (int)moved;           // (out of range, the one as the other)
         }
     } else if (threadIdx.x == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
     if (pos >= t.positions && t.cos) {
@@ -96,12 +100,62 @@ __device__ __forceinline__ void norm_fma2(float& x, float& y, float a0, float a1
         : "+f"(x), "+f"(y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
+// Whether a head is left to the end: the sum of its squares is not finite, or it is one without a norm and not rotated altogether (its zeros keep their sign).
+__device__ __forceinline__ bool norm_is_apart(float sum, bool normed, bool all_turned) { return !(sum < __int_as_float(0x7f800000)) || (!all_turned && !normed); }
+
+// The heads of a token that the kernel below leaves to the end: queries or keys, before which there are `before` others (a head's own lanes come back to
+// it).  f: the pairs' factors; turned: units that are rotated.  What is not rotated keeps to itself, whatever its neighbours hold, and without a norm it is a copy.
+template <typename T, int VEC, bool PAIRS>
+__device__ __noinline__ void norm_apart(const T* src, T* dst, int64_t src_head, int64_t dst_head, int before, int heads, const float* f, bool normed, float eps, int D, int lanes, int turned, int half) {
+    using P = TreePack<T, VEC>;
+    constexpr int to = kTreeMaxDim / 2;
+    const int per = D / (2 * VEC), sub = threadIdx.x / lanes, lane = threadIdx.x - sub * lanes, heads_at = blockDim.x / lanes;
+    const auto first = [&](int j) { return PAIRS || j >= half / VEC ? 2 * j * VEC : j * VEC; };
+    const auto second = [&](int j) { return j < half / VEC && !PAIRS ? j * VEC + half : first(j) + VEC; };
+    for (int h0 = -(before % heads_at); h0 < heads; h0 += heads_at) {
+        const int h = h0 + sub;
+        const bool in = h >= 0 && h < heads;
+        const T* const from = src + h * src_head;
+        float sum = 0.f, sum2 = 0.f;                       // (in the kernel's order, so that both see the same heads)
+        for (int j = lane; in && j < per; j += lanes) {
+            const P x = *reinterpret_cast<const P*>(from + first(j)), y = *reinterpret_cast<const P*>(from + second(j));
+#pragma unroll
+            for (int i = 0; i < 2 * VEC; i += 2) {
+                const float a = tree_widen(i < VEC ? x.x[i] : y.x[i - VEC]), b = tree_widen(i + 1 < VEC ? x.x[i + 1] : y.x[i + 1 - VEC]);
+                sum = fmaf(a, a, sum); sum2 = fmaf(b, b, sum2);
+            }
+        }
+        sum += sum2;
+        for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
+        if (!in || !norm_is_apart(sum, normed, turned == per)) continue;
+        const float r = normed ? rsqrtf(fmaf(sum, 1.f / (float)D, eps)) : 1.f;
+        for (int j = lane; j < per; j += lanes) {
+            const P x = *reinterpret_cast<const P*>(from + first(j)), y = *reinterpret_cast<const P*>(from + second(j));
+            P ya = x, yb = y;
+            const bool turn = j < turned;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                if (!turn && !normed) break;
+                const int ia = PAIRS ? 2 * i : i, ib = PAIRS ? 2 * i + 1 : VEC + i;
+                const float a = tree_widen(ia < VEC ? x.x[ia] : y.x[ia - VEC]), b = tree_widen(ib < VEC ? x.x[ib] : y.x[ib - VEC]), *g = f + j * VEC + i;
+                const float va = r * (turn ? fmaf(a, g[0], b * g[to]) : a * g[0]), vb = r * (turn ? fmaf(b, g[2 * to], a * g[3 * to]) : b * g[2 * to]);
+                tree_narrow(va, ia < VEC ? &ya.x[ia] : &yb.x[ia - VEC]);
+                tree_narrow(vb, ib < VEC ? &ya.x[ib] : &yb.x[ib - VEC]);
+            }
+            *reinterpret_cast<P*>(dst + h * dst_head + first(j)) = ya;
+            *reinterpret_cast<P*>(dst + h * dst_head + second(j)) = yb;
+        }
+    }
+}
+
 // The same for decoders that norm queries and keys: y = x / sqrt(mean(x^2) + eps) * weight per head, then the rotation.  A block per token;
 // a head is the work of `lanes` lanes next to one another (the power of two from D/(2 VEC) up, 32 at most), each with UNITS units of
 // it.  With r the root's inverse, a pair of dimensions (a, b) becomes
 //     y_a = r (x_a w_a cos - x_b w_b sin),  y_b = r (x_b w_b cos + x_a w_a sin),
 // whose four products of weights and cosines are the same for all heads of a kind: they are made once a token, in shared memory.  All of it is fp32; the
-// one rounding is the store's.
+// one rounding is the store's.  Dimensions that are not rotated go the same way with a sine of 0, but not in heads where that would show: those are left to the
+// end (norm_is_apart; with a branch for them in the loop the prompt below takes 9 % longer, with this no longer; one with half of its dimensions rotated and
+// queries alone normed 100 us where 85 were without).  Without any norm an offset alone is left, and that is tree_append_kernel's (65 us, 77 by this kernel).
 //
 // Measured: 8 x 2039 tokens, 32 + 2 x 8 heads of 128 (402 MB): 78 us, 5.2 TB/s, 79 % of the rate of a copy; bound by the chain of a head (load, sum over its
 // lanes, store: issue 58 %, 9 cycles of stalls on loads for an instruction).  The next head's loads ahead, or a warp to a token: 97 to 148 us.  16 x 20
@@ -111,6 +165,7 @@ __global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_ap
                                                                                                 T* cv, int B, int H, int K, int D, int lanes) {
     using P = TreePack<T, VEC>;
     __shared__ alignas(16) float factor[2][4][kTreeMaxDim / 2];        // of queries, of keys: x_a to y_a, x_b to y_a, x_b to y_b, x_a to y_b, by pair
+    __shared__ int turned_here;                            // units of a head that are rotated (read again at the end: the loop has no register for it)
     grid_dependency_wait();
     allow_dependents();
     const int tok = blockIdx.x, tid = threadIdx.x;
@@ -133,6 +188,7 @@ __global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_ap
     if (pos >= t.positions) { bad = bad || t.cos; pos = -1; }
     if (bad && tid == 0) atomicOr(pg.status, (uint32_t)DBA_TREE_BAD_INDEX);
     const int half = t.rot_dim / 2, turned = half / VEC;
+    if (tid == 0) turned_here = pos >= 0 ? turned : 0;
     for (int i = tid; i < D; i += NT) {
         const int side = i >= D / 2, p = i - side * (D / 2), j = p / VEC;
         // the pair's dimensions: of unit j, element p % VEC of either pack, or two neighbours
@@ -156,6 +212,8 @@ __global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_ap
     // heads: the queries' (where there are any), then the keys'
     const int q_heads = t.q ? H : 0, n = q_heads + (row >= 0 ? K : 0);
     const float inv_d = 1.f / (float)D;
+    const bool all_turned = pos >= 0 && turned == per;
+    bool left = false;                                     // heads of these lanes, to the end
 #pragma unroll 1
     for (int h0 = 0; h0 < n; h0 += heads_at) {
         const int h = h0 + sub;
@@ -176,9 +234,11 @@ __global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_ap
         for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
         const float r = (is_q ? nm.q_weight : nm.k_weight) ? rsqrtf(fmaf(sum, inv_d, nm.eps)) : 1.f;
         T* const dst = is_q ? (T*)t.q_out + (int64_t)tok * t.qo_token_stride + (int64_t)h * t.qo_head_stride : ck + row + (int64_t)(h - q_heads) * pg.head_stride;
+        const bool apart = norm_is_apart(sum, (is_q ? nm.q_weight : nm.k_weight) != nullptr, all_turned);
+        left = left || apart;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            if (h >= n || d0[u] < 0) continue;
+            if (h >= n || d0[u] < 0 || apart) continue;
             const float* const f = factor[is_q ? 0 : 1][0] + (lane + u * lanes) * VEC;
             constexpr int to = kTreeMaxDim / 2;            // the next of the four
             P ya, yb;
@@ -208,6 +268,15 @@ __global__ void __launch_bounds__(NT, UNITS > 1 ? 1 : NT == 64 ? 22 : 8) tree_ap
             *reinterpret_cast<P*>(dst + d0[u]) = ya;
             *reinterpret_cast<P*>(dst + d1[u]) = yb;
         }
+    }
+    if (__any_sync(kFullMask, left)) {
+        const int at = *(volatile int*)&turned_here, tok0 = blockIdx.x;
+        if (t.q)
+            norm_apart<T, VEC, PAIRS>((const T*)t.q + (int64_t)tok0 * t.q_token_stride, (T*)t.q_out + (int64_t)tok0 * t.qo_token_stride, t.q_head_stride, t.qo_head_stride, 0, H,
+                                      factor[0][0], nm.q_weight != nullptr, nm.eps, D, lanes, at, t.rot_dim / 2);
+        if (row >= 0)
+            norm_apart<T, VEC, PAIRS>((const T*)t.k + (int64_t)tok0 * t.k_token_stride, ck + row, t.k_head_stride, pg.head_stride, t.q ? H : 0, K, factor[1][0], nm.k_weight != nullptr, nm.eps, D,
+                                      lanes, at, t.rot_dim / 2);
     }
     if (row < 0) return;
     const int chunks = D * (int)sizeof(T) / 16;
@@ -265,17 +334,17 @@ __global__ void __launch_bounds__(kCThreads) tree_commit_kernel(const TreePages 
 }
 
 template <typename T, int VEC>
-cudaError_t launch_append_v(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, cudaStream_t st) {
+cudaError_t launch_append_v(const dba_tree_tokens& t, const int32_t* offset, const TreePages& pg, void* k, void* v, int B, int H, int K, int D, cudaStream_t st) {
     // Blocks of 64 threads once their number fills the machine several times over (8 x 2039 tokens of 48 heads of 128: 65.0
     // us, 128 threads 67.5, 256 81), of 128 before, where a block's own loop is what takes time (16 x 20 tokens: 4.8, 3.8, 3.6).
     const int threads = t.N >= 2048 ? 64 : kAThreads;
-    return t.pairs ? launch_after(tree_append_kernel<T, VEC, true>, dim3(t.N), dim3(threads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D)
-                   : launch_after(tree_append_kernel<T, VEC, false>, dim3(t.N), dim3(threads), 0, st, t, pg, (T*)k, (T*)v, B, H, K, D);
+    return t.pairs ? launch_after(tree_append_kernel<T, VEC, true>, dim3(t.N), dim3(threads), 0, st, t, offset, pg, (T*)k, (T*)v, B, H, K, D)
+                   : launch_after(tree_append_kernel<T, VEC, false>, dim3(t.N), dim3(threads), 0, st, t, offset, pg, (T*)k, (T*)v, B, H, K, D);
 }
 
 }  // namespace
 
-cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K, int32_t D,
+cudaError_t launch_tree_append(const dba_tree_tokens& t, const int32_t* offset, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K, int32_t D,
                                int dtype, cudaStream_t st, int* launches) {
     *launches += 1;
     // packs of 16 bytes where the two halves of a rotated head and what is left of it are whole numbers of them, else
@@ -284,12 +353,12 @@ cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, vo
     int vec = dtype == DBA_F32 ? 4 : 8;
     while (half % vec || rest % vec) vec >>= 1;
     if (dtype == DBA_F32)
-        return vec == 4 ? launch_append_v<float, 4>(t, pg, k, v, B, H, K, D, st) : vec == 2 ? launch_append_v<float, 2>(t, pg, k, v, B, H, K, D, st)
-                                                                                              : launch_append_v<float, 1>(t, pg, k, v, B, H, K, D, st);
-    return vec == 8   ? launch_append_v<__nv_bfloat16, 8>(t, pg, k, v, B, H, K, D, st)
-           : vec == 4 ? launch_append_v<__nv_bfloat16, 4>(t, pg, k, v, B, H, K, D, st)
-           : vec == 2 ? launch_append_v<__nv_bfloat16, 2>(t, pg, k, v, B, H, K, D, st)
-                      : launch_append_v<__nv_bfloat16, 1>(t, pg, k, v, B, H, K, D, st);
+        return vec == 4 ? launch_append_v<float, 4>(t, offset, pg, k, v, B, H, K, D, st) : vec == 2 ? launch_append_v<float, 2>(t, offset, pg, k, v, B, H, K, D, st)
+                                                                                              : launch_append_v<float, 1>(t, offset, pg, k, v, B, H, K, D, st);
+    return vec == 8   ? launch_append_v<__nv_bfloat16, 8>(t, offset, pg, k, v, B, H, K, D, st)
+           : vec == 4 ? launch_append_v<__nv_bfloat16, 4>(t, offset, pg, k, v, B, H, K, D, st)
+           : vec == 2 ? launch_append_v<__nv_bfloat16, 2>(t, offset, pg, k, v, B, H, K, D, st)
+                      : launch_append_v<__nv_bfloat16, 1>(t, offset, pg, k, v, B, H, K, D, st);
 }
 
 namespace {
@@ -317,6 +386,7 @@ cudaError_t launch_norm_v(const dba_tree_tokens& t, const dba_tree_norm& nm, con
 
 cudaError_t launch_tree_append_norm(const dba_tree_tokens& t, const dba_tree_norm& norm, const TreePages& pg, void* k, void* v, int32_t B, int32_t H,
                                     int32_t K, int32_t D, int dtype, cudaStream_t st, int* launches) {
+    if (!norm.q_weight && !norm.k_weight) return launch_tree_append(t, norm.offset, pg, k, v, B, H, K, D, dtype, st, launches);
     *launches += 1;
     const int half = t.rot_dim / 2, rest = (D - t.rot_dim) / 2;       // (packs as above)
     int vec = dtype == DBA_F32 ? 4 : 8;

@@ -63,7 +63,7 @@ void tree_mma_plan(int M, int K, int D, int sm_count, TreeAttendPlan* p);
 cudaError_t configure_tree_mma();
 cudaError_t launch_tree_mma(const TreeAttend& a, int rows, int grid, cudaStream_t st);
 cudaError_t launch_tree_attend(TreeAttend a, const TreeAttendPlan& plan, int dtype, cudaStream_t st, int* launches);
-cudaError_t launch_tree_append(const dba_tree_tokens& t, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K,
+cudaError_t launch_tree_append(const dba_tree_tokens& t, const int32_t* offset, const TreePages& pg, void* k, void* v, int32_t B, int32_t H, int32_t K,
                                int32_t D, int dtype, cudaStream_t st, int* launches);
 cudaError_t launch_tree_commit(const dba_kv_cache& c, const TreePages& pg, int32_t B, int32_t K, int32_t D, int32_t A, int dtype,
                                const int32_t* ctx_len, const int32_t* src, const int32_t* n, cudaStream_t st, int* launches);
