@@ -522,13 +522,16 @@ dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float*
  * keeps its tokens.  Keys carry their rotation with them, so what is kept goes on having its position.
  *   to_table: where what is kept goes: the sequence's own table (in place), or one whose entries are each either the own table's
  *   entry at the same index or a page that no table of this call names otherwise.  In place the copies of a (layer, sequence, key head)
- *   are made one after the other by one thread block; to other pages they spread over the machine.
+ *   are made one after the other by one thread block, and so they are where any page with one of the context's first `keep` places stays; to
+ *   other pages they spread over the machine.  Arena slots (0 .. A - 1) whose page has another entry in to_table are copied along, so that an
+ *   open tree goes on from there; entries of the arena that are the own table's cost nothing.
  *   Of the pages that hold the first A + keep places none may be another sequence's too where it is written.
  *   weight, weight_out: [layers, B, kv_heads] rows, layer_stride, seq_stride and head_stride apart (alike in both); may be the same.
  *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0.
  *   kept: scratch and result, [layers, B, kv_heads, keep]: the old context places of what is kept, -1 beyond.
  *   ctx_len_out, dropped: [B] optional: the new length, and the old less the new.  (ctx_len_out may be ctx_len.)
- * 0 <= recent <= keep, keep >= 1.  A place on a page outside the cache is not copied (DBA_TREE_BAD_PAGE).
+ * 0 <= recent <= keep, keep >= 1.  A place on a page outside the cache is not copied (context: DBA_TREE_BAD_PAGE; an
+ * arena slot without a page is not reported).
  */
 typedef struct {
     const float* weight;

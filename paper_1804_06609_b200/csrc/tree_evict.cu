@@ -6,7 +6,8 @@
 // and then keeps, what is above it and the first ones at it, in order, a stretch of the row to a warp.  Everything is decided by counts, so equal inputs give equal results.
 //
 // Copies: row i of what is kept comes from place kept[i] >= i.  Other pages: any order.  The same pages: rows in ascending order, each
-// batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.
+// batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.  Arena slots whose
+// page is another one in the new table go there too: nobody else writes or reads there.
 //
 // Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: the choice 33 us (128 rows, a block each, of up to 130 KB
 // of weights: the passes one after the other; 45 with the last one all over the row between barriers and the first digits counted after the load),
@@ -223,33 +224,24 @@ __global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a,
         if (a.e.dropped) a.e.dropped[b] = L - min(L, keep);
         if (a.e.ctx_len_out) a.e.ctx_len_out[b] = min(L, keep);
     }
-    // pages that stay the same: one block, in order
+    // context pages that stay the same: one block, in order; arena pages that do not
     const unsigned first_page = tree_page(a.from, (unsigned)a.A), pages = tree_page(a.from, (unsigned)(a.A + min(keep, a.ctx_cap) - 1)) + 1;
-    bool same = false;
-    for (unsigned i = first_page + tid; i < pages; i += kMThreads)
-        same = same || __ldg(a.to.table + (int64_t)b * a.to.table_stride + i) == __ldg(a.from.table + (int64_t)b * a.from.table_stride + i);
+    const unsigned arena_pages = a.A ? tree_page(a.from, (unsigned)(a.A - 1)) + 1 : 0;
+    bool same = false, moved = false;
+    for (unsigned i = (a.A ? 0 : first_page) + tid; i < pages; i += kMThreads) {
+        const bool alike = __ldg(a.to.table + (int64_t)b * a.to.table_stride + i) == __ldg(a.from.table + (int64_t)b * a.from.table_stride + i);
+        same = same || (alike && i >= first_page);
+        moved = moved || (!alike && i < arena_pages);
+    }
     same = __syncthreads_or(same);
+    if (a.A) moved = __syncthreads_or(moved);
     if (same && split > 0) return;
     const int chunks = a.D * a.es / 16;
     const int32_t* kept = a.e.kept + (((int64_t)l * a.B + b) * a.K + h) * keep;
     char* base = (values ? a.v : a.k) + l * a.layer_bytes + (int64_t)h * a.from.head_stride * a.es;
     const int step = same ? kMRowsAt : kMRowsAt * splits;
-    for (int i0 = split * kMRowsAt; i0 < keep; i0 += step) {
-        const int rows = min(kMRowsAt, keep - i0);
-        __syncthreads();
-        bool any = false;
-        if (tid < rows) {
-            const int src = __ldg(kept + i0 + tid);
-            int64_t r0 = -1, r1 = -1;
-            if (src >= 0) {
-                r0 = tree_row(a.from, b, a.A + src);
-                r1 = tree_row(a.to, b, a.A + i0 + tid);
-                any = true;
-            }
-            const bool skip = r0 < 0 || r1 < 0 || r0 == r1;
-            from_at[tid] = skip ? -1 : r0 * a.es; to_at[tid] = r1 * a.es;
-        }
-        if (!__syncthreads_or(any)) break;                 // (what is kept is at the front)
+    // `rows` of them from from_at (-1: none) to to_at
+    const auto copy = [&](int rows) {
         const int units = rows * chunks;
         for (int u0 = 0; u0 < units; u0 += kMCopies * kMThreads) {
             uint4 x[kMCopies];
@@ -271,6 +263,37 @@ __global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a,
             for (int c = 0; c < kMCopies; ++c)
                 if (to[c]) *reinterpret_cast<uint4*>(to[c]) = x[c];
         }
+    };
+    for (int i0 = split * kMRowsAt; i0 < keep; i0 += step) {
+        const int rows = min(kMRowsAt, keep - i0);
+        __syncthreads();
+        bool any = false;
+        if (tid < rows) {
+            const int src = __ldg(kept + i0 + tid);
+            int64_t r0 = -1, r1 = -1;
+            if (src >= 0) {
+                r0 = tree_row(a.from, b, a.A + src);
+                r1 = tree_row(a.to, b, a.A + i0 + tid);
+                any = true;
+            }
+            const bool skip = r0 < 0 || r1 < 0 || r0 == r1;
+            from_at[tid] = skip ? -1 : r0 * a.es; to_at[tid] = r1 * a.es;
+        }
+        if (!__syncthreads_or(any)) break;                 // (what is kept is at the front)
+        copy(rows);
+    }
+    if (!moved) return;
+    for (int i0 = split * kMRowsAt; i0 < a.A; i0 += step) {
+        const int rows = min(kMRowsAt, a.A - i0);
+        __syncthreads();
+        if (tid < rows) {
+            const auto quiet = [] { return false; };       // (whether a slot is in use is not known here)
+            const int64_t r0 = tree_row(a.from, b, i0 + tid, quiet), r1 = tree_row(a.to, b, i0 + tid, quiet);
+            const bool skip = r0 < 0 || r1 < 0 || r0 == r1;
+            from_at[tid] = skip ? -1 : r0 * a.es; to_at[tid] = r1 * a.es;
+        }
+        __syncthreads();
+        copy(rows);
     }
 }
 

@@ -371,7 +371,7 @@ class TokenTree:
     def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None):
         """Keeps `keep` tokens of every longer context: the last `recent` and, of the others, those of the largest weight, in their order,
         at the front.  weight [layers, B, kv_heads, context places] fp32 (without layers where k, v have none).  table_out, weight_out:
-        where to; default the same, in place.  Returns a dict of ctx_len and dropped [B], kept [(layers,) B, kv_heads, keep] (the old context
+        where to; default the same, in place (arena slots go along where table_out has other pages for them).  Returns a dict of ctx_len and dropped [B], kept [(layers,) B, kv_heads, keep] (the old context
         places, -1 beyond) and weight (weight_out); the first three are one of two sets of the handle's own tensors, in turn.  See
         dba_tree_evict."""
         torch, B, layers = self.torch, self.B, k.shape[:-4]

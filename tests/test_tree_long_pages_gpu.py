@@ -1,0 +1,63 @@
+"""Eviction of context tokens to tables whose pages differ from the own ones in the arena too."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from tests import long_model as L                                                       # noqa: E402
+from tests.test_tree_gpu import DT, _cache, _tree, dba                                  # noqa: E402,F401
+from tests.test_tree_long_gpu import _i32                                               # noqa: E402
+
+
+def _arena(k, table, A, ps):
+    """The arena's rows [layers, B, A, heads, D]."""
+    p = torch.arange(A, device=k.device)
+    return k[:, table.long()[:, p // ps], p % ps]
+
+
+@pytest.mark.parametrize("dtype,D,ps,W,ctx,keep,changed", [
+    ("bf16", 64, 64, 1, [200, 90, 20], 50, "all"), ("bf16", 64, 64, 1, [200, 90, 20], 50, "last"),       # the arena ends inside a page
+    ("bf16", 128, 5, 2, [700, 0, 300], 290, "all"), ("bf16", 128, 5, 2, [700, 0, 300], 290, "some"),
+    ("f32", 64, 16, 9, [100, 100, 31], 31, "all"), ("bf16", 64, 16, 2, [300, 3, 290], 280, "some"), ("bf16", 80, 7, 1, [100, 50, 20], 40, "last")])
+def test_eviction_takes_arena_slots_along_where_their_pages_change(dba, dtype, D, ps, W, ctx, keep, changed):
+    rng = torch.Generator().manual_seed(ps)
+    layers, B, K, A = 2, len(ctx), 2, 32 * W
+    per, first = -(-(A + max(ctx)) // ps), A // ps
+    pages = 2 * B * per + 2
+    k, v = (torch.randn(layers, pages, ps, K, D, generator=rng).to(DT[dtype]).cuda() for _ in range(2))
+    order = torch.randperm(pages, generator=rng).int().cuda()
+    table, out = order[:B * per].view(B, per), order[B * per:2 * B * per].view(B, per).clone()
+    if changed == "last":                                       # of the arena's pages the one in which it ends
+        out[:, :first] = table[:, :first]
+    elif changed == "some":
+        out[:, 1::2] = table[:, 1::2]
+    tree = _tree(dba, B, 1, K, K, D, ps, per, W, dtype)
+    w = torch.rand(layers, B, K, per * ps - A, generator=rng).cuda()
+    old_k, old_v, old_w = k.clone(), v.clone(), w.clone()
+    got = tree.evict(k, v, table, _i32(ctx), w, keep, recent=3, table_out=out)
+    assert tree.status() == 0
+    assert torch.equal(_arena(k, out, A, ps), _arena(old_k, table, A, ps)) and torch.equal(_arena(v, out, A, ps), _arena(old_v, table, A, ps))
+    for layer in range(layers):
+        for b in range(B):
+            for h in range(K):
+                stay = L.keep(old_w[layer, b, h, :ctx[b]].tolist(), keep, 3)
+                assert got["kept"][layer, b, h].tolist() == stay + [-1] * (keep - len(stay))
+                src, dst = (torch.tensor(x, device="cuda", dtype=torch.long) + A for x in (stay, range(len(stay))))
+                for x, old in ((k, old_k), (v, old_v)):
+                    assert torch.equal(x[layer, out[b].long()[dst // ps], dst % ps, h], old[layer, table[b].long()[src // ps], src % ps, h])
+    # pages that neither table names are as they were
+    rest = order[2 * B * per:].long()
+    assert torch.equal(k[:, rest], old_k[:, rest]) and torch.equal(v[:, rest], old_v[:, rest])
+
+
+def test_arena_pages_outside_the_cache_are_nobodys_concern(dba):
+    """Whether slots are in use is not known to an eviction: those without a page are neither copied nor reported."""
+    rng = torch.Generator().manual_seed(1)
+    k, v, table = _cache(rng, 2, 8, 16, 2, 64, "bf16", spare=20)
+    tree = _tree(dba, 2, 1, 2, 2, 64, 16, 8, 1)
+    out = table.clone()
+    table[0, 0], out[0, 0], out[1, 0], out[1, 1] = -1, 5, -1, 1 << 30
+    old = k.clone()
+    tree.evict(k, v, table, _i32([20, 90]), torch.rand(2, 2, 96, generator=rng).cuda(), 90, table_out=out)
+    assert tree.status() == 0 and torch.equal(k, old)
