@@ -508,8 +508,9 @@ dba_status dba_tree_append_norm(dba_tree* h, const dba_tree_tokens* tokens, cons
  *     weight_out[b, kh, p] = decay * weight_in[b, kh, p] + sum exp(scale <q, k_p> - lse)     for p < ctx_len[b]
  * over the open rows of the sequence and the query heads of key head kh.  lse is dba_tree_attend's (or ..._shared's) of the same
  * queries; a row whose lse is -inf is closed and counts nothing, whatever its query holds.  query->out and query->lse are not used.
- * weight_in may be NULL (zeros) and may be weight_out; element (b, kh, p) at base + b * seq_stride + kh * head_stride + p (no stride of 0 but
- * for a dimension of one); places from ctx_len on are left as they are.  A place on a page outside the cache receives nothing.
+ * weight_in may be NULL (zeros) and may be weight_out; element (b, kh, p) at base + b * seq_stride + kh * head_stride + p.  Rows must not
+ * overlap below ctx_len (a stride of 0, but for a dimension of one, is refused; the lengths are on the device, so more is not looked at).
+ * Places from ctx_len on are left as they are.  A place on a page outside the cache receives nothing.
  */
 dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float* lse_dev, const dba_kv_cache* cache, const int32_t* table_dev,
                           int64_t table_stride, const int32_t* ctx_len_dev, const float* weight_in, float* weight_out, int64_t seq_stride,
@@ -526,7 +527,8 @@ dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float*
  *   other pages they spread over the machine.  Arena slots (0 .. A - 1) whose page has another entry in to_table are copied along, so that an
  *   open tree goes on from there; entries of the arena that are the own table's cost nothing.
  *   Of the pages that hold the first A + keep places none may be another sequence's too where it is written.
- *   weight, weight_out: [layers, B, kv_heads] rows, layer_stride, seq_stride and head_stride apart (alike in both); may be the same.
+ *   weight, weight_out: [layers, B, kv_heads] rows, layer_stride, seq_stride and head_stride apart (alike in both); may be the same.  As dba_tree_weigh's,
+ *   rows must not overlap.
  *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0.
  *   kept: scratch and result, [layers, B, kv_heads, keep]: the old context places of what is kept, -1 beyond.
  *   ctx_len_out, dropped: [B] optional: the new length, and the old less the new.  (ctx_len_out may be ctx_len.)

@@ -51,6 +51,22 @@ class TreeEvicted(C.Structure):
                 ("ctx_len_out", C.c_void_p), ("dropped", C.c_void_p)]
 
 
+def _rows_apart(shape, strides, places):
+    """Whether rows of so many places, the strides apart, have none in common.  (A stride of 0 is refused by the call.)"""
+    span, dims = places, sorted((s, n) for s, n in zip(strides, shape) if n > 1 and s)
+    for s, n in dims:
+        if s < span:
+            break
+        span += s * (n - 1)
+    else:
+        return True
+    at = [0]                                             # (not one within the other: rows may still lie between one another's)
+    for s, n in dims:
+        at = [a + s * i for a in at for i in range(n)]
+    at.sort()
+    return all(b - a >= places for a, b in zip(at, at[1:]))
+
+
 class TokenTree:
     """Owns a dba_tree handle and its workspace.  Caches, tables, masks and lengths are the caller's tensors:
     k, v [pages, page_size, kv_heads, head_dim] (any strides with a unit inner one; both alike; commit and evict: a leading layer
@@ -334,12 +350,19 @@ class TokenTree:
         if code:
             _check(code, "dba_tree_commit")
 
+    _rows_last = None          # strides and shape last found to keep the rows of weights apart
+
     # [B, kv_heads, places] (evict: layers in front) fp32 with a unit inner stride: at least the places a table leaves the context
     def _weights(self, w, lead, what):
         B, sh, s = self.B, w.shape, w.stride()
+        places = self.max_pages * self.page_size - 32 * self.words
         if (w.dtype is not self._f32t or w.get_device() != self._dev or len(sh) != len(lead) + 3 or sh[:-1] != (*lead, B, self.kv_heads)
-                or sh[-1] < self.max_pages * self.page_size - 32 * self.words or s[-1] != 1):
+                or sh[-1] < places or s[-1] != 1):
             raise ValueError(f"{what}: fp32 [{'layers, ' if lead else ''}B, kv_heads, context places], unit inner stride")
+        if (s, sh) != self._rows_last:
+            if not _rows_apart(sh[:-1], s[:-1], places):
+                raise ValueError(f"{what}: rows that do not overlap")
+            self._rows_last = (s, sh)
         return s
 
     def weigh(self, q, k, table, ctx_len, lse, weight=None, decay=1.0, scale=None, out=None):
