@@ -110,7 +110,6 @@ class TokenTree:
                     self._scratch_at = (self.scratch.data_ptr() + 255) // 256 * 256
         self._prefix, self._norm, self._evict = TreePrefix(), TreeNorm(), TreeEvicted()
         self._prefix_ref, self._norm_ref, self._evict_ref = (C.byref(x) for x in (self._prefix, self._norm, self._evict))
-        self._evicted = self._evicted_key = None
         self._next = [(x, self._next_struct(x)) for x in self._next]
         self._turn = 0
         self._f_append, self._f_attend, self._f_advance, self._f_commit = L.dba_tree_append, L.dba_tree_attend, L.dba_tree_advance, L.dba_tree_commit
@@ -391,13 +390,28 @@ class TokenTree:
             _check(code, "dba_tree_weigh")
         return out
 
+    _evicted = _evicted_key = _evict_lens = None
+    _evict_turn, _evict_own = 0, ()
+
+    # Two sets in turn, as advance's, for every number of tokens to keep out of the same memory.  What a larger number outgrows is held on to: a recorded call
+    # (CUDA graph) may go on writing there.
+    def _evict_sets(self, layers, keep):
+        torch, shape = self.torch, (*layers, self.B, self.kv_heads, keep)
+        size, room = math.prod(shape), self._evict_own[-1].shape[1] if self._evict_own else 0
+        with torch.cuda.stream(self.stream):             # (the allocator gives freed memory out by stream)
+            if self._evict_lens is None:
+                self._evict_lens = torch.empty(2, 2, self.B, dtype=self._i32t, device=self.device)
+            if size > room:
+                self._evict_own += (torch.empty(2, max(size, 2 * room), dtype=self._i32t, device=self.device),)
+        return [(*self._evict_lens[i], self._evict_own[-1][i, :size].view(shape)) for i in (0, 1)]
+
     def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None):
         """Keeps `keep` tokens of every longer context: the last `recent` and, of the others, those of the largest weight, in their order,
         at the front.  weight [layers, B, kv_heads, context places] fp32 (without layers where k, v have none).  table_out, weight_out:
         where to; default the same, in place (arena slots go along where table_out has other pages for them).  Returns a dict of ctx_len and dropped [B], kept [(layers,) B, kv_heads, keep] (the old context
         places, -1 beyond) and weight (weight_out); the first three are one of two sets of the handle's own tensors, in turn.  See
         dba_tree_evict."""
-        torch, B, layers = self.torch, self.B, k.shape[:-4]
+        B, layers = self.B, k.shape[:-4]
         if len(layers) > 1:
             raise ValueError("k and v: [pages, page_size, kv_heads, head_dim], or layers in front")
         if keep < 1 or not 0 <= recent <= keep:
@@ -410,12 +424,10 @@ class TokenTree:
         cache, n = self._cache(k, v, len(layers)), self._i32(ctx_len, B, "ctx_len: int32 [B]")
         stride, stride_out = self._table(table), self._table(table_out)
         key = (*layers, keep)
-        if key != self._evicted_key:                     # (two sets in turn, as advance's)
-            with torch.cuda.stream(self.stream):         # (the allocator gives freed memory out by stream)
-                lens, kept = torch.empty(2, 2, B, dtype=self._i32t, device=self.device), torch.empty(2, *layers, B, self.kv_heads, keep, dtype=self._i32t, device=self.device)
-            self._evicted, self._evicted_key = [(lens[i, 0], lens[i, 1], kept[i]) for i in (0, 1)], key
-        new_len, dropped, kept = self._evicted[0]
-        self._evicted.reverse()
+        if key != self._evicted_key:
+            self._evicted, self._evicted_key = self._evict_sets(layers, keep), key
+        new_len, dropped, kept = self._evicted[self._evict_turn]
+        self._evict_turn = 1 - self._evict_turn
         e = self._evict
         e.weight, e.weight_out, e.layer_stride, e.seq_stride, e.head_stride = weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2]
         e.keep, e.recent, e.to_table, e.to_table_stride = keep, recent, table_out.data_ptr(), stride_out

@@ -61,3 +61,31 @@ def test_arena_pages_outside_the_cache_are_nobodys_concern(dba):
     old = k.clone()
     tree.evict(k, v, table, _i32([20, 90]), torch.rand(2, 2, 96, generator=rng).cuda(), 90, table_out=out)
     assert tree.status() == 0 and torch.equal(k, old)
+
+
+def test_a_recorded_eviction_goes_on_where_later_ones_keep_other_numbers(dba):
+    rng = torch.Generator().manual_seed(3)
+    side = torch.cuda.Stream()
+    k, v, table = _cache(rng, 2, 8, 16, 2, 64, "bf16")
+    tree = _tree(dba, 2, 1, 2, 2, 64, 16, 8, 0, stream=side)
+    n, w, out_w = _i32([128, 100]), torch.rand(2, 2, 128, generator=rng).cuda(), torch.zeros(2, 2, 128, device="cuda")
+    out = table.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        tree.evict(k.clone(), v.clone(), table, n, w, 50, recent=5, table_out=out, weight_out=out_w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = tree.evict(k, v, table, n, w, 50, recent=5, table_out=out, weight_out=out_w)
+    others = []
+    with torch.cuda.stream(side):
+        for keep in (10, 70, 127, 50):
+            tree.evict(k.clone(), v.clone(), table, n, w, keep, table_out=out, weight_out=out_w)
+            others += [torch.full((size,), 12345, dtype=torch.int32, device="cuda") for size in (2, 4, 2 * 2 * 2 * 10, 2 * 2 * 2 * 50, 2 * 2 * 2 * 70)]
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all((x == 12345).all() for x in others)
+    assert got["ctx_len"].tolist() == [50, 50] and got["dropped"].tolist() == [78, 50]
+    for b, c in enumerate((128, 100)):
+        for h in range(2):
+            assert got["kept"][b, h].tolist() == L.keep(w[b, h, :c].tolist(), 50, 5)
