@@ -165,7 +165,7 @@ def decode(B=4, k=8, steps=24, prompt=12, V=997, layers=2, heads=8, kv_heads=2, 
         tokens = out["token"].view(B, k)
         logits = model.step(tree, cache, table, tokens, nx, prefix, offset, weights).view(B, k, V)
         if keep:             # (the last quarter stays whatever it receives)
-            got = tree.evict(*cache, table, nx["ctx_len"], weights, keep, recent=(keep + 3) // 4)
+            got = tree.evict(*cache, table, nx["ctx_len"], weights, keep, recent=(keep + 3) // 4, slot_pos=slot_pos)
             nx["ctx_len"] = got["ctx_len"]
             offset += got["dropped"]
             evicted += int(got["dropped"].sum())

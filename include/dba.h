@@ -532,6 +532,8 @@ dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float*
  *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0.
  *   kept: scratch and result, [layers, B, kv_heads, keep]: the old context places of what is kept, -1 beyond.
  *   ctx_len_out, dropped: [B] optional: the new length, and the old less the new.  (ctx_len_out may be ctx_len.)
+ *   slot_pos: optional, dba_tree_advance's [B, 32 * words], rows slot_pos_stride apart: lowered by what the sequence has dropped.  An open tree needs that:
+ *   the positions of its tokens count the context before them, and the order in which they settle goes by them.
  * 0 <= recent <= keep, keep >= 1.  A place on a page outside the cache is not copied (context: DBA_TREE_BAD_PAGE; an
  * arena slot without a page is not reported).
  */
@@ -545,6 +547,8 @@ typedef struct {
     int32_t* kept;
     int32_t* ctx_len_out;
     int32_t* dropped;
+    int32_t* slot_pos;
+    int64_t slot_pos_stride;
 } dba_tree_evicted;
 dba_status dba_tree_evict(dba_tree* h, const dba_kv_cache* cache, const int32_t* table_dev, int64_t table_stride, const int32_t* ctx_len_dev,
                           const dba_tree_evicted* evict);

@@ -350,6 +350,7 @@ dba_status dba_tree_evict(dba_tree* h, const dba_kv_cache* cache, const int32_t*
                           const dba_tree_evicted* ev) {
     if (!h || !ctx_len_dev || !ev || !ev->weight || !ev->weight_out || !ev->to_table || !ev->kept || ev->keep < 1 || ev->recent < 0 || ev->recent > ev->keep)
         return DBA_ERR_INVALID_ARG;
+    if (ev->slot_pos && ev->slot_pos_stride < 32 * (int64_t)h->c.words) return DBA_ERR_INVALID_ARG;
     if (!cache || ev->layer_stride < (cache->layers > 1) || ev->seq_stride < (h->c.B > 1) || ev->head_stride < (h->c.kv_heads > 1)) return DBA_ERR_INVALID_ARG;
     TreeEvict a{};
     dba_status st = check_cache(h, cache, table_dev, table_stride, &a.from);

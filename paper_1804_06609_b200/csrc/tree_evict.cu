@@ -219,10 +219,15 @@ __global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a,
     grid_dependency_wait();
     allow_dependents();
     const int keep = a.e.keep;
-    if (split == 0 && h == 0 && l == 0 && !values && tid == 0) {
-        const int L = min(max(a.ctx_len[b], 0), a.ctx_cap);
-        if (a.e.dropped) a.e.dropped[b] = L - min(L, keep);
-        if (a.e.ctx_len_out) a.e.ctx_len_out[b] = min(L, keep);
+    if (split == 0 && h == 0 && l == 0 && !values) {
+        const int L = min(max(a.ctx_len[b], 0), a.ctx_cap), dropped = L - min(L, keep);
+        if (a.e.slot_pos && dropped > 0)
+            for (int i = tid; i < a.A; i += kMThreads) a.e.slot_pos[(int64_t)b * a.e.slot_pos_stride + i] -= dropped;
+        __syncthreads();                                   // (ctx_len_out may be ctx_len)
+        if (tid == 0) {
+            if (a.e.dropped) a.e.dropped[b] = dropped;
+            if (a.e.ctx_len_out) a.e.ctx_len_out[b] = min(L, keep);
+        }
     }
     // context pages that stay the same: one block, in order; arena pages that do not
     const unsigned first_page = tree_page(a.from, (unsigned)a.A), pages = tree_page(a.from, (unsigned)(a.A + min(keep, a.ctx_cap) - 1)) + 1;

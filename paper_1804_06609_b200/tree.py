@@ -48,7 +48,7 @@ class TreeNorm(C.Structure):
 class TreeEvicted(C.Structure):
     _fields_ = [("weight", C.c_void_p), ("weight_out", C.c_void_p), ("layer_stride", C.c_int64), ("seq_stride", C.c_int64), ("head_stride", C.c_int64),
                 ("keep", C.c_int32), ("recent", C.c_int32), ("to_table", C.c_void_p), ("to_table_stride", C.c_int64), ("kept", C.c_void_p),
-                ("ctx_len_out", C.c_void_p), ("dropped", C.c_void_p)]
+                ("ctx_len_out", C.c_void_p), ("dropped", C.c_void_p), ("slot_pos", C.c_void_p), ("slot_pos_stride", C.c_int64)]
 
 
 def _rows_apart(shape, strides, places):
@@ -303,6 +303,12 @@ class TokenTree:
     def _call_shared(self, *args):
         return lib().dba_tree_attend_shared(*args, self._prefix_ref, self._scratch_at, self._scratch_bytes)
 
+    def _slot_pos(self, slot_pos):
+        s = slot_pos.stride()
+        if slot_pos.dtype is not self._i32t or slot_pos.shape != self._shape_arena or s[1] != 1 or slot_pos.get_device() != self._dev:
+            raise ValueError("slot_pos: int32 [B, 32 * words]")
+        return s[0] if self.B > 1 else 32 * self.words
+
     def advance(self, backptr, masks, slot_pos, ctx_len, score=None, token=None, eos=-1, out=None):
         """The tree after a step: see dba_tree_advance.  backptr (and score, token: dba_step's outputs) [B, rows] or [B * rows];
         slot_pos [B, 32 * words] is updated in place.  Returns a dict of masks, slot, position, ctx_len, top, commit_src,
@@ -327,15 +333,13 @@ class TokenTree:
         else:
             out = self._next_views(out, n)
             nx = self._next_struct(out)
-        s = slot_pos.stride()
-        if slot_pos.dtype is not self._i32t or slot_pos.shape != self._shape_arena or s[1] != 1 or slot_pos.get_device() != dev:
-            raise ValueError("slot_pos: int32 [B, 32 * words]")
+        s = self._slot_pos(slot_pos)
         if score is not None and (score.dtype is not self._f32t or score.numel() != size or not score.is_contiguous() or score.get_device() != dev):
             raise ValueError("score: fp32 [B, rows]")
         code = self._f_advance(self._h, rows_in, self._i32(masks, B * rows_in * W, "masks: int32 [B, rows, words]"), n,
                                self._i32(backptr, size, "backptr: int32 [B, rows]"), None if score is None else score.data_ptr(),
                                None if token is None else self._i32(token, size, "token: int32 [B, rows]"), eos,
-                               slot_pos.data_ptr(), s[0] if B > 1 else 32 * W, self._i32(ctx_len, B, "ctx_len: int32 [B]"), C.byref(nx))
+                               slot_pos.data_ptr(), s, self._i32(ctx_len, B, "ctx_len: int32 [B]"), C.byref(nx))
         if code:
             _check(code, "dba_tree_advance")
         return {**out, "slot_pos": slot_pos}
@@ -405,12 +409,13 @@ class TokenTree:
                 self._evict_own += (torch.empty(2, max(size, 2 * room), dtype=self._i32t, device=self.device),)
         return [(*self._evict_lens[i], self._evict_own[-1][i, :size].view(shape)) for i in (0, 1)]
 
-    def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None):
+    def evict(self, k, v, table, ctx_len, weight, keep, recent=0, table_out=None, weight_out=None, slot_pos=None):
         """Keeps `keep` tokens of every longer context: the last `recent` and, of the others, those of the largest weight, in their order,
         at the front.  weight [layers, B, kv_heads, context places] fp32 (without layers where k, v have none).  table_out, weight_out:
-        where to; default the same, in place (arena slots go along where table_out has other pages for them).  Returns a dict of ctx_len and dropped [B], kept [(layers,) B, kv_heads, keep] (the old context
-        places, -1 beyond) and weight (weight_out); the first three are one of two sets of the handle's own tensors, in turn.  See
-        dba_tree_evict."""
+        where to; default the same, in place (arena slots go along where table_out has other pages for them).  slot_pos: advance's, of an open
+        tree, lowered in place by what is dropped, so that its tokens go on settling in their order.  Returns a dict of ctx_len and dropped
+        [B], kept [(layers,) B, kv_heads, keep] (the old context places, -1 beyond) and weight (weight_out); the first three are one of two
+        sets of the handle's own tensors, in turn.  See dba_tree_evict."""
         B, layers = self.B, k.shape[:-4]
         if len(layers) > 1:
             raise ValueError("k and v: [pages, page_size, kv_heads, head_dim], or layers in front")
@@ -426,9 +431,10 @@ class TokenTree:
         key = (*layers, keep)
         if key != self._evicted_key:
             self._evicted, self._evicted_key = self._evict_sets(layers, keep), key
+        e = self._evict
+        e.slot_pos, e.slot_pos_stride = (None, 0) if slot_pos is None else (slot_pos.data_ptr(), self._slot_pos(slot_pos))
         new_len, dropped, kept = self._evicted[self._evict_turn]
         self._evict_turn = 1 - self._evict_turn
-        e = self._evict
         e.weight, e.weight_out, e.layer_stride, e.seq_stride, e.head_stride = weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2]
         e.keep, e.recent, e.to_table, e.to_table_stride = keep, recent, table_out.data_ptr(), stride_out
         e.kept, e.ctx_len_out, e.dropped = kept.data_ptr(), new_len.data_ptr(), dropped.data_ptr()

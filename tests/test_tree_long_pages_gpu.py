@@ -89,3 +89,28 @@ def test_a_recorded_eviction_goes_on_where_later_ones_keep_other_numbers(dba):
     for b, c in enumerate((128, 100)):
         for h in range(2):
             assert got["kept"][b, h].tolist() == L.keep(w[b, h, :c].tolist(), 50, 5)
+
+
+@pytest.mark.parametrize("ps,keep", [(16, 12), (5, 3)])
+def test_tokens_that_settle_after_an_eviction_come_in_order(dba, ps, keep):
+    """An open tree's positions count the context before them: an eviction lowers them, or its later tokens would settle before its earlier ones."""
+    rng = torch.Generator().manual_seed(1)
+    B, W, A = 2, 1, 32
+    per = -(-(A + 60) // ps)
+    k, v, table = _cache(rng, B, per, ps, 1, 64, "bf16")
+    tree = _tree(dba, B, 2, 1, 1, 64, ps, per, W)
+    w, slot_pos = torch.rand(B, 1, per * ps - A, generator=rng).cuda(), torch.zeros(B, A, dtype=torch.int32, device="cuda")
+    nx = tree.advance(_i32([[0, 0], [0, 0]]), torch.zeros(B, 1, W, dtype=torch.int32, device="cuda"), slot_pos, _i32([24, 2]))
+    first = nx["slot"].clone()
+    nx = {key: x.clone() for key, x in nx.items() if key != "slot_pos"}
+    before = slot_pos.clone()
+    got = tree.evict(k, v, table, nx["ctx_len"], w, keep, slot_pos=slot_pos)
+    assert got["dropped"].tolist() == [24 - keep, 0] and torch.equal(slot_pos, before - got["dropped"][:, None])
+    nx = tree.advance(_i32([[0, 1], [0, 1]]), nx["masks"], slot_pos, got["ctx_len"].clone())
+    assert nx["commit_n"].tolist() == [0, 0] and nx["position"].tolist() == [[keep + 1] * 2, [3, 3]]
+    second = nx["slot"].clone()
+    lengths = nx["ctx_len"].clone()
+    nx = tree.advance(_i32([[1, 1], [1, 1]]), nx["masks"].clone(), slot_pos, lengths)
+    assert nx["commit_n"].tolist() == [2, 2]
+    assert nx["commit_src"][:, :2].tolist() == [[int(first[b, 1]), int(second[b, 1])] for b in range(B)]
+    assert tree.status() == 0

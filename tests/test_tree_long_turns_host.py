@@ -57,3 +57,18 @@ def test_many_numbers_to_keep_do_not_pile_up(monkeypatch):
     for keep in list(range(1, 300)) + list(range(300, 0, -1)):
         _evict(t, keep)
     assert len({call[2] for call in noted}) <= 24          # twice, for each doubling
+
+
+def test_positions_that_an_eviction_refuses(monkeypatch):
+    t, noted = _handle(monkeypatch)
+    evict = lambda slot_pos: t.evict(_kv(t), _kv(t), _i32(2, 8), _i32(2), torch.zeros(2, 2, 64), 10, slot_pos=slot_pos)  # noqa: E731
+    for bad in (_i32(2, 63), _i32(1, 64), _i32(2, 64).long(), _i32(64, 2).t(), _i32(128)):
+        with pytest.raises(ValueError):
+            evict(bad)
+    assert not noted
+    evict(_i32(2, 64))
+    assert t._evict.slot_pos_stride == 64
+    evict(_i32(2, 100)[:, :64])
+    assert t._evict.slot_pos_stride == 100
+    evict(None)
+    assert t._evict.slot_pos is None and len(noted) == 3
