@@ -16,7 +16,8 @@ chain by advancing from its last row.
     --keep n     contexts are thinned to n tokens after every step: the attention that tokens receive is added up (dba_tree_weigh), and those
                  that receive least go (dba_tree_evict)
 The weights are random, so the text means nothing; with --check every open
-hypothesis' logits are computed again from its whole text without a cache (not with --keep)."""
+hypothesis' logits are computed again from its whole text without a cache (with --keep every token sees there what was left for it when it came, by
+layer and key head, and the weights that tokens have received are added up again)."""
 from __future__ import annotations
 
 import argparse
@@ -77,8 +78,9 @@ class Decoder:
             x = self._after(w, x, o)
         return self._norm(x) @ self.unembed
 
-    def whole_text(self, text):
-        """Logits after the last token of `text` (a list), computed without a cache."""
+    def whole_text(self, text, seen=None):
+        """Logits after the last token of `text` (a list), computed without a cache, and its attention by layer, [heads, tokens].  seen: by layer, [kv_heads,
+        tokens, tokens]: whether a token sees another (None: all up to itself)."""
         torch, n, half = self.torch, len(text), self.dim // 2
         x = self.embed[torch.tensor(text, device=self.embed.device)]
         cos, sin = self.rotary[0][:n, None], self.rotary[1][:n, None]
@@ -88,16 +90,90 @@ class Decoder:
             a, b = y[..., :half], y[..., half:]
             return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).to(self.dtype)
         causal = torch.ones(n, n, dtype=torch.bool, device=x.device).tril()
-        for w in self.layers:
+        attention = []
+        for i, w in enumerate(self.layers):
             q, k, v = self._qkv(w, x)
             if w["norm"] is not None:
                 root = lambda y, c: y.float() * (y.float().square().mean(-1, keepdim=True) + w["norm"][2]).rsqrt() * c  # noqa: E731
                 q, k = root(q, w["norm"][0]), root(k, w["norm"][1])
             q, k = turn(q).float(), turn(k).float()
             k, v = (y.repeat_interleave(self.heads // self.kv_heads, 1).float() for y in (k, v))
-            s = torch.einsum("ihd,jhd->hij", q, k) * self.dim ** -0.5
-            x = self._after(w, x, torch.einsum("hij,jhd->ihd", s.masked_fill(~causal, -math.inf).softmax(-1), v).to(self.dtype))
-        return (self._norm(x) @ self.unembed)[-1]
+            sees = causal if seen is None else seen[i].repeat_interleave(self.heads // self.kv_heads, 0)
+            p = (torch.einsum("ihd,jhd->hij", q, k) * self.dim ** -0.5).masked_fill(~sees, -math.inf).softmax(-1)
+            attention.append(p[:, -1])
+            x = self._after(w, x, torch.einsum("hij,jhd->ihd", p, v).to(self.dtype))
+        return (self._norm(x) @ self.unembed)[-1], attention
+
+
+class Check:
+    """The hypotheses' texts, what each of their tokens has seen, and what settled tokens have received: kept beside a decoding, without a cache."""
+
+    def __init__(self, model, texts, k, before):
+        self.model, self.k, self.worst, self.worst_weight = model, k, 0.0, 0.0
+        self.settled = [before for _ in texts]             # tokens of a sequence that are no longer in the tree, those before all sentences among them
+        each = lambda x: [[[list(x) for _ in range(model.kv_heads)] for _ in texts] for _ in model.layers]  # noqa: E731
+        self.before, self.context, self.received = before, each(()), each(())       # by layer, sequence and key head: context places' tokens, and their weights
+        # a text, and by token, layer and key head what it has seen (None: all before it)
+        self.lines = [[(text, [None] * len(text))] * k for text in texts]
+
+    def step(self, nx, backptr, tokens, offset):
+        """The texts after a step, and what has settled by it."""
+        self.open = (nx["position"] >= 0).tolist()
+        position, n, new = nx["position"].tolist(), nx["commit_n"].tolist(), []
+        for b, count in enumerate(n):
+            for layer in range(len(self.model.layers)):
+                for h in range(self.model.kv_heads):
+                    self.context[layer][b][h] += range(self.settled[b], self.settled[b] + count)
+                    self.received[layer][b][h] += [0.0] * count
+            self.settled[b] += count
+            new.append([])
+            for j in range(self.k):
+                text, seen = self.lines[b][backptr[b][j]]
+                if not self.open[b][j]:
+                    new[b].append(([], []))
+                    continue
+                text = text + [tokens[b][j]]
+                assert position[b][j] + offset[b] == len(text) - 1
+                own = list(range(self.settled[b], len(text)))
+                sees = [[list(range(self.before)) + at[b][h] + own for h in range(self.model.kv_heads)] for at in self.context]
+                new[b].append((text, seen + [sees]))
+        self.lines = new
+
+    def logits(self, logits, weights):
+        """The step's logits [B, k, V] and, where contexts are thinned, the weights by layer, against those of whole texts."""
+        torch, K = self.model.torch, self.model.kv_heads
+        for b, lines in enumerate(self.lines):
+            for j, (text, rows) in enumerate(lines):
+                if not self.open[b][j]:
+                    continue
+                seen = None
+                if weights is not None:
+                    seen = torch.ones(len(self.model.layers), K, len(text), len(text), dtype=torch.bool).tril()
+                    for i, row in enumerate(rows):
+                        for layer, h in [] if row is None else [(x, h) for x in range(len(row)) for h in range(K)]:
+                            seen[layer, h, i] = False
+                            seen[layer, h, i, row[layer][h]] = True
+                    seen = seen.to(logits.device)
+                want, attention = self.model.whole_text(text, seen)
+                self.worst = max(self.worst, float((logits[b, j].float() - want.float()).abs().max()))
+                for layer, p in enumerate(attention if weights is not None else []):
+                    p = p.view(K, -1, len(text)).sum(1).tolist()
+                    for h in range(K):
+                        self.received[layer][b][h] = [x + p[h][at] for x, at in zip(self.received[layer][b][h], self.context[layer][b][h])]
+        if weights is not None:
+            got = weights.tolist()
+            for layer, by_sequence in enumerate(self.received):
+                for b, by_head in enumerate(by_sequence):
+                    for h, row in enumerate(by_head):
+                        self.worst_weight = max([self.worst_weight] + [abs(x - y) / (1 + y) for x, y in zip(got[layer][b][h], row)])
+
+    def evicted(self, kept):
+        """kept [layers, B, kv_heads, keep]: the context places that stay."""
+        for layer, by_sequence in enumerate(kept.tolist()):
+            for b, by_head in enumerate(by_sequence):
+                for h, places in enumerate(by_head):
+                    for rows in (self.context, self.received):
+                        rows[layer][b][h] = [rows[layer][b][h][p] for p in places if p >= 0]
 
 
 def take_in(dba, model, cache, pages, tokens, page_size, heads, kv_heads, dim, code):
@@ -121,7 +197,7 @@ def take_in(dba, model, cache, pages, tokens, page_size, heads, kv_heads, dim, c
 def decode(B=4, k=8, steps=24, prompt=12, V=997, layers=2, heads=8, kv_heads=2, dim=64, page_size=16, words=8, dtype="bf16", seed=0, check=False,
            shared=0, norm=False, keep=0):
     """Returns (tokens, lengths, scores, flags) of dba_finalize, the largest difference of a logit from the one computed without
-    a cache (check) and what fell on the way: settled tokens, the highest slot."""
+    a cache (check) and what fell on the way: settled and evicted tokens, the highest slot, the largest difference of a token's weight (over 1 + weight)."""
     import torch
     import paper_1804_06609_b200 as dba
     g = torch.Generator().manual_seed(seed)
@@ -154,7 +230,8 @@ def decode(B=4, k=8, steps=24, prompt=12, V=997, layers=2, heads=8, kv_heads=2, 
     chain_logits = model.step(tree, cache, table, texts, nx, prefix, offset).view(B, prompt, V)
     logits = torch.zeros(B, k, V, dtype=tdt, device="cuda")
     logits[:, 0] = chain_logits[:, -1]                       # the beam's one live hypothesis
-    worst, settled, top, evicted, lines = 0.0, 0, 0, 0, [[before + t] for t in texts.tolist()]
+    settled, top, evicted = 0, 0, 0
+    checked = Check(model, [before + t for t in texts.tolist()], k, shared) if check else None
     for step in range(steps):
         out = stepper.step(logits.view(B * k, V).contiguous())
         backptr = out["backptr"].view(B, k)
@@ -164,26 +241,23 @@ def decode(B=4, k=8, steps=24, prompt=12, V=997, layers=2, heads=8, kv_heads=2, 
         tree.commit(*cache, table, nx["ctx_len"], nx["commit_src"], nx["commit_n"])
         tokens = out["token"].view(B, k)
         logits = model.step(tree, cache, table, tokens, nx, prefix, offset, weights).view(B, k, V)
+        if check:
+            checked.step(nx, out["backptr"].view(B, k).tolist(), tokens.tolist(), [0] * B if offset is None else offset.tolist())
+            checked.logits(logits, weights)
+            settled, top = settled + int(nx["commit_n"].sum()), max(top, int(nx["top"].max()))
         if keep:             # (the last quarter stays whatever it receives)
             got = tree.evict(*cache, table, nx["ctx_len"], weights, keep, recent=(keep + 3) // 4, slot_pos=slot_pos)
             nx["ctx_len"] = got["ctx_len"]
             offset += got["dropped"]
             evicted += int(got["dropped"].sum())
-        if check and not keep:
-            bp, tk, opened = out["backptr"].view(B, k).tolist(), tokens.tolist(), (nx["position"] >= 0).tolist()
-            lines = [[lines[b][bp[b][j]] + [tk[b][j]] if opened[b][j] else [] for j in range(k)] for b in range(B)]
-            for b in range(B):
-                for j in range(k):
-                    if opened[b][j]:
-                        assert int(nx["position"][b, j]) == len(lines[b][j]) - 1 - shared
-                        worst = max(worst, float((logits[b, j].float() - model.whole_text(lines[b][j]).float()).abs().max()))
-        if check:
-            settled, top = settled + int(nx["commit_n"].sum()), max(top, int(nx["top"].max()))
+            if check:
+                checked.evicted(got["kept"])
     result = stepper.finalize()
     bits = tree.status()
     if bits:
         raise RuntimeError(f"token tree: status {bits}")
-    return result, worst, dict(settled=settled, top=top, evicted=evicted, context=nx["ctx_len"].tolist(), constraints=constraints)
+    worst, worst_weight = (checked.worst, checked.worst_weight) if check else (0.0, 0.0)
+    return result, worst, dict(settled=settled, top=top, evicted=evicted, context=nx["ctx_len"].tolist(), constraints=constraints, worst_weight=worst_weight)
 
 
 def main():
@@ -201,8 +275,9 @@ def main():
         print(f"sentence {b}: constraints {info['constraints'][b]}, {'completed' if flags[b] & 1 else 'not completed'}, score {score[b]:.3f}: {tokens[b, :length[b]].tolist()}")
     if a.keep:
         print(f"{info['evicted']} tokens evicted, contexts of {info['context']} tokens are left")
-    elif a.check:
-        print(f"largest difference of a logit from the whole text's: {worst:.3g}; {info['settled']} tokens settled, highest slot {info['top']}")
+    if a.check:
+        print(f"largest difference of a logit from the whole text's: {worst:.3g}; {info['settled']} tokens settled, highest slot {info['top']}"
+              + (f"; of a token's weight: {info['worst_weight']:.3g}" if a.keep else ""))
 
 
 if __name__ == "__main__":
