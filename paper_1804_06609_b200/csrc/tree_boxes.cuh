@@ -1,6 +1,7 @@
 // Copies of neighbouring places of a page by tensor maps: what the kernels that read a bf16 cache tile by tile share.
-// A box is up to 128 places in one instruction, where 16-byte copies are 2048 for a tile of 128 keys of 128: eight rows on 100003 shared tokens take 73 us
-// with boxes and 92 without; gathers of four places at a time, 340 on a document of 6007 tokens where these take 157.
+// A box is up to 128 places in one instruction, where 16-byte copies are 2048 for a tile of 128 keys of 128: eight rows on 100003 shared tokens took 73 us
+// with boxes and 92 without when the boxes came (now 66 with pages of 64, and 70 with pages of 5, which 16-byte copies fetch); gathers of four places at a
+// time, 340 on a document of 6007 tokens where these took 157.
 #pragma once
 #include <cuda.h>
 

@@ -9,10 +9,10 @@
 // batch read whole before it is written, by one block, since a row is written only where every later row's source lies behind it.  Arena slots whose
 // page is another one in the new table go there too: nobody else writes or reads there.
 //
-// Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: the choice 33 us (128 rows, a block each, of up to 130 KB
+// Measured: a quarter of four documents of up to 32768 tokens, four layers, 8 heads of 128: 220 us, the choice 33 (128 rows, a block each, of up to 130 KB
 // of weights: the passes one after the other; 45 with the last one all over the row between barriers and the first digits counted after the load),
-// the copies 183 us, 1.07 GB, 5.9 TB/s: HBM.  256 of some 300 tokens, one layer of four
-// sequences: 8 us, launches and dependent loads.
+// the copies 183 to 188, 1.07 GB, 5.8 TB/s: HBM.  In place 286: 256 blocks of copies, a barrier for every 32 KB.  256 of some 300 tokens, one layer of four
+// sequences: 8.8 us, in place 8.4: launches and dependent loads.
 #include "tree_device.cuh"
 
 namespace dba {

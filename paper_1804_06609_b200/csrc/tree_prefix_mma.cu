@@ -20,11 +20,13 @@
 // kernel (tree_prefix.cu).  Only the epilogue needs the kernel before this one, so the rest runs beside its last blocks.  Every wait on an
 // mbarrier is bounded: one that runs out winds the block down and marks the call as failed.
 //
-// Measured: beams of 20 on 64 sentences, 32 heads over 8 of 128, 6007 tokens (126 GFLOP, 40960 rows) 124 us beside 30 of the rows' own part: 1.0
-// PFLOP/s, 62 % of the rate of a large matrix product.  What bounds it is the softmax: a tile of 128 keys takes a stream's warps some 3500 cycles, of
-// which exponentials, sums and packing 2000, and the tensor cores, at 50 to 60 %, wait for them.  Eight rows on 100003 tokens (205 MB): 54 us,
-// of which the main loop 29, at HBM's rate.  Both sides of what was chosen, the document's call in us: half tiles 157, whole ones 170; a quarter of the exponentials as
-// polynomials 157, none 162, half of them 164; the first queries by one warp 156, by eight 154; the few rows' call with boxes 73, with cp.async 92.
+// Measured: beams of 20 on 64 sentences, 32 heads over 8 of 128, 6007 tokens (126 GFLOP, 40960 rows, and 5 of the rows' own part): the call 160 us with
+// idle time around it, 170 call after call at the clocks that this brings (0.82 and 0.77 PFLOP/s, 51 and 48 % of the rate of a large matrix product), 30 of them the
+// own part.  No pipe is full (tensor cores 51 %, exponentials 38 %, issue 46 %): what bounds it is the chain of a softmax warp, with two of them a scheduler.  A
+// tile of 128 keys takes a stream's warps some 3500 cycles, of which exponentials, sums and packing 2000, and the same warps write the outputs.  Eight rows on
+// 100003 tokens (205 MB): 54 us, of which the main loop 29, at HBM's rate.  Both sides of what was chosen, the document's call in us, all with idle time around
+// it and in one session: half tiles 157, whole ones 170; a quarter of the exponentials as polynomials 157, none 162, half of them 164; the first queries by one
+// warp 156, by eight 154.
 #include <cuda_bf16.h>
 
 #include "tree_boxes.cuh"
