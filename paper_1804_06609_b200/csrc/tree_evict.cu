@@ -42,10 +42,11 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
     const float* w = a.e.weight + row;
     float* out = a.e.weight_out + row;
     int32_t* kept = a.e.kept + (((int64_t)l * a.B + b) * a.K + h) * keep;
-    for (int i = n + tid; i < keep; i += NT) kept[i] = -1;
+    // (unsigned: lengths may be as large as an int is, and a step goes beyond)
+    for (unsigned i = (unsigned)n + tid; i < (unsigned)keep; i += NT) kept[i] = -1;
     if (L <= keep) {
-        for (int i = tid; i < L; i += NT) {
-            kept[i] = i;
+        for (unsigned i = tid; i < (unsigned)L; i += NT) {
+            kept[i] = (int)i;
             out[i] = w[i];
         }
         return;
@@ -96,10 +97,10 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
                 for (int i = tid; i < kEBins; i += NT) bins[i] = 0;
                 __syncthreads();
 #pragma unroll 4
-                for (int i0 = 0; i0 < old; i0 += NT) {
-                    const int i = i0 + tid;
-                    const uint32_t key = i < old ? weight_key(w[i]) : 0u;
-                    count(i < old && (key & known) == prefix, (key >> shift) & ((1u << bits) - 1u));
+                for (unsigned i0 = 0; i0 < (unsigned)old; i0 += NT) {
+                    const unsigned i = i0 + tid;
+                    const uint32_t key = i < (unsigned)old ? weight_key(w[i]) : 0u;
+                    count(i < (unsigned)old && (key & known) == prefix, (key >> shift) & ((1u << bits) - 1u));
                 }
             }
             __syncthreads();
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
             const int left = (int)bins[digit];
             if (pass < 2 && left <= kEFew) {               // few have it: ranked among one another
                 const uint32_t same = ~0u << shift;
-                for (int i = tid; i < old; i += NT) {
+                for (unsigned i = tid; i < (unsigned)old; i += NT) {
                     const uint32_t key = weight_key(w[i]);
                     if ((key & same) == prefix) few[atomicAdd(&n_few, 1)] = key;         // (in any order: only their number and size count)
                 }
@@ -156,8 +157,8 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
     const float at_least = none ? __int_as_float(0x7fc00000) : nan_at ? neg_inf() : unord32(bar), more = none ? at_least : nan_at ? neg_inf() : unord32(bar + 1u);
     int n_above = 0, n_at = 0;
 #pragma unroll 1
-    for (int at0 = 0; at0 < L; at0 += room) {
-        const int here = min(room, L - at0), choose = min(max(old - at0, 0), here);
+    for (unsigned at = 0; at < (unsigned)L; at += room) {
+        const int at0 = (int)at, here = min(room, L - at0), choose = min(max(old - at0, 0), here);
         const int stretch = (choose + 32 * warps - 1) / (32 * warps) * 32, lo = warp * stretch, hi = min(lo + stretch, choose);
         __syncthreads();                                   // (the last ones have been written, the counts read)
         if (!fits) {
@@ -185,10 +186,10 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
         for (int i0 = lo; i0 < hi; i0 += 32) {
             const int i = i0 + lane;
             const float x = i < hi ? held[i] : 0.f;
-            const bool above = i < hi && x >= more, at = i < hi && !above && (x >= at_least || nan_at);
-            const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at);
+            const bool above = i < hi && x >= more, at_bar = i < hi && !above && (x >= at_least || nan_at);
+            const uint32_t u = __ballot_sync(kFullMask, above), e = __ballot_sync(kFullMask, at_bar);
             const int mine_e = before_e + __popc(e & below);
-            if (above || (at && mine_e < m)) {
+            if (above || (at_bar && mine_e < m)) {
                 const int to = before_u + __popc(u & below) + min(mine_e, m);
                 kept[to] = at0 + i;
                 out[to] = x;
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(NT) tree_keep_kernel(const TreeEvict a, int ro
             out[to] = x;
         }
     }
-    for (int i = n + tid; i < L; i += NT) out[i] = 0.f;
+    for (unsigned i = (unsigned)n + tid; i < (unsigned)L; i += NT) out[i] = 0.f;
 }
 
 // Blocks: keys or values, layer, sequence, key head, split, the last counting fastest.
@@ -269,8 +270,8 @@ __global__ void __launch_bounds__(kMThreads) tree_move_kernel(const TreeEvict a,
                 if (to[c]) *reinterpret_cast<uint4*>(to[c]) = x[c];
         }
     };
-    for (int i0 = split * kMRowsAt; i0 < keep; i0 += step) {
-        const int rows = min(kMRowsAt, keep - i0);
+    for (unsigned at0 = split * kMRowsAt; at0 < (unsigned)keep; at0 += step) {
+        const int i0 = (int)at0, rows = min(kMRowsAt, keep - i0);
         __syncthreads();
         bool any = false;
         if (tid < rows) {
@@ -320,7 +321,7 @@ cudaError_t launch_tree_evict(const TreeEvict& a, cudaStream_t st, int* launches
     if (e != cudaSuccess) return e;
     // some eight blocks an SM, none without a batch of rows
     const int64_t rows = (int64_t)a.K * a.B * a.layers * 2;
-    const int most = (a.e.keep + kMRowsAt - 1) / kMRowsAt, want = (int)((8LL * a.sm_count + rows - 1) / rows), splits = want < most ? want : most;
+    const int most = (int)((a.e.keep + kMRowsAt - 1u) / kMRowsAt), want = (int)((8LL * a.sm_count + rows - 1) / rows), splits = want < most ? want : most;
     e = launch_after(tree_move_kernel, dim3((unsigned)(rows * splits)), dim3(kMThreads), 0, st, a, splits);
     *launches += 1;
     return e;

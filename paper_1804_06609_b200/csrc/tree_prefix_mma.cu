@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(XConf<DP, TMA>::threads, 1) tree_prefix_mma_ke
             shared_before = !two;
             const uint64_t dq = sw128_desc(msmem_u32(sm.q[qb]) + (two ? s * C::q_half : 0), 16);
             // rows of this stream's last tile behind the prefix' end
-            const int n_tail = pc.tile_end == pc.tiles && (pc.tiles - 1 - pc.tile) % by == (two ? 0 : s) ? pc.tiles * kXKeys - pc.len : 0;
+            const int n_tail = pc.tile_end == pc.tiles && (pc.tiles - 1 - pc.tile) % by == (two ? 0 : s) ? (int)((uint32_t)pc.tiles * kXKeys - (uint32_t)pc.len) : 0;
             uint32_t k_copy = 2 * (tiles0 + (two ? 0 : s)), v_copy = k_copy + 1;
 #pragma unroll 1
             for (int g = n ? -1 : 0; g < n; ++g) {

@@ -80,7 +80,7 @@ template <int KT, int ROWS, int HALF> struct PrefixCut {
     static __device__ __forceinline__ Sizes sizes(const TreePrefix& a, const PrefixGroup& p) {
         Sizes s;
         s.rows = (p.hi - p.lo) * a.n * a.G;
-        s.tiles = (p.len + KT - 1) / KT;
+        s.tiles = (int)((p.len + KT - 1u) / KT);           // (a length may be as large as an int is)
         s.blocks = (s.rows + ROWS - 1) / ROWS;
         if (s.tiles == 0 || s.blocks == 0) { s.full = s.rest = s.head = 0; return s; }
         s.full = (long long)cost(ROWS) * s.tiles + kExtra;

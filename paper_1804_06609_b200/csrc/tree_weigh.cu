@@ -80,13 +80,14 @@ __global__ void __launch_bounds__(kWThreads, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) t
     grid_dependency_wait();
     allow_dependents();
     const auto length_of = [&](int b) { return min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap); };
-    SpanRun run = span_run<kWThreads>(a.B, 1, &sm.span, [&](int b) { return (long long)a.K * ((length_of(b) + KT - 1) / KT); });
+    const auto tiles_of = [](int length) { return (int)((length + KT - 1u) / KT); };           // (a length may be as large as an int is)
+    SpanRun run = span_run<kWThreads>(a.B, 1, &sm.span, [&](int b) { return (long long)a.K * (tiles_of(length_of(b))); });
     if (run.t >= run.t_end) return;
     // a tile: its sequence and key head, where it begins, how many keys it has
     struct Tile { int b, h, p0, count; };
     const auto tile_of = [&](long long t) {                // (in ascending order)
-        int L = length_of(run.g), tiles = (L + KT - 1) / KT;
-        while (t - run.at >= (long long)a.K * tiles) { run.at += (long long)a.K * tiles; L = length_of(++run.g); tiles = (L + KT - 1) / KT; }
+        int L = length_of(run.g), tiles = tiles_of(L);
+        while (t - run.at >= (long long)a.K * tiles) { run.at += (long long)a.K * tiles; L = length_of(++run.g); tiles = tiles_of(L); }
         const int h = (int)((t - run.at) / tiles), p0 = (int)((t - run.at) - (long long)h * tiles) * KT;
         return Tile{run.g, h, p0, min(KT, L - p0)};
     };

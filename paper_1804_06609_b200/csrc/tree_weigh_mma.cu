@@ -53,7 +53,7 @@ struct YPiece { int b, h, len, tile, tile_end, group, blocks; };
 struct YRun {
     SpanRun r;
     YPiece p;
-    __device__ __forceinline__ int tiles_of(const TreeWeigh& a, int b) { return (min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap) + kYKeys - 1) / kYKeys; }
+    __device__ __forceinline__ int tiles_of(const TreeWeigh& a, int b) { return (int)((min(max(__ldg(a.ctx_len + b), 0), a.ctx_cap) + kYKeys - 1u) / kYKeys); }
     __device__ __forceinline__ void start(const SpanRun& run) { r = run; p.group = -1; p.tile_end = 0; }
     __device__ __forceinline__ bool next(const TreeWeigh& a) {
         const int M = a.n * a.G, groups = (M + 2 * kYQueries - 1) / (2 * kYQueries);
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(YConf<DP, TMA>::threads, 1) tree_weigh_mma_ker
         if (tid == 0) atomicOr(a.pages.status, (uint32_t)DBA_TREE_TIMEOUT);
         run.start(mine);
         while (run.next(a))
-            for (int p = pc.tile * kYKeys + tid; p < min(pc.tile_end * kYKeys, pc.len); p += C::threads)
+            for (uint32_t p = pc.tile * kYKeys + tid; p < min((uint32_t)pc.tile_end * kYKeys, (uint32_t)pc.len); p += C::threads)
                 a.out[(int64_t)pc.b * a.w_seq + (int64_t)pc.h * a.w_head + p] = __int_as_float(0x7fc00000);
     }
 }
