@@ -529,7 +529,7 @@ dba_status dba_tree_weigh(dba_tree* h, const dba_tree_query* query, const float*
  *   Of the pages that hold the first A + keep places none may be another sequence's too where it is written.
  *   weight, weight_out: [layers, B, kv_heads] rows, layer_stride, seq_stride and head_stride apart (alike in both); may be the same.  As dba_tree_weigh's,
  *   rows must not overlap.
- *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0.
+ *   weight_out's first min(ctx_len, keep) entries are those of the tokens kept, the others below the old ctx_len 0; from there on they are left as they are.
  *   kept: scratch and result, [layers, B, kv_heads, keep]: the old context places of what is kept, -1 beyond.
  *   ctx_len_out, dropped: [B] optional: the new length, and the old less the new.  (ctx_len_out may be ctx_len.)
  *   slot_pos: optional, dba_tree_advance's [B, 32 * words], rows slot_pos_stride apart: lowered by what the sequence has dropped.  An open tree needs that:

@@ -353,19 +353,19 @@ class TokenTree:
         if code:
             _check(code, "dba_tree_commit")
 
-    _rows_last = None          # strides and shape last found to keep the rows of weights apart
+    _rows_last = None          # strides, shape and leading dimensions of the weights last looked over
 
     # [B, kv_heads, places] (evict: layers in front) fp32 with a unit inner stride: at least the places a table leaves the context
     def _weights(self, w, lead, what):
-        B, sh, s = self.B, w.shape, w.stride()
-        places = self.max_pages * self.page_size - 32 * self.words
-        if (w.dtype is not self._f32t or w.get_device() != self._dev or len(sh) != len(lead) + 3 or sh[:-1] != (*lead, B, self.kv_heads)
-                or sh[-1] < places or s[-1] != 1):
-            raise ValueError(f"{what}: fp32 [{'layers, ' if lead else ''}B, kv_heads, context places], unit inner stride")
-        if (s, sh) != self._rows_last:
+        sh, s = w.shape, w.stride()
+        good = w.dtype is self._f32t and w.get_device() == self._dev
+        if not good or (s, sh, lead) != self._rows_last:
+            places = self.max_pages * self.page_size - 32 * self.words
+            if not good or len(sh) != len(lead) + 3 or sh[:-1] != (*lead, self.B, self.kv_heads) or sh[-1] < places or s[-1] != 1:
+                raise ValueError(f"{what}: fp32 [{'layers, ' if lead else ''}B, kv_heads, context places], unit inner stride")
             if not _rows_apart(sh[:-1], s[:-1], places):
                 raise ValueError(f"{what}: rows that do not overlap")
-            self._rows_last = (s, sh)
+            self._rows_last = (s, sh, lead)
         return s
 
     def weigh(self, q, k, table, ctx_len, lse, weight=None, decay=1.0, scale=None, out=None):
@@ -432,7 +432,8 @@ class TokenTree:
         if key != self._evicted_key:
             self._evicted, self._evicted_key = self._evict_sets(layers, keep), key
         e = self._evict
-        e.slot_pos, e.slot_pos_stride = (None, 0) if slot_pos is None else (slot_pos.data_ptr(), self._slot_pos(slot_pos))
+        if slot_pos is not None or e.slot_pos:
+            e.slot_pos, e.slot_pos_stride = (None, 0) if slot_pos is None else (slot_pos.data_ptr(), self._slot_pos(slot_pos))
         new_len, dropped, kept = self._evicted[self._evict_turn]
         self._evict_turn = 1 - self._evict_turn
         e.weight, e.weight_out, e.layer_stride, e.seq_stride, e.head_stride = weight.data_ptr(), weight_out.data_ptr(), s[0] if layers else 0, s[-3], s[-2]
